@@ -74,7 +74,7 @@ typedef enum {
     PLDP_ERR_TIMEOUT = 4      /* reserved: no call waits on the host          */
 } pldp_status;
 
-typedef enum { PLDP_F32 = 0, PLDP_BF16 = 1 } pldp_dtype;
+typedef enum { PLDP_F32 = 0, PLDP_BF16 = 1, PLDP_E4M3 = 2 /* caches only */ } pldp_dtype;
 
 typedef enum { PLDP_AGG_MAX = 0, PLDP_AGG_SUM = 1 } pldp_agg;
 
@@ -86,6 +86,7 @@ typedef enum { PLDP_AGG_MAX = 0, PLDP_AGG_SUM = 1 } pldp_agg;
 #define PLDP_ST_DRAFT_LEN    16u  /* draft_len outside [0, K]: clamped into it           */
 #define PLDP_ST_ROW_INDEX    32u  /* a row_idx entry outside [0, R): that row ignored    */
 #define PLDP_ST_TIMEOUT      64u  /* an on-chip copy did not complete in time: no result */
+#define PLDP_ST_PAGE        128u  /* a page table entry outside [0, n_pages): its positions skipped */
 
 #define PLDP_MAX_NGRAM 8          /* largest ngram_max accepted                          */
 
@@ -595,6 +596,239 @@ PLDP_API pldp_status pldp_identify_heads(const int32_t* ids, int64_t ids_stride,
  * 1 <= k <= R <= 8192.  counts: uint32 [R] (device).
  */
 PLDP_API pldp_status pldp_top_heads(const uint32_t* counts, int R, int k, int32_t* row_idx, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * The target model's cache around a step
+ * ---------------------------------------------------------------------------
+ * Verification's K+1 distributions come from one forward pass of the target model
+ * over x_t and the draft (Sec. 4.4).  In each of its layers these calls norm and
+ * rotate the new tokens' queries and keys and write keys and values to a paged
+ * cache (pldp_cache_append), attend over the cache (pldp_attend_cache), and rank the
+ * next step's candidates by that attention without its rows ever being written out
+ * (pldp_rank_cache, Eq. 2); pldp_cache_read takes positions back out of the cache,
+ * pldp_token_logprobs scores tokens under the logits.
+ *
+ * The step's tokens of sequence b are x_t and its draft: token i = 0..draft_len[b]
+ * stands at position seq_len[b]-1+i, as verification numbers them.  (A prompt, or a
+ * chunk of one that starts at position p, is the same with seq_len = p+1 and the
+ * tokens after its first as the draft.)  The positions of tokens that verification
+ * rejects are simply written again by the next step.
+ *
+ *  k, v       the pools of pages: the vector of position p, head h of sequence b is
+ *               base + pages[b][p / page_size]*page_stride + (p % page_size)*pos_stride
+ *                    + h*head_stride,  head_dim contiguous elements,
+ *             the same strides for both; strides in elements, so either order of
+ *             positions and heads within a page can be given.  Base 16-byte aligned,
+ *             strides multiples of 16 bytes.
+ *  dtype      PLDP_BF16, or PLDP_E4M3: 8-bit codes (4 exponent and 3 mantissa bits,
+ *             largest 448) and one fp32 scale for each vector,
+ *             value = code * scale, scales > 0 and finite.
+ *  k_scale, v_scale   float [n_pages, heads, page_size], contiguous (PLDP_E4M3; else NULL).
+ *  n_pages, page_size  >= 1, any size; max_pages * page_size < 2^31.
+ *  heads      key/value heads, 1..1024; head_dim a multiple of 16, 16..256.
+ *  pages      int32 [B, pages_stride]: the page of each page_size positions, max_pages
+ *             entries a sequence.  An entry outside [0, n_pages) sets PAGE: its
+ *             positions are not written, read as zeros and attended to by nothing.
+ */
+typedef struct {
+    void* k;
+    void* v;
+    pldp_dtype dtype;
+    float* k_scale;
+    float* v_scale;
+    int n_pages, page_size, heads, head_dim;
+    int64_t page_stride, pos_stride, head_stride;
+    const int32_t* pages;
+    int64_t pages_stride;
+    int max_pages;
+} pldp_cache;
+
+/*
+ * Appends a step's tokens to the cache.  For every token, in fp32:
+ *   queries and keys   x <- x * rsqrt(mean(x^2) + eps) * norm     (q_norm / k_norm not NULL)
+ *                      (a, b) <- (a cos - b sin, b cos + a sin)   (cos not NULL)
+ *   q_out <- bf16(q);  the cache's keys and values <- k, v rounded to bf16, or in a
+ *   PLDP_E4M3 cache scale = max|x| / 448 (1 for a vector of zeros), code = x / scale.
+ *
+ *  q, k, v    dtype (PLDP_F32 or PLDP_BF16): [B, n, q_heads or cache.heads, head_dim]
+ *             with strides of their own (sequence, token, head; elements), 16-byte
+ *             aligned, strides multiples of 16 bytes: slices of one projection's output
+ *             do.
+ *  n          tokens a sequence has room for, >= 1 (K+1).
+ *  q_heads    a multiple of cache.heads is needed by pldp_attend_cache only.
+ *  q_norm, k_norm   dtype [head_dim], 16-byte aligned, or NULL; eps >= 0.
+ *  cos, sin   float [rot_rows, rot/2], row p for position p, 16-byte aligned, or both
+ *             NULL.  rot even, 2..head_dim: the first rot elements rotate, in pairs
+ *             (e, e + rot/2), or (2e, 2e+1) when interleaved is not 0.
+ *  seq_len    int32 [B], 1..capacity (0: nothing to do; else SEQ_LEN, skipped); the
+ *             capacity is max_pages * page_size, and rot_rows where that is less.
+ *  draft_len  int32 [B], or NULL for n-1; outside [0, n-1]: DRAFT_LEN, clamped.
+ *  q_out      bf16 [B, n, q_heads, head_dim] with strides; may be q itself (bf16).
+ *  status     uint32 [B] or NULL.
+ * Tokens past draft_len leave q_out untouched, and so do tokens at or past the capacity
+ * (CAPACITY).
+ */
+typedef struct {
+    pldp_cache cache;
+    const void* q;
+    const void* k;
+    const void* v;
+    pldp_dtype dtype;
+    int B, n, q_heads;
+    int64_t q_strides[3], k_strides[3], v_strides[3]; /* sequence, token, head */
+    const void* q_norm;
+    const void* k_norm;
+    float eps;
+    const float* cos;
+    const float* sin;
+    int rot, interleaved;
+    int64_t rot_rows;
+    const int32_t* seq_len;
+    const int32_t* draft_len;
+    void* q_out;
+    int64_t q_out_strides[3];
+    uint32_t* status;
+} pldp_cache_append_args;
+
+PLDP_API pldp_status pldp_cache_append(const pldp_cache_append_args* args, void* stream);
+
+/*
+ * Reads positions start[b] .. start[b]+count[b]-1 of every sequence out of the cache into
+ * dense rows 0..count[b]-1.
+ *
+ *  k_out, v_out   dtype (PLDP_F32 or PLDP_BF16) [B, n, cache.heads, head_dim] with the
+ *             strides given (sequence, position, head; elements, the same for both),
+ *             16-byte aligned, strides multiples of 16 bytes; v_out or k_out may be NULL.
+ *  start      int32 [B], or NULL for 0.  count int32 [B], 0..n (else clamped,
+ *             SEQ_LEN); a start outside the capacity, or a count that passes it, is cut
+ *             there (CAPACITY).
+ * Rows at and past count[b] are left untouched.
+ */
+typedef struct {
+    pldp_cache cache;
+    const int32_t* start;
+    const int32_t* count;
+    int B, n;
+    pldp_dtype dtype;
+    void* k_out;
+    void* v_out;
+    int64_t out_strides[3];
+    uint32_t* status;
+} pldp_cache_read_args;
+
+PLDP_API pldp_status pldp_cache_read(const pldp_cache_read_args* args, void* stream);
+
+/*
+ * Attention of a step's tokens over the cache (their own keys and values included: append
+ * first).  Token i of sequence b, query head h, with kv head h / (q_heads / cache.heads):
+ *   s_j   = scale * q . k_j   for positions j = 0 .. seq_len[b]-1+i
+ *   out   = sum_j exp(s_j - lse) v_j,   lse = ln sum_j exp(s_j)
+ *
+ *  q          bf16 [B, n, q_heads, head_dim] with strides (sequence, token, head),
+ *             16-byte aligned, strides multiples of 16 bytes.
+ *  q_heads    a multiple of cache.heads.
+ *  seq_len, draft_len   as pldp_cache_append (the capacity is max_pages * page_size).
+ *  scale      finite; 1/sqrt(head_dim) as a rule.
+ *  out        bf16 [B, n, q_heads, head_dim] with strides, as q.
+ *  lse        float [B, n, q_heads], contiguous, or NULL.
+ *  workspace  pldp_attend_workspace_size bytes, 256-byte aligned, zeroed once before
+ *             first use (every call leaves it zeroed where that matters).
+ *  status     uint32 [B] or NULL.
+ * Rows with nothing to attend to (tokens past draft_len, sequences skipped, positions
+ * past the capacity) are written as zeros, their lse as -INFINITY.  Keys and values
+ * past a sequence's last new token are never used, whatever they hold; those of its new
+ * tokens must be finite for all of its rows.  Sums and the running maximum are held in
+ * fp32; results are the same for the same inputs, however the work is scheduled.
+ */
+typedef struct {
+    pldp_cache cache;
+    const void* q;
+    int B, n, q_heads;
+    int64_t q_strides[3];
+    const int32_t* seq_len;
+    const int32_t* draft_len;
+    float scale;
+    void* out;
+    int64_t out_strides[3];
+    float* lse;
+    uint32_t* status;
+    void* workspace;
+    size_t workspace_bytes;
+} pldp_attend_args;
+
+PLDP_API pldp_status pldp_attend_cache(const pldp_attend_args* args, void* stream);
+
+PLDP_API size_t pldp_attend_workspace_size(int B, int n, int q_heads, int heads, int head_dim);
+
+/*
+ * Ranking by attentions (Eq. 2, as pldp_rank_attention) straight from one layer's cache:
+ * the attention of one query row a sequence at the candidates, from the row's queries, the
+ * candidates' keys and the lse that pldp_attend_cache wrote,
+ *   score_j = max (or sum) over the selected heads h of exp(scale * q_h . k_j - lse_h),
+ * so no attention row is ever written out.  After verification the query t-1 of the new x_t
+ * is row accept_len[b] of the step, and the positions before it are kv_keep_len[b].
+ *
+ *  q, q_heads, q_strides, scale, lse   of the step's pldp_attend_cache (lse [B, n, q_heads]).
+ *  row        int32 [B] (accept_len), or NULL for row 0; outside [0, n): ROW_INDEX, no
+ *             result.
+ *  kv_len     int32 [B] (kv_keep_len), 0..capacity (else SEQ_LEN, no result): candidates
+ *             outside [0, kv_len) score -INFINITY and are never chosen.
+ *  heads      int32 [n_sel], or NULL for all q_heads (n_sel ignored): the selected query heads;
+ *             entries outside [0, q_heads) are ignored and set ROW_INDEX.
+ *             n_sel * head_dim <= 49152.
+ *  accumulate not 0: scores holds those of other layers, and a candidate's score is
+ *             the larger of both (MAX) or their sum (SUM): call layer by layer.
+ *  cand_pos, cand_count, C_cap   as written by pldp_find_candidates.
+ *  scores     float [B, C_cap] out, or NULL (not with accumulate).
+ *  best_pos, best_score, status  as pldp_rank_attention; ties go to the smaller j.
+ */
+typedef struct {
+    pldp_cache cache;
+    const void* q;
+    int B, n, q_heads;
+    int64_t q_strides[3];
+    const int32_t* row;
+    const int32_t* kv_len;
+    const float* lse;
+    const int32_t* heads;
+    int n_sel;
+    pldp_agg agg;
+    int accumulate;
+    float scale;
+    const int32_t* cand_pos;
+    const int32_t* cand_count;
+    int C_cap;
+    float* scores;
+    int32_t* best_pos;
+    float* best_score;
+    uint32_t* status;
+} pldp_rank_cache_args;
+
+PLDP_API pldp_status pldp_rank_cache(const pldp_rank_cache_args* args, void* stream);
+
+/*
+ * Log probabilities of given tokens, with the entropy and the likeliest alternatives, of
+ * `rows` rows of logits (a step's B * (K+1), say) at temperature T: x = logits / T,
+ *   lse = ln sum_v exp(x_v),  logprob = x_token - lse,  entropy = lse - sum_v p_v x_v.
+ *
+ *  logits     dtype [rows, V], contiguous.  -INFINITY is allowed (a masked token: p = 0).
+ *  tokens     int32 [rows], or NULL (no logprob); outside [0, V): logprob -INFINITY.
+ *  logprob, entropy   float [rows] out or NULL.
+ *  top        alternatives wanted, 0..32 and <= V: top_id int32 [rows, top] and top_logprob
+ *             float [rows, top], by descending logit, ties to the lower index (either
+ *             may be NULL).
+ *  workspace  pldp_token_logprobs_workspace_size bytes, 16-byte aligned; need not be
+ *             cleared.
+ * A row of -INFINITY throughout: logprob -INFINITY, entropy 0, top_id 0, 1, ... with
+ * -INFINITY.
+ */
+PLDP_API pldp_status pldp_token_logprobs(const void* logits, pldp_dtype dtype, int64_t rows, int V,
+                                         float temperature, const int32_t* tokens, float* logprob,
+                                         float* entropy, int top, int32_t* top_id,
+                                         float* top_logprob, void* workspace,
+                                         size_t workspace_bytes, void* stream);
+
+PLDP_API size_t pldp_token_logprobs_workspace_size(int64_t rows, int V);
 
 /* Message describing the last failed call on this host thread ("" if none). */
 PLDP_API const char* pldp_last_error(void);

@@ -41,9 +41,9 @@ from . import _build
 
 __all__ = [
     "build", "library_path", "PldpError",
-    "PLDP_F32", "PLDP_BF16", "PLDP_AGG_MAX", "PLDP_AGG_SUM",
+    "PLDP_F32", "PLDP_BF16", "PLDP_E4M3", "PLDP_AGG_MAX", "PLDP_AGG_SUM",
     "PLDP_ST_CAND_OVERFLOW", "PLDP_ST_TOKEN_RANGE", "PLDP_ST_CAPACITY", "PLDP_ST_SEQ_LEN",
-    "PLDP_ST_DRAFT_LEN", "PLDP_ST_ROW_INDEX", "PLDP_ST_TIMEOUT",
+    "PLDP_ST_DRAFT_LEN", "PLDP_ST_ROW_INDEX", "PLDP_ST_TIMEOUT", "PLDP_ST_PAGE",
     "PLDP_OK", "PLDP_ERR_INVALID_ARG", "PLDP_ERR_UNSUPPORTED", "PLDP_ERR_CUDA", "PLDP_ERR_TIMEOUT",
     "pldp_find_candidates", "pldp_rank_hidden", "pldp_rank_attention", "pldp_extract_draft",
     "pldp_verify_greedy", "pldp_verify_workspace_size", "pldp_verify_greedy_noalloc",
@@ -53,10 +53,13 @@ __all__ = [
     "pldp_verify_greedy_draft", "pldp_verify_draft_args",
     "pldp_verify_sample_draft", "pldp_verify_sample_draft_args", "pldp_verify_sample_draft_workspace_size",
     "pldp_rank_hidden_avg", "pldp_identify_heads", "pldp_top_heads",
+    "pldp_cache", "pldp_cache_args", "pldp_cache_append", "pldp_cache_append_args", "pldp_cache_read",
+    "pldp_cache_read_args", "pldp_attend_cache", "pldp_attend_args", "pldp_attend_workspace_size",
+    "pldp_rank_cache", "pldp_rank_cache_args", "pldp_token_logprobs", "pldp_token_logprobs_workspace_size",
     "pldp_version", "pldp_last_error",
 ]
 
-PLDP_F32, PLDP_BF16 = 0, 1
+PLDP_F32, PLDP_BF16, PLDP_E4M3 = 0, 1, 2
 PLDP_AGG_MAX, PLDP_AGG_SUM = 0, 1
 PLDP_ST_CAND_OVERFLOW = 1
 PLDP_ST_TOKEN_RANGE = 2
@@ -65,6 +68,7 @@ PLDP_ST_SEQ_LEN = 8
 PLDP_ST_DRAFT_LEN = 16
 PLDP_ST_ROW_INDEX = 32
 PLDP_ST_TIMEOUT = 64
+PLDP_ST_PAGE = 128
 
 PLDP_OK = 0
 PLDP_ERR_INVALID_ARG = 1
@@ -127,6 +131,65 @@ class pldp_verify_draft_args(ctypes.Structure):
         ("draft", ctypes.c_void_p), ("draft_len", ctypes.c_void_p), ("argmax", ctypes.c_void_p),
         ("accept_len", ctypes.c_void_p), ("next_token", ctypes.c_void_p), ("kv_keep_len", ctypes.c_void_p),
         ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t), ("next", pldp_draft_step_args),
+    ]
+
+
+class pldp_cache_args(ctypes.Structure):
+    """Mirror of the C description of a paged cache, pldp_cache (include/pldp.h)."""
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("dtype", ctypes.c_int),
+        ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+        ("n_pages", ctypes.c_int), ("page_size", ctypes.c_int), ("heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+        ("page_stride", ctypes.c_int64), ("pos_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+        ("pages", ctypes.c_void_p), ("pages_stride", ctypes.c_int64), ("max_pages", ctypes.c_int),
+    ]
+
+
+_STRIDES = ctypes.c_int64 * 3
+
+
+class pldp_cache_append_args(ctypes.Structure):
+    """Mirror of the C argument block of pldp_cache_append (include/pldp.h)."""
+    _fields_ = [
+        ("cache", pldp_cache_args), ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("dtype", ctypes.c_int), ("B", ctypes.c_int), ("n", ctypes.c_int), ("q_heads", ctypes.c_int),
+        ("q_strides", _STRIDES), ("k_strides", _STRIDES), ("v_strides", _STRIDES),
+        ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p), ("eps", ctypes.c_float),
+        ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("rot", ctypes.c_int), ("interleaved", ctypes.c_int),
+        ("rot_rows", ctypes.c_int64), ("seq_len", ctypes.c_void_p), ("draft_len", ctypes.c_void_p),
+        ("q_out", ctypes.c_void_p), ("q_out_strides", _STRIDES), ("status", ctypes.c_void_p),
+    ]
+
+
+class pldp_cache_read_args(ctypes.Structure):
+    """Mirror of the C argument block of pldp_cache_read (include/pldp.h)."""
+    _fields_ = [
+        ("cache", pldp_cache_args), ("start", ctypes.c_void_p), ("count", ctypes.c_void_p), ("B", ctypes.c_int),
+        ("n", ctypes.c_int), ("dtype", ctypes.c_int), ("k_out", ctypes.c_void_p), ("v_out", ctypes.c_void_p),
+        ("out_strides", _STRIDES), ("status", ctypes.c_void_p),
+    ]
+
+
+class pldp_attend_args(ctypes.Structure):
+    """Mirror of the C argument block of pldp_attend_cache (include/pldp.h)."""
+    _fields_ = [
+        ("cache", pldp_cache_args), ("q", ctypes.c_void_p), ("B", ctypes.c_int), ("n", ctypes.c_int),
+        ("q_heads", ctypes.c_int), ("q_strides", _STRIDES), ("seq_len", ctypes.c_void_p),
+        ("draft_len", ctypes.c_void_p), ("scale", ctypes.c_float), ("out", ctypes.c_void_p),
+        ("out_strides", _STRIDES), ("lse", ctypes.c_void_p), ("status", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class pldp_rank_cache_args(ctypes.Structure):
+    """Mirror of the C argument block of pldp_rank_cache (include/pldp.h)."""
+    _fields_ = [
+        ("cache", pldp_cache_args), ("q", ctypes.c_void_p), ("B", ctypes.c_int), ("n", ctypes.c_int),
+        ("q_heads", ctypes.c_int), ("q_strides", _STRIDES), ("row", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+        ("lse", ctypes.c_void_p), ("heads", ctypes.c_void_p), ("n_sel", ctypes.c_int), ("agg", ctypes.c_int),
+        ("accumulate", ctypes.c_int), ("scale", ctypes.c_float), ("cand_pos", ctypes.c_void_p),
+        ("cand_count", ctypes.c_void_p), ("C_cap", ctypes.c_int), ("scores", ctypes.c_void_p),
+        ("best_pos", ctypes.c_void_p), ("best_score", ctypes.c_void_p), ("status", ctypes.c_void_p),
     ]
 
 
@@ -219,6 +282,16 @@ def _load():
             lib.pldp_verify_sample.restype = ctypes.c_int
             lib.pldp_verify_sample_workspace_size.argtypes = [i32, i32, i32, i32]
             lib.pldp_verify_sample_workspace_size.restype = sz
+            for f, block in (("pldp_cache_append", pldp_cache_append_args), ("pldp_cache_read", pldp_cache_read_args),
+                             ("pldp_attend_cache", pldp_attend_args), ("pldp_rank_cache", pldp_rank_cache_args)):
+                getattr(lib, f).argtypes = [ctypes.POINTER(block), P]
+                getattr(lib, f).restype = ctypes.c_int
+            lib.pldp_attend_workspace_size.argtypes = [i32, i32, i32, i32, i32]
+            lib.pldp_attend_workspace_size.restype = sz
+            lib.pldp_token_logprobs.argtypes = [P, i32, i64, i32, f32, P, P, P, i32, P, P, P, sz, P]
+            lib.pldp_token_logprobs.restype = ctypes.c_int
+            lib.pldp_token_logprobs_workspace_size.argtypes = [i64, i32]
+            lib.pldp_token_logprobs_workspace_size.restype = sz
             lib.pldp_last_error.argtypes = []
             lib.pldp_last_error.restype = ctypes.c_char_p
             lib.pldp_version.argtypes = []
@@ -701,6 +774,213 @@ def pldp_verify_greedy_noalloc(logits, draft, draft_len, accept_len, next_token,
         p_ids, stride, _dense(seq_len, "seq_len", torch.int32, allow_none=True, n=B), T_cap,
         _dense(kv_keep_len, "kv_keep_len", torch.int32, allow_none=True, n=B),
         _dense(status, "status", _WORD, allow_none=True, n=B), _stream(stream)))
+
+
+# ----------------------------------------------------------------------------
+# the target model's cache around a step
+# ----------------------------------------------------------------------------
+class pldp_cache:
+    """One layer's paged cache, for the calls below: the description of pldp_cache in
+    include/pldp.h, made and checked once (it keeps the tensors alive).
+
+    k_cache, v_cache   CUDA tensors seen as [n_pages, page_size, heads, head_dim], bfloat16 or
+                       float8_e4m3fn, of the same shape and strides with unit inner stride
+                       (a pool held as [n_pages, heads, page_size, head_dim] is passed
+                       as ``pool.permute(0, 2, 1, 3)``).
+    pages              int32 [B, max_pages], rows may be strided.
+    k_scale, v_scale   float32 [n_pages, heads, page_size], contiguous, for float8_e4m3fn.
+    """
+
+    def __init__(self, k_cache, v_cache, pages, k_scale=None, v_scale=None):
+        kinds = {torch.bfloat16: PLDP_BF16, torch.float8_e4m3fn: PLDP_E4M3}
+        for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+            _dev(t, name)
+            if t.dim() != 4 or t.stride(3) != 1 or t.dtype not in kinds:
+                raise ValueError(f"{name} must be [n_pages, page_size, heads, head_dim] with unit inner stride, bfloat16 or "
+                                 "float8_e4m3fn")
+        if k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride() or k_cache.dtype != v_cache.dtype:
+            raise ValueError("k_cache and v_cache must have the same shape, strides and dtype")
+        n_pages, page_size, heads, head_dim = k_cache.shape
+        p_pages, stride, max_pages = _rows(pages, "pages")
+        a = self.args = pldp_cache_args()
+        a.k, a.v, a.dtype = _dev(k_cache, "k_cache"), _dev(v_cache, "v_cache"), kinds[k_cache.dtype]
+        if a.dtype == PLDP_E4M3:
+            for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+                if t is None or tuple(t.shape) != (n_pages, heads, page_size):
+                    raise ValueError(f"{name} must be [n_pages, heads, page_size] for a float8_e4m3fn cache")
+            a.k_scale, a.v_scale = _dense(k_scale, "k_scale", torch.float32), _dense(v_scale, "v_scale", torch.float32)
+        elif k_scale is not None or v_scale is not None:
+            raise ValueError("k_scale and v_scale belong to a float8_e4m3fn cache")
+        a.n_pages, a.page_size, a.heads, a.head_dim = n_pages, page_size, heads, head_dim
+        a.page_stride, a.pos_stride, a.head_stride = k_cache.stride()[:3]
+        a.pages, a.pages_stride, a.max_pages = p_pages, stride, max_pages
+        self.B, self.heads, self.head_dim, self.dtype = pages.shape[0], heads, head_dim, k_cache.dtype
+        self.tensors = (k_cache, v_cache, pages, k_scale, v_scale)
+
+
+def _vectors(t, name, shape, dtypes):
+    """A [sequences, tokens, heads, head_dim] tensor of `shape` (None: any) with unit inner
+    stride; returns (pointer, its three strides)."""
+    p = _dev(t, name)
+    if t.dim() != 4 or t.stride(3) != 1 or t.dtype not in dtypes:
+        raise ValueError(f"{name} must be [B, n, heads, head_dim] of {' or '.join(map(str, dtypes))} with unit inner stride")
+    if any(w is not None and w != g for w, g in zip(shape, t.shape)):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, the call needs {shape}")
+    return p, _STRIDES(*t.stride()[:3])
+
+
+def _step_cache(cache, B):
+    if not isinstance(cache, pldp_cache):
+        raise ValueError("cache must be a pldp_cache")
+    if B > cache.B:
+        raise ValueError(f"the cache's page table has {cache.B} rows, the call needs {B}")
+    return cache.args
+
+
+def pldp_cache_append(cache, q, k, v, seq_len, q_out, draft_len=None, q_norm=None, k_norm=None, eps=1e-6, cos=None,
+                      sin=None, interleaved=False, status=None, stream=None):
+    """Norms (q_norm / k_norm [head_dim], optional) and rotates (cos / sin float32 [positions,
+    rot/2], optional) the queries and keys of a step's tokens, x_t and the draft at positions
+    seq_len[b]-1 .. seq_len[b]-1+draft_len[b], writes the queries to q_out (bfloat16) and the keys
+    and values to the cache.  q [B, n, q_heads, head_dim], k and v [B, n, heads, head_dim], float32
+    or bfloat16, any strides of whole 16 bytes with unit inner stride (slices of one projection)."""
+    kinds = (torch.float32, torch.bfloat16)
+    a = pldp_cache_append_args()
+    a.q, a.q_strides = _vectors(q, "q", (None,) * 4, kinds)
+    B, n, Hq, D = q.shape
+    a.cache = _step_cache(cache, B)
+    if D != cache.head_dim:
+        raise ValueError(f"q has head_dim {D}, the cache {cache.head_dim}")
+    a.k, a.k_strides = _vectors(k, "k", (B, n, cache.heads, D), (q.dtype,))
+    a.v, a.v_strides = _vectors(v, "v", (B, n, cache.heads, D), (q.dtype,))
+    a.q_out, a.q_out_strides = _vectors(q_out, "q_out", (B, n, Hq, D), (torch.bfloat16,))
+    a.dtype, a.B, a.n, a.q_heads, a.eps = _code(q.dtype), B, n, Hq, float(eps)
+    a.q_norm = _dense(q_norm, "q_norm", q.dtype, allow_none=True, n=D)
+    a.k_norm = _dense(k_norm, "k_norm", q.dtype, allow_none=True, n=D)
+    if cos is not None or sin is not None:
+        if cos is None or sin is None or cos.dim() != 2 or cos.shape != sin.shape:
+            raise ValueError("cos and sin must both be [positions, rot/2]")
+        a.cos, a.sin = _dense(cos, "cos", torch.float32), _dense(sin, "sin", torch.float32)
+        a.rot_rows, a.rot = cos.shape[0], 2 * cos.shape[1]
+    a.interleaved = int(bool(interleaved))
+    a.seq_len = _dense(seq_len, "seq_len", torch.int32, n=B)
+    a.draft_len = _dense(draft_len, "draft_len", torch.int32, allow_none=True, n=B)
+    a.status = _dense(status, "status", _WORD, allow_none=True, n=B)
+    _check("pldp_cache_append", _load().pldp_cache_append(ctypes.byref(a), _stream(stream)))
+
+
+def pldp_cache_read(cache, start, count, k_out, v_out, status=None, stream=None):
+    """Positions start[b] .. start[b]+count[b]-1 (start None: from 0) of every sequence into rows
+    0 .. count[b]-1 of k_out and v_out [B, n, heads, head_dim], float32 or bfloat16 and of the same
+    strides; either may be None."""
+    one = k_out if k_out is not None else v_out
+    a = pldp_cache_read_args()
+    p, a.out_strides = _vectors(one, "k_out" if one is k_out else "v_out", (None,) * 4, (torch.float32, torch.bfloat16))
+    B, n = one.shape[:2]
+    a.cache = _step_cache(cache, B)
+    shape = (B, n, cache.heads, cache.head_dim)
+    for name, t in (("k_out", k_out), ("v_out", v_out)):
+        if t is not None:
+            setattr(a, name, _vectors(t, name, shape, (one.dtype,))[0])
+            if t.stride() != one.stride():
+                raise ValueError("k_out and v_out must have the same strides")
+    a.start = _dense(start, "start", torch.int32, allow_none=True, n=B)
+    a.count = _dense(count, "count", torch.int32, n=B)
+    a.B, a.n, a.dtype = B, n, _code(one.dtype)
+    a.status = _dense(status, "status", _WORD, allow_none=True, n=B)
+    _check("pldp_cache_read", _load().pldp_cache_read(ctypes.byref(a), _stream(stream)))
+
+
+def pldp_attend_workspace_size(B, n, q_heads, heads, head_dim) -> int:
+    return int(_load().pldp_attend_workspace_size(B, n, q_heads, heads, head_dim))
+
+
+def pldp_attend_cache(cache, q, seq_len, out, workspace, draft_len=None, lse=None, scale=None, status=None, stream=None):
+    """Attention of a step's tokens (x_t and the draft, appended before) over the cache.  q and
+    out bfloat16 [B, n, q_heads, head_dim]; lse float32 [B, n, q_heads] (optional); scale default
+    1/sqrt(head_dim).  workspace: uint8 CUDA tensor of pldp_attend_workspace_size(B, n, q_heads,
+    heads, head_dim) bytes, zeroed once before first use."""
+    a = pldp_attend_args()
+    a.q, a.q_strides = _vectors(q, "q", (None,) * 4, (torch.bfloat16,))
+    B, n, Hq, D = q.shape
+    a.cache = _step_cache(cache, B)
+    if D != cache.head_dim:
+        raise ValueError(f"q has head_dim {D}, the cache {cache.head_dim}")
+    a.out, a.out_strides = _vectors(out, "out", (B, n, Hq, D), (torch.bfloat16,))
+    a.B, a.n, a.q_heads = B, n, Hq
+    a.scale = D ** -0.5 if scale is None else float(scale)
+    a.seq_len = _dense(seq_len, "seq_len", torch.int32, n=B)
+    a.draft_len = _dense(draft_len, "draft_len", torch.int32, allow_none=True, n=B)
+    a.lse = _dense(lse, "lse", torch.float32, allow_none=True, n=B * n * Hq)
+    a.status = _dense(status, "status", _WORD, allow_none=True, n=B)
+    a.workspace = _dense(workspace, "workspace")
+    a.workspace_bytes = workspace.numel() * workspace.element_size()
+    _check("pldp_attend_cache", _load().pldp_attend_cache(ctypes.byref(a), _stream(stream)))
+
+
+def pldp_rank_cache(cache, q, row, kv_len, lse, cand_pos, cand_count, best_pos, heads=None, agg=PLDP_AGG_MAX, scale=None,
+                    scores=None, best_score=None, accumulate=False, status=None, stream=None):
+    """Eq. 2 from one layer's cache: candidate j scores the max (or sum) over the selected query
+    heads (int32 `heads`, None: all) of the attention probability exp(scale q.k_j - lse) of query
+    row[b] (None: 0) of the step, with q and lse as pldp_attend_cache had and wrote them.  After
+    verification row is accept_len and kv_len is kv_keep_len.  accumulate: scores holds other
+    layers' scores and takes the larger (or the sum)."""
+    a = pldp_rank_cache_args()
+    a.q, a.q_strides = _vectors(q, "q", (None,) * 4, (torch.bfloat16,))
+    B, n, Hq, D = q.shape
+    a.cache = _step_cache(cache, B)
+    if D != cache.head_dim:
+        raise ValueError(f"q has head_dim {D}, the cache {cache.head_dim}")
+    if not isinstance(cand_pos, torch.Tensor) or cand_pos.dim() != 2 or cand_pos.shape[0] < B:
+        raise ValueError("cand_pos must be [B, C_cap]")
+    a.B, a.n, a.q_heads, a.C_cap = B, n, Hq, cand_pos.shape[1]
+    a.row = _dense(row, "row", torch.int32, allow_none=True, n=B)
+    a.kv_len = _dense(kv_len, "kv_len", torch.int32, n=B)
+    a.lse = _dense(lse, "lse", torch.float32, n=B * n * Hq)
+    a.heads = _dense(heads, "heads", torch.int32, allow_none=True)
+    a.n_sel = 0 if heads is None else heads.numel()
+    if heads is not None and a.n_sel < 1:                # an empty tensor's null pointer would mean all heads
+        raise PldpError("pldp_rank_cache", PLDP_ERR_INVALID_ARG, "n_sel < 1")
+    a.agg = {"max": PLDP_AGG_MAX, "sum": PLDP_AGG_SUM}.get(agg, agg)
+    a.accumulate = int(bool(accumulate))
+    a.scale = D ** -0.5 if scale is None else float(scale)
+    a.cand_pos = _dense(cand_pos, "cand_pos", torch.int32)
+    a.cand_count = _dense(cand_count, "cand_count", torch.int32, n=B)
+    a.scores = _dense(scores, "scores", torch.float32, allow_none=True, n=B * cand_pos.shape[1])
+    a.best_pos = _dense(best_pos, "best_pos", torch.int32, n=B)
+    a.best_score = _dense(best_score, "best_score", torch.float32, allow_none=True, n=B)
+    a.status = _dense(status, "status", _WORD, allow_none=True, n=B)
+    _check("pldp_rank_cache", _load().pldp_rank_cache(ctypes.byref(a), _stream(stream)))
+
+
+def pldp_token_logprobs_workspace_size(rows, V) -> int:
+    return int(_load().pldp_token_logprobs_workspace_size(rows, V))
+
+
+def pldp_token_logprobs(logits, tokens, logprob, workspace, entropy=None, top_id=None, top_logprob=None, temperature=1.0,
+                        stream=None):
+    """Log probabilities under softmax(logits / temperature) of tokens (int32 [...], logprob float32
+    [...]; both None for neither), the entropy (float32 [...], optional) and the likeliest
+    alternatives (top_id int32 and top_logprob float32 [..., top], optional, top <= 32) of every row
+    of logits [..., V] (float32 or bfloat16, contiguous).  workspace: uint8 CUDA tensor of
+    pldp_token_logprobs_workspace_size(rows, V) bytes."""
+    p = _dense(logits, "logits")
+    if logits.dim() < 1 or logits.shape[-1] < 1:
+        raise ValueError("logits must be [..., V]")
+    V = logits.shape[-1]
+    rows = logits.numel() // V
+    tops = {t.shape[-1] if t.dim() else 0 for t in (top_id, top_logprob) if t is not None}
+    if len(tops) > 1:
+        raise ValueError("top_id and top_logprob must have the same last dimension")
+    top = tops.pop() if tops else 0
+    _check("pldp_token_logprobs", _load().pldp_token_logprobs(
+        p, _code(logits.dtype), rows, V, float(temperature),
+        _dense(tokens, "tokens", torch.int32, allow_none=True, n=rows),
+        _dense(logprob, "logprob", torch.float32, allow_none=True, n=rows),
+        _dense(entropy, "entropy", torch.float32, allow_none=True, n=rows), top,
+        _dense(top_id, "top_id", torch.int32, allow_none=True, n=rows * top),
+        _dense(top_logprob, "top_logprob", torch.float32, allow_none=True, n=rows * top),
+        _dense(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
 def pldp_version() -> int:

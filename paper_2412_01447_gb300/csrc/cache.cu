@@ -1,0 +1,432 @@
+// The paged cache around a step: pldp_cache_append and pldp_cache_read.
+#include <cuda_fp8.h>
+#include <math.h>
+
+#include "pldp_cache.cuh"
+
+namespace pldp {
+
+pldp_status check_rows(const char* fn, const char* name, const void* p, const int64_t* strides, size_t es) {
+    if (!aligned16(p)) return fail(PLDP_ERR_INVALID_ARG, "%s: %s is not 16-byte aligned", fn, name);
+    const int64_t v = static_cast<int64_t>(16 / es);
+    for (int i = 0; i < 3; ++i)
+        if (strides[i] < 0 || strides[i] % v)
+            return fail(PLDP_ERR_INVALID_ARG, "%s: %s strides must be multiples of 16 bytes", fn, name);
+    return PLDP_OK;
+}
+
+pldp_status cache_view(const char* fn, const pldp_cache& c, int B, CacheView* out) {
+    if (c.dtype != PLDP_BF16 && c.dtype != PLDP_E4M3)
+        return fail(PLDP_ERR_UNSUPPORTED, "%s: cache dtype %d", fn, static_cast<int>(c.dtype));
+    if (c.heads < 1 || c.heads > 1024 || c.head_dim < 16 || c.head_dim > kMaxHeadDim || c.head_dim % 16)
+        return fail(PLDP_ERR_UNSUPPORTED, "%s: %d cache heads of %d (1..1024 heads, a multiple of 16 up to %d)", fn,
+                    c.heads, c.head_dim, kMaxHeadDim);
+    if (c.n_pages < 1 || c.page_size < 1 || c.max_pages < 1 || c.pages_stride < c.max_pages)
+        return fail(PLDP_ERR_INVALID_ARG, "%s: n_pages, page_size and max_pages must be >= 1, pages_stride >= max_pages", fn);
+    const int64_t capacity = static_cast<int64_t>(c.max_pages) * c.page_size;
+    if (capacity > INT32_MAX) return fail(PLDP_ERR_INVALID_ARG, "%s: max_pages * page_size must be below 2^31", fn);
+    const int es = c.dtype == PLDP_BF16 ? 2 : 1;
+    const int64_t strides[3] = {c.page_stride, c.pos_stride, c.head_stride};
+    if (B > 0) {
+        if (!c.k || !c.v || !c.pages) return fail(PLDP_ERR_INVALID_ARG, "%s: null cache pointer", fn);
+        if (c.dtype == PLDP_E4M3 && (!c.k_scale || !c.v_scale))
+            return fail(PLDP_ERR_INVALID_ARG, "%s: a PLDP_E4M3 cache needs k_scale and v_scale", fn);
+        pldp_status st = check_rows(fn, "cache.k", c.k, strides, es);
+        if (st == PLDP_OK) st = check_rows(fn, "cache.v", c.v, strides, es);
+        if (st != PLDP_OK) return st;
+    }
+    CacheView& w = *out;
+    w.k = static_cast<uint8_t*>(c.k);
+    w.v = static_cast<uint8_t*>(c.v);
+    w.k_scale = c.k_scale;
+    w.v_scale = c.v_scale;
+    w.pages = c.pages;
+    w.pages_stride = c.pages_stride;
+    w.page_stride = c.page_stride * es;
+    w.pos_stride = c.pos_stride * es;
+    w.head_stride = c.head_stride * es;
+    w.n_pages = c.n_pages;
+    w.page_size = c.page_size;
+    w.heads = c.heads;
+    w.head_dim = c.head_dim;
+    w.max_pages = c.max_pages;
+    w.capacity = static_cast<int>(capacity);
+    w.vec_bytes = c.head_dim * es;
+    uint32_t l = 0;
+    while ((uint64_t(1) << l) < static_cast<uint64_t>(c.page_size)) ++l;
+    w.div_shift = l;
+    w.div_mul = static_cast<uint32_t>((((uint64_t(1) << l) - c.page_size) << 32) / c.page_size + 1);
+    return PLDP_OK;
+}
+
+namespace {
+
+// ---------------------------------------------------------------------------
+// append
+// ---------------------------------------------------------------------------
+struct Strides {
+    int64_t seq, tok, head;
+};
+
+struct AppendArgs {
+    CacheView c;
+    const void *q, *k, *v, *q_norm, *k_norm;
+    void* q_out;
+    Strides qs, ks, vs, os;
+    const float *cos, *sin;
+    const int32_t *seq_len, *draft_len;
+    uint32_t* status;
+    int n, q_heads, rot, interleaved, capacity, per;   // per: vectors a CTA takes
+    float eps;
+};
+
+constexpr int kAppendThreads = 128;
+
+// Eight elements as floats.
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8]) {
+    const uint4 r = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
+    x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+}
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&p);
+}
+__device__ __forceinline__ uint4 bf16_8(const float (&x)[8]) {
+    return make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
+}
+__device__ __forceinline__ uint32_t e4m3_quad(float a, float b, float c, float d) {
+    return static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3)) |
+           static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3)) << 16;
+}
+
+// One CTA takes `per` of one token's vectors (its query heads, then key heads, then value
+// heads), GS lanes a vector, eight elements a lane.  A lane's place in the vector is the
+// same for all of them, so the rotation's cosines and sines and the norms' weights are
+// loaded once and stay in registers.
+template <typename T, int GS, bool E4M3>
+__global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const AppendArgs a) {
+    pdl_enter();
+    constexpr int kGroups = kAppendThreads / GS;
+    __shared__ __align__(16) float stage[kGroups][GS * 8];
+    const CacheView& c = a.c;
+    const int b = blockIdx.x / a.n, i = blockIdx.x - b * a.n;
+    uint32_t st;
+    const StepTokens tk = step_tokens(a.seq_len, a.draft_len, b, a.n, a.capacity, st);
+    if (i == 0 && blockIdx.y == 0 && threadIdx.x == 0 && st && a.status) atomicOr(a.status + b, st);
+    if (i >= tk.count) return;
+    const int pos = tk.first + i, D = c.head_dim;
+    const int g = threadIdx.x / GS, at = threadIdx.x % GS, e0 = at * 8;
+    const bool in = e0 < D;
+    // the lanes of this vector's group: they take the same branches
+    const unsigned mates = GS == 32 ? 0xFFFFFFFFu : ((1u << (GS % 32)) - 1u) << ((threadIdx.x & 31) / GS * GS);
+
+    int64_t scale_at;
+    const int64_t off = locate(c, c.pages + b * c.pages_stride, pos, scale_at);
+    if (off < 0 && blockIdx.y == 0 && threadIdx.x == 0 && a.status) atomicOr(a.status + b, PLDP_ST_PAGE);
+
+    // y' = y cs + partner sn; elements that do not rotate: cs = 1, sn = 0, their own partner
+    float cs[8], sn[8], wq[8], wk[8];
+    const int half = a.rot >> 1;
+    const float* cr = a.cos ? a.cos + static_cast<int64_t>(pos) * half : nullptr;
+    const float* sr = a.cos ? a.sin + static_cast<int64_t>(pos) * half : nullptr;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int e = e0 + j;
+        cs[j] = 1.f, sn[j] = 0.f;
+        if (e < a.rot) {
+            const int p = a.interleaved ? e >> 1 : e < half ? e : e - half;
+            const bool second = a.interleaved ? e & 1 : e >= half;
+            cs[j] = __ldg(cr + p);
+            sn[j] = second ? __ldg(sr + p) : -__ldg(sr + p);
+        }
+        wq[j] = wk[j] = 1.f;
+    }
+    if (in && a.q_norm) load8(static_cast<const T*>(a.q_norm) + e0, wq);
+    if (in && a.k_norm) load8(static_cast<const T*>(a.k_norm) + e0, wk);
+
+    const int total = a.q_heads + 2 * c.heads;
+    const int lo = blockIdx.y * a.per, hi = min(lo + a.per, total);
+    for (int h0 = lo; h0 < hi; h0 += kGroups) {            // the same number of turns for every thread
+        const int h = h0 + g;
+        const bool live = h < hi && in;
+        const int kind = h < a.q_heads ? 0 : h < a.q_heads + c.heads ? 1 : 2;
+        const int head = kind == 0 ? h : kind == 1 ? h - a.q_heads : h - a.q_heads - c.heads;
+        const Strides& s = kind == 0 ? a.qs : kind == 1 ? a.ks : a.vs;
+        const T* src = static_cast<const T*>(kind == 0 ? a.q : kind == 1 ? a.k : a.v);
+        float y[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = 0.f;
+        if (live) load8(src + b * s.seq + i * s.tok + head * s.head + e0, y);
+        if (kind == 0 ? a.q_norm != nullptr : kind == 1 && a.k_norm != nullptr) {
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum = fmaf(y[j], y[j], sum);
+#pragma unroll
+            for (int o = GS / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(mates, sum, o, GS);
+            const float r = rsqrtf(sum / D + a.eps);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = y[j] * r * (kind == 0 ? wq[j] : wk[j]);
+        }
+        if (a.rot) {
+            if (a.interleaved) {
+                if (kind < 2) {
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2) {
+                        const float p = y[j], q = y[j + 1];
+                        y[j] = p * cs[j] + q * sn[j];
+                        y[j + 1] = q * cs[j + 1] + p * sn[j + 1];
+                    }
+                }
+            } else {
+                float* row = stage[g];
+                *reinterpret_cast<float4*>(row + e0) = make_float4(y[0], y[1], y[2], y[3]);
+                *reinterpret_cast<float4*>(row + e0 + 4) = make_float4(y[4], y[5], y[6], y[7]);
+                __syncwarp(mates);
+                if (kind < 2) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int e = e0 + j;
+                        if (e < a.rot) y[j] = y[j] * cs[j] + row[e < half ? e + half : e - half] * sn[j];
+                    }
+                }
+                __syncwarp(mates);
+            }
+        }
+        if (kind == 0) {
+            if (live)
+                *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.q_out) + b * a.os.seq + i * a.os.tok +
+                                          head * a.os.head + e0) = bf16_8(y);
+            continue;
+        }
+        if (off < 0) continue;
+        uint8_t* dst = (kind == 1 ? c.k : c.v) + off + head * c.head_stride;
+        if constexpr (E4M3) {
+            float m = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(y[j]));
+#pragma unroll
+            for (int o = GS / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(mates, m, o, GS));
+            const float scale = m > 0.f ? m / 448.f : 1.f;
+            if (live) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] /= scale;
+                *reinterpret_cast<uint2*>(dst + e0) = make_uint2(e4m3_quad(y[0], y[1], y[2], y[3]), e4m3_quad(y[4], y[5], y[6], y[7]));
+                if (at == 0)
+                    (kind == 1 ? c.k_scale : c.v_scale)[scale_at + static_cast<int64_t>(head) * c.page_size] = scale;
+            }
+        } else if (live) {
+            *reinterpret_cast<uint4*>(dst + 2 * e0) = bf16_8(y);
+        }
+    }
+}
+
+template <typename T, bool E4M3>
+cudaError_t launch_append(const AppendArgs& a, dim3 grid, cudaStream_t s) {
+    if (a.c.head_dim <= 64) return launch_pdl(cache_append_kernel<T, 8, E4M3>, grid, dim3(kAppendThreads), 0, s, 0, a);
+    if (a.c.head_dim <= 128) return launch_pdl(cache_append_kernel<T, 16, E4M3>, grid, dim3(kAppendThreads), 0, s, 0, a);
+    return launch_pdl(cache_append_kernel<T, 32, E4M3>, grid, dim3(kAppendThreads), 0, s, 0, a);
+}
+
+// ---------------------------------------------------------------------------
+// read
+// ---------------------------------------------------------------------------
+struct ReadArgs {
+    CacheView c;
+    const int32_t *start, *count;
+    void *k_out, *v_out;
+    Strides os;
+    uint32_t* status;
+    int n, per;   // per: positions a CTA takes
+};
+
+constexpr int kReadThreads = 256;
+
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) { *reinterpret_cast<uint4*>(p) = bf16_8(x); }
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+}
+__device__ __forceinline__ float2 e4m3_two(uint32_t codes) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(codes), __NV_E4M3);
+    return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+
+// One thread takes 16 bytes of one vector of keys and the same of values.
+template <typename O, bool E4M3>
+__global__ void __launch_bounds__(kReadThreads) cache_read_kernel(const ReadArgs a) {
+    pdl_enter();
+    const CacheView& c = a.c;
+    const int b = blockIdx.y;
+    int first = a.start ? __ldg(a.start + b) : 0, count = __ldg(a.count + b);
+    uint32_t st = 0;
+    if (count < 0 || count > a.n) {
+        st |= PLDP_ST_SEQ_LEN;
+        count = count < 0 ? 0 : a.n;
+    }
+    if (first < 0 || first > c.capacity) {
+        st |= PLDP_ST_CAPACITY;
+        count = 0;
+    } else if (count > c.capacity - first) {
+        st |= PLDP_ST_CAPACITY;
+        count = c.capacity - first;
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0 && st && a.status) atomicOr(a.status + b, st);
+    const int lo = blockIdx.x * a.per, hi = min(lo + a.per, count);
+    const uint32_t chunks = c.vec_bytes / 16, row = chunks * c.heads;
+    const uint32_t items = hi > lo ? static_cast<uint32_t>(hi - lo) * row : 0u;
+    const int32_t* table = c.pages + b * c.pages_stride;
+    for (uint32_t t = threadIdx.x; t < items; t += kReadThreads) {
+        const uint32_t r = t / row, in = t - r * row, head = in / chunks, ch = in - head * chunks;
+        const int i = lo + static_cast<int>(r);
+        int64_t scale_at;
+        const int64_t off = locate(c, table, first + i, scale_at);
+        if (off < 0 && in == 0 && a.status) atomicOr(a.status + b, PLDP_ST_PAGE);
+        const int64_t to = b * a.os.seq + i * a.os.tok + head * a.os.head + ch * (E4M3 ? 16 : 8);
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            O* out = static_cast<O*>(w ? a.v_out : a.k_out);
+            if (!out) continue;
+            uint4 raw = make_uint4(0u, 0u, 0u, 0u);
+            if (off >= 0) raw = ld_stream16((w ? c.v : c.k) + off + head * c.head_stride + ch * 16);
+            if constexpr (E4M3) {
+                const float scale =
+                    off >= 0 ? __ldg((w ? c.v_scale : c.k_scale) + scale_at + static_cast<int64_t>(head) * c.page_size) : 0.f;
+                const uint32_t q[4] = {raw.x, raw.y, raw.z, raw.w};
+                float x[8];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float2 lo2 = e4m3_two(q[k] & 0xFFFFu), hi2 = e4m3_two(q[k] >> 16);
+                    const int j = (k & 1) * 4;
+                    x[j] = lo2.x * scale, x[j + 1] = lo2.y * scale, x[j + 2] = hi2.x * scale, x[j + 3] = hi2.y * scale;
+                    if (k & 1) store8(out + to + (k >> 1) * 8, x);
+                }
+            } else {
+                const uint32_t q[4] = {raw.x, raw.y, raw.z, raw.w};
+                float x[8];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    x[2 * k] = __uint_as_float(q[k] << 16);
+                    x[2 * k + 1] = __uint_as_float(q[k] & 0xFFFF0000u);
+                }
+                store8(out + to, x);
+            }
+        }
+    }
+}
+
+Strides strides_of(const int64_t (&s)[3]) { return {s[0], s[1], s[2]}; }
+
+}  // namespace
+}  // namespace pldp
+
+using namespace pldp;
+
+extern "C" {
+
+PLDP_API pldp_status pldp_cache_append(const pldp_cache_append_args* p, void* stream) {
+    const char* fn = "cache_append";
+    if (!p) return fail(PLDP_ERR_INVALID_ARG, "%s: null argument block", fn);
+    if (p->B < 0 || p->n < 1 || p->q_heads < 1)
+        return fail(PLDP_ERR_INVALID_ARG, "%s: B < 0, n < 1 or q_heads < 1", fn);
+    if (p->dtype != PLDP_F32 && p->dtype != PLDP_BF16)
+        return fail(PLDP_ERR_UNSUPPORTED, "%s: dtype %d", fn, static_cast<int>(p->dtype));
+    if (p->q_heads > 65536) return fail(PLDP_ERR_UNSUPPORTED, "%s: more than 65536 query heads", fn);
+    AppendArgs a = {};
+    pldp_status st = cache_view(fn, p->cache, p->B, &a.c);
+    if (st != PLDP_OK) return st;
+    if ((p->cos == nullptr) != (p->sin == nullptr)) return fail(PLDP_ERR_INVALID_ARG, "%s: cos and sin go together", fn);
+    if (p->cos && (p->rot < 2 || p->rot > p->cache.head_dim || p->rot % 2 || p->rot_rows < 1))
+        return fail(PLDP_ERR_INVALID_ARG, "%s: rot must be even, 2..head_dim, and rot_rows >= 1", fn);
+    if (!(p->eps >= 0.f) || !isfinite(p->eps)) return fail(PLDP_ERR_INVALID_ARG, "%s: eps must be finite and >= 0", fn);
+    if (static_cast<int64_t>(p->B) * p->n > INT32_MAX)
+        return fail(PLDP_ERR_UNSUPPORTED, "%s: B * n must be below 2^31", fn);
+    if (p->B == 0) return PLDP_OK;
+    if (!p->q || !p->k || !p->v || !p->q_out || !p->seq_len) return fail(PLDP_ERR_INVALID_ARG, "%s: null pointer", fn);
+    const size_t es = p->dtype == PLDP_F32 ? 4 : 2;
+    if ((st = check_rows(fn, "q", p->q, p->q_strides, es)) != PLDP_OK) return st;
+    if ((st = check_rows(fn, "k", p->k, p->k_strides, es)) != PLDP_OK) return st;
+    if ((st = check_rows(fn, "v", p->v, p->v_strides, es)) != PLDP_OK) return st;
+    if ((st = check_rows(fn, "q_out", p->q_out, p->q_out_strides, 2)) != PLDP_OK) return st;
+    if (!aligned16(p->q_norm) || !aligned16(p->k_norm) || !aligned16(p->cos) || !aligned16(p->sin))
+        return fail(PLDP_ERR_INVALID_ARG, "%s: norms, cos and sin must be 16-byte aligned", fn);
+    a.q = p->q, a.k = p->k, a.v = p->v;
+    a.q_norm = p->q_norm, a.k_norm = p->k_norm;
+    a.q_out = p->q_out;
+    a.qs = strides_of(p->q_strides), a.ks = strides_of(p->k_strides), a.vs = strides_of(p->v_strides);
+    a.os = strides_of(p->q_out_strides);
+    a.cos = p->cos, a.sin = p->sin;
+    a.seq_len = p->seq_len, a.draft_len = p->draft_len;
+    a.status = p->status;
+    a.n = p->n, a.q_heads = p->q_heads;
+    a.rot = p->cos ? p->rot : 0, a.interleaved = p->interleaved != 0;
+    a.capacity = a.c.capacity;
+    if (p->cos && p->rot_rows < a.capacity) a.capacity = static_cast<int>(p->rot_rows);
+    a.eps = p->eps;
+    // a token's vectors over enough CTAs that two fit an SM's share of a small batch, no more
+    // than one turn of a CTA's groups each
+    const int total = p->q_heads + 2 * p->cache.heads, tokens = p->B * p->n;
+    const int groups = kAppendThreads / (p->cache.head_dim <= 64 ? 8 : p->cache.head_dim <= 128 ? 16 : 32);
+    const int most = (total + groups - 1) / groups;
+    int split = (8 * sm_count() + tokens - 1) / tokens;
+    split = split < 1 ? 1 : split > most ? most : split;
+    const int turns = (most + split - 1) / split;
+    a.per = turns * groups;
+    const dim3 grid(tokens, (total + a.per - 1) / a.per);
+    auto s = static_cast<cudaStream_t>(stream);
+    const bool q8 = p->cache.dtype == PLDP_E4M3;
+    cudaError_t e;
+    if (p->dtype == PLDP_F32) e = q8 ? launch_append<float, true>(a, grid, s) : launch_append<float, false>(a, grid, s);
+    else e = q8 ? launch_append<__nv_bfloat16, true>(a, grid, s) : launch_append<__nv_bfloat16, false>(a, grid, s);
+    if (e != cudaSuccess) return fail(PLDP_ERR_CUDA, "%s: launch failed: %s", fn, cudaGetErrorString(e));
+    return check_launch(fn);
+}
+
+PLDP_API pldp_status pldp_cache_read(const pldp_cache_read_args* p, void* stream) {
+    const char* fn = "cache_read";
+    if (!p) return fail(PLDP_ERR_INVALID_ARG, "%s: null argument block", fn);
+    if (p->B < 0 || p->n < 0) return fail(PLDP_ERR_INVALID_ARG, "%s: B < 0 or n < 0", fn);
+    if (p->B > 65535) return fail(PLDP_ERR_UNSUPPORTED, "%s: more than 65535 sequences", fn);
+    if (p->dtype != PLDP_F32 && p->dtype != PLDP_BF16)
+        return fail(PLDP_ERR_UNSUPPORTED, "%s: dtype %d", fn, static_cast<int>(p->dtype));
+    ReadArgs a = {};
+    pldp_status st = cache_view(fn, p->cache, p->B, &a.c);
+    if (st != PLDP_OK) return st;
+    if (p->B == 0 || p->n == 0) return PLDP_OK;
+    if (!p->count) return fail(PLDP_ERR_INVALID_ARG, "%s: null pointer", fn);
+    const size_t es = p->dtype == PLDP_F32 ? 4 : 2;
+    if ((st = check_rows(fn, "k_out", p->k_out, p->out_strides, es)) != PLDP_OK) return st;
+    if ((st = check_rows(fn, "v_out", p->v_out, p->out_strides, es)) != PLDP_OK) return st;
+    a.start = p->start, a.count = p->count;
+    a.k_out = p->k_out, a.v_out = p->v_out;
+    a.os = strides_of(p->out_strides);
+    a.status = p->status;
+    a.n = p->n;
+    // about four 16-byte pieces a thread, at least one position a CTA
+    const int row = a.c.vec_bytes / 16 * a.c.heads;
+    a.per = 4 * kReadThreads / row;
+    if (a.per < 1) a.per = 1;
+    const dim3 grid((p->n + a.per - 1) / a.per, p->B);
+    auto s = static_cast<cudaStream_t>(stream);
+    const bool q8 = p->cache.dtype == PLDP_E4M3;
+    cudaError_t e;
+    if (p->dtype == PLDP_F32)
+        e = q8 ? launch_pdl(cache_read_kernel<float, true>, grid, dim3(kReadThreads), 0, s, 0, a)
+               : launch_pdl(cache_read_kernel<float, false>, grid, dim3(kReadThreads), 0, s, 0, a);
+    else
+        e = q8 ? launch_pdl(cache_read_kernel<__nv_bfloat16, true>, grid, dim3(kReadThreads), 0, s, 0, a)
+               : launch_pdl(cache_read_kernel<__nv_bfloat16, false>, grid, dim3(kReadThreads), 0, s, 0, a);
+    if (e != cudaSuccess) return fail(PLDP_ERR_CUDA, "%s: launch failed: %s", fn, cudaGetErrorString(e));
+    return check_launch(fn);
+}
+
+}  // extern "C"
