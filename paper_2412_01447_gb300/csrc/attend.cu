@@ -260,10 +260,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const AttendArgs a)
         constexpr int kRowChunks = DP * (E4M3 ? 1 : 2) / 16, kRows = kCopyThreads / kRowChunks, kTurns = kTile / kRows;
         const int chunk = t % kRowChunks, row0 = t / kRowChunks;
         const bool in = chunk * 16 < c.vec_bytes;
-        // entry e of the ring: copies of e go out, then the oldest one in flight is handed over
-        constexpr int kLag = E4M3 ? S::kStages - 1 : S::kSlots - 2;
-        auto hand_over = [&](int e) {
-            if constexpr (E4M3) {
+        // Entry e of the ring.  bf16: the copies go straight into the slot and arrive on its barrier by
+        // themselves.  e4m3: they go to this thread's own places in a stage, and the oldest entry in
+        // flight is converted into its slot once it has come in.
+        constexpr int kLag = S::kStages - 1;
+        [[maybe_unused]] auto convert = [&](int e) {
+            {
                 const int slot = e % S::kSlots;
                 if (e >= S::kSlots) wait_for(&col.empty[slot], e / S::kSlots - 1, &col.dead);
                 const uint8_t* from = stages + (e % S::kStages) * S::kStage + t * 16;
@@ -290,17 +292,21 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const AttendArgs a)
             if (w.t0 == 0 && w.unit == 0 && t == 0 && st && a.status) atomicOr(a.status + w.b, st);
             const int64_t head = static_cast<int64_t>(w.unit / a.row_tiles) * c.head_stride;
             const int32_t* table = c.pages + w.b * c.pages_stride;
+            auto look = [&](int tile) {                        // the page of this thread's row, -1: no such position
+                const int pos = tile * kTile + t;
+                return tile < w.t1 && pos < w.keys ? __ldg(table + page_of(pos, c.div_mul, c.div_shift)) : -1;
+            };
+            int page = look(w.t0), page_next = look(w.t0 + 1);
             for (int tile = w.t0; tile < w.t1; ++tile) {
                 const int pos = tile * kTile + t;
-                int64_t off = -1, scale_at;
-                if (pos < w.keys) {
-                    off = locate(c, table, pos, scale_at);
-                    if (off < 0) {
-                        if (a.status) atomicOr(a.status + w.b, PLDP_ST_PAGE);
-                    } else {
-                        off += head;
-                    }
-                }
+                int64_t off = -1;
+                if (static_cast<unsigned>(page) < static_cast<unsigned>(c.n_pages))
+                    off = page * c.page_stride + head +
+                          (pos - static_cast<int>(page_of(pos, c.div_mul, c.div_shift)) * c.page_size) * c.pos_stride;
+                else if (pos < w.keys && a.status)
+                    atomicOr(a.status + w.b, PLDP_ST_PAGE);
+                page = page_next;
+                page_next = look(tile + 2);
                 col.offsets[turn][t] = off;
                 bar_sync(1, kCopyThreads);
                 for (int kv = 0; kv < 2; ++kv) {
@@ -322,10 +328,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const AttendArgs a)
                             copy16(d, o >= 0 ? base + o : base, o >= 0 ? 16 : 0);
                         }
                     }
-                    copy_commit();
-                    if (e >= kLag) {
-                        copy_wait<kLag>();
-                        hand_over(e - kLag);
+                    if constexpr (E4M3) {
+                        copy_commit();
+                        if (e >= kLag) {
+                            copy_wait<kLag>();
+                            convert(e - kLag);
+                        }
+                    } else {
+                        copy_arrive(&col.full[e % S::kSlots]);
                     }
                     ++e;
                 }
@@ -333,9 +343,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const AttendArgs a)
             }
             w.step(a);
         }
-        for (int left = min(e, kLag); left > 0; --left) {
-            copy_wait(left - 1);
-            hand_over(e - left);
+        if constexpr (E4M3) {
+            for (int left = min(e, kLag); left > 0; --left) {
+                copy_wait(left - 1);
+                convert(e - left);
+            }
+        } else {
+            copy_wait<0>();
         }
     } else if (warp == 12) {
         // ---- matrix instructions ----
@@ -349,6 +363,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const AttendArgs a)
             auto scores = [&](int entry, int k) {
                 const int slot = entry % S::kSlots;
                 wait_for(&col.full[slot], entry / S::kSlots, &col.dead);
+                fence_smem_async();
                 tmem_after_sync();
                 const uint64_t op = advance(k_op, slot * S::kSlot);
                 for (int s = 0; s < D / 16; ++s)
@@ -367,6 +382,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const AttendArgs a)
                     wait_for(&col.p_full, tile, &col.dead);
                     const int slot = (e + 1) % S::kSlots;
                     wait_for(&col.full[slot], (e + 1) / S::kSlots, &col.dead);
+                    fence_smem_async();
                     tmem_after_sync();
                     const uint64_t op = advance(v_op, slot * S::kSlot);
 #pragma unroll
