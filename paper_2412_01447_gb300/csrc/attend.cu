@@ -1,772 +1,18 @@
 // Attention of a step's tokens over the paged cache: pldp_attend_cache.
-#include <cuda_fp8.h>
-#include <cuda_fp16.h>
 #include <math.h>
 
-#include "pldp_cache.cuh"
-#include "pldp_tcgen05.cuh"
+#include "pldp_attend.cuh"
 
 namespace pldp {
 namespace {
-
-// ---------------------------------------------------------------------------
-// One pass over the keys, 128 at a time, all query rows of one key/value head at once (the
-// tokens' G = q_heads / heads heads each: up to NT rows, padded).  Both products have the
-// keys or the head's elements as the tensor core's 128 rows and the query rows as its columns,
-// so a few query rows waste nothing:
-//   S^T [128 keys, NT]  = K [128, D] Q^T [D, NT]
-//   O^T [D, NT]        += V^T [D, 128] P^T [128, NT]
-// S^T and O^T stay in tensor memory.  A thread owns one key (a lane of S^T) and half of the
-// columns: it applies the key's scale and the masks, takes weights w = 2^(x - m), adds them to
-// its own sums and writes them to shared memory as the next product's operand.  The running
-// maximum m of a column only moves when a score passes it by more than 2^8: then the column's
-// sums and its accumulators in tensor memory are scaled; otherwise no thread needs another's
-// scores, and the 128 of them agree on that with one barrier.
-//
-// Weights are rounded to 16 bits for the second product: in a bf16 cache as a sum of two bf16
-// (2^-17 of the weight; one alone would add as much error as the result's own rounding), in an
-// e4m3 cache as f16 (2^-12), in which the codes, at most 448, are exact as well.  The scales of an
-// e4m3 cache never touch its codes: k's multiplies the key's scores, v's goes into the exponent
-// (w = vs 2^(x - m), m the maximum of x + log2 vs) and is divided out of the sums.
-//
-// The keys of all sequences and heads form one list of tiles, cut into equal parts, one a CTA
-// (one a SM), so that ragged lengths and few long sequences keep every SM reading to the end.
-// What a CTA holds of a unit (sequence, head, rows) that others share goes to the workspace, and
-// the last of them joins the parts in order.
-// ---------------------------------------------------------------------------
-constexpr int kTile = 128;
-constexpr int kSoftmaxThreads = 256, kCopyThreads = 128, kThreads = kSoftmaxThreads + kCopyThreads + 32;
-constexpr int kMaxCtas = 192;             // parts of the list at most
-constexpr int kMaxShared = 232448;        // bytes a CTA, static and dynamic
-
-struct AttendArgs {
-    CacheView c;
-    const __nv_bfloat16* q;
-    __nv_bfloat16* out;
-    int64_t q_seq, q_tok, q_head, o_seq, o_tok, o_head;
-    const int32_t *seq_len, *draft_len;
-    float *lse, *parts;
-    uint32_t *status, *tickets;
-    int B, n, q_heads, group, row_tiles;
-    float scale2;                          // scale * log2(e)
-};
-
-template <int NT, int DP, bool E4M3>
-struct Shape {
-    static constexpr int kPanels = DP / 64;                    // of 64 elements (128 bytes) each
-    static constexpr int kSlot = kPanels * kTile * 128;        // one tile of keys or values
-    static constexpr int kQ = kPanels * NT * 128;
-    static constexpr int kRow = NT * 2 < 128 ? NT * 2 : 128;   // bytes of a row of P^T (a key's weights)
-    static constexpr int kP = NT * 2 * kTile;
-    static constexpr int kStage = E4M3 ? kTile * DP : 0;       // one tile's codes
-    static constexpr int kRest = kQ + kP * (E4M3 ? 1 : 2);
-    static constexpr int kColumns = NT == 128 ? 9216 : 6144;   // static: Columns
-    static constexpr int kRoom = kMaxShared - 1024 - kColumns - kRest;
-    static constexpr int kSlots = E4M3 ? (DP == 256 ? 2 : 3) : (kRoom / kSlot < 8 ? kRoom / kSlot : 8);
-    static constexpr int kStages = E4M3 ? ((kRoom - kSlots * kSlot) / kStage < 7 ? (kRoom - kSlots * kSlot) / kStage : 7) : 1;
-    static constexpr int kBlocks = DP == 256 ? 2 : 1;          // of 128 rows of O^T
-    static constexpr int kTmem = NT * (2 + kBlocks) <= 64 ? 64 : NT * (2 + kBlocks) <= 128 ? 128 : NT * (2 + kBlocks) <= 256 ? 256 : 512;
-    static constexpr int kUsed = kSlots * kSlot + kRest + kStages * kStage;
-    // V^T's 128 rows read two panels: with one (64 elements) the second lies behind the slot
-    static constexpr int kBytes = (kPanels > 1 || kUsed > (kSlots + 1) * kSlot ? kUsed : (kSlots + 1) * kSlot) + 1024;
-    static_assert(kSlots >= 2 && kStages >= 1 && kBytes <= kMaxShared - kColumns, "shared memory");
-};
-
-// What a column (query row) and the CTA's roles share.
-template <int NT>
-struct Columns {
-    int64_t q_at[NT], o_at[NT];     // element offsets, -1: no such row
-    int64_t offsets[2][kTile];      // byte offset of each key's vectors, -1: none
-    float neg_m[NT], factor[NT], sum[NT];
-    float part[4][NT];
-    int limit[NT];                  // last position that the row sees
-    int seen[NT];                   // whether m has been set
-    uint64_t full[8], empty[8], s_full[2], p_full, pv_done, q_full;
-    uint32_t tmem, amax;
-    int dead, last;
-    int b, unit, tile;              // where this CTA's part of the list starts
-    long long at, count;            // its first tile in the list, tiles in it
-    long long total;
-    int ctas;
-    long long warp_sum[kThreads / 32];
-};
-
-// Waits, with a limit; after one has run out no wait of this CTA blocks any more, and its results
-// are marked as none.
-__device__ __forceinline__ void wait_for(uint64_t* bar, uint32_t parity, int* dead) {
-    if (*static_cast<volatile int*>(dead)) return;
-    if (!mbar_wait(bar, parity & 1u, kMbarPolls)) *static_cast<volatile int*>(dead) = 1;
-}
-
-// The CTA's part of the list, unit by unit.
-struct Walk {
-    int b, unit, t0;
-    long long at, left;
-    // the unit's
-    int T, t1, first, tokens, keys;
-
-    __device__ __forceinline__ bool next(const AttendArgs& a, uint32_t* status) {
-        if (left <= 0) return false;
-        const StepTokens tk = step_tokens(a.seq_len, a.draft_len, b, a.n, a.c.capacity, *status);
-        first = tk.first, tokens = tk.count, keys = tk.first + tk.count;
-        T = keys > 0 ? (keys + kTile - 1) / kTile : 1;
-        t1 = left < T - t0 ? t0 + static_cast<int>(left) : T;
-        return true;
-    }
-    __device__ __forceinline__ void step(const AttendArgs& a) {
-        at += t1 - t0;
-        left -= t1 - t0;
-        t0 = 0;
-        if (++unit == a.c.heads * a.row_tiles) unit = 0, ++b;
-    }
-};
-
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-    const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&p);
-}
-__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
-    const __half2 p = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&p);
-}
-__device__ __forceinline__ uint32_t two_codes(uint32_t codes) {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(codes), __NV_E4M3);
-    return static_cast<uint32_t>(h.x) | static_cast<uint32_t>(h.y) << 16;
-}
-
-__device__ __forceinline__ float warp_max(float v) {
-    const uint32_t k = __reduce_max_sync(0xFFFFFFFFu, ordered_key(v));
-    return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
-}
-
-// Sums v[0..C) over the warp's lanes; column c's sum ends in lane bits: see the return value, the
-// first of the C / 32 (or one) columns that this lane holds in v[0..].
-template <int C>
-__device__ __forceinline__ int warp_columns(float (&v)[C], int lane) {
-    int first = 0, n = C;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        if (n > 1) {
-            n >>= 1;
-            const bool up = lane & o;
-#pragma unroll
-            for (int i = 0; i < C / 2; ++i)
-                if (i < n) {
-                    const float keep = up ? v[i + n] : v[i], send = up ? v[i] : v[i + n];
-                    v[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, send, o);
-                }
-            if (up) first += n;
-        } else {
-            v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], o);
-        }
-    }
-    return first;
-}
-
-template <int NT, int DP, bool E4M3>
-__global__ void __launch_bounds__(kThreads, 1) attend_kernel(const AttendArgs a) {
-    using S = Shape<NT, DP, E4M3>;
-    static_assert(sizeof(Columns<NT>) <= S::kColumns, "shared memory");
-    extern __shared__ uint8_t raw[];
-    __shared__ __align__(16) Columns<NT> col;
-    uint8_t* ring = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
-    uint8_t* const q_smem = ring + S::kSlots * S::kSlot;
-    uint8_t* const p_smem = q_smem + S::kQ;                     // (high part, and behind it the low part)
-    uint8_t* const stages = q_smem + S::kRest;
-    const CacheView& c = a.c;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = c.head_dim;
-    const int units = c.heads * a.row_tiles;
-
-    if (warp == 12) tmem_alloc(&col.tmem, S::kTmem);
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < 8; ++i) {
-            mbar_init(&col.full[i], kCopyThreads);
-            mbar_init(&col.empty[i], 1);
-        }
-        mbar_init(&col.s_full[0], 1);
-        mbar_init(&col.s_full[1], 1);
-        mbar_init(&col.p_full, kSoftmaxThreads);
-        mbar_init(&col.pv_done, 1);
-        mbar_init(&col.q_full, kSoftmaxThreads);
-        fence_mbar_init();
-        col.dead = 0;
-    }
-    pdl_enter();
-
-    // the list: every thread counts the tiles of a strip of sequences
-    {
-        const int strip = (a.B + kThreads - 1) / kThreads;
-        const int lo = min(a.B, static_cast<int>(threadIdx.x) * strip), hi = min(a.B, lo + strip);
-        long long mine = 0;
-        auto tiles_of = [&](int b) {
-            uint32_t st;
-            const StepTokens tk = step_tokens(a.seq_len, a.draft_len, b, a.n, c.capacity, st);
-            const int keys = tk.first + tk.count;
-            return keys > 0 ? (keys + kTile - 1) / kTile : 1;
-        };
-        for (int b = lo; b < hi; ++b) mine += tiles_of(b);
-        long long upto = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long t = __shfl_up_sync(0xFFFFFFFFu, upto, o);
-            if (lane >= o) upto += t;
-        }
-        if (lane == 31) col.warp_sum[warp] = upto;
-        __syncthreads();
-        long long total = 0;
-        for (int w = 0; w < kThreads / 32; ++w) {
-            if (w == warp) upto += total;
-            total += col.warp_sum[w];
-        }
-        total *= units;
-        const int ctas = static_cast<int>(total < gridDim.x ? total : gridDim.x);
-        const long long g0 = total * blockIdx.x / ctas, g1 = total * (blockIdx.x + 1ll) / ctas;
-        long long before = (upto - mine) * units;
-        if (blockIdx.x < ctas && before <= g0 && g0 < before + mine * units) {     // one thread's
-            int b = lo;
-            for (;; ++b) {
-                const long long t = static_cast<long long>(tiles_of(b)) * units;
-                if (g0 < before + t) break;
-                before += t;
-            }
-            const int T = tiles_of(b);
-            col.b = b;
-            col.unit = static_cast<int>((g0 - before) / T);
-            col.tile = static_cast<int>((g0 - before) % T);
-            col.at = g0;
-            col.count = g1 - g0;
-        }
-        if (threadIdx.x == 0) {
-            col.total = total;
-            col.ctas = ctas;
-            if (blockIdx.x >= ctas) col.count = 0;
-        }
-    }
-    tmem_before_sync();
-    __syncthreads();
-    tmem_after_sync();
-    const uint32_t tmem = col.tmem;
-    Walk w = {col.b, col.unit, col.tile, col.at, col.count, 0, 0, 0, 0, 0};
-    uint32_t st;
-
-    if (warp >= 8 && warp < 12) {
-        // ---- copies: the tiles of keys and values in turn into the ring ----
-        const int t = threadIdx.x - kSoftmaxThreads;
-        constexpr int kRowChunks = DP * (E4M3 ? 1 : 2) / 16, kRows = kCopyThreads / kRowChunks, kTurns = kTile / kRows;
-        const int chunk = t % kRowChunks, row0 = t / kRowChunks;
-        const bool in = chunk * 16 < c.vec_bytes;
-        // Entry e of the ring.  bf16: the copies go straight into the slot and arrive on its barrier by
-        // themselves.  e4m3: they go to this thread's own places in a stage, and the oldest entry in
-        // flight is converted into its slot once it has come in.
-        constexpr int kLag = S::kStages - 1;
-        [[maybe_unused]] auto convert = [&](int e) {
-            {
-                const int slot = e % S::kSlots;
-                if (e >= S::kSlots) wait_for(&col.empty[slot], e / S::kSlots - 1, &col.dead);
-                const uint8_t* from = stages + (e % S::kStages) * S::kStage + t * 16;
-                uint8_t* to = ring + slot * S::kSlot;
-                if (in) {
-#pragma unroll 4
-                    for (int i = 0; i < kTurns; ++i) {
-                        const int row = row0 + i * kRows;
-                        const uint4 x = *reinterpret_cast<const uint4*>(from + i * (kCopyThreads * 16));
-                        uint8_t* line = to + (chunk >> 2) * (kTile * 128) + row * 128;
-                        const int piece = (chunk & 3) * 2;
-                        *reinterpret_cast<uint4*>(line + ((piece ^ (row & 7)) << 4)) =
-                            make_uint4(two_codes(x.x & 0xFFFFu), two_codes(x.x >> 16), two_codes(x.y & 0xFFFFu), two_codes(x.y >> 16));
-                        *reinterpret_cast<uint4*>(line + (((piece + 1) ^ (row & 7)) << 4)) =
-                            make_uint4(two_codes(x.z & 0xFFFFu), two_codes(x.z >> 16), two_codes(x.w & 0xFFFFu), two_codes(x.w >> 16));
-                    }
-                }
-            }
-            fence_smem_async();
-            mbar_arrive(&col.full[e % S::kSlots]);
-        };
-        int e = 0, turn = 0;
-        while (w.next(a, &st)) {
-            if (w.t0 == 0 && w.unit == 0 && t == 0 && st && a.status) atomicOr(a.status + w.b, st);
-            const int64_t head = static_cast<int64_t>(w.unit / a.row_tiles) * c.head_stride;
-            const int32_t* table = c.pages + w.b * c.pages_stride;
-            auto look = [&](int tile) {                        // the page of this thread's row, -1: no such position
-                const int pos = tile * kTile + t;
-                return tile < w.t1 && pos < w.keys ? __ldg(table + page_of(pos, c.div_mul, c.div_shift)) : -1;
-            };
-            int page = look(w.t0), page_next = look(w.t0 + 1);
-            for (int tile = w.t0; tile < w.t1; ++tile) {
-                const int pos = tile * kTile + t;
-                int64_t off = -1;
-                if (static_cast<unsigned>(page) < static_cast<unsigned>(c.n_pages))
-                    off = page * c.page_stride + head +
-                          (pos - static_cast<int>(page_of(pos, c.div_mul, c.div_shift)) * c.page_size) * c.pos_stride;
-                else if (pos < w.keys && a.status)
-                    atomicOr(a.status + w.b, PLDP_ST_PAGE);
-                page = page_next;
-                page_next = look(tile + 2);
-                col.offsets[turn][t] = off;
-                bar_sync(1, kCopyThreads);
-                for (int kv = 0; kv < 2; ++kv) {
-                    const uint8_t* base = (kv ? c.v : c.k) + chunk * 16;
-                    uint32_t to;
-                    if constexpr (E4M3) {
-                        to = smem_u32(stages + (e % S::kStages) * S::kStage + t * 16);
-                    } else {
-                        const int slot = e % S::kSlots;
-                        if (e >= S::kSlots) wait_for(&col.empty[slot], e / S::kSlots - 1, &col.dead);
-                        to = smem_u32(ring + slot * S::kSlot) + (chunk >> 3) * (kTile * 128);
-                    }
-                    if (in) {
-#pragma unroll 4
-                        for (int i = 0; i < kTurns; ++i) {
-                            const int row = row0 + i * kRows;
-                            const int64_t o = col.offsets[turn][row];
-                            const uint32_t d = E4M3 ? to + i * (kCopyThreads * 16) : to + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
-                            copy16(d, o >= 0 ? base + o : base, o >= 0 ? 16 : 0);
-                        }
-                    }
-                    if constexpr (E4M3) {
-                        copy_commit();
-                        if (e >= kLag) {
-                            copy_wait<kLag>();
-                            convert(e - kLag);
-                        }
-                    } else {
-                        copy_arrive(&col.full[e % S::kSlots]);
-                    }
-                    ++e;
-                }
-                turn ^= 1;
-            }
-            w.step(a);
-        }
-        if constexpr (E4M3) {
-            for (int left = min(e, kLag); left > 0; --left) {
-                copy_wait(left - 1);
-                convert(e - left);
-            }
-        } else {
-            copy_wait<0>();
-        }
-    } else if (warp == 12) {
-        // ---- matrix instructions ----
-        if (lane == 0) {
-            const uint64_t q_op = smem_operand(smem_u32(q_smem), 16, 1024, swizzle_mode(128));
-            const uint64_t p_op = smem_operand(smem_u32(p_smem), kTile * 128, 8 * S::kRow, swizzle_mode(S::kRow));
-            const uint64_t k_op = smem_operand(smem_u32(ring), 16, 1024, swizzle_mode(128));
-            const uint64_t v_op = smem_operand(smem_u32(ring), kTile * 128, 1024, swizzle_mode(128));
-            constexpr uint32_t kScores = mma_form(128, NT, !E4M3, false, false), kValues = mma_form(128, NT, !E4M3, true, true);
-            int e = 0, tile = 0, segment = 0;       // entries, tiles and units so far
-            auto scores = [&](int entry, int k) {
-                const int slot = entry % S::kSlots;
-                wait_for(&col.full[slot], entry / S::kSlots, &col.dead);
-                fence_smem_async();
-                tmem_after_sync();
-                const uint64_t op = advance(k_op, slot * S::kSlot);
-                for (int s = 0; s < D / 16; ++s)
-                    mma_f16(tmem + (k & 1) * NT, advance(op, (s >> 2) * (kTile * 128) + (s & 3) * 32),
-                            advance(q_op, (s >> 2) * (NT * 128) + (s & 3) * 32), kScores, s > 0);
-                mma_commit(&col.empty[slot]);
-                mma_commit(&col.s_full[k & 1]);
-            };
-            while (w.next(a, &st)) {
-                const int count = w.t1 - w.t0;
-                wait_for(&col.q_full, segment, &col.dead);
-                tmem_after_sync();
-                scores(e, tile);
-                for (int i = 0; i < count; ++i, ++tile, e += 2) {
-                    if (i + 1 < count) scores(e + 2, tile + 1);
-                    wait_for(&col.p_full, tile, &col.dead);
-                    const int slot = (e + 1) % S::kSlots;
-                    wait_for(&col.full[slot], (e + 1) / S::kSlots, &col.dead);
-                    fence_smem_async();
-                    tmem_after_sync();
-                    const uint64_t op = advance(v_op, slot * S::kSlot);
-#pragma unroll
-                    for (int m = 0; m < S::kBlocks; ++m)
-#pragma unroll
-                        for (int part = 0; part < (E4M3 ? 1 : 2); ++part)
-#pragma unroll
-                            for (int s = 0; s < kTile / 16; ++s)
-                                mma_f16(tmem + (2 + m) * NT, advance(op, m * 2 * (kTile * 128) + s * 2048),
-                                        advance(p_op, part * S::kP + s * 16 * S::kRow), kValues, i > 0 || part > 0 || s > 0);
-                    mma_commit(&col.empty[slot]);
-                    mma_commit(&col.pv_done);
-                }
-                ++segment;
-                w.step(a);
-            }
-        }
-        __syncwarp();
-    } else {
-        // ---- softmax: two groups of 128 threads, each half of the columns, a key a thread ----
-        constexpr int C = NT / 2, CH = C < 32 ? C : 32, NCH = C / CH;
-        const int grp = warp >> 2, quad = warp & 3, j = quad * 32 + lane, c0 = grp * C, tid = threadIdx.x;
-        const uint32_t my_s = tmem + (static_cast<uint32_t>(quad * 32) << 16) + c0, my_o = my_s + 2 * NT;
-        constexpr float kLift = E4M3 ? 7.f : 0.f;       // f16 weights up to 2^15 instead of 2^8: fewer of them vanish
-        constexpr float kRoomUp = 8.f + kLift;
-        int tile_no = 0;
-        while (w.next(a, &st)) {
-            const int kv = w.unit / a.row_tiles, r0 = (w.unit - kv * a.row_tiles) * NT;
-            const int32_t* table = c.pages + w.b * c.pages_stride;
-            // the columns of this unit
-            if (tid < NT) {
-                const int r = r0 + tid, i = r / a.group, h = kv * a.group + (r - i * a.group);
-                const bool row = i < a.n;
-                col.q_at[tid] = row && i < w.tokens ? w.b * a.q_seq + i * a.q_tok + h * a.q_head : -1;
-                col.o_at[tid] = row ? w.b * a.o_seq + i * a.o_tok + h * a.o_head : -1;
-                col.limit[tid] = row && i < w.tokens ? w.first + i : -1;
-                col.neg_m[tid] = 0.f;
-                col.seen[tid] = 0;
-            }
-            if (tid == 0) col.amax = 0;
-            bar_sync(4, kSoftmaxThreads);
-            // the queries: 16-byte pieces, rows of 128 bytes swizzled
-            constexpr int kPieces = NT * DP / 8, kPer = (kPieces + kSoftmaxThreads - 1) / kSoftmaxThreads;
-            float back = 1.f;                               // what the scores are multiplied by for a scaled Q
-            {
-                uint4 x[kPer];
-#pragma unroll
-                for (int p = 0; p < kPer; ++p) {
-                    const int id = tid + p * kSoftmaxThreads, row = id / (DP / 8), piece = id % (DP / 8);
-                    x[p] = make_uint4(0u, 0u, 0u, 0u);
-                    if (id < kPieces && piece * 8 < D && col.q_at[row] >= 0)
-                        x[p] = *reinterpret_cast<const uint4*>(a.q + col.q_at[row] + piece * 8);
-                }
-                if constexpr (E4M3) {
-                    // bf16 to f16 exactly: the largest element to 2^14..2^15 by a power of two
-                    uint32_t most = 0;
-#pragma unroll
-                    for (int p = 0; p < kPer; ++p) {
-                        const uint32_t q4[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) most = max(most, max((q4[k] << 16) & 0x7FFF0000u, q4[k] & 0x7FFF0000u));
-                    }
-                    most = __reduce_max_sync(0xFFFFFFFFu, most);
-                    if (lane == 0) atomicMax(&col.amax, most);
-                    bar_sync(4, kSoftmaxThreads);
-                    const int ex = static_cast<int>(col.amax >> 23);                    // biased exponent
-                    const int up = ex == 0 || ex == 255 ? 0 : min(14 - (ex - 127), 120);
-                    const float lift = __uint_as_float(static_cast<uint32_t>(up + 127) << 23);
-                    back = __uint_as_float(static_cast<uint32_t>(127 - up) << 23);
-#pragma unroll
-                    for (int p = 0; p < kPer; ++p) {
-                        uint32_t q4[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            q4[k] = pack_f16(__uint_as_float(q4[k] << 16) * lift, __uint_as_float(q4[k] & 0xFFFF0000u) * lift);
-                        x[p] = make_uint4(q4[0], q4[1], q4[2], q4[3]);
-                    }
-                }
-#pragma unroll
-                for (int p = 0; p < kPer; ++p) {
-                    const int id = tid + p * kSoftmaxThreads, row = id / (DP / 8), piece = id % (DP / 8);
-                    if (id < kPieces)
-                        *reinterpret_cast<uint4*>(q_smem + (piece >> 3) * (NT * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4)) = x[p];
-                }
-            }
-            fence_smem_async();
-            tmem_before_sync();
-            mbar_arrive(&col.q_full);
-
-            float l[C];
-#pragma unroll
-            for (int i = 0; i < C; ++i) l[i] = 0.f;
-            bool settled = false;
-            const float f0 = a.scale2 * back;
-            // this thread's key of a tile: factor of its scores, log2 of its values' scale (-inf: no key), its
-            // inverse.  The page is looked up two tiles ahead and the scales loaded one ahead.
-            float f, g, inv, ks_next = 1.f, vs_next = 1.f;
-            auto look = [&](int tile) {
-                const int pos = tile * kTile + j;
-                int page = -1;
-                if (tile < w.t1 && pos < w.keys) page = __ldg(table + page_of(pos, c.div_mul, c.div_shift));
-                return static_cast<unsigned>(page) < static_cast<unsigned>(c.n_pages) ? page : -1;
-            };
-            auto fetch = [&](int tile, int page) {
-                if constexpr (E4M3) {
-                    const int pos = tile * kTile + j;
-                    if (page >= 0) {
-                        const int64_t at = (static_cast<int64_t>(page) * c.heads + kv) * c.page_size +
-                                           (pos - static_cast<int>(page_of(pos, c.div_mul, c.div_shift)) * c.page_size);
-                        ks_next = __ldg(c.k_scale + at);
-                        vs_next = __ldg(c.v_scale + at);
-                    }
-                }
-            };
-            auto take = [&](int page) {
-                f = 0.f, g = -INFINITY, inv = 1.f;
-                if (page >= 0) {
-                    f = f0, g = 0.f;
-                    if constexpr (E4M3) {
-                        const float vs = fmaxf(vs_next, 1e-37f);
-                        f *= ks_next;
-                        g = log2f(vs);
-                        inv = 1.f / vs;
-                    }
-                }
-            };
-            int page_next = look(w.t0);
-            fetch(w.t0, page_next);
-            take(page_next);
-            page_next = look(w.t0 + 1);
-            const int seen_by_all = w.first + r0 / a.group;    // the unit's first row sees positions up to here
-            for (int tile = w.t0; tile < w.t1; ++tile, ++tile_no) {
-                const uint32_t s_at = my_s + (tile_no & 1) * NT;
-                const int pos = tile * kTile + j;
-                const bool masked = tile * kTile + kTile - 1 > seen_by_all;
-                float x[CH];
-                // exponents of the weights of chunk ch against the present m
-                auto load = [&](int ch) {
-                    tmem_load(s_at + ch * CH, x);
-#pragma unroll
-                    for (int i = 0; i < CH; i += 4) {
-                        const float4 nm = *reinterpret_cast<const float4*>(&col.neg_m[c0 + ch * CH + i]);
-                        x[i] = fmaf(x[i], f, g + nm.x);
-                        x[i + 1] = fmaf(x[i + 1], f, g + nm.y);
-                        x[i + 2] = fmaf(x[i + 2], f, g + nm.z);
-                        x[i + 3] = fmaf(x[i + 3], f, g + nm.w);
-                    }
-                    if (masked) {
-#pragma unroll
-                        for (int i = 0; i < CH; ++i)
-                            if (pos > col.limit[c0 + ch * CH + i]) x[i] = -INFINITY;
-                    }
-                };
-                fetch(tile + 1, page_next);
-                const int page_after = look(tile + 2);
-                wait_for(&col.s_full[tile_no & 1], tile_no >> 1, &col.dead);
-                tmem_after_sync();
-                bool up = !settled;
-#pragma unroll
-                for (int ch = 0; ch < NCH; ++ch) {
-                    load(ch);
-                    float most = x[0];
-#pragma unroll
-                    for (int i = 1; i < CH; ++i) most = fmaxf(most, x[i]);
-                    up = up || most > kRoomUp;
-                }
-                if (bar_any(2 + grp, 128, up)) {
-                    // some column's maximum moves
-#pragma unroll
-                    for (int ch = 0; ch < NCH; ++ch) {
-                        if (NCH > 1) load(ch);
-                        float mine = -INFINITY;
-#pragma unroll
-                        for (int i = 0; i < CH; ++i) {
-                            const float top = warp_max(x[i]);
-                            if (lane == i) mine = top;
-                        }
-                        if (lane < CH) col.part[quad][c0 + ch * CH + lane] = mine;
-                    }
-                    bar_sync(2 + grp, 128);
-                    const int t = tid & 127;
-                    bool unset = false;
-                    if (t < C) {
-                        const int n = c0 + t;
-                        const float top = fmaxf(fmaxf(col.part[0][n], col.part[1][n]), fmaxf(col.part[2][n], col.part[3][n]));
-                        float by = 1.f;
-                        if (top > -INFINITY && top < INFINITY) {
-                            if (!col.seen[n]) {
-                                col.seen[n] = 1;
-                                col.neg_m[n] = kLift - top;
-                            } else if (top > kLift) {
-                                by = ex2(kLift - top);
-                                col.neg_m[n] += kLift - top;
-                            }
-                        }
-                        col.factor[n] = by;
-                        unset = !col.seen[n];
-                    }
-                    settled = !bar_any(2 + grp, 128, unset);
-#pragma unroll
-                    for (int i = 0; i < C; ++i) l[i] *= col.factor[c0 + i];
-                    if (tile > w.t0) {
-                        wait_for(&col.pv_done, tile_no - 1, &col.dead);
-                        tmem_after_sync();
-#pragma unroll
-                        for (int m = 0; m < S::kBlocks; ++m)
-#pragma unroll
-                            for (int i = 0; i < C; i += 8) {
-                                float o[8];
-                                tmem_load(my_o + m * NT + i, o);
-#pragma unroll
-                                for (int k = 0; k < 8; ++k) o[k] *= col.factor[c0 + i + k];
-                                tmem_store8(my_o + m * NT + i, o);
-                            }
-                        tmem_store_wait();
-                    }
-                    if (NCH == 1) load(0);
-                }
-                if (tile_no > 0) wait_for(&col.pv_done, tile_no - 1, &col.dead);   // the last tile's weights have been read
-#pragma unroll
-                for (int ch = 0; ch < NCH; ++ch) {
-                    if (NCH > 1) load(ch);
-#pragma unroll
-                    for (int i = 0; i < CH; i += 8) {
-                        float v[8];
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            v[k] = ex2(x[i + k]);
-                            if constexpr (E4M3) l[ch * CH + i + k] = fmaf(v[k], inv, l[ch * CH + i + k]);
-                            else l[ch * CH + i + k] += v[k];
-                        }
-                        const int byte = (c0 + ch * CH + i) * 2;                      // within the key's weights
-                        const int panel = byte / 128, in_row = byte % 128;
-                        constexpr int kMask = S::kRow / 16 - 1;
-                        const int line = j * S::kRow + in_row;
-                        // the swizzle: 16-byte pieces, by the address's bits from 128 bytes up
-                        uint8_t* to = p_smem + panel * (kTile * 128) + (line ^ (((line >> 7) & kMask) << 4));
-                        if constexpr (E4M3) {
-                            *reinterpret_cast<uint4*>(to) = make_uint4(pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7]));
-                        } else {
-                            uint32_t hi[4], lo[4];
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                hi[k] = pack_bf16(v[2 * k], v[2 * k + 1]);
-                                lo[k] = pack_bf16(v[2 * k] - __uint_as_float(hi[k] << 16),
-                                                  v[2 * k + 1] - __uint_as_float(hi[k] & 0xFFFF0000u));
-                            }
-                            *reinterpret_cast<uint4*>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                            *reinterpret_cast<uint4*>(to + S::kP) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-                        }
-                    }
-                }
-                fence_smem_async();
-                tmem_before_sync();
-                mbar_arrive(&col.p_full);
-                take(page_next);
-                page_next = page_after;
-            }
-            // the sums over the keys
-            {
-                constexpr int kOwn = C / 32 > 1 ? C / 32 : 1;
-                const int at = warp_columns<C>(l, lane);
-                constexpr int kLanes = C < 32 ? 32 / C : 1;              // lanes that hold the same column
-                if ((lane & (kLanes - 1)) == 0)
-#pragma unroll
-                    for (int i = 0; i < kOwn; ++i) col.part[quad][c0 + at + i] = l[i];
-                bar_sync(2 + grp, 128);
-                const int t = tid & 127;
-                if (t < C) {
-                    const int n = c0 + t;
-                    col.sum[n] = col.part[0][n] + col.part[1][n] + col.part[2][n] + col.part[3][n];
-                }
-            }
-            wait_for(&col.pv_done, tile_no - 1, &col.dead);
-            tmem_after_sync();
-            bar_sync(4, kSoftmaxThreads);
-            const bool whole = w.t0 == 0 && w.t1 == w.T;
-            const long long unit_at = w.at - w.t0;
-            // which of this CTA's two places in the workspace: the unit began in another's part, or in this one's
-            constexpr int kPart = NT * (DP + 2);
-            float* part = a.parts + static_cast<int64_t>(2 * blockIdx.x + (w.t0 == 0 ? 1 : 0)) * kPart;
-            auto lse_at = [&](int n) {
-                const int r = r0 + n, i = r / a.group;
-                return (static_cast<int64_t>(w.b) * a.n + i) * a.q_heads + kv * a.group + (r - i * a.group);
-            };
-            if (whole) {
-                if (tid < NT && a.lse && col.o_at[tid] >= 0) {
-                    const float s = col.limit[tid] >= 0 ? col.sum[tid] : 0.f;
-                    a.lse[lse_at(tid)] = s == 0.f ? -INFINITY : (log2f(s) - col.neg_m[tid]) * 0.69314718055994531f;
-                }
-            } else if (tid < NT) {
-                part[NT * DP + tid] = col.seen[tid] ? -col.neg_m[tid] : -INFINITY;
-                part[NT * DP + NT + tid] = col.sum[tid];
-            }
-#pragma unroll
-            for (int m = 0; m < S::kBlocks; ++m) {
-                const int d = m * 128 + j;
-#pragma unroll
-                for (int ch = 0; ch < NCH; ++ch) {
-                    float o[CH];
-                    tmem_load(my_o + m * NT + ch * CH, o);
-                    if (d < D) {
-#pragma unroll
-                        for (int i = 0; i < CH; ++i) {
-                            const int n = c0 + ch * CH + i;
-                            if (col.o_at[n] < 0) continue;
-                            if (whole) {
-                                const float s = col.sum[n];
-                                a.out[col.o_at[n] + d] = __float2bfloat16(s == 0.f || col.limit[n] < 0 ? 0.f : o[i] / s);
-                            } else {
-                                part[n * DP + d] = o[i];
-                            }
-                        }
-                    }
-                }
-            }
-            if (!whole) {
-                // the last of the unit's CTAs joins the parts
-                const long long total = col.total, end = unit_at + w.T - 1;
-                const int ctas = col.ctas;
-                const int c_first = static_cast<int>(((unit_at + 1) * ctas - 1) / total);
-                const int c_last = static_cast<int>(((end + 1) * ctas - 1) / total);
-                __threadfence();
-                bar_sync(4, kSoftmaxThreads);
-                if (tid == 0) {
-                    uint32_t* ticket = a.tickets + static_cast<int64_t>(w.b) * units + w.unit;
-                    const bool is_last = atomicAdd(ticket, 1u) == static_cast<uint32_t>(c_last - c_first);
-                    if (is_last) *ticket = 0u;
-                    col.last = is_last;
-                    __threadfence();
-                }
-                bar_sync(4, kSoftmaxThreads);
-                if (col.last) {
-                    __threadfence();
-                    for (int n = warp; n < NT; n += kSoftmaxThreads / 32) {
-                        const int64_t to = col.o_at[n];
-                        if (to < 0) continue;
-                        auto place = [&](int cta) { return a.parts + static_cast<int64_t>(2 * cta + (cta == c_first ? 1 : 0)) * kPart; };
-                        float M = -INFINITY, sum = 0.f;
-                        for (int k = c_first + lane; k <= c_last; k += 32) M = fmaxf(M, __ldcg(place(k) + NT * DP + n));
-                        M = warp_max(M);
-                        constexpr int kPer = DP / 32;
-                        float o[kPer];
-#pragma unroll
-                        for (int p = 0; p < kPer; ++p) o[p] = 0.f;
-                        if (M > -INFINITY && col.limit[n] >= 0)
-                            for (int k = c_first; k <= c_last; ++k) {
-                                const float* from = place(k);
-                                const float m = __ldcg(from + NT * DP + n);
-                                if (!(m > -INFINITY)) continue;
-                                const float by = ex2(m - M);
-                                sum = fmaf(by, __ldcg(from + NT * DP + NT + n), sum);
-#pragma unroll
-                                for (int p = 0; p < kPer; ++p)
-                                    if (lane + 32 * p < D) o[p] = fmaf(by, __ldcg(from + n * DP + lane + 32 * p), o[p]);
-                            }
-#pragma unroll
-                        for (int p = 0; p < kPer; ++p)
-                            if (lane + 32 * p < D) a.out[to + lane + 32 * p] = __float2bfloat16(sum == 0.f ? 0.f : o[p] / sum);
-                        if (lane == 0 && a.lse) a.lse[lse_at(n)] = sum == 0.f ? -INFINITY : (log2f(sum) + M) * 0.69314718055994531f;
-                    }
-                }
-            }
-            if (col.dead && tid == 0 && a.status) atomicOr(a.status + w.b, PLDP_ST_TIMEOUT);
-            tmem_before_sync();
-            bar_sync(4, kSoftmaxThreads);
-            w.step(a);
-        }
-    }
-    tmem_before_sync();
-    __syncthreads();
-    if (warp == 12) {
-        tmem_after_sync();
-        tmem_free(tmem, S::kTmem);
-    }
-}
 
 // Rows a CTA takes at once: the fewest columns that hold them all (one pass over the keys), up to
 // 128, or 32 for heads above 128 elements, whose tiles leave no more shared memory.
 int columns_of(int rows, int head_dim) {
     const int most = head_dim > 128 ? 32 : 128;
-    int nt = 16;
-    while (nt < rows && nt < most) nt *= 2;
-    return nt;
+    for (const int nt : {16, 32, 64, 96})
+        if (rows <= nt && nt <= most) return nt;
+    return most;
 }
 int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
@@ -781,30 +27,33 @@ Space space_of(int64_t B, int64_t n, int64_t q_heads, int64_t heads, int head_di
             static_cast<size_t>(2 * kMaxCtas) * nt * (padded_dim(head_dim) + 2) * sizeof(float)};
 }
 
-template <int NT, int DP, bool E4M3>
-cudaError_t launch(const AttendArgs& a, int ctas, cudaStream_t s) {
-    constexpr int bytes = Shape<NT, DP, E4M3>::kBytes;
-    const cudaError_t e = cudaFuncSetAttribute(attend_kernel<NT, DP, E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != cudaSuccess) return e;
-    return launch_pdl(attend_kernel<NT, DP, E4M3>, dim3(ctas), dim3(kThreads), bytes, s, 0, a);
-}
-template <int DP, bool E4M3>
-cudaError_t launch_columns(const AttendArgs& a, int nt, int ctas, cudaStream_t s) {
-    if (nt == 16) return launch<16, DP, E4M3>(a, ctas, s);
-    if (nt == 32) return launch<32, DP, E4M3>(a, ctas, s);
-    if constexpr (DP <= 128) {
-        if (nt == 64) return launch<64, DP, E4M3>(a, ctas, s);
-        return launch<128, DP, E4M3>(a, ctas, s);
-    } else {
-        return cudaErrorInvalidValue;
-    }
-}
-template <bool E4M3>
-cudaError_t launch_dim(const AttendArgs& a, int nt, int ctas, cudaStream_t s) {
-    const int dp = padded_dim(a.c.head_dim);
-    if (dp == 64) return launch_columns<64, E4M3>(a, nt, ctas, s);
-    if (dp == 128) return launch_columns<128, E4M3>(a, nt, ctas, s);
-    return launch_columns<256, E4M3>(a, nt, ctas, s);
+// The pool as a tensor of (element, position, head, page), its middle dimensions by ascending
+// stride, copied in boxes of `box` positions of one head of one page: 64 elements of bf16, swizzled as the
+// matrix instructions read them, or a whole vector of codes.
+bool pool_map(CUtensorMap* map, void* base, const CacheView& c, bool e4m3, int box, int pitch, bool* head_first) {
+    static const auto encode = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            f = nullptr;
+        return reinterpret_cast<CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                             const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                             CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill)>(f);
+    }();
+    if (!encode) return false;
+    // the stride of a dimension of one is never used; any that the map takes will do
+    const auto used = [&](int64_t stride, int size) { return static_cast<cuuint64_t>(size == 1 ? c.vec_bytes : stride); };
+    const cuuint64_t pos = used(c.pos_stride, c.page_size), head = used(c.head_stride, c.heads);
+    *head_first = head < pos;
+    const cuuint64_t d = c.head_dim, p = c.page_size, h = c.heads;
+    const cuuint64_t dims[4] = {d, *head_first ? h : p, *head_first ? p : h, static_cast<cuuint64_t>(c.n_pages)};
+    const cuuint64_t strides[3] = {*head_first ? head : pos, *head_first ? pos : head, used(c.page_stride, c.n_pages)};
+    const cuuint32_t inner = e4m3 ? pitch : 64, rows = box;
+    const cuuint32_t size[4] = {inner, *head_first ? 1u : rows, *head_first ? rows : 1u, 1u}, step[4] = {1u, 1u, 1u, 1u};
+    return encode(map, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, base, dims, strides, size, step,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, e4m3 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace
@@ -860,8 +109,18 @@ PLDP_API pldp_status pldp_attend_cache(const pldp_attend_args* p, void* stream) 
     const int64_t most = static_cast<int64_t>(p->B) * p->cache.heads * a.row_tiles * ((a.c.capacity + int64_t(kTile) - 1) / kTile);
     int ctas = sm_count() < kMaxCtas ? sm_count() : kMaxCtas;
     if (most < ctas) ctas = static_cast<int>(most);
+    const bool e4m3 = p->cache.dtype == PLDP_E4M3;
+    a.box = kTile;                                           // the largest power of two that divides the page, up to a tile
+    while (p->cache.page_size % a.box) a.box /= 2;
+    // a copy starts at a multiple of 128 bytes of shared memory: vectors side by side where a box of them is one
+    a.pitch = p->cache.head_dim * a.box % 128 == 0 ? p->cache.head_dim : p->cache.head_dim <= 128 ? 128 : 256;
+    Maps maps;
+    bool head_first = false;
+    if (!pool_map(&maps.k, a.c.k, a.c, e4m3, a.box, a.pitch, &head_first) || !pool_map(&maps.v, a.c.v, a.c, e4m3, a.box, a.pitch, &head_first))
+        return fail(PLDP_ERR_UNSUPPORTED, "%s: the cache's strides cannot be described to the copy engine", fn);
+    a.head_first = head_first;
     auto s = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = p->cache.dtype == PLDP_E4M3 ? launch_dim<true>(a, nt, ctas, s) : launch_dim<false>(a, nt, ctas, s);
+    const cudaError_t e = e4m3 ? launch_attend_e4m3(a, maps, nt, ctas, s) : launch_attend_bf16(a, maps, nt, ctas, s);
     if (e != cudaSuccess) return fail(PLDP_ERR_CUDA, "%s: launch failed: %s", fn, cudaGetErrorString(e));
     return check_launch(fn);
 }
