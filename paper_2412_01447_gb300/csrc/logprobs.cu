@@ -6,70 +6,304 @@
 namespace pldp {
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kWarps = kThreads / 32;
+// With x = logits / T in units of log2 (y = logit * c, c = log2(e) / T) and the row's maximum M,
+//   L = sum 2^(y - M),  U = sum 2^(y - M) (y - M):
+//   logprob = ln2 (y_token - M - log2 L),   entropy = ln2 (log2 L - U / L).
+//
+// 1. A pass reads the logits once, in units of 2 KB of a row, a warp a unit (four 16-byte loads a lane):
+//    L and U against the unit's own maximum, and the maximum of each 512 bytes.
+// 2. One warp a row joins them.  The row's top k elements lie in the k chunks of 512 bytes whose maxima
+//    are largest (ties to the lower chunk): each element elsewhere has k such maxima before it.
+//    So the warp picks those chunks, rereads them (4% of a row of 128256 bf16 for k = 20) and keeps the k
+//    best keys, one a lane, sorted.
+//
+// Bound by reading the logits.  1664 rows of 128256 bf16 (427 MB), k = 20, L2 flushed: @TIME@.
+constexpr int kThreads = 256, kWarps = kThreads / 32, kLoads = 4;
+constexpr int kBlocksPerSm = 5, kWaves = 11;
 constexpr int kMaxTop = 32;
+constexpr int kUnitBytes = kLoads * 32 * 16;
 
 struct LogprobArgs {
     const int32_t* tokens;
     float *logprob, *entropy, *top_logprob;
     int32_t* top_id;
-    int V, top;
-    float inv_t;
+    float4* maxima;      // [rows * units]: of each load
+    float2* sums;        // [rows * units]: L, U against the largest of them
+    int64_t rows;
+    uint32_t V, units;   // units a row
+    uint32_t lead;       // elements from a 16-byte boundary to the first logit
+    int top;
+    float c;
 };
 
-// One CTA a row: the maximum, the sums against it, then the alternatives one by one.
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float ordered_value(uint32_t o) {
+    return __uint_as_float((o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o);
+}
+__device__ __forceinline__ float warp_max(float v) { return ordered_value(__reduce_max_sync(0xFFFFFFFFu, ordered_key(v))); }
+__device__ __forceinline__ void unpack(const uint4& x, float (&e)[8]) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        e[2 * k] = __uint_as_float(w[k] << 16);
+        e[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void unpack(const uint4& x, float (&e)[4]) {
+    e[0] = __uint_as_float(x.x), e[1] = __uint_as_float(x.y), e[2] = __uint_as_float(x.z), e[3] = __uint_as_float(x.w);
+}
+
+// Rows that are not whole vectors, or do not start at one: a row starts `head` elements into a
+// vector, units are cut at whole vectors all the same, and the two vectors that other rows share are
+// read element by element, -inf in the place of what is not the row's.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) logprobs_kernel(const T* __restrict__ logits, const LogprobArgs a) {
-    pdl_enter();
-    __shared__ unsigned long long keys[kWarps];
-    __shared__ float sums[2][kWarps];
-    const int64_t r = blockIdx.x;
-    const T* x = logits + r * a.V;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    unsigned long long last = ~0ull;
-    float m = -INFINITY, l = 0.f, t = 0.f, lse = -INFINITY;
-    for (int k = 0; k <= a.top; ++k) {                  // turn 0 is the maximum, which turn 1 finds again
-        unsigned long long best = 0;
-        for (int v = threadIdx.x; v < a.V; v += kThreads) {
-            const unsigned long long key = pack_key(to_f32(x[v]), v);
-            if (key < last && key > best) best = key;
+__device__ __forceinline__ uint32_t head_of(const LogprobArgs& a, int64_t r) {
+    return static_cast<uint32_t>((static_cast<uint64_t>(r) * a.V + a.lead) % (16 / sizeof(T)));
+}
+template <typename T>
+__device__ __noinline__ uint4 cut_vector(const T* row, int64_t at, int64_t V) {   // elements at.. of a row, some outside [0, V)
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int j = 0; j < static_cast<int>(16 / sizeof(T)); ++j) {
+        const bool in = at + j >= 0 && at + j < V;
+        if constexpr (sizeof(T) == 2)
+            w[j / 2] |= (in ? static_cast<uint32_t>(__bfloat16_as_ushort(row[at + j])) : 0xFF80u) << (16 * (j % 2));
+        else
+            w[j] = in ? __float_as_uint(row[at + j]) : 0xFF800000u;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// The vector at element `at` of a row (relative to its first, head elements before it a vector's start).
+template <typename T, bool CUT>
+__device__ __forceinline__ uint4 row_vector(const T* row, int64_t at, int64_t V) {
+    if (CUT && (at < 0 || at + static_cast<int>(16 / sizeof(T)) > V)) return cut_vector<T>(row, at, V);
+    return ld_stream16(row + at);
+}
+
+template <typename T, bool CUT>
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm) logprob_sums_kernel(const T* __restrict__ logits, const LogprobArgs a) {
+    pdl_wait_only();
+    constexpr int VW = 16 / sizeof(T), P = kUnitBytes / sizeof(T);
+    const int lane = threadIdx.x & 31;
+    const int64_t W = static_cast<int64_t>(gridDim.x) * kWarps, total = a.rows * a.units;
+    for (int64_t u = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5); u < total; u += W) {
+        const uint32_t r = static_cast<uint32_t>(static_cast<uint64_t>(u) / a.units);      // rows and units are below 2^31
+        const uint32_t k = static_cast<uint32_t>(u - static_cast<int64_t>(r) * a.units);
+        const uint32_t head = CUT ? head_of<T>(a, r) : 0u;
+        const T* row = logits + static_cast<int64_t>(r) * a.V;
+        const int64_t e0 = static_cast<int64_t>(k) * P - head + lane * VW;
+        uint4 raw[kLoads];
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q) {
+            const int64_t at = e0 + q * 32 * VW;
+            raw[q] = sizeof(T) == 2 ? make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u)
+                                    : make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u);
+            if (at < static_cast<int64_t>(a.V)) raw[q] = row_vector<T, CUT>(row, at, a.V);
         }
-        best = warp_max_u64(best);
-        __syncthreads();
-        if (lane == 0) keys[warp] = best;
-        __syncthreads();
-        best = warp_max_u64(lane < kWarps ? keys[lane] : 0ull);
-        if (k == 0) {
-            m = key_value(best) * a.inv_t;
-            if (m > -INFINITY)
-                for (int v = threadIdx.x; v < a.V; v += kThreads) {
-                    const float d = to_f32(x[v]) * a.inv_t - m, e = expf(d);
-                    l += e;
-                    if (e > 0.f) t += e * d;
-                }
-            l = warp_sum(l), t = warp_sum(t);
-            __syncthreads();
-            if (lane == 0) sums[0][warp] = l, sums[1][warp] = t;
-            __syncthreads();
-            l = warp_sum(lane < kWarps ? sums[0][lane] : 0.f);
-            t = warp_sum(lane < kWarps ? sums[1][lane] : 0.f);
-            if (m > -INFINITY) lse = m + logf(l);
-            if (threadIdx.x == 0) {
-                if (a.entropy) a.entropy[r] = m > -INFINITY ? logf(l) - t / l : 0.f;
-                if (a.logprob && a.tokens) {
-                    const int tok = a.tokens[r];
-                    a.logprob[r] = tok >= 0 && tok < a.V && m > -INFINITY ? to_f32(x[tok]) * a.inv_t - lse : -INFINITY;
+        float top[kLoads], m = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q) {
+            top[q] = vmax(raw[q], T());
+            m = fmaxf(m, top[q]);
+        }
+        // a lane's sums against its own maximum, the differences first (l - m) and the factor after, so that
+        // large offsets and the lowest values cost nothing; what weighs nothing must not make 0 * inf
+        float L = 0.f, U = 0.f;
+        if (m > -INFINITY) {
+            const uint64_t c2 = pack_f32x2(a.c, a.c), m2 = pack_f32x2(-m, -m);
+            uint64_t l2 = 0, u2 = 0;
+#pragma unroll
+            for (int q = 0; q < kLoads; ++q) {
+                float e[VW];
+                unpack(raw[q], e);
+#pragma unroll
+                for (int j = 0; j < VW; j += 2) {
+                    const uint64_t y = fma_f32x2(add_f32x2(pack_f32x2(e[j], e[j + 1]), m2), c2, 0ull);
+                    const float y0 = fmaxf(lo_f32(y), -1000.f), y1 = fmaxf(hi_f32(y), -1000.f);
+                    const uint64_t w = pack_f32x2(ex2(y0), ex2(y1));
+                    l2 = add_f32x2(l2, w);
+                    u2 = fma_f32x2(w, pack_f32x2(y0, y1), u2);
                 }
             }
-        } else {
-            last = best;
-            if (threadIdx.x == 0) {
-                if (a.top_id) a.top_id[r * a.top + k - 1] = static_cast<int>(key_index(best));
-                if (a.top_logprob) a.top_logprob[r * a.top + k - 1] = m > -INFINITY ? key_value(best) * a.inv_t - lse : -INFINITY;
+            L = lo_f32(l2) + hi_f32(l2);
+            U = lo_f32(u2) + hi_f32(u2);
+        }
+        float4 best;
+        best.x = warp_max(top[0]);
+        best.y = warp_max(top[1]);
+        best.z = warp_max(top[2]);
+        best.w = warp_max(top[3]);
+        const float M = fmaxf(fmaxf(best.x, best.y), fmaxf(best.z, best.w));
+        if (L != 0.f) {
+            const float d = fmaxf((m - M) * a.c, -1000.f), by = ex2(d);
+            U = (U + L * d) * by;
+            L *= by;
+        }
+        L = warp_sum(L);
+        U = warp_sum(U);
+        if (lane == 0) {
+            a.maxima[u] = best;
+            a.sums[u] = make_float2(L, U);
+        }
+    }
+}
+
+__device__ __forceinline__ unsigned long long warp_best(unsigned long long v) {   // the largest key of the warp
+    const uint32_t hi = __reduce_max_sync(0xFFFFFFFFu, static_cast<uint32_t>(v >> 32));
+    const uint32_t lo = __reduce_max_sync(0xFFFFFFFFu, static_cast<uint32_t>(v >> 32) == hi ? static_cast<uint32_t>(v) : 0u);
+    return static_cast<unsigned long long>(hi) << 32 | lo;
+}
+
+constexpr int kFinishThreads = 128;
+constexpr int kHeld = 16;      // chunk maxima a lane holds: rows of up to 512 chunks; longer ones are read again each time
+
+template <typename T, bool CUT>
+__global__ void __launch_bounds__(kFinishThreads) logprob_finish_kernel(const T* __restrict__ logits, const LogprobArgs a) {
+    pdl_enter();
+    constexpr int VW = 16 / sizeof(T), CE = 32 * VW;              // elements of a chunk
+    const int lane = threadIdx.x & 31;
+    const int64_t r = static_cast<int64_t>(blockIdx.x) * (kFinishThreads / 32) + (threadIdx.x >> 5);
+    if (r >= a.rows) return;
+    const T* row = logits + r * a.V;
+    const float4* maxima = a.maxima + r * a.units;
+    const float* chunk_max = reinterpret_cast<const float*>(maxima);
+    const float2* sums = a.sums + r * a.units;
+    int token = -1;
+    float at_token = -INFINITY;
+    if (a.tokens) {
+        token = __ldg(a.tokens + r);
+        if (token >= 0 && token < static_cast<int>(a.V)) at_token = to_f32(row[token]);
+    }
+    const uint32_t chunks = a.units * kLoads;
+    float held[kHeld];
+    float M = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+        const uint32_t ch = lane + 32u * i;
+        held[i] = ch < chunks ? __ldcg(chunk_max + ch) : -INFINITY;
+        M = fmaxf(M, held[i]);
+    }
+    for (uint32_t ch = lane + 32u * kHeld; ch < chunks; ch += 32) M = fmaxf(M, __ldcg(chunk_max + ch));
+    M = warp_max(M);
+    float L = 0.f, U = 0.f;
+    if (M > -INFINITY)
+        for (uint32_t k = lane; k < a.units; k += 32) {
+            const float2 s = __ldcg(sums + k);
+            const float4 t = __ldcg(maxima + k);
+            const float d = fmaxf((fmaxf(fmaxf(t.x, t.y), fmaxf(t.z, t.w)) - M) * a.c, -1000.f), by = ex2(d);
+            if (s.x != 0.f) {
+                L = fmaf(s.x, by, L);
+                U = fmaf(s.y + s.x * d, by, U);
+            }
+        }
+    L = warp_sum(L);
+    U = warp_sum(U);
+    constexpr float kLn2 = 0.69314718055994531f;
+    const float log_l = log2f(L);                                 // L >= 1 unless the row is empty
+    if (lane == 0) {
+        if (a.logprob) a.logprob[r] = at_token > -INFINITY ? ((at_token - M) * a.c - log_l) * kLn2 : -INFINITY;
+        if (a.entropy) a.entropy[r] = M > -INFINITY ? (log_l - U / L) * kLn2 : 0.f;
+    }
+    if (a.top == 0) return;
+
+    // the chunks: one a turn, the largest maximum first; lane i keeps the i-th
+    unsigned long long last = ~0ull;
+    uint32_t mine = 0;
+    float floor_value = -INFINITY;                                // the k-th chunk's maximum, where there are k
+    const int want = min(static_cast<uint32_t>(a.top), chunks);
+    unsigned long long own = 0;
+    auto best_own = [&] {                                         // this lane's next chunk
+        own = 0;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const uint32_t ch = lane + 32u * i;
+            const unsigned long long key = pack_key(held[i], ch);
+            if (ch < chunks && key < last && key > own) own = key;
+        }
+        for (uint32_t ch = lane + 32u * kHeld; ch < chunks; ch += 32) {
+            const unsigned long long key = pack_key(__ldcg(chunk_max + ch), ch);
+            if (key < last && key > own) own = key;
+        }
+    };
+    best_own();
+    for (int i = 0; i < want; ++i) {
+        last = warp_best(own);
+        if (lane == i) mine = key_index(last);
+        if (own == last) best_own();
+    }
+    if (want == a.top) floor_value = key_value(last);
+
+    // their elements: lane i ends with the i-th best key
+    const uint32_t head = CUT ? head_of<T>(a, r) : 0u;
+    unsigned long long list = 0;
+    constexpr int kAhead = 4;
+    for (int i0 = 0; i0 < want; i0 += kAhead) {
+        uint4 raw[kAhead];
+        int64_t first[kAhead];
+#pragma unroll
+        for (int p = 0; p < kAhead; ++p) {
+            const uint32_t ch = __shfl_sync(0xFFFFFFFFu, mine, min(i0 + p, want - 1));
+            first[p] = static_cast<int64_t>(ch) * CE - head + lane * VW;
+            raw[p] = make_uint4(0u, 0u, 0u, 0u);
+            if (i0 + p < want && first[p] < static_cast<int64_t>(a.V)) raw[p] = row_vector<T, CUT>(row, first[p], a.V);
+        }
+#pragma unroll
+        for (int p = 0; p < kAhead; ++p) {
+            if (i0 + p >= want) break;
+            float e[VW];
+            unpack(raw[p], e);
+            unsigned taken = 0;
+            while (true) {
+                const unsigned long long kth = __shfl_sync(0xFFFFFFFFu, list, a.top - 1);
+                unsigned long long cand = 0;
+                int which = 0;
+#pragma unroll
+                for (int j = 0; j < VW; ++j) {
+                    const int64_t v = first[p] + j;
+                    const unsigned long long key = pack_key(e[j], static_cast<uint32_t>(v));
+                    if (v >= 0 && v < static_cast<int64_t>(a.V) && !(taken >> j & 1u) && e[j] >= floor_value && key > kth && key > cand)
+                        cand = key, which = j;
+                }
+                if (!__any_sync(0xFFFFFFFFu, cand != 0)) break;
+                const unsigned long long best = warp_best(cand);
+                if (cand == best) taken |= 1u << which;
+                const int place = __popc(__ballot_sync(0xFFFFFFFFu, list > best));
+                const unsigned long long above = __shfl_up_sync(0xFFFFFFFFu, list, 1);
+                if (lane > place) list = above;
+                if (lane == place) list = best;
             }
         }
     }
+    if (lane < a.top) {
+        if (a.top_id) a.top_id[r * a.top + lane] = static_cast<int>(key_index(list));
+        if (a.top_logprob) {
+            const float x = key_value(list);
+            a.top_logprob[r * a.top + lane] = x > -INFINITY ? ((x - M) * a.c - log_l) * kLn2 : -INFINITY;
+        }
+    }
+}
+
+// Units of a row: whole vectors from the one that holds its first element, wherever in it that is.
+int64_t units_of(int64_t V, size_t es, bool cut) {
+    const int64_t VW = 16 / static_cast<int64_t>(es), P = kUnitBytes / static_cast<int64_t>(es);
+    return (V + (cut ? VW - 1 : 0) + P - 1) / P;
+}
+
+template <typename T, bool CUT>
+cudaError_t launch(const void* logits, const LogprobArgs& a, cudaStream_t s) {
+    const T* x = static_cast<const T*>(logits);
+    const int64_t total = a.rows * a.units, most = static_cast<int64_t>(kBlocksPerSm) * kWaves * sm_count();
+    int64_t blocks = (total + kWarps - 1) / kWarps;
+    if (blocks > most) blocks = most;
+    const cudaError_t e = launch_pdl(logprob_sums_kernel<T, CUT>, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, s, 0, x, a);
+    if (e != cudaSuccess) return e;
+    constexpr int per = kFinishThreads / 32;
+    return launch_pdl(logprob_finish_kernel<T, CUT>, dim3(static_cast<unsigned>((a.rows + per - 1) / per)), dim3(kFinishThreads), 0,
+                      s, 0, x, a);
 }
 
 }  // namespace
@@ -81,7 +315,8 @@ extern "C" {
 
 PLDP_API size_t pldp_token_logprobs_workspace_size(int64_t rows, int V) {
     if (rows < 0 || V < 1) return 0;
-    return 256;
+    const size_t units = static_cast<size_t>(rows) * units_of(V, 4, true);     // fp32 has the most
+    return (units * (sizeof(float4) + sizeof(float2)) + 255) / 256 * 256;
 }
 
 PLDP_API pldp_status pldp_token_logprobs(const void* logits, pldp_dtype dtype, int64_t rows, int V, float temperature,
@@ -104,14 +339,22 @@ PLDP_API pldp_status pldp_token_logprobs(const void* logits, pldp_dtype dtype, i
     if (workspace_bytes < need)
         return fail(PLDP_ERR_INVALID_ARG, "%s: workspace needs %zu bytes, has %zu", fn, need, workspace_bytes);
     if (!aligned16(workspace)) return fail(PLDP_ERR_INVALID_ARG, "%s: workspace is not 16-byte aligned", fn);
-    LogprobArgs a = {tokens, logprob, entropy, top_logprob, top_id, V, top_id || top_logprob ? top : 0, 1.f / temperature};
+    const size_t es = dtype == PLDP_F32 ? 4 : 2;
+    if (reinterpret_cast<uintptr_t>(logits) % es) return fail(PLDP_ERR_INVALID_ARG, "%s: logits are not aligned to their elements", fn);
+    LogprobArgs a = {};
+    a.tokens = tokens, a.logprob = logprob, a.entropy = entropy;
+    a.top_id = top_id, a.top_logprob = top_logprob, a.top = top_id || top_logprob ? top : 0;
+    a.rows = rows, a.V = static_cast<uint32_t>(V);
+    a.lead = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(logits) % 16 / es);
+    const bool cut = a.lead != 0 || static_cast<size_t>(V) * es % 16 != 0;
+    a.units = static_cast<uint32_t>(units_of(V, es, cut));
+    a.maxima = static_cast<float4*>(workspace);
+    a.sums = reinterpret_cast<float2*>(a.maxima + rows * a.units);
+    a.c = 1.4426950408889634f / temperature;
     auto s = static_cast<cudaStream_t>(stream);
-    const dim3 grid(static_cast<unsigned>(rows));
-    const cudaError_t e =
-        dtype == PLDP_F32
-            ? launch_pdl(logprobs_kernel<float>, grid, dim3(kThreads), 0, s, 0, static_cast<const float*>(logits), a)
-            : launch_pdl(logprobs_kernel<__nv_bfloat16>, grid, dim3(kThreads), 0, s, 0,
-                         static_cast<const __nv_bfloat16*>(logits), a);
+    cudaError_t e;
+    if (dtype == PLDP_F32) e = cut ? launch<float, true>(logits, a, s) : launch<float, false>(logits, a, s);
+    else e = cut ? launch<__nv_bfloat16, true>(logits, a, s) : launch<__nv_bfloat16, false>(logits, a, s);
     if (e != cudaSuccess) return fail(PLDP_ERR_CUDA, "%s: launch failed: %s", fn, cudaGetErrorString(e));
     return check_launch(fn);
 }
