@@ -80,7 +80,7 @@ struct Shape {
     static constexpr int kWeights = E4M3 ? NT : 2 * NT;        // columns of the second product
     static constexpr int kStage = E4M3 ? kTile * (DP < 128 ? 128 : DP) : 0;    // one tile's codes
     static constexpr int kRest = kQ + kP * (E4M3 ? 1 : 2);
-    static constexpr int kColumns = NT >= 96 ? 7168 : 4096;    // static: Columns
+    static constexpr int kColumns = NT >= 96 ? 8192 : 4608;    // static: Columns
     static constexpr int kRoom = kMaxShared - 1024 - kColumns - kRest;
     static constexpr int kSlots = E4M3 ? (DP == 256 ? 2 : 3) : (kRoom / kSlot < 8 ? kRoom / kSlot : 8);
     static constexpr int kStages = E4M3 ? ((kRoom - kSlots * kSlot) / kStage < 7 ? (kRoom - kSlots * kSlot) / kStage : 7) : 0;
@@ -98,7 +98,7 @@ struct Shape {
 template <int NT>
 struct Columns {
     int64_t q_at[NT], o_at[NT];     // element offsets, -1: no such row
-    float neg_m[NT], factor[NT], sum[NT];
+    float neg_m[NT], factor[NT], sum[NT], inverse[NT];
     float part[4][NT];
     int limit[NT];                  // last position that the row sees
     int seen[NT];                   // whether m has been set
@@ -163,6 +163,32 @@ __device__ __forceinline__ uint32_t two_codes(uint32_t codes) {
 __device__ __forceinline__ float warp_max(float v) {
     const uint32_t k = __reduce_max_sync(0xFFFFFFFFu, ordered_key(v));
     return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
+}
+
+// A load that stays where it is written, ahead of its use.
+__device__ __forceinline__ int load_now(const int32_t* p) {
+    int v;
+    asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ float load_now(const float* p) {
+    float v;
+    asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(v) : "l"(p));
+    return v;
+}
+
+// Two, four or eight floats past the caches of an SM (another SM wrote them).
+__device__ __forceinline__ void load_floats(const float* p, float (&v)[2]) {
+    const float2 x = __ldcg(reinterpret_cast<const float2*>(p));
+    v[0] = x.x, v[1] = x.y;
+}
+__device__ __forceinline__ void load_floats(const float* p, float (&v)[4]) {
+    const float4 x = __ldcg(reinterpret_cast<const float4*>(p));
+    v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+}
+__device__ __forceinline__ void load_floats(const float* p, float (&v)[8]) {
+    const float4 x = __ldcg(reinterpret_cast<const float4*>(p)), y = __ldcg(reinterpret_cast<const float4*>(p) + 1);
+    v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w, v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
 }
 
 // Sums v[0..C) over the warp's lanes, C = 8, 16 or a multiple of 16: each lane ends with the sums of the
@@ -302,7 +328,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 const int32_t* table = c.pages + w.b * c.pages_stride;
                 auto look = [&](int tile, int q) {                         // the page of box lane + 32 q
                     const int at = lane + 32 * q, pos = tile * kTile + at * a.box;
-                    return tile < w.t1 && at < boxes && pos < w.keys ? __ldg(table + page_of(pos, c.div_mul, c.div_shift)) : 0;
+                    return tile < w.t1 && at < boxes && pos < w.keys ? load_now(table + page_of(pos, c.div_mul, c.div_shift)) : 0;
                 };
                 int page[4];
 #pragma unroll
@@ -517,7 +543,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
             auto look = [&](int tile) {
                 const int pos = tile * kTile + j;
                 int page = -1;
-                if (tile < w.t1 && pos < w.keys) page = __ldg(table + page_of(pos, c.div_mul, c.div_shift));
+                if (tile < w.t1 && pos < w.keys) page = load_now(table + page_of(pos, c.div_mul, c.div_shift));
                 return static_cast<unsigned>(page) < static_cast<unsigned>(c.n_pages) ? page : -1;
             };
             auto fetch = [&](int tile, int page) {
@@ -526,8 +552,8 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                     if (page >= 0) {
                         const int64_t at = (static_cast<int64_t>(page) * c.heads + kv) * c.page_size +
                                            (pos - static_cast<int>(page_of(pos, c.div_mul, c.div_shift)) * c.page_size);
-                        ks_next = __ldg(c.k_scale + at);
-                        vs_next = __ldg(c.v_scale + at);
+                        ks_next = load_now(c.k_scale + at);
+                        vs_next = load_now(c.v_scale + at);
                     }
                 }
             };
@@ -696,7 +722,9 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 const int t = tid & 127;
                 if (t < C) {
                     const int n = c0 + t;
-                    col.sum[n] = col.part[0][n] + col.part[1][n] + col.part[2][n] + col.part[3][n];
+                    const float s = col.part[0][n] + col.part[1][n] + col.part[2][n] + col.part[3][n];
+                    col.sum[n] = s;
+                    col.inverse[n] = s == 0.f || col.limit[n] < 0 ? 0.f : 1.f / s;      // 0: an empty row
                 }
             }
             wait_for(&col.pv_done, tile_no - 1, &col.dead);
@@ -739,8 +767,8 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                             const int n = c0 + ch * CH + i;
                             if (col.o_at[n] < 0) continue;
                             if (whole) {
-                                const float s = col.sum[n];
-                                a.out[col.o_at[n] + d] = __float2bfloat16(s == 0.f || col.limit[n] < 0 ? 0.f : o[i] / s);
+                                const float by = col.inverse[n];
+                                a.out[col.o_at[n] + d] = __float2bfloat16(by == 0.f ? 0.f : o[i] * by);
                             } else {
                                 part[n * DP + d] = o[i];
                             }
@@ -766,32 +794,57 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 bar_sync(4, kSoftmaxThreads);
                 if (col.last) {
                     __threadfence();
-                    for (int n = warp; n < NT; n += kSoftmaxThreads / 32) {
-                        const int64_t to = col.o_at[n];
-                        if (to < 0) continue;
-                        auto place = [&](int cta) { return a.parts + static_cast<int64_t>(2 * cta + (cta == c_first ? 1 : 0)) * kPart; };
-                        float M = -INFINITY, sum = 0.f;
-                        for (int k = c_first + lane; k <= c_last; k += 32) M = fmaxf(M, __ldcg(place(k) + NT * DP + n));
-                        M = warp_max(M);
-                        constexpr int kPer = DP / 32;
-                        float o[kPer];
+                    // two rows a warp at once, some parts of each in flight; a lane holds V elements side by side
+                    constexpr int kWarps = kSoftmaxThreads / 32, V = DP / 32, F = V == 2 ? 8 : V == 4 ? 4 : 2;
+                    const int parts = c_last - c_first + 1;
+                    auto place = [&](int k) { return a.parts + static_cast<int64_t>(2 * (c_first + k) + (k == 0 ? 1 : 0)) * kPart; };
+                    for (int n0 = warp; n0 < NT; n0 += 2 * kWarps) {
+                        float M[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f}, o[2][V] = {};
+                        for (int k = lane; k < parts; k += 32)
 #pragma unroll
-                        for (int p = 0; p < kPer; ++p) o[p] = 0.f;
-                        if (M > -INFINITY && col.limit[n] >= 0)
-                            for (int k = c_first; k <= c_last; ++k) {
-                                const float* from = place(k);
-                                const float m = __ldcg(from + NT * DP + n);
-                                if (!(m > -INFINITY)) continue;
-                                const float by = ex2(m - M);
-                                sum = fmaf(by, __ldcg(from + NT * DP + NT + n), sum);
+                            for (int r = 0; r < 2; ++r)
+                                if (n0 + r * kWarps < NT) M[r] = fmaxf(M[r], __ldcg(place(k) + NT * DP + n0 + r * kWarps));
 #pragma unroll
-                                for (int p = 0; p < kPer; ++p)
-                                    if (lane + 32 * p < D) o[p] = fmaf(by, __ldcg(from + n * DP + lane + 32 * p), o[p]);
-                            }
+                        for (int r = 0; r < 2; ++r) M[r] = warp_max(M[r]);
+                        for (int k0 = 0; k0 < parts; k0 += F) {
+                            float x[2][F][V], m[2][F], l[2][F];
 #pragma unroll
-                        for (int p = 0; p < kPer; ++p)
-                            if (lane + 32 * p < D) a.out[to + lane + 32 * p] = __float2bfloat16(sum == 0.f ? 0.f : o[p] / sum);
-                        if (lane == 0 && a.lse) a.lse[lse_at(n)] = sum == 0.f ? -INFINITY : (log2f(sum) + M) * 0.69314718055994531f;
+                            for (int q = 0; q < F; ++q)
+#pragma unroll
+                                for (int r = 0; r < 2; ++r) {
+                                    const int n = n0 + r * kWarps;
+                                    m[r][q] = -INFINITY;
+                                    if (k0 + q < parts && n < NT && col.o_at[n] >= 0) {
+                                        const float* from = place(k0 + q);
+                                        m[r][q] = __ldcg(from + NT * DP + n);
+                                        l[r][q] = __ldcg(from + NT * DP + NT + n);
+                                        load_floats(from + n * DP + lane * V, x[r][q]);
+                                    }
+                                }
+#pragma unroll
+                            for (int q = 0; q < F; ++q)
+#pragma unroll
+                                for (int r = 0; r < 2; ++r)
+                                    if (m[r][q] > -INFINITY) {
+                                        const float by = ex2(m[r][q] - M[r]);
+                                        sum[r] = fmaf(by, l[r][q], sum[r]);
+#pragma unroll
+                                        for (int p = 0; p < V; ++p) o[r][p] = fmaf(by, x[r][q][p], o[r][p]);
+                                    }
+                        }
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            const int n = n0 + r * kWarps;
+                            if (n >= NT || col.o_at[n] < 0) continue;
+                            const bool none = sum[r] == 0.f || col.limit[n] < 0;
+                            const float by = none ? 0.f : 1.f / sum[r];
+                            if (lane * V < D)
+#pragma unroll
+                                for (int p = 0; p < V; p += 2)
+                                    *reinterpret_cast<uint32_t*>(a.out + col.o_at[n] + lane * V + p) =
+                                        none ? 0u : pack_bf16(o[r][p] * by, o[r][p + 1] * by);
+                            if (lane == 0 && a.lse) a.lse[lse_at(n)] = none ? -INFINITY : (log2f(sum[r]) + M[r]) * 0.69314718055994531f;
+                        }
                     }
                 }
             }
