@@ -50,7 +50,9 @@ namespace {
 // its own sums and writes them to shared memory as the next product's operand.  The running
 // maximum m of a column only moves when a score passes it by more than 2^8: then the column's
 // sums and its accumulators in tensor memory are scaled; otherwise no thread needs another's
-// scores, and the 128 of them agree on that with one barrier.
+// scores, and the 128 of them agree on that with one barrier.  bf16 weights have fp32's range: there the
+// maximum may be passed by 2^64, and m starts as the first key's score, whose weight is then 1, so that the
+// sums cannot vanish.
 //
 // Weights are rounded to 16 bits for the second product: in a bf16 cache as a sum of two bf16
 // (2^-17 of the weight; one alone would add as much error as the result's own rounding), the second
@@ -79,7 +81,9 @@ struct Shape {
     static constexpr int kP = NT * 2 * kTile;                  // weights of a tile, 16 bits each
     static constexpr int kWeights = E4M3 ? NT : 2 * NT;        // columns of the second product
     static constexpr int kStage = E4M3 ? kTile * (DP < 128 ? 128 : DP) : 0;    // one tile's codes
-    static constexpr int kRest = kQ + kP * (E4M3 ? 1 : 2);
+    static constexpr int kPs = kP * (E4M3 ? 1 : 2);            // with the low parts
+    static constexpr int kWeightTiles = NT <= 64 && DP <= 128 ? 2 : 1;     // tiles of weights held
+    static constexpr int kRest = kQ + kPs * kWeightTiles;
     static constexpr int kColumns = NT >= 96 ? 8192 : 4608;    // static: Columns
     static constexpr int kRoom = kMaxShared - 1024 - kColumns - kRest;
     static constexpr int kSlots = E4M3 ? (DP == 256 ? 2 : 3) : (kRoom / kSlot < 8 ? kRoom / kSlot : 8);
@@ -102,13 +106,12 @@ struct Columns {
     float part[4][NT];
     int limit[NT];                  // last position that the row sees
     int seen[NT];                   // whether m has been set
-    uint64_t full[8], empty[8], stage_full[8], stage_empty[8], s_full[2], p_full, pv_done, q_full;
+    uint64_t full[8], empty[8], stage_full[8], stage_empty[8], s_full[2], p_full[2], pv_done[2], q_full;
     uint32_t tmem, amax;
     int dead, last;
     int b, unit, tile;              // where this CTA's part of the list starts
     long long at, count;            // its first tile in the list, tiles in it
-    long long total;
-    int ctas;
+    long long each, extra;          // tiles a CTA, and CTAs that have one more
     long long warp_sum[16];
 };
 
@@ -155,11 +158,17 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
     const __half2 p = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&p);
 }
-__device__ __forceinline__ uint32_t two_codes(uint32_t codes) {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(codes), __NV_E4M3);
-    return static_cast<uint32_t>(h.x) | static_cast<uint32_t>(h.y) << 16;
+// Four e4m3 codes as four f16.
+__device__ __forceinline__ uint2 four_codes(uint32_t codes) {
+    uint2 h;
+    asm("{\n\t.reg .b16 lo, hi;\n\t"
+        "mov.b32 {lo, hi}, %2;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %0, lo;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %1, hi;\n\t}"
+        : "=r"(h.x), "=r"(h.y)
+        : "r"(codes));
+    return h;
 }
-
 __device__ __forceinline__ float warp_max(float v) {
     const uint32_t k = __reduce_max_sync(0xFFFFFFFFu, ordered_key(v));
     return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
@@ -175,20 +184,6 @@ __device__ __forceinline__ float load_now(const float* p) {
     float v;
     asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(v) : "l"(p));
     return v;
-}
-
-// Two, four or eight floats past the caches of an SM (another SM wrote them).
-__device__ __forceinline__ void load_floats(const float* p, float (&v)[2]) {
-    const float2 x = __ldcg(reinterpret_cast<const float2*>(p));
-    v[0] = x.x, v[1] = x.y;
-}
-__device__ __forceinline__ void load_floats(const float* p, float (&v)[4]) {
-    const float4 x = __ldcg(reinterpret_cast<const float4*>(p));
-    v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
-}
-__device__ __forceinline__ void load_floats(const float* p, float (&v)[8]) {
-    const float4 x = __ldcg(reinterpret_cast<const float4*>(p)), y = __ldcg(reinterpret_cast<const float4*>(p) + 1);
-    v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w, v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
 }
 
 // Sums v[0..C) over the warp's lanes, C = 8, 16 or a multiple of 16: each lane ends with the sums of the
@@ -247,8 +242,10 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
         }
         mbar_init(&col.s_full[0], 1);
         mbar_init(&col.s_full[1], 1);
-        mbar_init(&col.p_full, kSoftmaxThreads);
-        mbar_init(&col.pv_done, 1);
+        mbar_init(&col.p_full[0], kSoftmaxThreads);
+        mbar_init(&col.p_full[1], kSoftmaxThreads);
+        mbar_init(&col.pv_done[0], 1);
+        mbar_init(&col.pv_done[1], 1);
         mbar_init(&col.q_full, kSoftmaxThreads);
         fence_mbar_init();
         col.dead = 0;
@@ -282,7 +279,11 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
         }
         total *= units;
         const int ctas = static_cast<int>(total < gridDim.x ? total : gridDim.x);
-        const long long g0 = total * blockIdx.x / ctas, g1 = total * (blockIdx.x + 1ll) / ctas;
+        // the first `extra` CTAs take one tile more than the others
+        const long long each = total >> 32 ? total / ctas : static_cast<uint32_t>(total) / static_cast<uint32_t>(ctas);
+        const long long extra = total - each * ctas;
+        const long long g0 = each * blockIdx.x + min(static_cast<long long>(blockIdx.x), extra);
+        const long long g1 = g0 + each + (blockIdx.x < extra ? 1 : 0);
         long long before = (upto - mine) * units;
         if (blockIdx.x < ctas && before <= g0 && g0 < before + mine * units) {     // one thread's
             int b = lo;
@@ -299,8 +300,8 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
             col.count = g1 - g0;
         }
         if (threadIdx.x == 0) {
-            col.total = total;
-            col.ctas = ctas;
+            col.each = each;
+            col.extra = extra;
             if (blockIdx.x >= ctas) col.count = 0;
         }
     }
@@ -315,15 +316,17 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
         // e4m3: 16 warps start with 128 registers a thread; the softmax takes what the others leave:
         // 256 * 176 + 128 * 88 + 128 * 64 = 64512 of 65536
         if constexpr (E4M3) fewer_registers<64>();
-        if (warp == S::kCopyWarp) {
-            // ---- copies: the tiles of keys and values in turn, a box (positions of one page) a lane ----
+        if (warp == S::kCopyWarp || warp == S::kCopyWarp + 1) {
+            // ---- copies: one warp the tiles of keys, one those of values; a box (positions of one page) a lane ----
             constexpr int kDepth = E4M3 ? S::kStages : S::kSlots;
             uint64_t* const arrived = E4M3 ? col.stage_full : col.full;
             uint64_t* const left = E4M3 ? col.stage_empty : col.empty;
             const int boxes = kTile / a.box;                               // of a tile, 1..128
-            int e = 0;
+            const int kv = warp - S::kCopyWarp;
+            const CUtensorMap* map = kv ? &v_map : &k_map;
+            int e = kv;                                                    // entries of the ring: keys and values in turn
             while (w.next(a, &st)) {
-                if (w.t0 == 0 && w.unit == 0 && lane == 0 && st && a.status) atomicOr(a.status + w.b, st);
+                if (kv == 0 && w.t0 == 0 && w.unit == 0 && lane == 0 && st && a.status) atomicOr(a.status + w.b, st);
                 const int head = w.unit / a.row_tiles;
                 const int32_t* table = c.pages + w.b * c.pages_stride;
                 auto look = [&](int tile, int q) {                         // the page of box lane + 32 q
@@ -333,38 +336,35 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 int page[4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) page[q] = look(w.t0, q);
-                for (int tile = w.t0; tile < w.t1; ++tile) {
+                for (int tile = w.t0; tile < w.t1; ++tile, e += 2) {
                     int next[4];
 #pragma unroll
                     for (int q = 0; q < 4; ++q) next[q] = look(tile + 1, q);
                     // boxes that hold a position below the sequence's end
                     const int full = max(0, min(boxes, (w.keys - tile * kTile + a.box - 1) / a.box));
-                    for (int kv = 0; kv < 2; ++kv, ++e) {
-                        const int at = e % kDepth;
-                        if (e >= kDepth) wait_for(&left[at], e / kDepth - 1, &col.dead);
-                        if (lane == 0) mbar_arrive_expect_tx(&arrived[at], full * a.box * (E4M3 ? a.pitch : S::kPanels * 128));
-                        __syncwarp();
-                        uint8_t* dst = E4M3 ? stages + at * S::kStage : ring + at * S::kSlot;
-                        const CUtensorMap* map = kv ? &v_map : &k_map;
+                    const int at = e % kDepth;
+                    if (e >= kDepth) wait_for(&left[at], e / kDepth - 1, &col.dead);
+                    if (lane == 0) mbar_arrive_expect_tx(&arrived[at], full * a.box * (E4M3 ? a.pitch : S::kPanels * 128));
+                    __syncwarp();
+                    uint8_t* dst = E4M3 ? stages + at * S::kStage : ring + at * S::kSlot;
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const int box = lane + 32 * q;
-                            if (box >= full) break;
-                            const int pos = tile * kTile + box * a.box;
-                            const int slot = pos - static_cast<int>(page_of(pos, c.div_mul, c.div_shift)) * c.page_size;
-                            int pg = page[q];
-                            if (static_cast<unsigned>(pg) >= static_cast<unsigned>(c.n_pages)) {
-                                pg = c.n_pages;                            // outside the tensor: zeros
-                                if (kv == 0 && a.status) atomicOr(a.status + w.b, PLDP_ST_PAGE);
-                            }
-                            const int c1 = a.head_first ? head : slot, c2 = a.head_first ? slot : head;
-                            if constexpr (E4M3) {
-                                tma_box(dst + box * a.box * a.pitch, map, 0, c1, c2, pg, &arrived[at]);
-                            } else {
+                    for (int q = 0; q < 4; ++q) {
+                        const int box = lane + 32 * q;
+                        if (box >= full) break;
+                        const int pos = tile * kTile + box * a.box;
+                        const int slot = pos - static_cast<int>(page_of(pos, c.div_mul, c.div_shift)) * c.page_size;
+                        int pg = page[q];
+                        if (static_cast<unsigned>(pg) >= static_cast<unsigned>(c.n_pages)) {
+                            pg = c.n_pages;                            // outside the tensor: zeros
+                            if (kv == 0 && a.status) atomicOr(a.status + w.b, PLDP_ST_PAGE);
+                        }
+                        const int c1 = a.head_first ? head : slot, c2 = a.head_first ? slot : head;
+                        if constexpr (E4M3) {
+                            tma_box(dst + box * a.box * a.pitch, map, 0, c1, c2, pg, &arrived[at]);
+                        } else {
 #pragma unroll
-                                for (int p = 0; p < S::kPanels; ++p)
-                                    tma_box(dst + p * (kTile * 128) + box * a.box * 128, map, p * 64, c1, c2, pg, &arrived[at]);
-                            }
+                            for (int p = 0; p < S::kPanels; ++p)
+                                tma_box(dst + p * (kTile * 128) + box * a.box * 128, map, p * 64, c1, c2, pg, &arrived[at]);
                         }
                     }
 #pragma unroll
@@ -376,20 +376,24 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
         } else if (warp == S::kMmaWarp) {
             // ---- matrix instructions ----
             if (lane == 0) {
+                // the operands' descriptors in two words: addresses move the low one, in units of 16 bytes
                 const uint64_t q_op = smem_operand(smem_u32(q_smem), 16, 1024, swizzle_mode(128));
                 const uint64_t p_op = smem_operand(smem_u32(p_smem), kTile * S::kRow, 8 * S::kRow, swizzle_mode(S::kRow));
                 const uint64_t k_op = smem_operand(smem_u32(ring), 16, 1024, swizzle_mode(128));
                 const uint64_t v_op = smem_operand(smem_u32(ring), kTile * 128, 1024, swizzle_mode(128));
+                const uint32_t q_lo = static_cast<uint32_t>(q_op), q_hi = q_op >> 32, p_lo = static_cast<uint32_t>(p_op), p_hi = p_op >> 32;
+                const uint32_t k_lo = static_cast<uint32_t>(k_op), k_hi = k_op >> 32, v_lo = static_cast<uint32_t>(v_op), v_hi = v_op >> 32;
                 constexpr uint32_t kScores = mma_form(128, NT, !E4M3, false, false), kValues = mma_form(128, S::kWeights, !E4M3, true, true);
                 int e = 0, tile = 0, segment = 0;       // entries, tiles and units so far
                 auto scores = [&](int entry, int k) {
                     const int slot = entry % S::kSlots;
                     wait_for(&col.full[slot], entry / S::kSlots, &col.dead);
                     tmem_after_sync();
-                    const uint64_t op = advance(k_op, slot * S::kSlot);
-                    for (int s = 0; s < D / 16; ++s)
-                        mma_f16(tmem + (k & 1) * NT, advance(op, (s >> 2) * (kTile * 128) + (s & 3) * 32),
-                                advance(q_op, (s >> 2) * (NT * 128) + (s & 3) * 32), kScores, s > 0);
+                    const uint32_t op = k_lo + slot * (S::kSlot / 16), to = tmem + (k & 1) * NT;
+#pragma unroll
+                    for (int s = 0; s < DP / 16; ++s)
+                        if (s == 0 || s * 16 < D)
+                            mma_f16(to, op + (s >> 2) * (kTile * 8) + (s & 3) * 2, k_hi, q_lo + (s >> 2) * (NT * 8) + (s & 3) * 2, q_hi, kScores, s > 0);
                     mma_commit(&col.empty[slot]);
                     mma_commit(&col.s_full[k & 1]);
                 };
@@ -400,19 +404,20 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                     scores(e, tile);
                     for (int i = 0; i < count; ++i, ++tile, e += 2) {
                         if (i + 1 < count) scores(e + 2, tile + 1);
-                        wait_for(&col.p_full, tile, &col.dead);
                         const int slot = (e + 1) % S::kSlots;
                         wait_for(&col.full[slot], (e + 1) / S::kSlots, &col.dead);
+                        wait_for(&col.p_full[tile % S::kWeightTiles], tile / S::kWeightTiles, &col.dead);
                         tmem_after_sync();
-                        const uint64_t op = advance(v_op, slot * S::kSlot);
+                        const uint32_t op = v_lo + slot * (S::kSlot / 16), from = p_lo + tile % S::kWeightTiles * (S::kPs / 16);
+                        const uint32_t more = i > 0;
 #pragma unroll
                         for (int m = 0; m < S::kBlocks; ++m)
 #pragma unroll
                             for (int s = 0; s < kTile / 16; ++s)
-                                mma_f16(tmem + 2 * NT + m * S::kWeights, advance(op, m * 2 * (kTile * 128) + s * 2048),
-                                        advance(p_op, s * 16 * S::kRow), kValues, i > 0 || s > 0);
+                                mma_f16(tmem + 2 * NT + m * S::kWeights, op + m * 2 * (kTile * 8) + s * 128, v_hi, from + s * S::kRow, p_hi,
+                                        kValues, s > 0 ? 1u : more);
                         mma_commit(&col.empty[slot]);
-                        mma_commit(&col.pv_done);
+                        mma_commit(&col.pv_done[tile & 1]);
                     }
                     ++segment;
                     w.step(a);
@@ -446,10 +451,9 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                                 uint4 x = make_uint4(0u, 0u, 0u, 0u);
                                 if (row < rows) x = *reinterpret_cast<const uint4*>(from + i * kRows * a.pitch);
                                 uint8_t* line = to + row * 128;
-                                *reinterpret_cast<uint4*>(line + ((piece ^ (row & 7)) << 4)) =
-                                    make_uint4(two_codes(x.x & 0xFFFFu), two_codes(x.x >> 16), two_codes(x.y & 0xFFFFu), two_codes(x.y >> 16));
-                                *reinterpret_cast<uint4*>(line + (((piece + 1) ^ (row & 7)) << 4)) =
-                                    make_uint4(two_codes(x.z & 0xFFFFu), two_codes(x.z >> 16), two_codes(x.w & 0xFFFFu), two_codes(x.w >> 16));
+                                const uint2 h0 = four_codes(x.x), h1 = four_codes(x.y), h2 = four_codes(x.z), h3 = four_codes(x.w);
+                                *reinterpret_cast<uint4*>(line + ((piece ^ (row & 7)) << 4)) = make_uint4(h0.x, h0.y, h1.x, h1.y);
+                                *reinterpret_cast<uint4*>(line + (((piece + 1) ^ (row & 7)) << 4)) = make_uint4(h2.x, h2.y, h3.x, h3.y);
                             }
                         }
                         fence_smem_async();
@@ -467,8 +471,9 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
         const int grp = warp >> 2, quad = warp & 3, j = quad * 32 + lane, c0 = grp * C, tid = threadIdx.x;
         const uint32_t my_s = tmem + (static_cast<uint32_t>(quad * 32) << 16) + c0, my_o = my_s + 2 * NT;
         constexpr float kLift = E4M3 ? 7.f : 0.f;       // f16 weights up to 2^15 instead of 2^8: fewer of them vanish
-        constexpr float kRoomUp = 8.f + kLift;
+        constexpr float kRoomUp = E4M3 ? 8.f + kLift : 64.f;
         int tile_no = 0;
+        auto values_done = [&](int k) { wait_for(&col.pv_done[k & 1], k >> 1, &col.dead); };   // the second product of tile k
         while (w.next(a, &st)) {
             const int kv = w.unit / a.row_tiles, r0 = (w.unit - kv * a.row_tiles) * NT;
             const int32_t* table = c.pages + w.b * c.pages_stride;
@@ -480,7 +485,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 col.o_at[tid] = row ? w.b * a.o_seq + i * a.o_tok + h * a.o_head : -1;
                 col.limit[tid] = row && i < w.tokens ? w.first + i : -1;
                 col.neg_m[tid] = 0.f;
-                col.seen[tid] = 0;
+                col.seen[tid] = !(row && i < w.tokens);        // rows that take no part need no maximum
             }
             if (tid == 0) col.amax = 0;
             bar_sync(4, kSoftmaxThreads);
@@ -576,6 +581,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
             const int seen_by_all = w.first + r0 / a.group;    // the unit's first row sees positions up to here
             for (int tile = w.t0; tile < w.t1; ++tile, ++tile_no) {
                 const uint32_t s_at = my_s + (tile_no & 1) * NT;
+                uint8_t* const p_now = p_smem + tile_no % S::kWeightTiles * S::kPs;
                 const int pos = tile * kTile + j;
                 const bool masked = tile * kTile + kTile - 1 > seen_by_all;
                 float x[CH];
@@ -600,7 +606,24 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 const int page_after = look(tile + 2);
                 wait_for(&col.s_full[tile_no & 1], tile_no >> 1, &col.dead);
                 tmem_after_sync();
-                bool up = !settled;
+                bool up = E4M3 && !settled;
+                if (!E4M3 && !settled) {
+                    // the first key's scores do for a maximum: its own weight is then 1 (2^kLift)
+#pragma unroll
+                    for (int ch = 0; ch < NCH; ++ch) {
+                        load(ch);
+                        if (j == 0)
+#pragma unroll
+                            for (int i = 0; i < CH; ++i) {
+                                const int n = c0 + ch * CH + i;
+                                if (!col.seen[n] && x[i] > -INFINITY && x[i] < INFINITY) col.neg_m[n] = kLift - x[i], col.seen[n] = 1;
+                            }
+                        __syncwarp();
+                    }
+                    bar_sync(2 + grp, 128);
+                    settled = !bar_any(2 + grp, 128, (tid & 127) < C && !col.seen[c0 + (tid & 127)]);
+                    up = !settled;
+                }
 #pragma unroll
                 for (int ch = 0; ch < NCH; ++ch) {
                     load(ch);
@@ -645,7 +668,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
 #pragma unroll
                     for (int i = 0; i < C; ++i) l[i] *= col.factor[c0 + i];
                     if (tile > w.t0) {
-                        wait_for(&col.pv_done, tile_no - 1, &col.dead);
+                        values_done(tile_no - 1);
                         tmem_after_sync();
 #pragma unroll
                         for (int m = 0; m < S::kCols / NT - 2; ++m)             // blocks and parts
@@ -661,7 +684,8 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                     }
                     if (NCH == 1) load(0);
                 }
-                if (tile_no > 0) wait_for(&col.pv_done, tile_no - 1, &col.dead);   // the last tile's weights have been read
+                // the weights that were in their place have been read
+                if (tile_no >= S::kWeightTiles) values_done(tile_no - S::kWeightTiles);
 #pragma unroll
                 for (int ch = 0; ch < NCH; ++ch) {
                     if (NCH > 1) load(ch);
@@ -679,7 +703,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                         constexpr int kMask = S::kRow / 16 - 1;
                         const int line = j * S::kRow + in_row;
                         // the swizzle: 16-byte pieces, by the address's bits from 128 bytes up
-                        uint8_t* to = p_smem + panel * (kTile * S::kRow) + (line ^ (((line >> 7) & kMask) << 4));
+                        uint8_t* to = p_now + panel * (kTile * S::kRow) + (line ^ (((line >> 7) & kMask) << 4));
                         if constexpr (E4M3) {
                             *reinterpret_cast<uint4*>(to) = make_uint4(pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7]));
                         } else {
@@ -708,7 +732,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 }
                 fence_smem_async();
                 tmem_before_sync();
-                mbar_arrive(&col.p_full);
+                mbar_arrive(&col.p_full[tile_no % S::kWeightTiles]);
                 take(page_next);
                 page_next = page_after;
             }
@@ -727,10 +751,11 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                     col.inverse[n] = s == 0.f || col.limit[n] < 0 ? 0.f : 1.f / s;      // 0: an empty row
                 }
             }
-            wait_for(&col.pv_done, tile_no - 1, &col.dead);
+            values_done(tile_no - 1);
             tmem_after_sync();
             bar_sync(4, kSoftmaxThreads);
             const bool whole = w.t0 == 0 && w.t1 == w.T;
+            const int rows = min(NT, a.n * a.group - r0);           // columns that are rows of the output
             const long long unit_at = w.at - w.t0;
             // which of this CTA's two places in the workspace: the unit began in another's part, or in this one's
             constexpr int kPart = NT * (DP + 2);
@@ -761,27 +786,32 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
 #pragma unroll
                         for (int i = 0; i < CH; ++i) o[i] += low[i];
                     }
-                    if (d < D) {
+                    if (d >= D) {
+                    } else if (whole) {
 #pragma unroll
                         for (int i = 0; i < CH; ++i) {
                             const int n = c0 + ch * CH + i;
-                            if (col.o_at[n] < 0) continue;
-                            if (whole) {
-                                const float by = col.inverse[n];
-                                a.out[col.o_at[n] + d] = __float2bfloat16(by == 0.f ? 0.f : o[i] * by);
-                            } else {
-                                part[n * DP + d] = o[i];
-                            }
+                            const float by = col.inverse[n];
+                            if (n < rows) a.out[col.o_at[n] + d] = __float2bfloat16(by == 0.f ? 0.f : o[i] * by);
                         }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < CH; ++i)
+                            if (c0 + ch * CH + i < rows) part[(c0 + ch * CH + i) * DP + d] = o[i];
                     }
+                    __syncwarp();
                 }
             }
             if (!whole) {
                 // the last of the unit's CTAs joins the parts
-                const long long total = col.total, end = unit_at + w.T - 1;
-                const int ctas = col.ctas;
-                const int c_first = static_cast<int>(((unit_at + 1) * ctas - 1) / total);
-                const int c_last = static_cast<int>(((end + 1) * ctas - 1) / total);
+                const long long each = col.each, extra = col.extra;
+                auto owner = [&](long long at) {                         // the CTA whose part holds a tile
+                    const long long edge = (each + 1) * extra;
+                    const long long x = at < edge ? at : at - edge, y = at < edge ? each + 1 : each;
+                    const long long q = (x | y) >> 32 ? x / y : static_cast<uint32_t>(x) / static_cast<uint32_t>(y);
+                    return static_cast<int>(at < edge ? q : extra + q);
+                };
+                const int c_first = owner(unit_at), c_last = owner(unit_at + w.T - 1);
                 __threadfence();
                 bar_sync(4, kSoftmaxThreads);
                 if (tid == 0) {
@@ -794,57 +824,54 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 bar_sync(4, kSoftmaxThreads);
                 if (col.last) {
                     __threadfence();
-                    // two rows a warp at once, some parts of each in flight; a lane holds V elements side by side
-                    constexpr int kWarps = kSoftmaxThreads / 32, V = DP / 32, F = V == 2 ? 8 : V == 4 ? 4 : 2;
+                    // the parts' factors 2^(m - M) / sum first, in the weights' place (64 parts a turn at most), then
+                    // sums over the parts, V elements of a row a thread
+                    constexpr int V = 4, kRowItems = DP / V, kFactors = 64;
+                    static_assert(kFactors * NT * 4 <= S::kPs * S::kWeightTiles, "factors");
+                    float* factors = reinterpret_cast<float*>(p_smem);               // [part][row]
                     const int parts = c_last - c_first + 1;
                     auto place = [&](int k) { return a.parts + static_cast<int64_t>(2 * (c_first + k) + (k == 0 ? 1 : 0)) * kPart; };
-                    for (int n0 = warp; n0 < NT; n0 += 2 * kWarps) {
-                        float M[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f}, o[2][V] = {};
-                        for (int k = lane; k < parts; k += 32)
-#pragma unroll
-                            for (int r = 0; r < 2; ++r)
-                                if (n0 + r * kWarps < NT) M[r] = fmaxf(M[r], __ldcg(place(k) + NT * DP + n0 + r * kWarps));
-#pragma unroll
-                        for (int r = 0; r < 2; ++r) M[r] = warp_max(M[r]);
-                        for (int k0 = 0; k0 < parts; k0 += F) {
-                            float x[2][F][V], m[2][F], l[2][F];
-#pragma unroll
-                            for (int q = 0; q < F; ++q)
-#pragma unroll
-                                for (int r = 0; r < 2; ++r) {
-                                    const int n = n0 + r * kWarps;
-                                    m[r][q] = -INFINITY;
-                                    if (k0 + q < parts && n < NT && col.o_at[n] >= 0) {
-                                        const float* from = place(k0 + q);
-                                        m[r][q] = __ldcg(from + NT * DP + n);
-                                        l[r][q] = __ldcg(from + NT * DP + NT + n);
-                                        load_floats(from + n * DP + lane * V, x[r][q]);
-                                    }
+                    float M = -INFINITY, sum = 0.f;
+                    if (tid < rows) {
+#pragma unroll 4
+                        for (int k = 0; k < parts; ++k) M = fmaxf(M, __ldcg(place(k) + NT * DP + tid));
+                        if (M > -INFINITY && col.limit[tid] >= 0)
+#pragma unroll 4
+                            for (int k = 0; k < parts; ++k)
+                                sum = fmaf(ex2(__ldcg(place(k) + NT * DP + tid) - M), __ldcg(place(k) + NT * DP + NT + tid), sum);
+                        if (a.lse) a.lse[lse_at(tid)] = sum == 0.f ? -INFINITY : (log2f(sum) + M) * 0.69314718055994531f;
+                    }
+                    const float inverse = sum == 0.f ? 0.f : 1.f / sum;
+                    for (int k0 = 0; k0 < parts; k0 += kFactors) {
+                        const int k1 = min(parts, k0 + kFactors);
+                        if (tid < rows)
+#pragma unroll 4
+                            for (int k = k0; k < k1; ++k)
+                                factors[(k - k0) * NT + tid] = inverse == 0.f ? 0.f : ex2(__ldcg(place(k) + NT * DP + tid) - M) * inverse;
+                        bar_sync(4, kSoftmaxThreads);
+                        for (int item = tid; item < rows * kRowItems; item += kSoftmaxThreads) {
+                            const int n = item / kRowItems, d = item % kRowItems * V;
+                            if (d >= D) continue;
+                            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+                            const float* sums = place(0) + n * DP + d;               // the first round's sums stay in its place
+                            if (k0 > 0) o = __ldcg(reinterpret_cast<const float4*>(sums));
+#pragma unroll 4
+                            for (int k = k0; k < k1; ++k) {
+                                const float by = factors[(k - k0) * NT + n];
+                                const float4 x = __ldcg(reinterpret_cast<const float4*>(place(k) + n * DP + d));
+                                if (by != 0.f) {
+                                    o.x = fmaf(by, x.x, o.x);
+                                    o.y = fmaf(by, x.y, o.y);
+                                    o.z = fmaf(by, x.z, o.z);
+                                    o.w = fmaf(by, x.w, o.w);
                                 }
-#pragma unroll
-                            for (int q = 0; q < F; ++q)
-#pragma unroll
-                                for (int r = 0; r < 2; ++r)
-                                    if (m[r][q] > -INFINITY) {
-                                        const float by = ex2(m[r][q] - M[r]);
-                                        sum[r] = fmaf(by, l[r][q], sum[r]);
-#pragma unroll
-                                        for (int p = 0; p < V; ++p) o[r][p] = fmaf(by, x[r][q][p], o[r][p]);
-                                    }
+                            }
+                            if (k1 < parts)
+                                __stcg(reinterpret_cast<float4*>(const_cast<float*>(sums)), o);
+                            else
+                                *reinterpret_cast<uint2*>(a.out + col.o_at[n] + d) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
                         }
-#pragma unroll
-                        for (int r = 0; r < 2; ++r) {
-                            const int n = n0 + r * kWarps;
-                            if (n >= NT || col.o_at[n] < 0) continue;
-                            const bool none = sum[r] == 0.f || col.limit[n] < 0;
-                            const float by = none ? 0.f : 1.f / sum[r];
-                            if (lane * V < D)
-#pragma unroll
-                                for (int p = 0; p < V; p += 2)
-                                    *reinterpret_cast<uint32_t*>(a.out + col.o_at[n] + lane * V + p) =
-                                        none ? 0u : pack_bf16(o[r][p] * by, o[r][p + 1] * by);
-                            if (lane == 0 && a.lse) a.lse[lse_at(n)] = none ? -INFINITY : (log2f(sum[r]) + M[r]) * 0.69314718055994531f;
-                        }
+                        bar_sync(4, kSoftmaxThreads);
                     }
                 }
             }

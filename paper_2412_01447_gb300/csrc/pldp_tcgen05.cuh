@@ -19,8 +19,6 @@ __device__ __forceinline__ uint64_t smem_operand(uint32_t addr, uint32_t lead, u
     return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | static_cast<uint64_t>((lead >> 4) & 0x3FFFu) << 16 |
            static_cast<uint64_t>((stride >> 4) & 0x3FFFu) << 32 | uint64_t(1) << 46 | mode << 61;
 }
-__device__ __forceinline__ uint64_t advance(uint64_t operand, uint32_t bytes) { return operand + (bytes >> 4); }
-
 // The instruction: M x N, 16 deep, both operands bf16 (or f16), fp32 accumulators; `a_rows`
 // (`b_rows`) where M (N) runs along the operand's rows instead of the contraction.
 __host__ __device__ constexpr uint32_t mma_form(int M, int N, bool bf16, bool a_rows, bool b_rows) {
@@ -28,12 +26,16 @@ __host__ __device__ constexpr uint32_t mma_form(int M, int N, bool bf16, bool a_
            static_cast<uint32_t>(N >> 3) << 17 | static_cast<uint32_t>(M >> 4) << 24;
 }
 
-__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t form, bool accumulate) {
+// Operands by the two words of their descriptors: an address moves the low one only.
+__device__ __forceinline__ void mma_f16(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t form,
+                                        uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d), "l"(a), "l"(b), "r"(form), "r"(static_cast<uint32_t>(accumulate))
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+        "mov.b64 a, {%1, %2};\n\t"
+        "mov.b64 b, {%3, %4};\n\t"
+        "setp.ne.u32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n\t}"
+        ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(form), "r"(accumulate)
         : "memory");
 }
 // Arrives on `bar` when this thread's matrix instructions so far are done.
