@@ -71,8 +71,8 @@ constexpr int kMaxShared = 232448;        // bytes a CTA, static and dynamic
 
 template <int NT, int DP, bool E4M3>
 struct Shape {
-    // warps: 8 softmax, (e4m3: 4 that convert,) one of matrix instructions, one of copies, idle ones
-    static constexpr int kMmaWarp = E4M3 ? 12 : 8, kCopyWarp = kMmaWarp + 1;
+    // warps: 8 softmax, (e4m3: 4 that convert,) one of matrix instructions, two of copies, one that looks up keys
+    static constexpr int kMmaWarp = E4M3 ? 12 : 8, kCopyWarp = kMmaWarp + 1, kKeyWarp = kMmaWarp + 3;
     static constexpr int kThreads = (E4M3 ? 16 : 12) * 32;
     static constexpr int kPanels = DP / 64;                    // of 64 elements (128 bytes) each
     static constexpr int kSlot = kPanels * kTile * 128;        // one tile of keys or values
@@ -84,9 +84,11 @@ struct Shape {
     static constexpr int kPs = kP * (E4M3 ? 1 : 2);            // with the low parts
     static constexpr int kWeightTiles = NT <= 64 && DP <= 128 ? 2 : 1;     // tiles of weights held
     static constexpr int kRest = kQ + kPs * kWeightTiles;
-    static constexpr int kColumns = NT >= 96 ? 8192 : 4608;    // static: Columns
+    static constexpr int kColumns = NT * 56 + 2688 + (E4M3 ? 4096 : 0);    // static: Columns
     static constexpr int kRoom = kMaxShared - 1024 - kColumns - kRest;
-    static constexpr int kSlots = E4M3 ? (DP == 256 ? 2 : 3) : (kRoom / kSlot < 8 ? kRoom / kSlot : 8);
+    // e4m3: what three stages leave
+    static constexpr int kMost = E4M3 ? (kRoom - 3 * kStage) / kSlot : kRoom / kSlot;
+    static constexpr int kSlots = kMost > (E4M3 ? 6 : 8) ? (E4M3 ? 6 : 8) : kMost < 2 ? 2 : kMost;
     static constexpr int kStages = E4M3 ? ((kRoom - kSlots * kSlot) / kStage < 7 ? (kRoom - kSlots * kSlot) / kStage : 7) : 0;
     static constexpr int kBlocks = DP == 256 ? 2 : 1;          // of 128 rows of O^T
     static constexpr int kCols = 2 * NT + kBlocks * kWeights;
@@ -99,14 +101,16 @@ struct Shape {
 };
 
 // What a column (query row) and the CTA's roles share.
-template <int NT>
+template <int NT, bool E4M3>
 struct Columns {
     int64_t q_at[NT], o_at[NT];     // element offsets, -1: no such row
     float neg_m[NT], factor[NT], sum[NT], inverse[NT];
     float part[4][NT];
+    // of the keys of four tiles: log2 of the values' scale (-inf: no key); e4m3: the keys' scale, the values' inverted
+    float key_log[4][kTile], key_scale[E4M3 ? 4 : 1][E4M3 ? kTile : 1], key_inverse[E4M3 ? 4 : 1][E4M3 ? kTile : 1];
     int limit[NT];                  // last position that the row sees
     int seen[NT];                   // whether m has been set
-    uint64_t full[8], empty[8], stage_full[8], stage_empty[8], s_full[2], p_full[2], pv_done[2], q_full;
+    uint64_t full[8], empty[8], stage_full[8], stage_empty[8], s_full[2], p_full[2], pv_done[2], q_full, key_empty[4];
     uint32_t tmem, amax;
     int dead, last;
     int b, unit, tile;              // where this CTA's part of the list starts
@@ -115,11 +119,14 @@ struct Columns {
     long long warp_sum[16];
 };
 
-// Waits, with a limit; after one has run out no wait of this CTA blocks any more, and its results
+// Waits, with a limit; after one has run out no wait of this CTA blocks for long any more, and its results
 // are marked as none.
 __device__ __forceinline__ void wait_for(uint64_t* bar, uint32_t parity, int* dead) {
-    if (*static_cast<volatile int*>(dead)) return;
-    if (!mbar_wait(bar, parity & 1u, kMbarPolls)) *static_cast<volatile int*>(dead) = 1;
+    for (uint32_t i = 0; i < kMbarPolls / 16; ++i) {
+        if (mbar_wait(bar, parity & 1u, 16)) return;
+        if (*static_cast<volatile int*>(dead)) return;
+    }
+    *static_cast<volatile int*>(dead) = 1;
 }
 
 // The CTA's part of the list, unit by unit.
@@ -221,9 +228,9 @@ __global__ void __launch_bounds__(Shape<NT, DP, E4M3>::kThreads, 1)
 attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
     using S = Shape<NT, DP, E4M3>;
     constexpr int kThreads = S::kThreads;
-    static_assert(sizeof(Columns<NT>) <= S::kColumns, "shared memory");
+    static_assert(sizeof(Columns<NT, E4M3>) <= S::kColumns, "shared memory");
     extern __shared__ uint8_t raw[];
-    __shared__ __align__(16) Columns<NT> col;
+    __shared__ __align__(16) Columns<NT, E4M3> col;
     uint8_t* ring = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
     uint8_t* const q_smem = ring + S::kSlots * S::kSlot;
     uint8_t* const p_smem = q_smem + S::kQ;                     // (high part, and behind it the low part)
@@ -235,18 +242,21 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
     if (warp == S::kMmaWarp) tmem_alloc(&col.tmem, S::kTmem);
     if (threadIdx.x == 0) {
         for (int i = 0; i < 8; ++i) {
-            mbar_init(&col.full[i], E4M3 ? kConvertThreads : 1);
+            mbar_init(&col.full[i], E4M3 ? kConvertThreads / 32 : 1);
             mbar_init(&col.empty[i], 1);
             mbar_init(&col.stage_full[i], 1);
-            mbar_init(&col.stage_empty[i], kConvertThreads);
+            mbar_init(&col.stage_empty[i], kConvertThreads / 32);
         }
         mbar_init(&col.s_full[0], 1);
         mbar_init(&col.s_full[1], 1);
-        mbar_init(&col.p_full[0], kSoftmaxThreads);
-        mbar_init(&col.p_full[1], kSoftmaxThreads);
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(&col.key_empty[i], kSoftmaxThreads / 32);
+        }
+        mbar_init(&col.p_full[0], kSoftmaxThreads / 32);
+        mbar_init(&col.p_full[1], kSoftmaxThreads / 32);
         mbar_init(&col.pv_done[0], 1);
         mbar_init(&col.pv_done[1], 1);
-        mbar_init(&col.q_full, kSoftmaxThreads);
+        mbar_init(&col.q_full, kSoftmaxThreads / 32);
         fence_mbar_init();
         col.dead = 0;
     }
@@ -373,6 +383,66 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 w.step(a);
             }
             // the last copies have arrived before this CTA ends: every slot is waited for by its reader
+        } else if (warp == S::kKeyWarp) {
+            // ---- the keys of each tile, four a lane: whether there is one, and e4m3's scales ----
+            int tile_no = 0;
+            while (w.next(a, &st)) {
+                const int kv = w.unit / a.row_tiles;
+                const int32_t* table = c.pages + w.b * c.pages_stride;
+                int page[4];
+                [[maybe_unused]] float ks[4], vs[4];
+                auto look = [&](int tile, int (&to)[4]) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int pos = tile * kTile + lane + 32 * i;
+                        to[i] = tile < w.t1 && pos < w.keys ? load_now(table + page_of(pos, c.div_mul, c.div_shift)) : -1;
+                    }
+                };
+                auto fetch = [&](int tile, const int (&from)[4], float (&k)[4], float (&v)[4]) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int pos = tile * kTile + lane + 32 * i;
+                        k[i] = v[i] = 1.f;
+                        if (static_cast<unsigned>(from[i]) < static_cast<unsigned>(c.n_pages)) {
+                            const int slot = pos - static_cast<int>(page_of(pos, c.div_mul, c.div_shift)) * c.page_size;
+                            const int64_t at = static_cast<int64_t>(from[i]) * (c.heads * c.page_size) + (kv * c.page_size + slot);
+                            k[i] = load_now(c.k_scale + at);
+                            v[i] = load_now(c.v_scale + at);
+                        }
+                    }
+                };
+                // pages are looked up two tiles ahead, scales loaded one ahead
+                look(w.t0, page);
+                if constexpr (E4M3) fetch(w.t0, page, ks, vs);
+                int page_next[4];
+                look(w.t0 + 1, page_next);
+                for (int tile = w.t0; tile < w.t1; ++tile, ++tile_no) {
+                    int page_after[4];
+                    [[maybe_unused]] float ks_next[4], vs_next[4];
+                    if constexpr (E4M3) fetch(tile + 1, page_next, ks_next, vs_next);
+                    look(tile + 2, page_after);
+                    const int at = tile_no & 3;
+                    if (tile_no >= 4) wait_for(&col.key_empty[at], (tile_no >> 2) - 1, &col.dead);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = lane + 32 * i;
+                        const bool there = static_cast<unsigned>(page[i]) < static_cast<unsigned>(c.n_pages);
+                        if constexpr (E4M3) {
+                            const float v = fmaxf(vs[i], 1e-37f);
+                            col.key_log[at][key] = there ? log2f(v) : -INFINITY;
+                            col.key_scale[at][key] = there ? ks[i] * a.scale2 : 0.f;
+                            col.key_inverse[at][key] = 1.f / v;
+                            ks[i] = ks_next[i], vs[i] = vs_next[i];
+                        } else {
+                            col.key_log[at][key] = there ? 0.f : -INFINITY;
+                        }
+                        page[i] = page_next[i], page_next[i] = page_after[i];
+                    }
+                    bar_arrive(5 + at, 160);             // for the one half of the columns, and for the other
+                    bar_arrive(9 + at, 160);
+                }
+                w.step(a);
+            }
         } else if (warp == S::kMmaWarp) {
             // ---- matrix instructions ----
             if (lane == 0) {
@@ -457,8 +527,9 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                             }
                         }
                         fence_smem_async();
-                        mbar_arrive(&col.full[slot]);
-                        mbar_arrive(&col.stage_empty[stage]);
+                        __syncwarp();
+                        mbar_arrive_if(&col.full[slot], lane == 0);
+                        mbar_arrive_if(&col.stage_empty[stage], lane == 0);
                     }
                 }
                 w.step(a);
@@ -476,7 +547,6 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
         auto values_done = [&](int k) { wait_for(&col.pv_done[k & 1], k >> 1, &col.dead); };   // the second product of tile k
         while (w.next(a, &st)) {
             const int kv = w.unit / a.row_tiles, r0 = (w.unit - kv * a.row_tiles) * NT;
-            const int32_t* table = c.pages + w.b * c.pages_stride;
             // the columns of this unit
             if (tid < NT) {
                 const int r = r0 + tid, i = r / a.group, h = kv * a.group + (r - i * a.group);
@@ -535,55 +605,34 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
             }
             fence_smem_async();
             tmem_before_sync();
-            mbar_arrive(&col.q_full);
+            __syncwarp();
+            mbar_arrive_if(&col.q_full, lane == 0);
 
             float l[C];
 #pragma unroll
             for (int i = 0; i < C; ++i) l[i] = 0.f;
             bool settled = false;
-            const float f0 = a.scale2 * back;
-            // this thread's key of a tile: factor of its scores, log2 of its values' scale (-inf: no key), its
-            // inverse.  The page is looked up two tiles ahead and the scales loaded one ahead.
-            float f, g, inv, ks_next = 1.f, vs_next = 1.f;
-            auto look = [&](int tile) {
-                const int pos = tile * kTile + j;
-                int page = -1;
-                if (tile < w.t1 && pos < w.keys) page = load_now(table + page_of(pos, c.div_mul, c.div_shift));
-                return static_cast<unsigned>(page) < static_cast<unsigned>(c.n_pages) ? page : -1;
-            };
-            auto fetch = [&](int tile, int page) {
-                if constexpr (E4M3) {
-                    const int pos = tile * kTile + j;
-                    if (page >= 0) {
-                        const int64_t at = (static_cast<int64_t>(page) * c.heads + kv) * c.page_size +
-                                           (pos - static_cast<int>(page_of(pos, c.div_mul, c.div_shift)) * c.page_size);
-                        ks_next = load_now(c.k_scale + at);
-                        vs_next = load_now(c.v_scale + at);
-                    }
-                }
-            };
-            auto take = [&](int page) {
-                f = 0.f, g = -INFINITY, inv = 1.f;
-                if (page >= 0) {
-                    f = f0, g = 0.f;
-                    if constexpr (E4M3) {
-                        const float vs = fmaxf(vs_next, 1e-37f);
-                        f *= ks_next;
-                        g = log2f(vs);
-                        inv = 1.f / vs;
-                    }
-                }
-            };
-            int page_next = look(w.t0);
-            fetch(w.t0, page_next);
-            take(page_next);
-            page_next = look(w.t0 + 1);
+            [[maybe_unused]] const float f0 = a.scale2;
             const int seen_by_all = w.first + r0 / a.group;    // the unit's first row sees positions up to here
             for (int tile = w.t0; tile < w.t1; ++tile, ++tile_no) {
                 const uint32_t s_at = my_s + (tile_no & 1) * NT;
                 uint8_t* const p_now = p_smem + tile_no % S::kWeightTiles * S::kPs;
                 const int pos = tile * kTile + j;
                 const bool masked = tile * kTile + kTile - 1 > seen_by_all;
+                // this thread's key: the factor of its scores, log2 of its values' scale (-inf: no key) and its inverse
+                const int at = tile_no & 3;
+                bar_sync(5 + 4 * grp + at, 160);
+                const float g = col.key_log[at][j];
+                float f = f0;
+                [[maybe_unused]] float inv = 1.f;
+                if constexpr (E4M3) {
+                    f = col.key_scale[at][j] * back;
+                    inv = col.key_inverse[at][j];
+                } else if (g != 0.f) {
+                    f = 0.f;
+                }
+                __syncwarp();
+                mbar_arrive_if(&col.key_empty[at], lane == 0);
                 float x[CH];
                 // exponents of the weights of chunk ch against the present m
                 auto load = [&](int ch) {
@@ -602,8 +651,6 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                             if (pos > col.limit[c0 + ch * CH + i]) x[i] = -INFINITY;
                     }
                 };
-                fetch(tile + 1, page_next);
-                const int page_after = look(tile + 2);
                 wait_for(&col.s_full[tile_no & 1], tile_no >> 1, &col.dead);
                 tmem_after_sync();
                 bool up = E4M3 && !settled;
@@ -632,11 +679,50 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                     for (int i = 1; i < CH; ++i) most = fmaxf(most, x[i]);
                     up = up || most > kRoomUp;
                 }
+                auto sum = [&](int ch) {
+#pragma unroll
+                    for (int i = 0; i < CH; ++i) {
+                        if constexpr (E4M3) l[ch * CH + i] = fmaf(x[i], inv, l[ch * CH + i]);
+                        else l[ch * CH + i] += x[i];
+                    }
+                };
+                auto weights = [&] {
+#pragma unroll
+                    for (int ch = 0; ch < NCH; ++ch) {
+                        if (NCH > 1) load(ch);
+#pragma unroll
+                        for (int i = 0; i < CH; i += 8) {
+                            float* v = x + i;
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) v[k] = ex2(v[k]);
+                            const int byte = (c0 + ch * CH + i) * 2;                      // within the key's weights
+                            const int panel = byte / S::kRow, in_row = byte % S::kRow;
+                            constexpr int kMask = S::kRow / 16 - 1;
+                            const int line = j * S::kRow + in_row;
+                            // the swizzle: 16-byte pieces, by the address's bits from 128 bytes up
+                            uint8_t* to = p_now + panel * (kTile * S::kRow) + (line ^ (((line >> 7) & kMask) << 4));
+                            if constexpr (E4M3) {
+                                *reinterpret_cast<uint4*>(to) = make_uint4(pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7]));
+                            } else {
+                                uint32_t hi[4], lo[4];
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) {
+                                    hi[k] = pack_bf16(v[2 * k], v[2 * k + 1]);
+                                    lo[k] = pack_bf16(v[2 * k] - __uint_as_float(hi[k] << 16),
+                                                      v[2 * k + 1] - __uint_as_float(hi[k] & 0xFFFF0000u));
+                                }
+                                *reinterpret_cast<uint4*>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                                *reinterpret_cast<uint4*>(to + S::kP) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                            }
+                        }
+                        if (NCH > 1) sum(ch);
+                    }
+                };
                 if (bar_any(2 + grp, 128, up)) {
                     // some column's maximum moves
 #pragma unroll
                     for (int ch = 0; ch < NCH; ++ch) {
-                        if (NCH > 1) load(ch);
+                        load(ch);
                         float mine = -INFINITY;
 #pragma unroll
                         for (int i = 0; i < CH; ++i) {
@@ -684,41 +770,11 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                     }
                     if (NCH == 1) load(0);
                 }
-                // the weights that were in their place have been read
-                if (tile_no >= S::kWeightTiles) values_done(tile_no - S::kWeightTiles);
-#pragma unroll
-                for (int ch = 0; ch < NCH; ++ch) {
-                    if (NCH > 1) load(ch);
-#pragma unroll
-                    for (int i = 0; i < CH; i += 8) {
-                        float v[8];
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            v[k] = ex2(x[i + k]);
-                            if constexpr (E4M3) l[ch * CH + i + k] = fmaf(v[k], inv, l[ch * CH + i + k]);
-                            else l[ch * CH + i + k] += v[k];
-                        }
-                        const int byte = (c0 + ch * CH + i) * 2;                      // within the key's weights
-                        const int panel = byte / S::kRow, in_row = byte % S::kRow;
-                        constexpr int kMask = S::kRow / 16 - 1;
-                        const int line = j * S::kRow + in_row;
-                        // the swizzle: 16-byte pieces, by the address's bits from 128 bytes up
-                        uint8_t* to = p_now + panel * (kTile * S::kRow) + (line ^ (((line >> 7) & kMask) << 4));
-                        if constexpr (E4M3) {
-                            *reinterpret_cast<uint4*>(to) = make_uint4(pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7]));
-                        } else {
-                            uint32_t hi[4], lo[4];
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                hi[k] = pack_bf16(v[2 * k], v[2 * k + 1]);
-                                lo[k] = pack_bf16(v[2 * k] - __uint_as_float(hi[k] << 16),
-                                                  v[2 * k + 1] - __uint_as_float(hi[k] & 0xFFFF0000u));
-                            }
-                            *reinterpret_cast<uint4*>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                            *reinterpret_cast<uint4*>(to + S::kP) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-                        }
-                    }
-                }
+                // The weights that were in their place have been read: of two tiles' places, by the second product of
+                // tile_no - 2, which was issued before the first one of tile_no.
+                if (S::kWeightTiles == 1 && tile_no > 0) values_done(tile_no - 1);
+                weights();
+                if (NCH == 1) sum(0);
                 if constexpr (!E4M3) {
                     // what the pages hold past the end is not used: zeros, in the values' tile
                     if (tile * kTile + kTile > w.keys) {
@@ -732,9 +788,8 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 }
                 fence_smem_async();
                 tmem_before_sync();
-                mbar_arrive(&col.p_full[tile_no % S::kWeightTiles]);
-                take(page_next);
-                page_next = page_after;
+                __syncwarp();
+                mbar_arrive_if(&col.p_full[tile_no % S::kWeightTiles], lane == 0);
             }
             // the sums over the keys
             {

@@ -120,6 +120,15 @@ __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
+// The same for the threads that say so, without a branch.
+__device__ __forceinline__ void mbar_arrive_if(uint64_t* bar, bool mine) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.u32 p, %1, 0;\n\t"
+        "@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}"
+        ::"r"(smem_u32(bar)), "r"(static_cast<uint32_t>(mine))
+        : "memory");
+}
 // Makes this thread's shared memory writes visible to the matrix instructions' reads.
 __device__ __forceinline__ void fence_smem_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -144,6 +153,9 @@ __device__ __forceinline__ void more_registers() {
 // Named barriers of a block: all of `threads`; the second form tells whether any of them says so.
 __device__ __forceinline__ void bar_sync(int id, int threads) {
     asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(int id, int threads) {     // without waiting for the others
+    asm volatile("barrier.cta.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 __device__ __forceinline__ bool bar_any(int id, int threads, bool mine) {
     uint32_t any;
