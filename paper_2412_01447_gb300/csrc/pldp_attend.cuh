@@ -428,10 +428,11 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                         const int key = lane + 32 * i;
                         const bool there = static_cast<unsigned>(page[i]) < static_cast<unsigned>(c.n_pages);
                         if constexpr (E4M3) {
+                            // (lg2.approx is 2^-22 off at most: as much as the weight's own exponential)
                             const float v = fmaxf(vs[i], 1e-37f);
-                            col.key_log[at][key] = there ? log2f(v) : -INFINITY;
+                            col.key_log[at][key] = there ? __log2f(v) : -INFINITY;
                             col.key_scale[at][key] = there ? ks[i] * a.scale2 : 0.f;
-                            col.key_inverse[at][key] = 1.f / v;
+                            col.key_inverse[at][key] = __frcp_rn(v);
                             ks[i] = ks_next[i], vs[i] = vs_next[i];
                         } else {
                             col.key_log[at][key] = there ? 0.f : -INFINITY;
@@ -867,9 +868,9 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                     return static_cast<int>(at < edge ? q : extra + q);
                 };
                 const int c_first = owner(unit_at), c_last = owner(unit_at + w.T - 1);
-                __threadfence();
                 bar_sync(4, kSoftmaxThreads);
                 if (tid == 0) {
+                    __threadfence();                                     // of all that the barrier has seen written
                     uint32_t* ticket = a.tickets + static_cast<int64_t>(w.b) * units + w.unit;
                     const bool is_last = atomicAdd(ticket, 1u) == static_cast<uint32_t>(c_last - c_first);
                     if (is_last) *ticket = 0u;
@@ -878,9 +879,8 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 }
                 bar_sync(4, kSoftmaxThreads);
                 if (col.last) {
-                    __threadfence();
-                    // the parts' factors 2^(m - M) / sum first, in the weights' place (64 parts a turn at most), then
-                    // sums over the parts, V elements of a row a thread
+                    // The parts' factors 2^(m - M) / sum first, in the weights' place (64 parts a turn at most), then
+                    // sums over the parts, V elements of a row a thread.
                     constexpr int V = 4, kRowItems = DP / V, kFactors = 64;
                     static_assert(kFactors * NT * 4 <= S::kPs * S::kWeightTiles, "factors");
                     float* factors = reinterpret_cast<float*>(p_smem);               // [part][row]
@@ -888,21 +888,39 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                     auto place = [&](int k) { return a.parts + static_cast<int64_t>(2 * (c_first + k) + (k == 0 ? 1 : 0)) * kPart; };
                     float M = -INFINITY, sum = 0.f;
                     if (tid < rows) {
-#pragma unroll 4
-                        for (int k = 0; k < parts; ++k) M = fmaxf(M, __ldcg(place(k) + NT * DP + tid));
-                        if (M > -INFINITY && col.limit[tid] >= 0)
-#pragma unroll 4
-                            for (int k = 0; k < parts; ++k)
-                                sum = fmaf(ex2(__ldcg(place(k) + NT * DP + tid) - M), __ldcg(place(k) + NT * DP + NT + tid), sum);
+                        const bool live = col.limit[tid] >= 0;
+                        for (int k0 = 0; k0 < parts; k0 += 8) {                      // eight parts' m and sum in flight
+                            float m[8], part_sum[8], top = M;
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) {
+                                m[q] = -INFINITY, part_sum[q] = 0.f;
+                                if (live && k0 + q < parts) {
+                                    m[q] = __ldcg(place(k0 + q) + NT * DP + tid);
+                                    part_sum[q] = __ldcg(place(k0 + q) + NT * DP + NT + tid);
+                                }
+                            }
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) {
+                                top = fmaxf(top, m[q]);
+                                if (k0 + q < min(parts, kFactors)) factors[(k0 + q) * NT + tid] = m[q];
+                            }
+                            if (!(top > -INFINITY)) continue;
+                            sum *= ex2(M - top);                                     // (2^-inf of the first)
+                            M = top;
+#pragma unroll
+                            for (int q = 0; q < 8; ++q)
+                                if (m[q] > -INFINITY) sum = fmaf(ex2(m[q] - M), part_sum[q], sum);
+                        }
                         if (a.lse) a.lse[lse_at(tid)] = sum == 0.f ? -INFINITY : (log2f(sum) + M) * 0.69314718055994531f;
                     }
                     const float inverse = sum == 0.f ? 0.f : 1.f / sum;
                     for (int k0 = 0; k0 < parts; k0 += kFactors) {
                         const int k1 = min(parts, k0 + kFactors);
                         if (tid < rows)
-#pragma unroll 4
-                            for (int k = k0; k < k1; ++k)
-                                factors[(k - k0) * NT + tid] = inverse == 0.f ? 0.f : ex2(__ldcg(place(k) + NT * DP + tid) - M) * inverse;
+                            for (int k = k0; k < k1; ++k) {
+                                const float m = k0 == 0 ? factors[k * NT + tid] : __ldcg(place(k) + NT * DP + tid);
+                                factors[(k - k0) * NT + tid] = inverse == 0.f ? 0.f : ex2(m - M) * inverse;
+                            }
                         bar_sync(4, kSoftmaxThreads);
                         for (int item = tid; item < rows * kRowItems; item += kSoftmaxThreads) {
                             const int n = item / kRowItems, d = item % kRowItems * V;
@@ -910,7 +928,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
                             const float* sums = place(0) + n * DP + d;               // the first round's sums stay in its place
                             if (k0 > 0) o = __ldcg(reinterpret_cast<const float4*>(sums));
-#pragma unroll 4
+#pragma unroll 8
                             for (int k = k0; k < k1; ++k) {
                                 const float by = factors[(k - k0) * NT + n];
                                 const float4 x = __ldcg(reinterpret_cast<const float4*>(place(k) + n * DP + d));
