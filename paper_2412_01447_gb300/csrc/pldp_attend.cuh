@@ -122,11 +122,13 @@ struct Columns {
 // Waits, with a limit; after one has run out no wait of this CTA blocks for long any more, and its results
 // are marked as none.
 __device__ __forceinline__ void wait_for(uint64_t* bar, uint32_t parity, int* dead) {
-    for (uint32_t i = 0; i < kMbarPolls / 16; ++i) {
-        if (mbar_wait(bar, parity & 1u, 16)) return;
-        if (*static_cast<volatile int*>(dead)) return;
+    uint32_t polls = 0;
+#pragma unroll 1
+    while (!mbar_wait(bar, parity & 1u, 1)) {
+        if (++polls < kMbarPolls && !*static_cast<volatile int*>(dead)) continue;
+        *static_cast<volatile int*>(dead) = 1;
+        break;
     }
-    *static_cast<volatile int*>(dead) = 1;
 }
 
 // The CTA's part of the list, unit by unit.
@@ -273,6 +275,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
             const int keys = tk.first + tk.count;
             return keys > 0 ? (keys + kTile - 1) / kTile : 1;
         };
+#pragma unroll 1
         for (int b = lo; b < hi; ++b) mine += tiles_of(b);
         long long upto = mine;
 #pragma unroll
@@ -283,6 +286,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
         if (lane == 31) col.warp_sum[warp] = upto;
         __syncthreads();
         long long total = 0;
+#pragma unroll 1
         for (int w = 0; w < kThreads / 32; ++w) {
             if (w == warp) upto += total;
             total += col.warp_sum[w];
@@ -297,6 +301,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
         long long before = (upto - mine) * units;
         if (blockIdx.x < ctas && before <= g0 && g0 < before + mine * units) {     // one thread's
             int b = lo;
+#pragma unroll 1
             for (;; ++b) {
                 const long long t = static_cast<long long>(tiles_of(b)) * units;
                 if (g0 < before + t) break;
@@ -335,21 +340,18 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
             const int kv = warp - S::kCopyWarp;
             const CUtensorMap* map = kv ? &v_map : &k_map;
             int e = kv;                                                    // entries of the ring: keys and values in turn
+#pragma unroll 1
             while (w.next(a, &st)) {
                 if (kv == 0 && w.t0 == 0 && w.unit == 0 && lane == 0 && st && a.status) atomicOr(a.status + w.b, st);
                 const int head = w.unit / a.row_tiles;
                 const int32_t* table = c.pages + w.b * c.pages_stride;
-                auto look = [&](int tile, int q) {                         // the page of box lane + 32 q
-                    const int at = lane + 32 * q, pos = tile * kTile + at * a.box;
-                    return tile < w.t1 && at < boxes && pos < w.keys ? load_now(table + page_of(pos, c.div_mul, c.div_shift)) : 0;
+                auto look = [&](int tile, int box) {
+                    const int pos = tile * kTile + box * a.box;
+                    return tile < w.t1 && box < boxes && pos < w.keys ? load_now(table + page_of(pos, c.div_mul, c.div_shift)) : 0;
                 };
-                int page[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) page[q] = look(w.t0, q);
-                for (int tile = w.t0; tile < w.t1; ++tile, e += 2) {
-                    int next[4];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) next[q] = look(tile + 1, q);
+                // pages are looked up two tiles ahead, into two registers in turn: a copy from one to the other would
+                // wait for the load
+                auto turn = [&](int tile, int& page) {
                     // boxes that hold a position below the sequence's end
                     const int full = max(0, min(boxes, (w.keys - tile * kTile + a.box - 1) / a.box));
                     const int at = e % kDepth;
@@ -357,28 +359,33 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                     if (lane == 0) mbar_arrive_expect_tx(&arrived[at], full * a.box * (E4M3 ? a.pitch : S::kPanels * 128));
                     __syncwarp();
                     uint8_t* dst = E4M3 ? stages + at * S::kStage : ring + at * S::kSlot;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const int box = lane + 32 * q;
-                        if (box >= full) break;
+#pragma unroll 1
+                    for (int box = lane; box < full; box += 32) {
                         const int pos = tile * kTile + box * a.box;
                         const int slot = pos - static_cast<int>(page_of(pos, c.div_mul, c.div_shift)) * c.page_size;
-                        int pg = page[q];
+                        int pg = box < 32 ? page : look(tile, box);        // (pages that 4 does not divide have more)
                         if (static_cast<unsigned>(pg) >= static_cast<unsigned>(c.n_pages)) {
-                            pg = c.n_pages;                            // outside the tensor: zeros
+                            pg = c.n_pages;                                // outside the tensor: zeros
                             if (kv == 0 && a.status) atomicOr(a.status + w.b, PLDP_ST_PAGE);
                         }
                         const int c1 = a.head_first ? head : slot, c2 = a.head_first ? slot : head;
                         if constexpr (E4M3) {
                             tma_box(dst + box * a.box * a.pitch, map, 0, c1, c2, pg, &arrived[at]);
                         } else {
-#pragma unroll
+#pragma unroll 1
                             for (int p = 0; p < S::kPanels; ++p)
                                 tma_box(dst + p * (kTile * 128) + box * a.box * 128, map, p * 64, c1, c2, pg, &arrived[at]);
                         }
                     }
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) page[q] = next[q];
+                    __syncwarp();
+                    page = look(tile + 2, lane);
+                    e += 2;
+                };
+                int page = look(w.t0, lane), page_b = look(w.t0 + 1, lane);
+#pragma unroll 1
+                for (int tile = w.t0; tile < w.t1; tile += 2) {
+                    turn(tile, page);
+                    if (tile + 1 < w.t1) turn(tile + 1, page_b);
                 }
                 w.step(a);
             }
@@ -386,6 +393,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
         } else if (warp == S::kKeyWarp) {
             // ---- the keys of each tile, four a lane: whether there is one, and e4m3's scales ----
             int tile_no = 0;
+#pragma unroll 1
             while (w.next(a, &st)) {
                 const int kv = w.unit / a.row_tiles;
                 const int32_t* table = c.pages + w.b * c.pages_stride;
@@ -411,16 +419,11 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                         }
                     }
                 };
-                // pages are looked up two tiles ahead, scales loaded one ahead
-                look(w.t0, page);
-                if constexpr (E4M3) fetch(w.t0, page, ks, vs);
-                int page_next[4];
-                look(w.t0 + 1, page_next);
-                for (int tile = w.t0; tile < w.t1; ++tile, ++tile_no) {
-                    int page_after[4];
-                    [[maybe_unused]] float ks_next[4], vs_next[4];
-                    if constexpr (E4M3) fetch(tile + 1, page_next, ks_next, vs_next);
-                    look(tile + 2, page_after);
+                // Scales are loaded one tile ahead and pages two, into two sets of registers in turn: a copy from one to
+                // the other would wait for the loads.
+                auto turn = [&](int tile, int (&page)[4], float (&ks)[4], float (&vs)[4], int (&page2)[4], float (&ks2)[4],
+                                float (&vs2)[4]) {
+                    if constexpr (E4M3) fetch(tile + 1, page2, ks2, vs2);
                     const int at = tile_no & 3;
                     if (tile_no >= 4) wait_for(&col.key_empty[at], (tile_no >> 2) - 1, &col.dead);
 #pragma unroll
@@ -433,14 +436,24 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                             col.key_log[at][key] = there ? __log2f(v) : -INFINITY;
                             col.key_scale[at][key] = there ? ks[i] * a.scale2 : 0.f;
                             col.key_inverse[at][key] = __frcp_rn(v);
-                            ks[i] = ks_next[i], vs[i] = vs_next[i];
                         } else {
                             col.key_log[at][key] = there ? 0.f : -INFINITY;
                         }
-                        page[i] = page_next[i], page_next[i] = page_after[i];
                     }
                     bar_arrive(5 + at, 160);             // for the one half of the columns, and for the other
                     bar_arrive(9 + at, 160);
+                    look(tile + 2, page);
+                    ++tile_no;
+                };
+                int page_b[4];
+                [[maybe_unused]] float ks_b[4], vs_b[4];
+                look(w.t0, page);
+                look(w.t0 + 1, page_b);
+                if constexpr (E4M3) fetch(w.t0, page, ks, vs);
+#pragma unroll 1
+                for (int tile = w.t0; tile < w.t1; tile += 2) {
+                    turn(tile, page, ks, vs, page_b, ks_b, vs_b);
+                    if (tile + 1 < w.t1) turn(tile + 1, page_b, ks_b, vs_b, page, ks, vs);
                 }
                 w.step(a);
             }
@@ -468,11 +481,13 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                     mma_commit(&col.empty[slot]);
                     mma_commit(&col.s_full[k & 1]);
                 };
+#pragma unroll 1
                 while (w.next(a, &st)) {
                     const int count = w.t1 - w.t0;
                     wait_for(&col.q_full, segment, &col.dead);
                     tmem_after_sync();
                     scores(e, tile);
+#pragma unroll 1
                     for (int i = 0; i < count; ++i, ++tile, e += 2) {
                         if (i + 1 < count) scores(e + 2, tile + 1);
                         const int slot = (e + 1) % S::kSlots;
@@ -505,9 +520,12 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
             const int chunk = t % kRowChunks, row0 = t / kRowChunks;
             const bool in = chunk * 16 < D;
             int e = 0;
+#pragma unroll 1
             while (w.next(a, &st)) {
+#pragma unroll 1
                 for (int tile = w.t0; tile < w.t1; ++tile) {
                     const int rows = min(kTile, w.keys - tile * kTile);          // the rest is zeros
+#pragma unroll 1
                     for (int kv = 0; kv < 2; ++kv, ++e) {
                         const int slot = e % S::kSlots, stage = e % S::kStages;
                         const uint8_t* from = stages + stage * S::kStage + row0 * a.pitch + chunk * 16;
@@ -546,6 +564,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
         constexpr float kRoomUp = E4M3 ? 8.f + kLift : 64.f;
         int tile_no = 0;
         auto values_done = [&](int k) { wait_for(&col.pv_done[k & 1], k >> 1, &col.dead); };   // the second product of tile k
+#pragma unroll 1
         while (w.next(a, &st)) {
             const int kv = w.unit / a.row_tiles, r0 = (w.unit - kv * a.row_tiles) * NT;
             // the columns of this unit
@@ -615,6 +634,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
             bool settled = false;
             [[maybe_unused]] const float f0 = a.scale2;
             const int seen_by_all = w.first + r0 / a.group;    // the unit's first row sees positions up to here
+#pragma unroll 1
             for (int tile = w.t0; tile < w.t1; ++tile, ++tile_no) {
                 const uint32_t s_at = my_s + (tile_no & 1) * NT;
                 uint8_t* const p_now = p_smem + tile_no % S::kWeightTiles * S::kPs;
@@ -782,6 +802,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                         const int e = 2 * tile_no + 1, slot = e % S::kSlots;
                         wait_for(&col.full[slot], e / S::kSlots, &col.dead);
                         if (pos >= w.keys)
+#pragma unroll 1
                             for (int p = grp; p < 8 * S::kPanels; p += 2)
                                 *reinterpret_cast<uint4*>(ring + slot * S::kSlot + (p >> 3) * (kTile * 128) + j * 128 + (p & 7) * 16) =
                                     make_uint4(0u, 0u, 0u, 0u);
@@ -889,6 +910,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                     float M = -INFINITY, sum = 0.f;
                     if (tid < rows) {
                         const bool live = col.limit[tid] >= 0;
+#pragma unroll 1
                         for (int k0 = 0; k0 < parts; k0 += 8) {                      // eight parts' m and sum in flight
                             float m[8], part_sum[8], top = M;
 #pragma unroll
@@ -914,14 +936,17 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                         if (a.lse) a.lse[lse_at(tid)] = sum == 0.f ? -INFINITY : (log2f(sum) + M) * 0.69314718055994531f;
                     }
                     const float inverse = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll 1
                     for (int k0 = 0; k0 < parts; k0 += kFactors) {
                         const int k1 = min(parts, k0 + kFactors);
                         if (tid < rows)
+#pragma unroll 1
                             for (int k = k0; k < k1; ++k) {
                                 const float m = k0 == 0 ? factors[k * NT + tid] : __ldcg(place(k) + NT * DP + tid);
                                 factors[(k - k0) * NT + tid] = inverse == 0.f ? 0.f : ex2(m - M) * inverse;
                             }
                         bar_sync(4, kSoftmaxThreads);
+#pragma unroll 1
                         for (int item = tid; item < rows * kRowItems; item += kSoftmaxThreads) {
                             const int n = item / kRowItems, d = item % kRowItems * V;
                             if (d >= D) continue;
