@@ -649,22 +649,34 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 if constexpr (E4M3) {
                     f = col.key_scale[at][j] * back;
                     inv = col.key_inverse[at][j];
-                } else if (g != 0.f) {
-                    f = 0.f;
                 }
                 __syncwarp();
                 mbar_arrive_if(&col.key_empty[at], lane == 0);
+                const uint64_t f2 = pack_f32x2(f, f);
+                [[maybe_unused]] const uint64_t g2 = pack_f32x2(g, g), inv2 = pack_f32x2(inv, inv);
                 float x[CH];
                 // exponents of the weights of chunk ch against the present m
                 auto load = [&](int ch) {
                     tmem_load(s_at + ch * CH, x);
 #pragma unroll
                     for (int i = 0; i < CH; i += 4) {
+                        // (two columns an instruction)
                         const float4 nm = *reinterpret_cast<const float4*>(&col.neg_m[c0 + ch * CH + i]);
-                        x[i] = fmaf(x[i], f, g + nm.x);
-                        x[i + 1] = fmaf(x[i + 1], f, g + nm.y);
-                        x[i + 2] = fmaf(x[i + 2], f, g + nm.z);
-                        x[i + 3] = fmaf(x[i + 3], f, g + nm.w);
+                        uint64_t lo = pack_f32x2(nm.x, nm.y), hi = pack_f32x2(nm.z, nm.w);
+                        if constexpr (E4M3) {
+                            lo = add_f32x2(lo, g2);
+                            hi = add_f32x2(hi, g2);
+                        }
+                        lo = fma_f32x2(pack_f32x2(x[i], x[i + 1]), f2, lo);
+                        hi = fma_f32x2(pack_f32x2(x[i + 2], x[i + 3]), f2, hi);
+                        x[i] = lo_f32(lo), x[i + 1] = hi_f32(lo);
+                        x[i + 2] = lo_f32(hi), x[i + 3] = hi_f32(hi);
+                    }
+                    if constexpr (!E4M3) {
+                        if (g != 0.f) {                            // no such page
+#pragma unroll
+                            for (int i = 0; i < CH; ++i) x[i] = -INFINITY;
+                        }
                     }
                     if (masked) {
 #pragma unroll
@@ -702,9 +714,12 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 }
                 auto sum = [&](int ch) {
 #pragma unroll
-                    for (int i = 0; i < CH; ++i) {
-                        if constexpr (E4M3) l[ch * CH + i] = fmaf(x[i], inv, l[ch * CH + i]);
-                        else l[ch * CH + i] += x[i];
+                    for (int i = 0; i < CH; i += 2) {
+                        const uint64_t w2 = pack_f32x2(x[i], x[i + 1]);
+                        uint64_t l2 = pack_f32x2(l[ch * CH + i], l[ch * CH + i + 1]);
+                        if constexpr (E4M3) l2 = fma_f32x2(w2, inv2, l2);
+                        else l2 = add_f32x2(w2, l2);
+                        l[ch * CH + i] = lo_f32(l2), l[ch * CH + i + 1] = hi_f32(l2);
                     }
                 };
                 auto weights = [&] {
