@@ -119,16 +119,33 @@ struct Columns {
     long long warp_sum[16];
 };
 
+// Whether a phase is over; the answer takes some 120 cycles, which other questions and work can share.
+__device__ __forceinline__ bool over(uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity & 1u, 1); }
 // Waits, with a limit; after one has run out no wait of this CTA blocks for long any more, and its results
 // are marked as none.
+__device__ __forceinline__ void wait_more(bool done, uint64_t* bar, uint32_t parity, int* dead) {
+    // (one statement: the loop as C++ came to a hundred instructions at each of its places)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b32 n, x;\n\t"
+        "mov.u32 n, 0;\n\t"
+        "setp.ne.u32 p, %0, 0;\n\t"
+        "@p bra DONE;\n\t"
+        "AGAIN:\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "@p bra DONE;\n\t"
+        "add.u32 n, n, 1;\n\t"
+        "ld.volatile.shared.u32 x, [%3];\n\t"
+        "setp.ne.u32 p, x, 0;\n\t"
+        "@p bra DONE;\n\t"
+        "setp.lt.u32 p, n, %4;\n\t"
+        "@p bra AGAIN;\n\t"
+        "st.volatile.shared.u32 [%3], 1;\n\t"
+        "DONE:\n\t}" ::"r"(static_cast<uint32_t>(done)),
+        "r"(smem_u32(bar)), "r"(parity & 1u), "r"(smem_u32(dead)), "n"(kMbarPolls)
+        : "memory");
+}
 __device__ __forceinline__ void wait_for(uint64_t* bar, uint32_t parity, int* dead) {
-    uint32_t polls = 0;
-#pragma unroll 1
-    while (!mbar_wait(bar, parity & 1u, 1)) {
-        if (++polls < kMbarPolls && !*static_cast<volatile int*>(dead)) continue;
-        *static_cast<volatile int*>(dead) = 1;
-        break;
-    }
+    wait_more(over(bar, parity), bar, parity, dead);
 }
 
 // The CTA's part of the list, unit by unit.
@@ -469,42 +486,51 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 const uint32_t k_lo = static_cast<uint32_t>(k_op), k_hi = k_op >> 32, v_lo = static_cast<uint32_t>(v_op), v_hi = v_op >> 32;
                 constexpr uint32_t kScores = mma_form(128, NT, !E4M3, false, false), kValues = mma_form(128, S::kWeights, !E4M3, true, true);
                 int e = 0, tile = 0, segment = 0;       // entries, tiles and units so far
-                auto scores = [&](int entry, int k) {
-                    const int slot = entry % S::kSlots;
-                    wait_for(&col.full[slot], entry / S::kSlots, &col.dead);
-                    tmem_after_sync();
-                    const uint32_t op = k_lo + slot * (S::kSlot / 16), to = tmem + (k & 1) * NT;
-#pragma unroll
-                    for (int s = 0; s < DP / 16; ++s)
-                        if (s == 0 || s * 16 < D)
-                            mma_f16(to, op + (s >> 2) * (kTile * 8) + (s & 3) * 2, k_hi, q_lo + (s >> 2) * (NT * 8) + (s & 3) * 2, q_hi, kScores, s > 0);
-                    mma_commit(&col.empty[slot]);
-                    mma_commit(&col.s_full[k & 1]);
-                };
+                auto arrived = [&](int entry) { return over(&col.full[entry % S::kSlots], entry / S::kSlots); };
 #pragma unroll 1
                 while (w.next(a, &st)) {
                     const int count = w.t1 - w.t0;
+                    bool keys = arrived(e);
                     wait_for(&col.q_full, segment, &col.dead);
                     tmem_after_sync();
-                    scores(e, tile);
+                    // turn i: the scores of the unit's tile i, then the second product of tile i - 1
 #pragma unroll 1
-                    for (int i = 0; i < count; ++i, ++tile, e += 2) {
-                        if (i + 1 < count) scores(e + 2, tile + 1);
-                        const int slot = (e + 1) % S::kSlots;
-                        wait_for(&col.full[slot], (e + 1) / S::kSlots, &col.dead);
-                        wait_for(&col.p_full[tile % S::kWeightTiles], tile / S::kWeightTiles, &col.dead);
-                        tmem_after_sync();
-                        const uint32_t op = v_lo + slot * (S::kSlot / 16), from = p_lo + tile % S::kWeightTiles * (S::kPs / 16);
-                        const uint32_t more = i > 0;
+                    for (int i = 0; i <= count; ++i, ++tile, e += 2) {
+                        const int before = tile - 1, v_slot = (e - 1) % S::kSlots;
+                        const bool values = i > 0 && arrived(e - 1);
+                        if (i < count) {
+                            const int slot = e % S::kSlots;
+                            wait_more(keys, &col.full[slot], e / S::kSlots, &col.dead);
+                            tmem_after_sync();
+                            const uint32_t op = k_lo + slot * (S::kSlot / 16), to = tmem + (tile & 1) * NT;
 #pragma unroll
-                        for (int m = 0; m < S::kBlocks; ++m)
+                            for (int s = 0; s < DP / 16; ++s)
+                                if (s == 0 || s * 16 < D)
+                                    mma_f16(to, op + (s >> 2) * (kTile * 8) + (s & 3) * 2, k_hi, q_lo + (s >> 2) * (NT * 8) + (s & 3) * 2, q_hi,
+                                            kScores, s > 0);
+                            mma_commit(&col.s_full[tile & 1]);
+                            mma_commit(&col.empty[slot]);
+                        }
+                        const bool weights = i > 0 && over(&col.p_full[before % S::kWeightTiles], before / S::kWeightTiles);
+                        keys = i + 1 < count && arrived(e + 2);                   // the next turn's question
+                        if (i > 0) {
+                            wait_more(values, &col.full[v_slot], (e - 1) / S::kSlots, &col.dead);
+                            wait_more(weights, &col.p_full[before % S::kWeightTiles], before / S::kWeightTiles, &col.dead);
+                            tmem_after_sync();
+                            const uint32_t op = v_lo + v_slot * (S::kSlot / 16), from = p_lo + before % S::kWeightTiles * (S::kPs / 16);
+                            const uint32_t more = i > 1;
 #pragma unroll
-                            for (int s = 0; s < kTile / 16; ++s)
-                                mma_f16(tmem + 2 * NT + m * S::kWeights, op + m * 2 * (kTile * 8) + s * 128, v_hi, from + s * S::kRow, p_hi,
-                                        kValues, s > 0 ? 1u : more);
-                        mma_commit(&col.empty[slot]);
-                        mma_commit(&col.pv_done[tile & 1]);
+                            for (int m = 0; m < S::kBlocks; ++m)
+#pragma unroll
+                                for (int s = 0; s < kTile / 16; ++s)
+                                    mma_f16(tmem + 2 * NT + m * S::kWeights, op + m * 2 * (kTile * 8) + s * 128, v_hi, from + s * S::kRow, p_hi,
+                                            kValues, s > 0 ? 1u : more);
+                            mma_commit(&col.pv_done[before & 1]);
+                            mma_commit(&col.empty[v_slot]);
+                        }
                     }
+                    --tile;                                                       // the turn behind the last tile
+                    e -= 2;
                     ++segment;
                     w.step(a);
                 }
@@ -531,8 +557,10 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                         const uint8_t* from = stages + stage * S::kStage + row0 * a.pitch + chunk * 16;
                         uint8_t* to = ring + slot * S::kSlot + (chunk >> 2) * (kTile * 128);
                         const int piece = (chunk & 3) * 2;
-                        wait_for(&col.stage_full[stage], e / S::kStages, &col.dead);
-                        if (e >= S::kSlots) wait_for(&col.empty[slot], e / S::kSlots - 1, &col.dead);
+                        const bool codes = over(&col.stage_full[stage], e / S::kStages);
+                        const bool room = e < S::kSlots || over(&col.empty[slot], e / S::kSlots - 1);
+                        wait_more(codes, &col.stage_full[stage], e / S::kStages, &col.dead);
+                        wait_more(room, &col.empty[slot], e / S::kSlots - 1, &col.dead);
                         if (in) {
 #pragma unroll
                             for (int i = 0; i < kTurns; ++i) {
