@@ -208,6 +208,10 @@ _CALLS = ("pldp_find_candidates", "pldp_rank_hidden", "pldp_rank_attention", "pl
           "pldp_verify_sample_draft", "pldp_identify_heads", "pldp_top_heads")
 
 
+# ... and of its `CacheLibrary`.
+_CACHE_CALLS = ("pldp_cache_append", "pldp_cache_read", "pldp_attend_cache", "pldp_rank_cache", "pldp_token_logprobs")
+
+
 def _load_calls(lib):
     """The native form of the calls below, bound to the loaded library.  Each takes a
     call's arguments, makes its checks and returns the library's status, or None when a
@@ -221,6 +225,7 @@ def _load_calls(lib):
         m = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(m)
         m.bind(tuple(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in _CALLS))
+        m.bind_cache(tuple(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in _CACHE_CALLS))
     except Exception as e:                               # the Python below makes every call by itself
         warnings.warn(f"{os.path.basename(path)} does not load, the binding's calls go through ctypes: {e}",
                       RuntimeWarning, stacklevel=2)
@@ -815,6 +820,7 @@ class pldp_cache:
         a.page_stride, a.pos_stride, a.head_stride = k_cache.stride()[:3]
         a.pages, a.pages_stride, a.max_pages = p_pages, stride, max_pages
         self.B, self.heads, self.head_dim, self.dtype = pages.shape[0], heads, head_dim, k_cache.dtype
+        self.address = ctypes.addressof(a)                   # for the native calls
         self.tensors = (k_cache, v_cache, pages, k_scale, v_scale)
 
 
@@ -844,6 +850,10 @@ def pldp_cache_append(cache, q, k, v, seq_len, q_out, draft_len=None, q_norm=Non
     seq_len[b]-1 .. seq_len[b]-1+draft_len[b], writes the queries to q_out (bfloat16) and the keys
     and values to the cache.  q [B, n, q_heads, head_dim], k and v [B, n, heads, head_dim], float32
     or bfloat16, any strides of whole 16 bytes with unit inner stride (slices of one projection)."""
+    if _calls is not None and type(cache) is pldp_cache and _done("pldp_cache_append", _calls.cache_append(
+            cache.address, cache.B, q, k, v, seq_len, q_out, draft_len, q_norm, k_norm, eps, cos, sin, interleaved, status,
+            stream)):
+        return
     kinds = (torch.float32, torch.bfloat16)
     a = pldp_cache_append_args()
     a.q, a.q_strides = _vectors(q, "q", (None,) * 4, kinds)
@@ -873,6 +883,9 @@ def pldp_cache_read(cache, start, count, k_out, v_out, status=None, stream=None)
     """Positions start[b] .. start[b]+count[b]-1 (start None: from 0) of every sequence into rows
     0 .. count[b]-1 of k_out and v_out [B, n, heads, head_dim], float32 or bfloat16 and of the same
     strides; either may be None."""
+    if _calls is not None and type(cache) is pldp_cache and _done("pldp_cache_read", _calls.cache_read(
+            cache.address, cache.B, start, count, k_out, v_out, status, stream)):
+        return
     one = k_out if k_out is not None else v_out
     a = pldp_cache_read_args()
     p, a.out_strides = _vectors(one, "k_out" if one is k_out else "v_out", (None,) * 4, (torch.float32, torch.bfloat16))
@@ -900,6 +913,9 @@ def pldp_attend_cache(cache, q, seq_len, out, workspace, draft_len=None, lse=Non
     out bfloat16 [B, n, q_heads, head_dim]; lse float32 [B, n, q_heads] (optional); scale default
     1/sqrt(head_dim).  workspace: uint8 CUDA tensor of pldp_attend_workspace_size(B, n, q_heads,
     heads, head_dim) bytes, zeroed once before first use."""
+    if _calls is not None and type(cache) is pldp_cache and _done("pldp_attend_cache", _calls.attend_cache(
+            cache.address, cache.B, q, seq_len, out, workspace, draft_len, lse, scale, status, stream)):
+        return
     a = pldp_attend_args()
     a.q, a.q_strides = _vectors(q, "q", (None,) * 4, (torch.bfloat16,))
     B, n, Hq, D = q.shape
@@ -925,6 +941,11 @@ def pldp_rank_cache(cache, q, row, kv_len, lse, cand_pos, cand_count, best_pos, 
     row[b] (None: 0) of the step, with q and lse as pldp_attend_cache had and wrote them.  After
     verification row is accept_len and kv_len is kv_keep_len.  accumulate: scores holds other
     layers' scores and takes the larger (or the sum)."""
+    agg = {"max": PLDP_AGG_MAX, "sum": PLDP_AGG_SUM}.get(agg, agg)
+    if _calls is not None and type(cache) is pldp_cache and _done("pldp_rank_cache", _calls.rank_cache(
+            cache.address, cache.B, q, row, kv_len, lse, cand_pos, cand_count, best_pos, heads, agg, scale, scores, best_score,
+            accumulate, status, stream)):
+        return
     a = pldp_rank_cache_args()
     a.q, a.q_strides = _vectors(q, "q", (None,) * 4, (torch.bfloat16,))
     B, n, Hq, D = q.shape
@@ -941,7 +962,7 @@ def pldp_rank_cache(cache, q, row, kv_len, lse, cand_pos, cand_count, best_pos, 
     a.n_sel = 0 if heads is None else heads.numel()
     if heads is not None and a.n_sel < 1:                # an empty tensor's null pointer would mean all heads
         raise PldpError("pldp_rank_cache", PLDP_ERR_INVALID_ARG, "n_sel < 1")
-    a.agg = {"max": PLDP_AGG_MAX, "sum": PLDP_AGG_SUM}.get(agg, agg)
+    a.agg = agg
     a.accumulate = int(bool(accumulate))
     a.scale = D ** -0.5 if scale is None else float(scale)
     a.cand_pos = _dense(cand_pos, "cand_pos", torch.int32)
@@ -964,6 +985,9 @@ def pldp_token_logprobs(logits, tokens, logprob, workspace, entropy=None, top_id
     alternatives (top_id int32 and top_logprob float32 [..., top], optional, top <= 32) of every row
     of logits [..., V] (float32 or bfloat16, contiguous).  workspace: uint8 CUDA tensor of
     pldp_token_logprobs_workspace_size(rows, V) bytes."""
+    if _calls is not None and _done("pldp_token_logprobs", _calls.token_logprobs(
+            logits, tokens, logprob, workspace, entropy, top_id, top_logprob, temperature, stream)):
+        return
     p = _dense(logits, "logits")
     if logits.dim() < 1 or logits.shape[-1] < 1:
         raise ValueError("logits must be [..., V]")

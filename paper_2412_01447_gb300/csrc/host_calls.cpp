@@ -42,6 +42,15 @@ struct Library {
     decltype(&pldp_top_heads) top_heads;
 } lib;
 
+// The same for the calls of the cache and of token scoring (bind_cache()); unbound, each is left to Python.
+struct CacheLibrary {
+    decltype(&pldp_cache_append) append;
+    decltype(&pldp_cache_read) read;
+    decltype(&pldp_attend_cache) attend;
+    decltype(&pldp_rank_cache) rank;
+    decltype(&pldp_token_logprobs) logprobs;
+} cache_lib;
+
 #ifdef PLDP_TEST_ANY_DEVICE
 constexpr bool kAnyDevice = true;    // test build: host tensors pass, so that the checks run without a GPU
 #else
@@ -164,6 +173,45 @@ struct Args {
         const at::Tensor* t = tensor(o);
         if (t && t->dim() != 3) ok = false;
         return ok ? t : nullptr;
+    }
+    // A [sequences, tokens, heads, head_dim] tensor with unit inner stride, and its other strides.
+    const at::Tensor* vectors(PyObject* o, int64_t (&strides)[3], bool optional = false) {
+        const at::Tensor* t = tensor(o, optional);
+        if (!t) return nullptr;
+        if (t->dim() != 4 || t->stride(3) != 1) {
+            ok = false;
+            return nullptr;
+        }
+        for (int i = 0; i < 3; ++i) strides[i] = t->stride(i);
+        for (int i = 0; i < 4; ++i)
+            if (t->size(i) > INT32_MAX) ok = false;
+        return t;
+    }
+    // Of the shape and type that the call needs.
+    void* vectors(PyObject* o, int64_t (&strides)[3], int64_t B, int64_t n, int64_t heads, int64_t d, c10::ScalarType type,
+                  bool optional = false) {
+        const at::Tensor* t = vectors(o, strides, optional);
+        if (!t) return nullptr;
+        if (t->size(0) != B || t->size(1) != n || t->size(2) != heads || t->size(3) != d || t->scalar_type() != type) {
+            ok = false;
+            return nullptr;
+        }
+        return t->data_ptr();
+    }
+    // The description that a pldp_cache object holds, by its address, with a page table of at least B rows.
+    pldp_cache cache(PyObject* address, PyObject* rows, int64_t B) {
+        pldp_cache c = {};
+        const int64_t at = integer(address, 1, INT64_MAX);
+        if (B > integer(rows, 0, INT64_MAX)) ok = false;
+        if (ok) std::memcpy(&c, reinterpret_cast<const void*>(at), sizeof c);
+        return c;
+    }
+    int flag(PyObject* o) {
+        if (o != Py_True && o != Py_False) ok = false;
+        return o == Py_True;
+    }
+    float scale(PyObject* o, int64_t head_dim) {               // None: 1 / sqrt(head_dim)
+        return o == Py_None ? static_cast<float>(std::pow(static_cast<double>(head_dim), -0.5)) : real(o);
     }
     void* stream(PyObject* o) {
         if (o == nullptr || o == Py_None) return c10::cuda::getCurrentCUDAStream().stream();
@@ -624,9 +672,169 @@ PLDP_CALL(top_heads) {
     PLDP_END
 }
 
-// bind(addresses): the library's entry points, in the order of `Library`.
-PyObject* bind(PyObject*, PyObject* addresses) noexcept {
-    constexpr Py_ssize_t count = sizeof(Library) / sizeof(void*);
+// cache's address, its page table's rows, q, k, v, seq_len, q_out, draft_len, q_norm, k_norm, eps, cos, sin, interleaved,
+// status, stream
+PLDP_CALL(cache_append) {
+    PLDP_BEGIN(16)
+    pldp_cache_append_args p = {};
+    const at::Tensor* q = a.vectors(v[2], p.q_strides);
+    if (!q || !cache_lib.append) Py_RETURN_NONE;
+    const int64_t B = q->size(0), n_ = q->size(1), Hq = q->size(2), D = q->size(3);
+    const c10::ScalarType type = q->scalar_type();
+    p.cache = a.cache(v[0], v[1], B);
+    if (p.cache.head_dim != D) a.ok = false;
+    p.dtype = a.code(q);
+    p.q = q->data_ptr();
+    p.k = a.vectors(v[3], p.k_strides, B, n_, p.cache.heads, D, type);
+    p.v = a.vectors(v[4], p.v_strides, B, n_, p.cache.heads, D, type);
+    p.q_out = a.vectors(v[6], p.q_out_strides, B, n_, Hq, D, at::kBFloat16);
+    p.B = static_cast<int>(B), p.n = static_cast<int>(n_), p.q_heads = static_cast<int>(Hq);
+    p.seq_len = a.ints(v[5], B);
+    p.draft_len = a.ints(v[7], B, true);
+    p.q_norm = a.dense(v[8], D, true, type);
+    p.k_norm = a.dense(v[9], D, true, type);
+    p.eps = a.real(v[10]);
+    if (v[11] != Py_None || v[12] != Py_None) {
+        const at::Tensor *c = a.tensor(v[11]), *s = a.tensor(v[12]);
+        if (!c || !s || c->dim() != 2 || s->dim() != 2 || c->size(0) != s->size(0) || c->size(1) != s->size(1) ||
+            c->size(1) > INT32_MAX / 2)
+            Py_RETURN_NONE;
+        p.cos = a.floats(v[11], -1);
+        p.sin = a.floats(v[12], -1);
+        p.rot_rows = c->size(0);
+        p.rot = 2 * static_cast<int>(c->size(1));
+    }
+    p.interleaved = a.flag(v[13]);
+    p.status = a.words(v[14], B);
+    void* s = a.stream(v[15]);
+    return finish(a, [&] { return cache_lib.append(&p, s); });
+    PLDP_END
+}
+
+// cache's address, its page table's rows, start, count, k_out, v_out, status, stream
+PLDP_CALL(cache_read) {
+    PLDP_BEGIN(8)
+    pldp_cache_read_args p = {};
+    const at::Tensor* one = a.vectors(v[4] != Py_None ? v[4] : v[5], p.out_strides);
+    if (!one || !cache_lib.read) Py_RETURN_NONE;
+    const int64_t B = one->size(0), n_ = one->size(1);
+    p.cache = a.cache(v[0], v[1], B);
+    p.dtype = a.code(one);
+    int64_t ks[3], vs[3];
+    p.k_out = a.vectors(v[4], ks, B, n_, p.cache.heads, p.cache.head_dim, one->scalar_type(), true);
+    p.v_out = a.vectors(v[5], vs, B, n_, p.cache.heads, p.cache.head_dim, one->scalar_type(), true);
+    for (int i = 0; i < 3; ++i)
+        if ((v[4] != Py_None && ks[i] != p.out_strides[i]) || (v[5] != Py_None && vs[i] != p.out_strides[i])) a.ok = false;
+    p.B = static_cast<int>(B), p.n = static_cast<int>(n_);
+    p.start = a.ints(v[2], B, true);
+    p.count = a.ints(v[3], B);
+    p.status = a.words(v[6], B);
+    void* s = a.stream(v[7]);
+    return finish(a, [&] { return cache_lib.read(&p, s); });
+    PLDP_END
+}
+
+// cache's address, its page table's rows, q, seq_len, out, workspace, draft_len, lse, scale, status, stream
+PLDP_CALL(attend_cache) {
+    PLDP_BEGIN(11)
+    pldp_attend_args p = {};
+    const at::Tensor* q = a.vectors(v[2], p.q_strides);
+    if (!q || !cache_lib.attend) Py_RETURN_NONE;
+    const int64_t B = q->size(0), n_ = q->size(1), Hq = q->size(2), D = q->size(3);
+    p.cache = a.cache(v[0], v[1], B);
+    if (p.cache.head_dim != D || q->scalar_type() != at::kBFloat16) a.ok = false;
+    p.q = q->data_ptr();
+    p.out = a.vectors(v[4], p.out_strides, B, n_, Hq, D, at::kBFloat16);
+    p.B = static_cast<int>(B), p.n = static_cast<int>(n_), p.q_heads = static_cast<int>(Hq);
+    p.seq_len = a.ints(v[3], B);
+    p.workspace = a.bytes(v[5], &p.workspace_bytes);
+    p.draft_len = a.ints(v[6], B, true);
+    p.lse = a.floats(v[7], B * n_ * Hq, true);
+    p.scale = a.scale(v[8], D);
+    p.status = a.words(v[9], B);
+    void* s = a.stream(v[10]);
+    return finish(a, [&] { return cache_lib.attend(&p, s); });
+    PLDP_END
+}
+
+// cache's address, its page table's rows, q, row, kv_len, lse, cand_pos, cand_count, best_pos, heads, agg, scale, scores,
+// best_score, accumulate, status, stream
+PLDP_CALL(rank_cache) {
+    PLDP_BEGIN(17)
+    pldp_rank_cache_args p = {};
+    const at::Tensor* q = a.vectors(v[2], p.q_strides);
+    const at::Tensor* cand = a.tensor(v[6]);
+    if (!q || !cand || !cache_lib.rank) Py_RETURN_NONE;
+    const int64_t B = q->size(0), n_ = q->size(1), Hq = q->size(2), D = q->size(3);
+    if (cand->dim() != 2 || cand->size(0) < B || q->scalar_type() != at::kBFloat16) Py_RETURN_NONE;
+    p.cache = a.cache(v[0], v[1], B);
+    if (p.cache.head_dim != D) a.ok = false;
+    p.q = q->data_ptr();
+    p.B = static_cast<int>(B), p.n = static_cast<int>(n_), p.q_heads = static_cast<int>(Hq);
+    p.C_cap = a.cols(v[6]);
+    p.row = a.ints(v[3], B, true);
+    p.kv_len = a.ints(v[4], B);
+    p.lse = a.floats(v[5], B * n_ * Hq);
+    p.cand_pos = a.ints(v[6], -1);
+    p.cand_count = a.ints(v[7], B);
+    p.best_pos = a.ints(v[8], B);
+    p.heads = a.ints(v[9], -1, true);
+    if (v[9] != Py_None) {
+        const int64_t n_sel = p.heads ? THPVariable_Unpack(v[9]).numel() : 0;
+        if (n_sel < 1 || n_sel > INT32_MAX) a.ok = false;
+        p.n_sel = static_cast<int>(n_sel);
+    }
+    p.agg = static_cast<pldp_agg>(a.integer(v[10]));
+    p.scale = a.scale(v[11], D);
+    p.scores = a.floats(v[12], B * p.C_cap, true);
+    p.best_score = a.floats(v[13], B, true);
+    p.accumulate = a.flag(v[14]);
+    p.status = a.words(v[15], B);
+    void* s = a.stream(v[16]);
+    return finish(a, [&] { return cache_lib.rank(&p, s); });
+    PLDP_END
+}
+
+// logits, tokens, logprob, workspace, entropy, top_id, top_logprob, temperature, stream
+PLDP_CALL(token_logprobs) {
+    PLDP_BEGIN(9)
+    const at::Tensor* x = a.tensor(v[0]);
+    if (!x || !cache_lib.logprobs || !x->is_contiguous() || x->dim() < 1) Py_RETURN_NONE;
+    const int64_t V = x->size(-1);
+    if (V < 1 || V > INT32_MAX) Py_RETURN_NONE;
+    const int64_t rows = x->numel() / V;
+    const void* logits = x->data_ptr();
+    const pldp_dtype code = a.code(x);
+    int64_t top = -1;
+    for (PyObject* o : {v[5], v[6]}) {
+        const at::Tensor* t = a.tensor(o, true);
+        if (!t) continue;
+        const int64_t k = t->dim() ? t->size(-1) : 0;
+        if (top >= 0 && top != k) a.ok = false;
+        top = k;
+    }
+    if (top < 0) top = 0;
+    if (top > INT32_MAX) a.ok = false;
+    const int32_t* tokens = a.ints(v[1], rows, true);
+    float* lp = a.floats(v[2], rows, true);
+    size_t bytes = 0;
+    void* ws = a.bytes(v[3], &bytes);
+    float* ent = a.floats(v[4], rows, true);
+    int32_t* ids = a.ints(v[5], a.ok ? rows * top : 0, true);
+    float* tops = a.floats(v[6], a.ok ? rows * top : 0, true);
+    const float T = a.real(v[7]);
+    void* s = a.stream(v[8]);
+    return finish(a, [&] {
+        return cache_lib.logprobs(logits, code, rows, static_cast<int>(V), T, tokens, lp, ent, static_cast<int>(top), ids, tops,
+                                  ws, bytes, s);
+    });
+    PLDP_END
+}
+
+// Entry points' addresses into a table of them.
+template <typename T>
+PyObject* bind_table(T& table, PyObject* addresses) {
+    constexpr Py_ssize_t count = sizeof(T) / sizeof(void*);
     if (!PyTuple_CheckExact(addresses) || PyTuple_GET_SIZE(addresses) != count) {
         PyErr_SetString(PyExc_ValueError, "bind: a tuple with every entry point's address");
         return nullptr;
@@ -639,16 +847,21 @@ PyObject* bind(PyObject*, PyObject* addresses) noexcept {
             return nullptr;
         }
     }
-    std::memcpy(&lib, p, sizeof p);
+    std::memcpy(&table, p, sizeof p);
     Py_RETURN_NONE;
 }
+
+// bind(addresses), bind_cache(addresses): the library's entry points, in the order of `Library` and `CacheLibrary`.
+PyObject* bind(PyObject*, PyObject* addresses) noexcept { return bind_table(lib, addresses); }
+PyObject* bind_cache(PyObject*, PyObject* addresses) noexcept { return bind_table(cache_lib, addresses); }
 
 #define PLDP_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     PLDP_METHOD(find_candidates), PLDP_METHOD(rank_hidden), PLDP_METHOD(rank_attention), PLDP_METHOD(extract_draft),
     PLDP_METHOD(draft_step), PLDP_METHOD(index_build), PLDP_METHOD(verify_greedy), PLDP_METHOD(verify_greedy_draft),
     PLDP_METHOD(verify_sample), PLDP_METHOD(verify_sample_draft), PLDP_METHOD(identify_heads), PLDP_METHOD(top_heads),
-    {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+    PLDP_METHOD(cache_append), PLDP_METHOD(cache_read), PLDP_METHOD(attend_cache), PLDP_METHOD(rank_cache),
+    PLDP_METHOD(token_logprobs), {"bind", bind, METH_O, nullptr}, {"bind_cache", bind_cache, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pldp_calls", "Native argument checks of the PLD+ binding.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
