@@ -76,11 +76,11 @@ struct AppendArgs {
     const float *cos, *sin;
     const int32_t *seq_len, *draft_len;
     uint32_t* status;
-    int n, q_heads, rot, interleaved, capacity, per;   // per: vectors a CTA takes
-    float eps;
+    int n, q_heads, rot, interleaved, capacity, tokens;
+    float eps, inverse_dim;
 };
 
-constexpr int kAppendThreads = 128;
+constexpr int kAppendThreads = 256, kAppendBlocks = 4;
 
 // Eight elements as floats.
 __device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8]) {
@@ -109,132 +109,196 @@ __device__ __forceinline__ uint32_t e4m3_quad(float a, float b, float c, float d
            static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3)) << 16;
 }
 
-// One CTA takes `per` of one token's vectors (its query heads, then key heads, then value
-// heads), GS lanes a vector, eight elements a lane.  A lane's place in the vector is the
-// same for all of them, so the rotation's cosines and sines and the norms' weights are
-// loaded once and stay in registers.
+template <typename T>
+struct Raw {                            // eight elements as they are in memory
+    uint4 x[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+        for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) x[i] = *(reinterpret_cast<const uint4*>(p) + i);
+    }
+    __device__ __forceinline__ void unpack(float (&y)[8]) const { load8(reinterpret_cast<const T*>(x), y); }
+};
+
+// A vector (a query, key or value head of one token) is GS lanes', eight elements a lane; a CTA takes a token, its
+// vectors kAppendThreads / GS at a time, the next one's elements on their way while one is worked on, and then
+// its next token.  Instructions are what bounds it, so what a token's vectors share (its position, its
+// page, the rotation's cosines and sines of this lane's elements) is worked out once a token.
 template <typename T, int GS, bool E4M3>
-__global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const AppendArgs a) {
+__global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_kernel(const AppendArgs a) {
     pdl_enter();
     constexpr int kGroups = kAppendThreads / GS;
-    __shared__ __align__(16) float stage[kGroups][GS * 8];
+    __shared__ __align__(16) float stage[2][kGroups][GS * 8];
     const CacheView& c = a.c;
-    const int b = blockIdx.x / a.n, i = blockIdx.x - b * a.n;
-    uint32_t st;
-    const StepTokens tk = step_tokens(a.seq_len, a.draft_len, b, a.n, a.capacity, st);
-    if (i == 0 && blockIdx.y == 0 && threadIdx.x == 0 && st && a.status) atomicOr(a.status + b, st);
-    if (i >= tk.count) return;
-    const int pos = tk.first + i, D = c.head_dim;
-    const int g = threadIdx.x / GS, at = threadIdx.x % GS, e0 = at * 8;
-    const bool in = e0 < D;
+    const int D = c.head_dim, g = threadIdx.x / GS, at = threadIdx.x % GS, e0 = at * 8;
+    const int first = g + blockIdx.y * kGroups, step = kGroups * gridDim.y;     // of this group's vectors
+    const int k_first = a.q_heads, v_first = a.q_heads + c.heads, total = v_first + c.heads;
+    const bool live = e0 < D;
     // the lanes of this vector's group: they take the same branches
     const unsigned mates = GS == 32 ? 0xFFFFFFFFu : ((1u << (GS % 32)) - 1u) << ((threadIdx.x & 31) / GS * GS);
-
-    int64_t scale_at;
-    const int64_t off = locate(c, c.pages + b * c.pages_stride, pos, scale_at);
-    if (off < 0 && blockIdx.y == 0 && threadIdx.x == 0 && a.status) atomicOr(a.status + b, PLDP_ST_PAGE);
-
-    // y' = y cs + partner sn; elements that do not rotate: cs = 1, sn = 0, their own partner
-    float cs[8], sn[8], wq[8], wk[8];
     const int half = a.rot >> 1;
-    const float* cr = a.cos ? a.cos + static_cast<int64_t>(pos) * half : nullptr;
-    const float* sr = a.cos ? a.sin + static_cast<int64_t>(pos) * half : nullptr;
+    // where this lane's partners in the rotation are, when its eight elements rotate alike (or not at all)
+    const bool alike = a.interleaved || (half & 7) == 0;
+    const int partner = e0 < half ? e0 + half : e0 < a.rot ? e0 - half : e0;
+#pragma unroll 1
+    for (int token = blockIdx.x; token < a.tokens; token += gridDim.x) {
+        const int b = token / a.n, i = token - b * a.n;
+        const T* q = static_cast<const T*>(a.q) + (b * a.qs.seq + i * a.qs.tok + e0);
+        const T* k = static_cast<const T*>(a.k) + (b * a.ks.seq + i * a.ks.tok + e0);
+        const T* v = static_cast<const T*>(a.v) + (b * a.vs.seq + i * a.vs.tok + e0);
+        auto source = [&](int h) {
+            return h < k_first ? q + h * a.qs.head : h < v_first ? k + (h - k_first) * a.ks.head : v + (h - v_first) * a.vs.head;
+        };
+        Raw<T> next;
+        if (first < total && live) next.load(source(first));
+        uint32_t st;
+        const StepTokens tk = step_tokens(a.seq_len, a.draft_len, b, a.n, a.capacity, st);
+        if (i == 0 && threadIdx.x == 0 && blockIdx.y == 0 && st && a.status) atomicOr(a.status + b, st);
+        if (i >= tk.count) continue;
+        const int pos = tk.first + i;
+        // y' = y cs + partner sn; an element that does not rotate is its own partner, cs = 1, sn = 0
+        float cs[8], sn[8];
+        {
+            const float* cr = a.cos + static_cast<int64_t>(pos) * half;
+            const float* sr = a.sin + static_cast<int64_t>(pos) * half;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int e = e0 + j;
-        cs[j] = 1.f, sn[j] = 0.f;
-        if (e < a.rot) {
-            const int p = a.interleaved ? e >> 1 : e < half ? e : e - half;
-            const bool second = a.interleaved ? e & 1 : e >= half;
-            cs[j] = __ldg(cr + p);
-            sn[j] = second ? __ldg(sr + p) : -__ldg(sr + p);
-        }
-        wq[j] = wk[j] = 1.f;
-    }
-    if (in && a.q_norm) load8(static_cast<const T*>(a.q_norm) + e0, wq);
-    if (in && a.k_norm) load8(static_cast<const T*>(a.k_norm) + e0, wk);
-
-    const int total = a.q_heads + 2 * c.heads;
-    const int lo = blockIdx.y * a.per, hi = min(lo + a.per, total);
-    for (int h0 = lo; h0 < hi; h0 += kGroups) {            // the same number of turns for every thread
-        const int h = h0 + g;
-        const bool live = h < hi && in;
-        const int kind = h < a.q_heads ? 0 : h < a.q_heads + c.heads ? 1 : 2;
-        const int head = kind == 0 ? h : kind == 1 ? h - a.q_heads : h - a.q_heads - c.heads;
-        const Strides& s = kind == 0 ? a.qs : kind == 1 ? a.ks : a.vs;
-        const T* src = static_cast<const T*>(kind == 0 ? a.q : kind == 1 ? a.k : a.v);
-        float y[8];
+            for (int j = 0; j < 8; ++j) cs[j] = 1.f, sn[j] = 0.f;
+            if (alike && (half & 3) == 0) {                // whole vectors of the tables' rows
+                if (e0 < a.rot) {
+                    if (a.interleaved) {
+                        const float4 x = __ldg(reinterpret_cast<const float4*>(cr + (e0 >> 1))), y = __ldg(reinterpret_cast<const float4*>(sr + (e0 >> 1)));
+                        if (e0 + 8 <= a.rot) {
+                            cs[0] = cs[1] = x.x, cs[2] = cs[3] = x.y, cs[4] = cs[5] = x.z, cs[6] = cs[7] = x.w;
+                            sn[0] = -y.x, sn[1] = y.x, sn[2] = -y.y, sn[3] = y.y, sn[4] = -y.z, sn[5] = y.z, sn[6] = -y.w, sn[7] = y.w;
+                        }
+                    } else {
+                        const int p = e0 < half ? e0 : e0 - half;
+                        const float sign = e0 < half ? -1.f : 1.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = 0.f;
-        if (live) load8(src + b * s.seq + i * s.tok + head * s.head + e0, y);
-        if (kind == 0 ? a.q_norm != nullptr : kind == 1 && a.k_norm != nullptr) {
-            float sum = 0.f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum = fmaf(y[j], y[j], sum);
-#pragma unroll
-            for (int o = GS / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(mates, sum, o, GS);
-            const float r = rsqrtf(sum / D + a.eps);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = y[j] * r * (kind == 0 ? wq[j] : wk[j]);
-        }
-        if (a.rot) {
-            if (a.interleaved) {
-                if (kind < 2) {
-#pragma unroll
-                    for (int j = 0; j < 8; j += 2) {
-                        const float p = y[j], q = y[j + 1];
-                        y[j] = p * cs[j] + q * sn[j];
-                        y[j + 1] = q * cs[j + 1] + p * sn[j + 1];
+                        for (int j = 0; j < 8; j += 4) {
+                            const float4 x = __ldg(reinterpret_cast<const float4*>(cr + p + j)), y = __ldg(reinterpret_cast<const float4*>(sr + p + j));
+                            cs[j] = x.x, cs[j + 1] = x.y, cs[j + 2] = x.z, cs[j + 3] = x.w;
+                            sn[j] = sign * y.x, sn[j + 1] = sign * y.y, sn[j + 2] = sign * y.z, sn[j + 3] = sign * y.w;
+                        }
                     }
                 }
             } else {
-                float* row = stage[g];
-                *reinterpret_cast<float4*>(row + e0) = make_float4(y[0], y[1], y[2], y[3]);
-                *reinterpret_cast<float4*>(row + e0 + 4) = make_float4(y[4], y[5], y[6], y[7]);
-                __syncwarp(mates);
-                if (kind < 2) {
+#pragma unroll 1
+                for (int j = 0; j < 8; ++j) {
+                    const int e = e0 + j;
+                    if (e >= a.rot) break;
+                    const int p = a.interleaved ? e >> 1 : e < half ? e : e - half;
+                    const float s = __ldg(sr + p), x = __ldg(cr + p), y = (a.interleaved ? e & 1 : e >= half) ? s : -s;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int e = e0 + j;
-                        if (e < a.rot) y[j] = y[j] * cs[j] + row[e < half ? e + half : e - half] * sn[j];
+                    for (int k = 0; k < 8; ++k)
+                        if (k == j) cs[k] = x, sn[k] = y;
+                }
+            }
+        }
+        int64_t scale_at;
+        const int64_t off = locate(c, c.pages + b * c.pages_stride, pos, scale_at);
+        if (off < 0 && threadIdx.x == 0 && blockIdx.y == 0 && a.status) atomicOr(a.status + b, PLDP_ST_PAGE);
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.q_out) + (b * a.os.seq + i * a.os.tok + e0);
+#pragma unroll 1
+        for (int h = first, turn = 0; h < total; h += step, turn ^= 1) {
+            float y[8];
+            if (live) {
+                next.unpack(y);
+                if (h + step < total) next.load(source(h + step));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = 0.f;
+            }
+            const int kind = h < k_first ? 0 : h < v_first ? 1 : 2;
+            const T* norm = static_cast<const T*>(kind == 0 ? a.q_norm : kind == 1 ? a.k_norm : nullptr);
+            if (norm) {
+                float w[8], sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j] = 0.f;
+                if (live) load8(norm + e0, w);
+                uint64_t two = 0;                          // (two elements an instruction)
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) two = fma_f32x2(pack_f32x2(y[j], y[j + 1]), pack_f32x2(y[j], y[j + 1]), two);
+                sum = lo_f32(two) + hi_f32(two);
+#pragma unroll
+                for (int o = GS / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(mates, sum, o, GS);
+                const float r = rsqrtf(fmaf(sum, a.inverse_dim, a.eps));
+                const uint64_t r2 = pack_f32x2(r, r);
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) {
+                    const uint64_t z = fma_f32x2(fma_f32x2(pack_f32x2(y[j], y[j + 1]), r2, 0ull), pack_f32x2(w[j], w[j + 1]), 0ull);
+                    y[j] = lo_f32(z), y[j + 1] = hi_f32(z);
+                }
+            }
+            if (a.rot && kind < 2) {
+                if (a.interleaved) {
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2) {
+                        const float p = y[j];
+                        y[j] = p * cs[j] + y[j + 1] * sn[j];
+                        y[j + 1] = y[j + 1] * cs[j + 1] + p * sn[j + 1];
+                    }
+                } else {
+                    float* row = stage[turn][g];
+                    *reinterpret_cast<float4*>(row + e0) = make_float4(y[0], y[1], y[2], y[3]);
+                    *reinterpret_cast<float4*>(row + e0 + 4) = make_float4(y[4], y[5], y[6], y[7]);
+                    __syncwarp(mates);
+                    if (alike) {
+                        const float4 lo = *reinterpret_cast<const float4*>(row + partner), hi = *reinterpret_cast<const float4*>(row + partner + 4);
+                        y[0] = y[0] * cs[0] + lo.x * sn[0], y[1] = y[1] * cs[1] + lo.y * sn[1];
+                        y[2] = y[2] * cs[2] + lo.z * sn[2], y[3] = y[3] * cs[3] + lo.w * sn[3];
+                        y[4] = y[4] * cs[4] + hi.x * sn[4], y[5] = y[5] * cs[5] + hi.y * sn[5];
+                        y[6] = y[6] * cs[6] + hi.z * sn[6], y[7] = y[7] * cs[7] + hi.w * sn[7];
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const int e = e0 + j;
+                            if (e < a.rot) y[j] = y[j] * cs[j] + row[e < half ? e + half : e - half] * sn[j];
+                        }
                     }
                 }
-                __syncwarp(mates);
             }
-        }
-        if (kind == 0) {
-            if (live)
-                *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.q_out) + b * a.os.seq + i * a.os.tok +
-                                          head * a.os.head + e0) = bf16_8(y);
-            continue;
-        }
-        if (off < 0) continue;
-        uint8_t* dst = (kind == 1 ? c.k : c.v) + off + head * c.head_stride;
-        if constexpr (E4M3) {
-            float m = 0.f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(y[j]));
-#pragma unroll
-            for (int o = GS / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(mates, m, o, GS));
-            const float scale = m > 0.f ? m / 448.f : 1.f;
-            if (live) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] /= scale;
-                *reinterpret_cast<uint2*>(dst + e0) = make_uint2(e4m3_quad(y[0], y[1], y[2], y[3]), e4m3_quad(y[4], y[5], y[6], y[7]));
-                if (at == 0)
-                    (kind == 1 ? c.k_scale : c.v_scale)[scale_at + static_cast<int64_t>(head) * c.page_size] = scale;
+            if (kind == 0) {
+                if (live) *reinterpret_cast<uint4*>(out + h * a.os.head) = bf16_8(y);
+                continue;
             }
-        } else if (live) {
-            *reinterpret_cast<uint4*>(dst + 2 * e0) = bf16_8(y);
+            if (off < 0) continue;
+            const int head = kind == 1 ? h - k_first : h - v_first;
+            uint8_t* dst = (kind == 1 ? c.k : c.v) + off + head * c.head_stride;
+            if constexpr (E4M3) {
+                float m = 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(y[j]));
+#pragma unroll
+                for (int o = GS / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(mates, m, o, GS));
+                // (a vector below 1e-28 throughout is held as if it were that large)
+                const float scale = m > 0.f ? fmaxf(m * (1.f / 448.f), 1e-30f) : 1.f, inverse = __fdividef(1.f, scale);
+                if (live) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) y[j] *= inverse;
+                    *reinterpret_cast<uint2*>(dst + e0) = make_uint2(e4m3_quad(y[0], y[1], y[2], y[3]), e4m3_quad(y[4], y[5], y[6], y[7]));
+                    if (at == 0) (kind == 1 ? c.k_scale : c.v_scale)[scale_at + static_cast<int64_t>(head) * c.page_size] = scale;
+                }
+            } else if (live) {
+                *reinterpret_cast<uint4*>(dst + 2 * e0) = bf16_8(y);
+            }
         }
     }
 }
 
+template <typename T, int GS, bool E4M3>
+cudaError_t launch_append_group(const AppendArgs& a, cudaStream_t s) {
+    // few tokens: a token's vectors over as many CTAs as take them at once (1 x 11 tokens of 48: 6.5 us with the read
+    // behind it, 7.5 us with one CTA a token)
+    const int most = kAppendBlocks * sm_count(), groups = kAppendThreads / GS, turns = (a.q_heads + 2 * a.c.heads + groups - 1) / groups;
+    const bool few = static_cast<int64_t>(a.tokens) * turns <= most;
+    return launch_pdl(cache_append_kernel<T, GS, E4M3>, dim3(a.tokens < most ? a.tokens : most, few ? turns : 1), dim3(kAppendThreads), 0,
+                      s, 0, a);
+}
 template <typename T, bool E4M3>
-cudaError_t launch_append(const AppendArgs& a, dim3 grid, cudaStream_t s) {
-    if (a.c.head_dim <= 64) return launch_pdl(cache_append_kernel<T, 8, E4M3>, grid, dim3(kAppendThreads), 0, s, 0, a);
-    if (a.c.head_dim <= 128) return launch_pdl(cache_append_kernel<T, 16, E4M3>, grid, dim3(kAppendThreads), 0, s, 0, a);
-    return launch_pdl(cache_append_kernel<T, 32, E4M3>, grid, dim3(kAppendThreads), 0, s, 0, a);
+cudaError_t launch_append(const AppendArgs& a, cudaStream_t s) {
+    if (a.c.head_dim <= 64) return launch_append_group<T, 8, E4M3>(a, s);
+    if (a.c.head_dim <= 128) return launch_append_group<T, 16, E4M3>(a, s);
+    return launch_append_group<T, 32, E4M3>(a, s);
 }
 
 // ---------------------------------------------------------------------------
@@ -372,21 +436,13 @@ PLDP_API pldp_status pldp_cache_append(const pldp_cache_append_args* p, void* st
     a.capacity = a.c.capacity;
     if (p->cos && p->rot_rows < a.capacity) a.capacity = static_cast<int>(p->rot_rows);
     a.eps = p->eps;
-    // a token's vectors over enough CTAs that two fit an SM's share of a small batch, no more
-    // than one turn of a CTA's groups each
-    const int total = p->q_heads + 2 * p->cache.heads, tokens = p->B * p->n;
-    const int groups = kAppendThreads / (p->cache.head_dim <= 64 ? 8 : p->cache.head_dim <= 128 ? 16 : 32);
-    const int most = (total + groups - 1) / groups;
-    int split = (8 * sm_count() + tokens - 1) / tokens;
-    split = split < 1 ? 1 : split > most ? most : split;
-    const int turns = (most + split - 1) / split;
-    a.per = turns * groups;
-    const dim3 grid(tokens, (total + a.per - 1) / a.per);
+    a.tokens = p->B * p->n;
+    a.inverse_dim = 1.f / p->cache.head_dim;
     auto s = static_cast<cudaStream_t>(stream);
     const bool q8 = p->cache.dtype == PLDP_E4M3;
     cudaError_t e;
-    if (p->dtype == PLDP_F32) e = q8 ? launch_append<float, true>(a, grid, s) : launch_append<float, false>(a, grid, s);
-    else e = q8 ? launch_append<__nv_bfloat16, true>(a, grid, s) : launch_append<__nv_bfloat16, false>(a, grid, s);
+    if (p->dtype == PLDP_F32) e = q8 ? launch_append<float, true>(a, s) : launch_append<float, false>(a, s);
+    else e = q8 ? launch_append<__nv_bfloat16, true>(a, s) : launch_append<__nv_bfloat16, false>(a, s);
     if (e != cudaSuccess) return fail(PLDP_ERR_CUDA, "%s: launch failed: %s", fn, cudaGetErrorString(e));
     return check_launch(fn);
 }
