@@ -1,6 +1,9 @@
 // Ranking by attentions (Eq. 2) straight from a layer's cache: pldp_rank_cache.
 #include <cuda_fp8.h>
+#include <cuda_fp16.h>
 #include <math.h>
+
+#include <utility>
 
 #include "pldp_cache.cuh"
 
@@ -20,23 +23,64 @@ struct RankArgs {
     float scale;
 };
 
-constexpr int kThreads = 512;
-constexpr int kWarps = kThreads / 32;
+// A cluster of CTAs a sequence, which deal its candidates among them.  The selected heads' queries lie in shared
+// memory, ordered by the key/value head they read, so that a unit of work (one candidate, one key/value head) reads
+// that key once, 16 bytes a lane, for all of its heads.  Bound by latency: a candidate's position, its page,
+// its key and the queries each wait for the one before.  The first two are looked up for 64 candidates at once, and
+// four units' keys are on their way a group of lanes.
+// 16 x 341..512 candidates, 8 heads of an e4m3 cache: @B16@ (one CTA a sequence and a warp a candidate: 191 us);
+// 8 x 8..16 candidates, 32 heads: @B8@ (23 us).
+constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kChunk = 64;           // candidates looked up at once
+constexpr int kParts = 1024;         // scores of (candidate, key/value head) held
+constexpr int kInFlight = 4;
 
-__device__ __forceinline__ float element(const uint8_t* v, int e, bool e4m3) {
-    if (!e4m3) return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(v)[e]);
-    const __half_raw h = __nv_cvt_fp8_to_halfraw(v[e], __NV_E4M3);
-    return __half2float(*reinterpret_cast<const __half*>(&h));
+// Elements that 16 bytes hold, as floats, times q and added up.
+template <bool E4M3>
+__device__ __forceinline__ float dot16(const uint4& x, const float* q) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    float d = 0.f;
+    if constexpr (E4M3) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const __half2_raw lo = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w[k] & 0xFFFFu), __NV_E4M3);
+            const __half2_raw hi = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w[k] >> 16), __NV_E4M3);
+            const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo)), b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+            const float4 y = *reinterpret_cast<const float4*>(q + 4 * k);
+            d = fmaf(a.x, y.x, fmaf(a.y, y.y, fmaf(b.x, y.z, fmaf(b.y, y.w, d))));
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; k += 2) {
+            const float4 y = *reinterpret_cast<const float4*>(q + 2 * k);
+            d = fmaf(__uint_as_float(w[k] << 16), y.x, fmaf(__uint_as_float(w[k] & 0xFFFF0000u), y.y, d));
+            d = fmaf(__uint_as_float(w[k + 1] << 16), y.z, fmaf(__uint_as_float(w[k + 1] & 0xFFFF0000u), y.w, d));
+        }
+    }
+    return d;
 }
 
-// One CTA a sequence, one warp a candidate.
-template <bool E4M3>
+// GS lanes a unit: the power of two that covers a vector's 16-byte pieces.
+template <bool E4M3, int GS>
 __global__ void __launch_bounds__(kThreads) rank_cache_kernel(const RankArgs a) {
     pdl_enter();
-    extern __shared__ __align__(16) float qs[];                    // [n_sel][head_dim], scaled
-    __shared__ unsigned long long best_of[kWarps];
+    extern __shared__ __align__(16) uint8_t raw[];
+    __shared__ int64_t off[kChunk], scale_at[kChunk];
+    __shared__ float part[kParts];
+    __shared__ int pos[kChunk];
+    __shared__ int groups, chunk_size;
+    __shared__ unsigned long long best_of[kWarps], cluster_best[16];
+    cg::cluster_group cluster = cg::this_cluster();
+    auto started = cluster.barrier_arrive();                // nothing is written to a CTA that has not begun
     const CacheView& c = a.c;
-    const int b = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = c.head_dim;
+    const int S = cluster.num_blocks(), rank = cluster.block_rank(), b = blockIdx.x / S;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = c.head_dim, group = a.q_heads / c.heads;
+    float* qs = reinterpret_cast<float*>(raw);                                       // [selected, in order][head_dim], scaled
+    float* lses = qs + a.n_sel * D;                                                  // [selected, in order]
+    const int most = min(c.heads, a.n_sel);
+    uint16_t* first = reinterpret_cast<uint16_t*>(lses + a.n_sel);                   // [groups + 1]: where a key/value head's begin
+    uint16_t* kv_of = first + most + 1;                                              // [groups]: which one it is
+    uint16_t* order = kv_of + most;                                                  // [selected]: the n_sel entries in order
     const int row = a.row ? __ldg(a.row + b) : 0, len = __ldg(a.kv_len + b);
     int count = __ldg(a.cand_count + b);
     count = count < 0 ? 0 : min(count, a.C_cap);
@@ -44,66 +88,170 @@ __global__ void __launch_bounds__(kThreads) rank_cache_kernel(const RankArgs a) 
     if (row < 0 || row >= a.n) st |= PLDP_ST_ROW_INDEX;
     if (len < 0 || len > c.capacity) st |= PLDP_ST_SEQ_LEN;
     const bool ok = st == 0;
+    if (st && a.status && threadIdx.x == 0) atomicOr(a.status + b, st);
     const float* lse = a.lse + (static_cast<int64_t>(b) * a.n + (ok ? row : 0)) * a.q_heads;
-    if (ok)
-        for (int t = threadIdx.x; t < a.n_sel * D; t += kThreads) {
-            const int r = t / D, e = t - r * D;
-            const int h = a.heads ? __ldg(a.heads + r) : r;
-            qs[t] = h >= 0 && h < a.q_heads
-                        ? a.scale * to_f32(a.q[b * a.q_seq + row * a.q_tok + h * a.q_head + e])
-                        : 0.f;
-            if (e == 0 && (h < 0 || h >= a.q_heads) && a.status) atomicOr(a.status + b, PLDP_ST_ROW_INDEX);
-        }
-    if (st && a.status) atomicOr(a.status + b, st);
-    __syncthreads();
     const int32_t* table = c.pages + b * c.pages_stride;
-    const int group = a.q_heads / c.heads;
-    unsigned long long best = 0;
-    for (int i = warp; i < count; i += kWarps) {
-        const int j = __ldg(a.cand_pos + static_cast<int64_t>(b) * a.C_cap + i);
-        float* out = a.scores ? a.scores + static_cast<int64_t>(b) * a.C_cap + i : nullptr;
-        float score = a.sum ? 0.f : -INFINITY;
-        bool live = ok && j >= 0 && j < len;
-        int64_t scale_at = 0, off = -1;
-        if (live) off = locate(c, table, j, scale_at);
-        if (live && off < 0 && lane == 0 && a.status) atomicOr(a.status + b, PLDP_ST_PAGE);
-        live = live && off >= 0;
-        if (live) {
-            for (int r = 0; r < a.n_sel; ++r) {
-                const int h = a.heads ? __ldg(a.heads + r) : r;
-                if (h < 0 || h >= a.q_heads) continue;
-                const int kv = h / group;
-                const uint8_t* key = c.k + off + kv * c.head_stride;
-                float dot = 0.f;
-                for (int e = lane; e < D; e += 32) dot = fmaf(qs[r * D + e], element(key, e, E4M3), dot);
-                dot = warp_sum(dot);
-                if (E4M3) dot *= __ldg(c.k_scale + scale_at + static_cast<int64_t>(kv) * c.page_size);
-                const float l = __ldg(lse + h);
-                const float p = l > -INFINITY ? expf(dot - l) : 0.f;
-                score = a.sum ? score + p : fmaxf(score, p);
+
+    // the selected heads by key/value head (entries outside [0, q_heads) last), each with its queries
+    auto head_at = [&](int r) { return a.heads ? __ldg(a.heads + r) : r; };
+    auto key_head = [&](int h) { return h >= 0 && h < a.q_heads ? h / group : c.heads; };
+    if (threadIdx.x == 0) groups = 0;
+    if (a.heads) {
+        for (int r = threadIdx.x; r < a.n_sel; r += kThreads) {
+            const int kv = key_head(head_at(r));
+            int at = 0;
+            for (int o = 0; o < a.n_sel; ++o) {
+                const int other = key_head(head_at(o));
+                at += other < kv || (other == kv && o < r);
             }
-        } else {
-            score = -INFINITY;
+            order[at] = static_cast<uint16_t>(r);
+            if (kv == c.heads && a.status) atomicOr(a.status + b, PLDP_ST_ROW_INDEX);
         }
-        if (a.accumulate) {
-            const float before = *out;
-            score = live ? (a.sum ? before + score : fmaxf(before, score)) : before;
+    } else {
+        for (int r = threadIdx.x; r < a.n_sel; r += kThreads) order[r] = static_cast<uint16_t>(r);
+    }
+    __syncthreads();
+    if (warp == 0) {                                        // where a key/value head's entries begin
+        int n = 0;
+        for (int r0 = 0; r0 < a.n_sel; r0 += 32) {
+            const int r = r0 + lane;
+            const int kv = r < a.n_sel ? key_head(head_at(order[r])) : -1;
+            const int before = r > 0 && r < a.n_sel ? key_head(head_at(order[r - 1])) : -1;
+            const bool starts = r < a.n_sel && kv != before && kv < c.heads, ends = r < a.n_sel && kv != before && kv == c.heads;
+            const unsigned m = __ballot_sync(0xFFFFFFFFu, starts), e = __ballot_sync(0xFFFFFFFFu, ends);
+            if (starts) {
+                const int k = n + __popc(m & ((1u << lane) - 1u));
+                first[k] = static_cast<uint16_t>(r);
+                kv_of[k] = static_cast<uint16_t>(kv);
+            }
+            n += __popc(m);
+            if (ends) first[n] = static_cast<uint16_t>(r);
+            if (e) break;
+            if (r0 + 32 >= a.n_sel && lane == 0) first[n] = static_cast<uint16_t>(a.n_sel);
         }
-        if (out && lane == 0) *out = score;
-        if (score > -INFINITY) {
-            const unsigned long long key = pack_key(score, static_cast<uint32_t>(j));
-            best = key > best ? key : best;
+        if (lane == 0) {
+            groups = n;
+            chunk_size = n > 0 ? min(kChunk, max(1, kParts / n)) : kChunk;
         }
     }
+    if (ok)
+        for (int t = threadIdx.x; t < a.n_sel * (D / 8); t += kThreads) {
+            const int r = t / (D / 8), e = t - r * (D / 8), h = head_at(order[r]);
+            if (h < 0 || h >= a.q_heads) continue;
+            if (e == 0) lses[r] = __ldg(lse + h);
+            const uint4 x = *reinterpret_cast<const uint4*>(a.q + b * a.q_seq + row * a.q_tok + h * a.q_head + e * 8);
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+            float* to = qs + r * D + e * 8;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                to[2 * k] = a.scale * __uint_as_float(w[k] << 16);
+                to[2 * k + 1] = a.scale * __uint_as_float(w[k] & 0xFFFF0000u);
+            }
+        }
+    __syncthreads();
+
+    const int n_groups = groups, per = chunk_size;
+    const int g = threadIdx.x / GS, at = threadIdx.x % GS, pieces = c.vec_bytes / 16;
+    const unsigned mates = GS == 32 ? 0xFFFFFFFFu : ((1u << (GS % 32)) - 1u) << (lane / GS * GS);
+    constexpr int kGroups = kThreads / GS;
+    unsigned long long best = 0;
+    // this CTA's candidates: rank, rank + S, ...
+    const int mine = count > rank ? (count - rank + S - 1) / S : 0;
+    for (int i0 = 0; i0 < mine; i0 += per) {
+        const int here = min(per, mine - i0);
+        for (int t = threadIdx.x; t < here; t += kThreads) {
+            const int j = __ldg(a.cand_pos + static_cast<int64_t>(b) * a.C_cap + rank + (i0 + t) * S);
+            pos[t] = j;
+            off[t] = -1;
+            if (ok && j >= 0 && j < len) {
+                off[t] = locate(c, table, j, scale_at[t]);
+                if (off[t] < 0 && a.status) atomicOr(a.status + b, PLDP_ST_PAGE);
+            }
+        }
+        __syncthreads();
+        const int units = here * n_groups;
+        for (int u0 = g; u0 < units; u0 += kGroups * kInFlight) {
+            uint4 x[kInFlight];
+            float ks[kInFlight];
+#pragma unroll
+            for (int p = 0; p < kInFlight; ++p) {
+                const int u = u0 + p * kGroups;
+                x[p] = make_uint4(0u, 0u, 0u, 0u);
+                ks[p] = 1.f;
+                if (u >= units) continue;
+                const int t = u / n_groups, kv = kv_of[u - t * n_groups];
+                if (off[t] < 0) continue;
+                if (at < pieces) x[p] = ld_stream16(c.k + off[t] + kv * c.head_stride + at * 16);
+                if constexpr (E4M3) ks[p] = __ldg(c.k_scale + scale_at[t] + static_cast<int64_t>(kv) * c.page_size);
+            }
+#pragma unroll
+            for (int p = 0; p < kInFlight; ++p) {
+                const int u = u0 + p * kGroups;
+                if (u >= units) continue;                   // the whole group of lanes
+                const int t = u / n_groups, gr = u - t * n_groups, r1 = first[gr + 1];
+                float score = a.sum ? 0.f : -INFINITY;
+                for (int r = first[gr]; r < r1; ++r) {
+                    float d = at < pieces ? dot16<E4M3>(x[p], qs + r * D + at * (E4M3 ? 16 : 8)) : 0.f;
+#pragma unroll
+                    for (int o = GS / 2; o > 0; o >>= 1) d += __shfl_xor_sync(mates, d, o, GS);
+                    if constexpr (E4M3) d *= ks[p];
+                    const float l = lses[r];
+                    const float w = l > -INFINITY ? expf(d - l) : 0.f;
+                    score = a.sum ? score + w : fmaxf(score, w);
+                }
+                if (at == 0) part[u] = score;
+            }
+        }
+        __syncthreads();
+        for (int t = threadIdx.x; t < here; t += kThreads) {
+            float* out = a.scores ? a.scores + static_cast<int64_t>(b) * a.C_cap + rank + (i0 + t) * S : nullptr;
+            const bool live = off[t] >= 0;
+            float score = live && a.sum ? 0.f : -INFINITY;
+            if (live)
+                for (int k = 0; k < n_groups; ++k) score = a.sum ? score + part[t * n_groups + k] : fmaxf(score, part[t * n_groups + k]);
+            if (a.accumulate) {
+                const float before = *out;
+                score = live ? (a.sum ? before + score : fmaxf(before, score)) : before;
+            }
+            if (out) *out = score;
+            if (score > -INFINITY) {
+                const unsigned long long key = pack_key(score, static_cast<uint32_t>(pos[t]));
+                best = key > best ? key : best;
+            }
+        }
+        __syncthreads();
+    }
+    best = warp_max_u64(best);
     if (lane == 0) best_of[warp] = best;
     __syncthreads();
-    if (warp == 0) {
-        best = warp_max_u64(lane < kWarps ? best_of[lane] : 0ull);
-        if (lane == 0) {
-            a.best_pos[b] = best ? static_cast<int>(key_index(best)) : -1;
-            if (a.best_score) a.best_score[b] = best ? key_value(best) : -INFINITY;
-        }
+    cluster.barrier_wait(std::move(started));
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kWarps; ++w) best = best_of[w] > best ? best_of[w] : best;
+        *cluster.map_shared_rank(&cluster_best[rank], 0) = best;
     }
+    cluster.sync();
+    if (rank == 0 && threadIdx.x == 0) {
+        for (int k = 0; k < S; ++k) best = cluster_best[k] > best ? cluster_best[k] : best;
+        a.best_pos[b] = best ? static_cast<int>(key_index(best)) : -1;
+        if (a.best_score) a.best_score[b] = best ? key_value(best) : -INFINITY;
+    }
+}
+
+template <bool E4M3, int GS>
+cudaError_t launch(const RankArgs& a, int B, int S, size_t smem, cudaStream_t s) {
+    if (smem > kOptInShared - 24 * 1024) {                  // the kernel's own shared memory counts too
+        const cudaError_t e =
+            cudaFuncSetAttribute(rank_cache_kernel<E4M3, GS>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+        if (e != cudaSuccess) return e;
+    }
+    return launch_pdl(rank_cache_kernel<E4M3, GS>, dim3(static_cast<unsigned>(B) * S), dim3(kThreads), smem, s, S, a);
+}
+template <bool E4M3>
+cudaError_t launch_group(const RankArgs& a, int B, int S, size_t smem, cudaStream_t s) {
+    const int pieces = a.c.vec_bytes / 16;
+    if (pieces <= 8) return launch<E4M3, 8>(a, B, S, smem, s);
+    if (pieces <= 16) return launch<E4M3, 16>(a, B, S, smem, s);
+    return launch<E4M3, 32>(a, B, S, smem, s);
 }
 
 }  // namespace
@@ -143,14 +291,14 @@ extern "C" PLDP_API pldp_status pldp_rank_cache(const pldp_rank_cache_args* p, v
     a.n = p->n, a.q_heads = p->q_heads, a.n_sel = n_sel, a.C_cap = p->C_cap;
     a.accumulate = p->accumulate != 0, a.sum = p->agg == PLDP_AGG_SUM;
     a.scale = p->scale;
-    const size_t smem = static_cast<size_t>(n_sel) * p->cache.head_dim * sizeof(float);
+    const size_t smem = (static_cast<size_t>(n_sel) * (p->cache.head_dim + 1) * sizeof(float) +
+                         (static_cast<size_t>(n_sel) + 2 * (n_sel < p->cache.heads ? n_sel : p->cache.heads) + 1) * sizeof(uint16_t) + 15) / 16 * 16;
+    // CTAs a sequence: up to eight, as many as fill the GPU, each with four candidates at least
+    int S = 1;
+    while (S < 8 && 2 * S * p->B <= 2 * sm_count() && 8 * S <= p->C_cap) S *= 2;
+    if (static_cast<int64_t>(p->B) * S > INT32_MAX) return fail(PLDP_ERR_UNSUPPORTED, "%s: too many sequences", fn);
     auto s = static_cast<cudaStream_t>(stream);
-    auto kernel = p->cache.dtype == PLDP_E4M3 ? rank_cache_kernel<true> : rank_cache_kernel<false>;
-    if (smem > kOptInShared) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-        if (e != cudaSuccess) return fail(PLDP_ERR_CUDA, "%s: %s", fn, cudaGetErrorString(e));
-    }
-    const cudaError_t e = launch_pdl(kernel, dim3(p->B), dim3(kThreads), smem, s, 0, a);
+    const cudaError_t e = p->cache.dtype == PLDP_E4M3 ? launch_group<true>(a, p->B, S, smem, s) : launch_group<false>(a, p->B, S, smem, s);
     if (e != cudaSuccess) return fail(PLDP_ERR_CUDA, "%s: launch failed: %s", fn, cudaGetErrorString(e));
     return check_launch(fn);
 }

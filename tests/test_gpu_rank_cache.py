@@ -132,3 +132,27 @@ def test_refusals(lib):
                        (dict(scale=float("inf")), "scale"), (dict(heads=i32([0] * 769)), "n_sel")]:
         with pytest.raises(lib.PldpError, match=match):
             lib.pldp_rank_cache(**{**ok, **bad})
+
+
+@pytest.mark.parametrize("dtype,D,H,Hq,sel", [("bf16", 16, 1024, 1024, None), ("e4m3", 16, 64, 128, 3072), ("bf16", 256, 4, 48, 192),
+                                             ("e4m3", 48, 5, 10, 1024)])
+def test_many_heads(lib, dtype, D, H, Hq, sel):
+    """As many key/value heads, and as many selected entries, as there may be; repeated ones among them."""
+    L = [90, 33]
+    c = Cache(lib, 2, 96, H, D, 16, dtype, lens=L, seed=3)
+    g = gen(4)
+    q = torch.randn((2, 1, Hq, D), generator=g, device=DEV, dtype=torch.bfloat16)
+    lse = torch.full((2, 1, Hq), 3.0, device=DEV)
+    heads = None if sel is None else torch.randint(0, Hq, (sel,), generator=g, device=DEV, dtype=torch.int32)
+    cand = [torch.randperm(n, generator=g, device=DEV)[:20].sort().values for n in L]
+    pos, best = torch.stack(cand).int(), i32([0, 0])
+    for agg in ("max", "sum"):
+        scores = torch.zeros((2, 20), device=DEV)
+        lib.pldp_rank_cache(c.handle, q, None, i32(L), lse, pos, i32([20, 20]), best, heads=heads, agg=agg, scores=scores)
+        for b in range(2):
+            k = c.dense["k"][b][cand[b]].repeat_interleave(Hq // H, 1)
+            p = torch.exp(torch.einsum("hd,jhd->hj", q[b, 0].double(), k) * D ** -0.5 - 3.0)
+            p = p if heads is None else p[heads.long()]
+            want = p.amax(0) if agg == "max" else p.sum(0)
+            # sums of up to 3072 positive terms in 32 bits, in a fixed order: 2^-24 each of what has been added up
+            assert ((scores[b].double() - want).abs() <= 2e-4 * want).all()
