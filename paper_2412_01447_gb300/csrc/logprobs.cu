@@ -12,10 +12,9 @@ namespace {
 //
 // 1. A pass reads the logits once, in units of 2 KB of a row, a warp a unit (four 16-byte loads a lane):
 //    L and U against the unit's own maximum, and the maximum of each 512 bytes.
-// 2. One warp a row joins them.  The row's top k elements lie in the k chunks of 512 bytes whose maxima
-//    are largest (ties to the lower chunk): each element elsewhere has k such maxima before it.
-//    So the warp picks those chunks, rereads them (4% of a row of 128256 bf16 for k = 20) and keeps the k
-//    best keys, one a lane, sorted.
+// 2. One CTA a row joins them.  The row's top k elements lie in the k chunks of 512 bytes whose maxima
+//    are largest (ties to the lower chunk): each element elsewhere has k such maxima before it.  So only
+//    those are read again (4% of a row of 128256 bf16 for k = 20).
 //
 // Bound by reading the logits.  1664 rows of 128256 bf16 (427 MB), k = 20, L2 flushed: @TIME@.
 constexpr int kThreads = 256, kWarps = kThreads / 32, kLoads = 4;
@@ -158,73 +157,19 @@ __device__ __forceinline__ unsigned long long warp_best(unsigned long long v) { 
     return static_cast<unsigned long long>(hi) << 32 | lo;
 }
 
-constexpr int kFinishThreads = 128;
-constexpr int kHeld = 16;      // chunk maxima a lane holds: rows of up to 512 chunks; longer ones are read again each time
-
+// The k best elements of a row by one warp, whatever the row holds: the k chunks with the largest maxima in
+// order, then their elements into a list of the best, one a lane.  (Each turn waits for the last.)
 template <typename T, bool CUT>
-__global__ void __launch_bounds__(kFinishThreads) logprob_finish_kernel(const T* __restrict__ logits, const LogprobArgs a) {
-    pdl_enter();
+__device__ __noinline__ unsigned long long best_in_turn(const T* row, const float* chunk_max, uint32_t chunks, uint32_t head, int64_t V,
+                                                        int top) {
     constexpr int VW = 16 / sizeof(T), CE = 32 * VW;              // elements of a chunk
     const int lane = threadIdx.x & 31;
-    const int64_t r = static_cast<int64_t>(blockIdx.x) * (kFinishThreads / 32) + (threadIdx.x >> 5);
-    if (r >= a.rows) return;
-    const T* row = logits + r * a.V;
-    const float4* maxima = a.maxima + r * a.units;
-    const float* chunk_max = reinterpret_cast<const float*>(maxima);
-    const float2* sums = a.sums + r * a.units;
-    int token = -1;
-    float at_token = -INFINITY;
-    if (a.tokens) {
-        token = __ldg(a.tokens + r);
-        if (token >= 0 && token < static_cast<int>(a.V)) at_token = to_f32(row[token]);
-    }
-    const uint32_t chunks = a.units * kLoads;
-    float held[kHeld];
-    float M = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
-        const uint32_t ch = lane + 32u * i;
-        held[i] = ch < chunks ? __ldcg(chunk_max + ch) : -INFINITY;
-        M = fmaxf(M, held[i]);
-    }
-    for (uint32_t ch = lane + 32u * kHeld; ch < chunks; ch += 32) M = fmaxf(M, __ldcg(chunk_max + ch));
-    M = warp_max(M);
-    float L = 0.f, U = 0.f;
-    if (M > -INFINITY)
-        for (uint32_t k = lane; k < a.units; k += 32) {
-            const float2 s = __ldcg(sums + k);
-            const float4 t = __ldcg(maxima + k);
-            const float d = fmaxf((fmaxf(fmaxf(t.x, t.y), fmaxf(t.z, t.w)) - M) * a.c, -1000.f), by = ex2(d);
-            if (s.x != 0.f) {
-                L = fmaf(s.x, by, L);
-                U = fmaf(s.y + s.x * d, by, U);
-            }
-        }
-    L = warp_sum(L);
-    U = warp_sum(U);
-    constexpr float kLn2 = 0.69314718055994531f;
-    const float log_l = log2f(L);                                 // L >= 1 unless the row is empty
-    if (lane == 0) {
-        if (a.logprob) a.logprob[r] = at_token > -INFINITY ? ((at_token - M) * a.c - log_l) * kLn2 : -INFINITY;
-        if (a.entropy) a.entropy[r] = M > -INFINITY ? (log_l - U / L) * kLn2 : 0.f;
-    }
-    if (a.top == 0) return;
-
-    // the chunks: one a turn, the largest maximum first; lane i keeps the i-th
-    unsigned long long last = ~0ull;
+    unsigned long long last = ~0ull, own = 0, list = 0;
     uint32_t mine = 0;
-    float floor_value = -INFINITY;                                // the k-th chunk's maximum, where there are k
-    const int want = min(static_cast<uint32_t>(a.top), chunks);
-    unsigned long long own = 0;
+    const int want = min(static_cast<uint32_t>(top), chunks);
     auto best_own = [&] {                                         // this lane's next chunk
         own = 0;
-#pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
-            const uint32_t ch = lane + 32u * i;
-            const unsigned long long key = pack_key(held[i], ch);
-            if (ch < chunks && key < last && key > own) own = key;
-        }
-        for (uint32_t ch = lane + 32u * kHeld; ch < chunks; ch += 32) {
+        for (uint32_t ch = lane; ch < chunks; ch += 32) {
             const unsigned long long key = pack_key(__ldcg(chunk_max + ch), ch);
             if (key < last && key > own) own = key;
         }
@@ -235,55 +180,166 @@ __global__ void __launch_bounds__(kFinishThreads) logprob_finish_kernel(const T*
         if (lane == i) mine = key_index(last);
         if (own == last) best_own();
     }
-    if (want == a.top) floor_value = key_value(last);
-
-    // their elements: lane i ends with the i-th best key
-    const uint32_t head = CUT ? head_of<T>(a, r) : 0u;
-    unsigned long long list = 0;
-    constexpr int kAhead = 4;
-    for (int i0 = 0; i0 < want; i0 += kAhead) {
-        uint4 raw[kAhead];
-        int64_t first[kAhead];
+    for (int i = 0; i < want; ++i) {
+        const int64_t first = static_cast<int64_t>(__shfl_sync(0xFFFFFFFFu, mine, i)) * CE - head + lane * VW;
+        uint4 raw = make_uint4(0u, 0u, 0u, 0u);
+        if (first < V) raw = row_vector<T, CUT>(row, first, V);
+        float e[VW];
+        unpack(raw, e);
+        unsigned taken = 0;
+        while (true) {
+            const unsigned long long kth = __shfl_sync(0xFFFFFFFFu, list, top - 1);
+            unsigned long long cand = 0;
+            int which = 0;
 #pragma unroll
-        for (int p = 0; p < kAhead; ++p) {
-            const uint32_t ch = __shfl_sync(0xFFFFFFFFu, mine, min(i0 + p, want - 1));
-            first[p] = static_cast<int64_t>(ch) * CE - head + lane * VW;
-            raw[p] = make_uint4(0u, 0u, 0u, 0u);
-            if (i0 + p < want && first[p] < static_cast<int64_t>(a.V)) raw[p] = row_vector<T, CUT>(row, first[p], a.V);
+            for (int j = 0; j < VW; ++j) {
+                const int64_t v = first + j;
+                const unsigned long long key = pack_key(e[j], static_cast<uint32_t>(v));
+                if (v >= 0 && v < V && !(taken >> j & 1u) && key > kth && key > cand) cand = key, which = j;
+            }
+            if (!__any_sync(0xFFFFFFFFu, cand != 0)) break;
+            const unsigned long long best = warp_best(cand);
+            if (cand == best) taken |= 1u << which;
+            const int place = __popc(__ballot_sync(0xFFFFFFFFu, list > best));
+            const unsigned long long above = __shfl_up_sync(0xFFFFFFFFu, list, 1);
+            if (lane > place) list = above;
+            if (lane == place) list = best;
         }
+    }
+    return list;
+}
+
+constexpr int kFinishThreads = 128, kFinishWarps = kFinishThreads / 32;
+constexpr int kChunkList = 64, kElementList = 256;    // chunks and elements that a row's alternatives are picked from
+
+// One CTA a row.  The k-th largest of the threads' own largest chunk maxima is a value that k elements reach: the
+// chunks that reach it (k, or a few more) are read again, the elements that reach it counted against one
+// another for their places.  Rows that have more of either (few distinct values) take them in turn.
+template <typename T, bool CUT>
+__global__ void __launch_bounds__(kFinishThreads) logprob_finish_kernel(const T* __restrict__ logits, const LogprobArgs a) {
+    pdl_enter();
+    constexpr int VW = 16 / sizeof(T), CE = 32 * VW;
+    __shared__ float maxima_of[kFinishThreads];
+    __shared__ float part[3][kFinishWarps];
+    __shared__ uint32_t list[kChunkList];
+    __shared__ unsigned long long elements[kElementList];
+    __shared__ int chunk_count, element_count;
+    __shared__ float floor_value;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int64_t r = blockIdx.x, V = a.V;
+    const T* row = logits + r * V;
+    const float4* maxima = a.maxima + r * a.units;
+    const float* chunk_max = reinterpret_cast<const float*>(maxima);
+    const float2* sums = a.sums + r * a.units;
+    const uint32_t chunks = a.units * kLoads;
+    float at_token = -INFINITY;
+    if (tid == 0 && a.tokens) {
+        const int token = __ldg(a.tokens + r);
+        if (token >= 0 && token < static_cast<int>(a.V)) at_token = to_f32(row[token]);
+    }
+    float own = -INFINITY;
+    for (uint32_t ch = tid; ch < chunks; ch += kFinishThreads) own = fmaxf(own, __ldcg(chunk_max + ch));
+    maxima_of[tid] = own;
+    const float top_of_warp = warp_max(own);
+    if (lane == 0) part[0][warp] = top_of_warp;
+    if (tid == 0) {
+        chunk_count = element_count = 0;
+        floor_value = -INFINITY;
+    }
+    __syncthreads();
+    const float M = fmaxf(fmaxf(part[0][0], part[0][1]), fmaxf(part[0][2], part[0][3]));
+    float L = 0.f, U = 0.f;
+    if (M > -INFINITY)
+        for (uint32_t k = tid; k < a.units; k += kFinishThreads) {
+            const float2 s = __ldcg(sums + k);
+            const float4 t = __ldcg(maxima + k);
+            const float d = fmaxf((fmaxf(fmaxf(t.x, t.y), fmaxf(t.z, t.w)) - M) * a.c, -1000.f), by = ex2(d);
+            if (s.x != 0.f) {
+                L = fmaf(s.x, by, L);
+                U = fmaf(s.y + s.x * d, by, U);
+            }
+        }
+    L = warp_sum(L);
+    U = warp_sum(U);
+    if (lane == 0) part[1][warp] = L, part[2][warp] = U;
+    // this thread's place among the maxima
+    if (a.top) {
+        int place = 0;
+#pragma unroll 8
+        for (int t = 0; t < kFinishThreads; t += 4) {
+            const float4 o = *reinterpret_cast<const float4*>(maxima_of + t);
+            place += (o.x > own || (o.x == own && t < tid)) + (o.y > own || (o.y == own && t + 1 < tid)) +
+                     (o.z > own || (o.z == own && t + 2 < tid)) + (o.w > own || (o.w == own && t + 3 < tid));
+        }
+        if (place == a.top - 1) floor_value = own;
+    }
+    __syncthreads();
+    constexpr float kLn2 = 0.69314718055994531f;
+    L = (part[1][0] + part[1][1]) + (part[1][2] + part[1][3]);
+    U = (part[2][0] + part[2][1]) + (part[2][2] + part[2][3]);
+    const float log_l = log2f(L);                                 // L >= 1 unless the row is empty
+    if (tid == 0) {
+        if (a.logprob) a.logprob[r] = at_token > -INFINITY ? ((at_token - M) * a.c - log_l) * kLn2 : -INFINITY;
+        if (a.entropy) a.entropy[r] = M > -INFINITY ? (log_l - U / L) * kLn2 : 0.f;
+    }
+    if (a.top == 0) return;
+    const float reach = floor_value;
+    for (uint32_t ch = tid; ch < chunks; ch += kFinishThreads)
+        if (__ldcg(chunk_max + ch) >= reach) {
+            const int at = atomicAdd(&chunk_count, 1);
+            if (at < kChunkList) list[at] = ch;
+        }
+    __syncthreads();
+    const uint32_t head = CUT ? head_of<T>(a, r) : 0u;
+    const int n = chunk_count;
+    if (n <= kChunkList) {
+        constexpr int kAhead = 4;
+        for (int i0 = warp; i0 < n; i0 += kFinishWarps * kAhead) {
+            uint4 raw[kAhead];
+            int64_t first[kAhead];
 #pragma unroll
-        for (int p = 0; p < kAhead; ++p) {
-            if (i0 + p >= want) break;
-            float e[VW];
-            unpack(raw[p], e);
-            unsigned taken = 0;
-            while (true) {
-                const unsigned long long kth = __shfl_sync(0xFFFFFFFFu, list, a.top - 1);
-                unsigned long long cand = 0;
-                int which = 0;
+            for (int p = 0; p < kAhead; ++p) {
+                const int i = i0 + p * kFinishWarps;
+                first[p] = V;
+                if (i < n) first[p] = static_cast<int64_t>(list[i]) * CE - head + lane * VW;
+                if (first[p] < V) raw[p] = row_vector<T, CUT>(row, first[p], V);
+            }
+#pragma unroll
+            for (int p = 0; p < kAhead; ++p) {
+                if (first[p] >= V) continue;
+                float e[VW];
+                unpack(raw[p], e);
 #pragma unroll
                 for (int j = 0; j < VW; ++j) {
                     const int64_t v = first[p] + j;
-                    const unsigned long long key = pack_key(e[j], static_cast<uint32_t>(v));
-                    if (v >= 0 && v < static_cast<int64_t>(a.V) && !(taken >> j & 1u) && e[j] >= floor_value && key > kth && key > cand)
-                        cand = key, which = j;
+                    if (e[j] >= reach && v >= 0 && v < V) {
+                        const int at = atomicAdd(&element_count, 1);
+                        if (at < kElementList) elements[at] = pack_key(e[j], static_cast<uint32_t>(v));
+                    }
                 }
-                if (!__any_sync(0xFFFFFFFFu, cand != 0)) break;
-                const unsigned long long best = warp_best(cand);
-                if (cand == best) taken |= 1u << which;
-                const int place = __popc(__ballot_sync(0xFFFFFFFFu, list > best));
-                const unsigned long long above = __shfl_up_sync(0xFFFFFFFFu, list, 1);
-                if (lane > place) list = above;
-                if (lane == place) list = best;
             }
         }
     }
-    if (lane < a.top) {
-        if (a.top_id) a.top_id[r * a.top + lane] = static_cast<int>(key_index(list));
+    __syncthreads();
+    const int m = element_count;
+    auto put = [&](int place, unsigned long long key) {
+        if (a.top_id) a.top_id[r * a.top + place] = static_cast<int>(key_index(key));
         if (a.top_logprob) {
-            const float x = key_value(list);
-            a.top_logprob[r * a.top + lane] = x > -INFINITY ? ((x - M) * a.c - log_l) * kLn2 : -INFINITY;
+            const float x = key_value(key);
+            a.top_logprob[r * a.top + place] = x > -INFINITY ? ((x - M) * a.c - log_l) * kLn2 : -INFINITY;
         }
+    };
+    if (n <= kChunkList && m <= kElementList) {
+        // (the order in which they came into the list does not matter: the keys are all different)
+        for (int i = tid; i < m; i += kFinishThreads) {
+            const unsigned long long key = elements[i];
+            int place = 0;
+            for (int t = 0; t < m; ++t) place += elements[t] > key;
+            if (place < a.top) put(place, key);
+        }
+    } else if (warp == 0) {
+        const unsigned long long key = best_in_turn<T, CUT>(row, chunk_max, chunks, head, V, a.top);
+        if (lane < a.top) put(lane, key);
     }
 }
 
@@ -301,9 +357,7 @@ cudaError_t launch(const void* logits, const LogprobArgs& a, cudaStream_t s) {
     if (blocks > most) blocks = most;
     const cudaError_t e = launch_pdl(logprob_sums_kernel<T, CUT>, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, s, 0, x, a);
     if (e != cudaSuccess) return e;
-    constexpr int per = kFinishThreads / 32;
-    return launch_pdl(logprob_finish_kernel<T, CUT>, dim3(static_cast<unsigned>((a.rows + per - 1) / per)), dim3(kFinishThreads), 0,
-                      s, 0, x, a);
+    return launch_pdl(logprob_finish_kernel<T, CUT>, dim3(static_cast<unsigned>(a.rows)), dim3(kFinishThreads), 0, s, 0, x, a);
 }
 
 }  // namespace
