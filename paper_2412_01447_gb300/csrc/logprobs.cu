@@ -30,6 +30,7 @@ struct LogprobArgs {
     float2* sums;        // [rows * units]: L, U against the largest of them
     int64_t rows;
     uint32_t V, units;   // units a row
+    uint32_t step_rows, step_units;   // of the grid's warps: their number in rows and units
     uint32_t lead;       // elements from a 16-byte boundary to the first logit
     int top;
     float c;
@@ -40,10 +41,11 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ float ordered_value(uint32_t o) {
-    return __uint_as_float((o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o);
+__device__ __forceinline__ float warp_max(float v) {
+    float m;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
+    return m;
 }
-__device__ __forceinline__ float warp_max(float v) { return ordered_value(__reduce_max_sync(0xFFFFFFFFu, ordered_key(v))); }
 __device__ __forceinline__ void unpack(const uint4& x, float (&e)[8]) {
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
@@ -88,20 +90,25 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) logprob_sums_kernel(co
     pdl_wait_only();
     constexpr int VW = 16 / sizeof(T), P = kUnitBytes / sizeof(T);
     const int lane = threadIdx.x & 31;
-    const int64_t W = static_cast<int64_t>(gridDim.x) * kWarps, total = a.rows * a.units;
-    for (int64_t u = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5); u < total; u += W) {
-        const uint32_t r = static_cast<uint32_t>(static_cast<uint64_t>(u) / a.units);      // rows and units are below 2^31
-        const uint32_t k = static_cast<uint32_t>(u - static_cast<int64_t>(r) * a.units);
+    // the grid's warps take units in turn: each turn is step_rows rows and step_units units further
+    const uint32_t start = blockIdx.x * kWarps + (threadIdx.x >> 5), V = a.V;
+    uint32_t r = start / a.units, k = start - r * a.units;
+#pragma unroll 1
+    for (; r < a.rows; r += a.step_rows, k += a.step_units) {
+        if (k >= a.units) {
+            k -= a.units;
+            if (++r >= a.rows) break;
+        }
         const uint32_t head = CUT ? head_of<T>(a, r) : 0u;
-        const T* row = logits + static_cast<int64_t>(r) * a.V;
-        const int64_t e0 = static_cast<int64_t>(k) * P - head + lane * VW;
+        const T* row = logits + static_cast<int64_t>(r) * V;
+        const int32_t e0 = static_cast<int32_t>(k * P - head + lane * VW);      // (V + a unit is below 2^31)
         uint4 raw[kLoads];
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) {
-            const int64_t at = e0 + q * 32 * VW;
+            const int32_t at = e0 + q * 32 * VW;
             raw[q] = sizeof(T) == 2 ? make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u)
                                     : make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u);
-            if (at < static_cast<int64_t>(a.V)) raw[q] = row_vector<T, CUT>(row, at, a.V);
+            if (at < static_cast<int32_t>(V)) raw[q] = row_vector<T, CUT>(row, at, V);
         }
         float top[kLoads], m = -INFINITY;
 #pragma unroll
@@ -115,18 +122,25 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) logprob_sums_kernel(co
         if (m > -INFINITY) {
             const uint64_t c2 = pack_f32x2(a.c, a.c), m2 = pack_f32x2(-m, -m);
             uint64_t l2 = 0, u2 = 0;
+            auto add = [&](bool far) {
 #pragma unroll
-            for (int q = 0; q < kLoads; ++q) {
-                float e[VW];
-                unpack(raw[q], e);
+                for (int q = 0; q < kLoads; ++q) {
+                    float e[VW];
+                    unpack(raw[q], e);
 #pragma unroll
-                for (int j = 0; j < VW; j += 2) {
-                    const uint64_t y = fma_f32x2(add_f32x2(pack_f32x2(e[j], e[j + 1]), m2), c2, 0ull);
-                    const float y0 = fmaxf(lo_f32(y), -1000.f), y1 = fmaxf(hi_f32(y), -1000.f);
-                    const uint64_t w = pack_f32x2(ex2(y0), ex2(y1));
-                    l2 = add_f32x2(l2, w);
-                    u2 = fma_f32x2(w, pack_f32x2(y0, y1), u2);
+                    for (int j = 0; j < VW; j += 2) {
+                        uint64_t y = fma_f32x2(add_f32x2(pack_f32x2(e[j], e[j + 1]), m2), c2, 0ull);
+                        if (far) y = pack_f32x2(fmaxf(lo_f32(y), -1000.f), fmaxf(hi_f32(y), -1000.f));
+                        const uint64_t w = pack_f32x2(ex2(lo_f32(y)), ex2(hi_f32(y)));
+                        l2 = add_f32x2(l2, w);
+                        u2 = fma_f32x2(w, y, u2);
+                    }
                 }
+            };
+            add(false);
+            if (!(hi_f32(u2) + lo_f32(u2) > -INFINITY)) {          // 0 * inf somewhere
+                l2 = u2 = 0;
+                add(true);
             }
             L = lo_f32(l2) + hi_f32(l2);
             U = lo_f32(u2) + hi_f32(u2);
@@ -145,6 +159,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) logprob_sums_kernel(co
         L = warp_sum(L);
         U = warp_sum(U);
         if (lane == 0) {
+            const int64_t u = static_cast<int64_t>(r) * a.units + k;
             a.maxima[u] = best;
             a.sums[u] = make_float2(L, U);
         }
@@ -219,7 +234,7 @@ template <typename T, bool CUT>
 __global__ void __launch_bounds__(kFinishThreads) logprob_finish_kernel(const T* __restrict__ logits, const LogprobArgs a) {
     pdl_enter();
     constexpr int VW = 16 / sizeof(T), CE = 32 * VW;
-    __shared__ float maxima_of[kFinishThreads];
+    __shared__ __align__(16) uint32_t maxima_of[kFinishThreads];
     __shared__ float part[3][kFinishWarps];
     __shared__ uint32_t list[kChunkList];
     __shared__ unsigned long long elements[kElementList];
@@ -239,7 +254,9 @@ __global__ void __launch_bounds__(kFinishThreads) logprob_finish_kernel(const T*
     }
     float own = -INFINITY;
     for (uint32_t ch = tid; ch < chunks; ch += kFinishThreads) own = fmaxf(own, __ldcg(chunk_max + ch));
-    maxima_of[tid] = own;
+    // (a float's order, its last seven bits given up for the thread's: all different, lower threads first)
+    const uint32_t own_key = (ordered_key(own) & ~127u) | (127u - tid);
+    maxima_of[tid] = own_key;
     const float top_of_warp = warp_max(own);
     if (lane == 0) part[0][warp] = top_of_warp;
     if (tid == 0) {
@@ -267,11 +284,14 @@ __global__ void __launch_bounds__(kFinishThreads) logprob_finish_kernel(const T*
         int place = 0;
 #pragma unroll 8
         for (int t = 0; t < kFinishThreads; t += 4) {
-            const float4 o = *reinterpret_cast<const float4*>(maxima_of + t);
-            place += (o.x > own || (o.x == own && t < tid)) + (o.y > own || (o.y == own && t + 1 < tid)) +
-                     (o.z > own || (o.z == own && t + 2 < tid)) + (o.w > own || (o.w == own && t + 3 < tid));
+            const uint4 o = *reinterpret_cast<const uint4*>(maxima_of + t);
+            place += (o.x > own_key) + (o.y > own_key) + (o.z > own_key) + (o.w > own_key);
         }
-        if (place == a.top - 1) floor_value = own;
+        if (place == a.top - 1) {
+            const uint32_t low = own_key & ~127u;          // at most this thread's maximum, as at most the others before it
+            floor_value = __uint_as_float(low & 0x80000000u ? low & 0x7FFFFFFFu : ~low);
+            if (!(own > -INFINITY)) floor_value = -INFINITY;
+        }
     }
     __syncthreads();
     constexpr float kLn2 = 0.69314718055994531f;
@@ -350,11 +370,13 @@ int64_t units_of(int64_t V, size_t es, bool cut) {
 }
 
 template <typename T, bool CUT>
-cudaError_t launch(const void* logits, const LogprobArgs& a, cudaStream_t s) {
+cudaError_t launch(const void* logits, LogprobArgs a, cudaStream_t s) {
     const T* x = static_cast<const T*>(logits);
     const int64_t total = a.rows * a.units, most = static_cast<int64_t>(kBlocksPerSm) * kWaves * sm_count();
     int64_t blocks = (total + kWarps - 1) / kWarps;
     if (blocks > most) blocks = most;
+    a.step_rows = static_cast<uint32_t>(blocks * kWarps / a.units);
+    a.step_units = static_cast<uint32_t>(blocks * kWarps % a.units);
     const cudaError_t e = launch_pdl(logprob_sums_kernel<T, CUT>, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, s, 0, x, a);
     if (e != cudaSuccess) return e;
     return launch_pdl(logprob_finish_kernel<T, CUT>, dim3(static_cast<unsigned>(a.rows)), dim3(kFinishThreads), 0, s, 0, x, a);
@@ -384,7 +406,8 @@ PLDP_API pldp_status pldp_token_logprobs(const void* logits, pldp_dtype dtype, i
         return fail(PLDP_ERR_INVALID_ARG, "%s: temperature must be positive and finite", fn);
     if (top < 0 || top > V || top > kMaxTop)
         return fail(PLDP_ERR_INVALID_ARG, "%s: top must be 0..%d and at most V", fn, kMaxTop);
-    if (rows > (int64_t(1) << 31) - 1) return fail(PLDP_ERR_UNSUPPORTED, "%s: 2^31 rows or more", fn);
+    if (rows >= int64_t(1) << 31 || V > INT32_MAX - 4096)
+        return fail(PLDP_ERR_UNSUPPORTED, "%s: 2^31 rows, or 2^31 - 4096 logits a row, or more", fn);
     if ((tokens == nullptr) != (logprob == nullptr))
         return fail(PLDP_ERR_INVALID_ARG, "%s: tokens and logprob go together", fn);
     if (rows == 0) return PLDP_OK;
