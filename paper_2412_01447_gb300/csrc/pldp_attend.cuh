@@ -326,8 +326,10 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
             }
             const int T = tiles_of(b);
             col.b = b;
-            col.unit = static_cast<int>((g0 - before) / T);
-            col.tile = static_cast<int>((g0 - before) % T);
+            const long long in = g0 - before;
+            const int unit = in >> 32 ? static_cast<int>(in / T) : static_cast<int>(static_cast<uint32_t>(in) / static_cast<uint32_t>(T));
+            col.unit = unit;
+            col.tile = static_cast<int>(in - static_cast<long long>(unit) * T);
             col.at = g0;
             col.count = g1 - g0;
         }
@@ -934,12 +936,13 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 const int c_first = owner(unit_at), c_last = owner(unit_at + w.T - 1);
                 bar_sync(4, kSoftmaxThreads);
                 if (tid == 0) {
-                    __threadfence();                                     // of all that the barrier has seen written
+                    // after all that the barrier has seen written, before what the others wrote is read
                     uint32_t* ticket = a.tickets + static_cast<int64_t>(w.b) * units + w.unit;
-                    const bool is_last = atomicAdd(ticket, 1u) == static_cast<uint32_t>(c_last - c_first);
+                    uint32_t before;
+                    asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(ticket) : "memory");
+                    const bool is_last = before == static_cast<uint32_t>(c_last - c_first);
                     if (is_last) *ticket = 0u;
                     col.last = is_last;
-                    __threadfence();
                 }
                 bar_sync(4, kSoftmaxThreads);
                 if (col.last) {
@@ -996,15 +999,21 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
                             const float* sums = place(0) + n * DP + d;               // the first round's sums stay in its place
                             if (k0 > 0) o = __ldcg(reinterpret_cast<const float4*>(sums));
-#pragma unroll 8
-                            for (int k = k0; k < k1; ++k) {
-                                const float by = factors[(k - k0) * NT + n];
-                                const float4 x = __ldcg(reinterpret_cast<const float4*>(place(k) + n * DP + d));
-                                if (by != 0.f) {
-                                    o.x = fmaf(by, x.x, o.x);
-                                    o.y = fmaf(by, x.y, o.y);
-                                    o.z = fmaf(by, x.z, o.z);
-                                    o.w = fmaf(by, x.w, o.w);
+#pragma unroll 1
+                            for (int k = k0; k < k1; k += 8) {                       // eight parts in flight
+                                float4 x[8];
+#pragma unroll
+                                for (int q = 0; q < 8; ++q)
+                                    if (k + q < k1) x[q] = __ldcg(reinterpret_cast<const float4*>(place(k + q) + n * DP + d));
+#pragma unroll
+                                for (int q = 0; q < 8; ++q) {
+                                    if (k + q >= k1) break;
+                                    const float by = factors[(k + q - k0) * NT + n];
+                                    if (by == 0.f) continue;                          // (its part may hold anything)
+                                    o.x = fmaf(by, x[q].x, o.x);
+                                    o.y = fmaf(by, x[q].y, o.y);
+                                    o.z = fmaf(by, x[q].z, o.z);
+                                    o.w = fmaf(by, x[q].w, o.w);
                                 }
                             }
                             if (k1 < parts)
