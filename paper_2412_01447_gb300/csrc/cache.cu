@@ -76,7 +76,9 @@ struct AppendArgs {
     const float *cos, *sin;
     const int32_t *seq_len, *draft_len;
     uint32_t* status;
-    int n, q_heads, rot, interleaved, capacity, tokens;
+    int n, q_heads, rot, interleaved, capacity;
+    uint32_t tokens, at_once;           // tokens in all, and a CTA's at a time
+    int share;                          // groups of lanes a token
     float eps, inverse_dim;
 };
 
@@ -120,7 +122,7 @@ struct Raw {                            // eight elements as they are in memory
 };
 
 // A vector (a query, key or value head of one token) is GS lanes', eight elements a lane; a CTA takes a token, its
-// vectors kAppendThreads / GS at a time, the next one's elements on their way while one is worked on, and then
+// vectors kAppendThreads / GS at a time (or several tokens of fewer vectors), the next one's elements on their way while one is worked on, and then
 // its next token.  Instructions are what bounds it, so what a token's vectors share (its position, its
 // page, the rotation's cosines and sines of this lane's elements) is worked out once a token.
 template <typename T, int GS, bool E4M3>
@@ -130,7 +132,8 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
     __shared__ __align__(16) float stage[2][kGroups][GS * 8];
     const CacheView& c = a.c;
     const int D = c.head_dim, g = threadIdx.x / GS, at = threadIdx.x % GS, e0 = at * 8;
-    const int first = g + blockIdx.y * kGroups, step = kGroups * gridDim.y;     // of this group's vectors
+    const int sub = g / a.share, first = g - sub * a.share + blockIdx.y * a.share, step = a.share * gridDim.y;   // this group's vectors
+    if (sub >= static_cast<int>(a.at_once)) return;
     const int k_first = a.q_heads, v_first = a.q_heads + c.heads, total = v_first + c.heads;
     const bool live = e0 < D;
     // the lanes of this vector's group: they take the same branches
@@ -140,8 +143,8 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
     const bool alike = a.interleaved || (half & 7) == 0;
     const int partner = e0 < half ? e0 + half : e0 < a.rot ? e0 - half : e0;
 #pragma unroll 1
-    for (int token = blockIdx.x; token < a.tokens; token += gridDim.x) {
-        const int b = token / a.n, i = token - b * a.n;
+    for (uint32_t token = blockIdx.x * a.at_once + sub; token < a.tokens; token += gridDim.x * a.at_once) {
+        const int b = token / static_cast<uint32_t>(a.n), i = token - b * a.n;
         const T* q = static_cast<const T*>(a.q) + (b * a.qs.seq + i * a.qs.tok + e0);
         const T* k = static_cast<const T*>(a.k) + (b * a.ks.seq + i * a.ks.tok + e0);
         const T* v = static_cast<const T*>(a.v) + (b * a.vs.seq + i * a.vs.tok + e0);
@@ -152,7 +155,7 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
         if (first < total && live) next.load(source(first));
         uint32_t st;
         const StepTokens tk = step_tokens(a.seq_len, a.draft_len, b, a.n, a.capacity, st);
-        if (i == 0 && threadIdx.x == 0 && blockIdx.y == 0 && st && a.status) atomicOr(a.status + b, st);
+        if (i == 0 && first == 0 && at == 0 && st && a.status) atomicOr(a.status + b, st);
         if (i >= tk.count) continue;
         const int pos = tk.first + i;
         // y' = y cs + partner sn; an element that does not rotate is its own partner, cs = 1, sn = 0
@@ -196,7 +199,7 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
         }
         int64_t scale_at;
         const int64_t off = locate(c, c.pages + b * c.pages_stride, pos, scale_at);
-        if (off < 0 && threadIdx.x == 0 && blockIdx.y == 0 && a.status) atomicOr(a.status + b, PLDP_ST_PAGE);
+        if (off < 0 && first == 0 && at == 0 && a.status) atomicOr(a.status + b, PLDP_ST_PAGE);
         __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.q_out) + (b * a.os.seq + i * a.os.tok + e0);
 #pragma unroll 1
         for (int h = first, turn = 0; h < total; h += step, turn ^= 1) {
@@ -286,13 +289,16 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
 }
 
 template <typename T, int GS, bool E4M3>
-cudaError_t launch_append_group(const AppendArgs& a, cudaStream_t s) {
+cudaError_t launch_append_group(AppendArgs a, cudaStream_t s) {
     // few tokens: a token's vectors over as many CTAs as take them at once (1 x 11 tokens of 48: 6.5 us with the read
     // behind it, 7.5 us with one CTA a token)
-    const int most = kAppendBlocks * sm_count(), groups = kAppendThreads / GS, turns = (a.q_heads + 2 * a.c.heads + groups - 1) / groups;
-    const bool few = static_cast<int64_t>(a.tokens) * turns <= most;
-    return launch_pdl(cache_append_kernel<T, GS, E4M3>, dim3(a.tokens < most ? a.tokens : most, few ? turns : 1), dim3(kAppendThreads), 0,
-                      s, 0, a);
+    const uint32_t most = kAppendBlocks * sm_count(), groups = kAppendThreads / GS, total = a.q_heads + 2 * a.c.heads;
+    const uint32_t turns = (total + groups - 1) / groups;
+    a.share = static_cast<int>(total < groups ? total : groups);
+    a.at_once = groups / a.share;
+    const uint32_t ctas = (a.tokens + a.at_once - 1) / a.at_once;
+    const bool few = static_cast<uint64_t>(ctas) * turns <= most;
+    return launch_pdl(cache_append_kernel<T, GS, E4M3>, dim3(ctas < most ? ctas : most, few ? turns : 1), dim3(kAppendThreads), 0, s, 0, a);
 }
 template <typename T, bool E4M3>
 cudaError_t launch_append(const AppendArgs& a, cudaStream_t s) {
