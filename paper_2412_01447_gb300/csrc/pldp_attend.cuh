@@ -477,67 +477,91 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 w.step(a);
             }
         } else if (warp == S::kMmaWarp) {
-            // ---- matrix instructions ----
-            if (lane == 0) {
-                // the operands' descriptors in two words: addresses move the low one, in units of 16 bytes
-                const uint64_t q_op = smem_operand(smem_u32(q_smem), 16, 1024, swizzle_mode(128));
-                const uint64_t p_op = smem_operand(smem_u32(p_smem), kTile * S::kRow, 8 * S::kRow, swizzle_mode(S::kRow));
-                const uint64_t k_op = smem_operand(smem_u32(ring), 16, 1024, swizzle_mode(128));
-                const uint64_t v_op = smem_operand(smem_u32(ring), kTile * 128, 1024, swizzle_mode(128));
-                const uint32_t q_lo = static_cast<uint32_t>(q_op), q_hi = q_op >> 32, p_lo = static_cast<uint32_t>(p_op), p_hi = p_op >> 32;
-                const uint32_t k_lo = static_cast<uint32_t>(k_op), k_hi = k_op >> 32, v_lo = static_cast<uint32_t>(v_op), v_hi = v_op >> 32;
-                constexpr uint32_t kScores = mma_form(128, NT, !E4M3, false, false), kValues = mma_form(128, S::kWeights, !E4M3, true, true);
-                int e = 0, tile = 0, segment = 0;       // entries, tiles and units so far
-                auto arrived = [&](int entry) { return over(&col.full[entry % S::kSlots], entry / S::kSlots); };
+            // ---- matrix instructions: one lane issues them, three ask the barriers ----
+            // the operands' descriptors in two words: addresses move the low one, in units of 16 bytes
+            const uint64_t q_op = smem_operand(smem_u32(q_smem), 16, 1024, swizzle_mode(128));
+            const uint64_t p_op = smem_operand(smem_u32(p_smem), kTile * S::kRow, 8 * S::kRow, swizzle_mode(S::kRow));
+            const uint64_t k_op = smem_operand(smem_u32(ring), 16, 1024, swizzle_mode(128));
+            const uint64_t v_op = smem_operand(smem_u32(ring), kTile * 128, 1024, swizzle_mode(128));
+            const uint32_t q_lo = static_cast<uint32_t>(q_op), q_hi = q_op >> 32, p_lo = static_cast<uint32_t>(p_op), p_hi = p_op >> 32;
+            const uint32_t k_lo = static_cast<uint32_t>(k_op), k_hi = k_op >> 32, v_lo = static_cast<uint32_t>(v_op), v_hi = v_op >> 32;
+            constexpr uint32_t kScores = mma_form(128, NT, !E4M3, false, false), kValues = mma_form(128, S::kWeights, !E4M3, true, true);
+            // Each lane's own barrier (or none): until all are over.  One wait for three costs what one does.
+            auto wait_all = [&](uint64_t* bar, uint32_t parity) {
+                bool done = bar == nullptr || over(bar, parity);
+                uint32_t polls = 0;
 #pragma unroll 1
-                while (w.next(a, &st)) {
-                    const int count = w.t1 - w.t0;
-                    bool keys = arrived(e);
-                    wait_for(&col.q_full, segment, &col.dead);
-                    tmem_after_sync();
-                    // turn i: the scores of the unit's tile i, then the second product of tile i - 1
-#pragma unroll 1
-                    for (int i = 0; i <= count; ++i, ++tile, e += 2) {
-                        const int before = tile - 1, v_slot = (e - 1) % S::kSlots;
-                        const bool values = i > 0 && arrived(e - 1);
-                        if (i < count) {
-                            const int slot = e % S::kSlots;
-                            wait_more(keys, &col.full[slot], e / S::kSlots, &col.dead);
-                            tmem_after_sync();
-                            const uint32_t op = k_lo + slot * (S::kSlot / 16), to = tmem + (tile & 1) * NT;
-#pragma unroll
-                            for (int s = 0; s < DP / 16; ++s)
-                                if (s == 0 || s * 16 < D)
-                                    mma_f16(to, op + (s >> 2) * (kTile * 8) + (s & 3) * 2, k_hi, q_lo + (s >> 2) * (NT * 8) + (s & 3) * 2, q_hi,
-                                            kScores, s > 0);
-                            mma_commit(&col.s_full[tile & 1]);
-                            mma_commit(&col.empty[slot]);
-                        }
-                        const bool weights = i > 0 && over(&col.p_full[before % S::kWeightTiles], before / S::kWeightTiles);
-                        keys = i + 1 < count && arrived(e + 2);                   // the next turn's question
-                        if (i > 0) {
-                            wait_more(values, &col.full[v_slot], (e - 1) / S::kSlots, &col.dead);
-                            wait_more(weights, &col.p_full[before % S::kWeightTiles], before / S::kWeightTiles, &col.dead);
-                            tmem_after_sync();
-                            const uint32_t op = v_lo + v_slot * (S::kSlot / 16), from = p_lo + before % S::kWeightTiles * (S::kPs / 16);
-                            const uint32_t more = i > 1;
-#pragma unroll
-                            for (int m = 0; m < S::kBlocks; ++m)
-#pragma unroll
-                                for (int s = 0; s < kTile / 16; ++s)
-                                    mma_f16(tmem + 2 * NT + m * S::kWeights, op + m * 2 * (kTile * 8) + s * 128, v_hi, from + s * S::kRow, p_hi,
-                                            kValues, s > 0 ? 1u : more);
-                            mma_commit(&col.pv_done[before & 1]);
-                            mma_commit(&col.empty[v_slot]);
-                        }
+                while (!__all_sync(0xFFFFFFFFu, done)) {
+                    if (++polls >= kMbarPolls || *static_cast<volatile int*>(&col.dead)) {
+                        *static_cast<volatile int*>(&col.dead) = 1;
+                        break;
                     }
-                    --tile;                                                       // the turn behind the last tile
-                    e -= 2;
-                    ++segment;
-                    w.step(a);
+                    if (!done) done = over(bar, parity);
                 }
+                __syncwarp();
+            };
+            const uint32_t lead = elect_lane(), base = __shfl_sync(0xFFFFFFFFu, tmem, 0);
+            // where the next tile's keys, values, weights and scores lie, and the parities of their arrivals
+            uint32_t k_slot = 0, k_parity = 0, v_slot = 1, v_parity = 0, place = 0, p_parity = 0, scores_at = 0, segment = 0;
+            auto second = [](uint32_t& slot, uint32_t& parity) {       // entries go two by two: keys and values in turn
+                slot += 2;
+                if (slot >= S::kSlots) slot -= S::kSlots, parity ^= 1u;
+            };
+#pragma unroll 1
+            while (w.next(a, &st)) {
+                const int count = __shfl_sync(0xFFFFFFFFu, w.t1 - w.t0, 0);
+                // (In a short ring the keys of tile i + 2, or the values before them, come only when the
+                // values of tile i have gone: their wait cannot come first.)
+                constexpr bool kTogether = S::kSlots >= 6;
+                // Turn i: the second product of the unit's tile i, then the scores of tile i + 2, whose place in
+                // tensor memory tile i's weights have left; turns -2 and -1 have scores only.  (In this order the
+                // scores' arrival also says that the second product two tiles before is done.)
+#pragma unroll 1
+                for (int i = -2; i < count; ++i) {
+                    const bool scores = i + 2 < count, values = i >= 0;
+                    uint64_t* bar = nullptr;
+                    uint32_t parity = 0;
+                    if (kTogether && lane == 0 && scores) bar = &col.full[k_slot], parity = k_parity;
+                    if (lane == 1 && values) bar = &col.full[v_slot], parity = v_parity;
+                    if (lane == 2 && values) bar = &col.p_full[place], parity = p_parity;
+                    if (lane == 2 && i == -2) bar = &col.q_full, parity = segment;
+                    wait_all(bar, parity);
+                    tmem_after_sync();
+                    if (values) {
+                        const uint32_t op = __shfl_sync(0xFFFFFFFFu, v_lo + v_slot * (S::kSlot / 16), 0);
+                        const uint32_t from = __shfl_sync(0xFFFFFFFFu, p_lo + place * (S::kPs / 16), 0), more = i > 0;
+#pragma unroll
+                        for (int m = 0; m < S::kBlocks; ++m)
+#pragma unroll
+                            for (int s = 0; s < kTile / 16; ++s)
+                                mma_f16(base + 2 * NT + m * S::kWeights, op + m * 2 * (kTile * 8) + s * 128, v_hi, from + s * S::kRow, p_hi,
+                                        kValues, s > 0 ? 1u : more, lead);
+                        mma_commit(&col.pv_done[scores_at], lead);
+                        mma_commit(&col.empty[v_slot], lead);
+                        second(v_slot, v_parity);
+                        if (S::kWeightTiles == 1 || (place ^= 1u) == 0) p_parity ^= 1u;
+                    }
+                    if (scores) {
+                        if (!kTogether) {
+                            wait_all(lane == 0 ? &col.full[k_slot] : nullptr, k_parity);
+                            tmem_after_sync();
+                        }
+                        const uint32_t op = __shfl_sync(0xFFFFFFFFu, k_lo + k_slot * (S::kSlot / 16), 0);
+                        const uint32_t to = __shfl_sync(0xFFFFFFFFu, tmem + scores_at * NT, 0);
+#pragma unroll
+                        for (int s = 0; s < DP / 16; ++s)
+                            if (s == 0 || s * 16 < D)
+                                mma_f16(to, op + (s >> 2) * (kTile * 8) + (s & 3) * 2, k_hi, q_lo + (s >> 2) * (NT * 8) + (s & 3) * 2, q_hi,
+                                        kScores, s > 0, lead);
+                        mma_commit(&col.s_full[scores_at], lead);
+                        mma_commit(&col.empty[k_slot], lead);
+                        second(k_slot, k_parity);
+                    }
+                    scores_at ^= 1u;                                  // (of tile i + 2, as of tile i)
+                }
+                ++segment;
+                w.step(a);
             }
-            __syncwarp();
         }
     } else if (E4M3 && warp >= 8) {
         // ---- e4m3: the codes of a tile of keys or values to f16, 16 at a time ----

@@ -26,21 +26,39 @@ __host__ __device__ constexpr uint32_t mma_form(int M, int N, bool bf16, bool a_
            static_cast<uint32_t>(N >> 3) << 17 | static_cast<uint32_t>(M >> 4) << 24;
 }
 
-// Operands by the two words of their descriptors: an address moves the low one only.
+// Operands by the two words of their descriptors: an address moves the low one only.  All lanes of a warp come
+// here with the same values, and the one that leads issues: a branch around these would make every operand one
+// lane's (81 cycles an instruction instead of 45).
 __device__ __forceinline__ void mma_f16(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t form,
-                                        uint32_t accumulate) {
+                                        uint32_t accumulate, uint32_t lead) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 a, b;\n\t"
         "mov.b64 a, {%1, %2};\n\t"
         "mov.b64 b, {%3, %4};\n\t"
         "setp.ne.u32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n\t}"
-        ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(form), "r"(accumulate)
+        "setp.ne.u32 q, %7, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n\t}"
+        ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(form), "r"(accumulate), "r"(lead)
         : "memory");
 }
-// Arrives on `bar` when this thread's matrix instructions so far are done.
-__device__ __forceinline__ void mma_commit(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+// The lane of a converged warp that leads, always the same one.
+__device__ __forceinline__ uint32_t elect_lane() {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r));
+    return r;
+}
+// Arrives on `bar` when the leading thread's matrix instructions so far are done.
+__device__ __forceinline__ void mma_commit(uint64_t* bar, uint32_t lead) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.u32 q, %1, 0;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)),
+        "r"(lead)
+        : "memory");
 }
 
 __device__ __forceinline__ void tmem_alloc(uint32_t* out, uint32_t columns) {
