@@ -106,8 +106,8 @@ struct Columns {
     int64_t q_at[NT], o_at[NT];     // element offsets, -1: no such row
     float neg_m[NT], factor[NT], sum[NT], inverse[NT];
     float part[4][NT];
-    // of the keys of four tiles: log2 of the values' scale (-inf: no key); e4m3: the keys' scale, the values' inverted
-    float key_log[4][kTile], key_scale[E4M3 ? 4 : 1][E4M3 ? kTile : 1], key_inverse[E4M3 ? 4 : 1][E4M3 ? kTile : 1];
+    // of the keys of four tiles: 0 or, where there is none, -inf; e4m3: the scales of the key and of the value
+    alignas(16) float key[4][kTile], key_scale[E4M3 ? 4 : 1][E4M3 ? kTile : 4], value_scale[E4M3 ? 4 : 1][E4M3 ? kTile : 4];
     int limit[NT];                  // last position that the row sees
     int seen[NT];                   // whether m has been set
     uint64_t full[8], empty[8], stage_full[8], stage_empty[8], s_full[2], p_full[2], pv_done[2], q_full, key_empty[4];
@@ -210,6 +210,23 @@ __device__ __forceinline__ float load_now(const float* p) {
     float v;
     asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(v) : "l"(p));
     return v;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+    float y;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// N words (one, or four on a boundary of 16 bytes) from global to shared memory, later; and until all copies but
+// those of the last N groups, this one with them, are done.
+template <int N>
+__device__ __forceinline__ void copy_words(float* to, const float* from) {
+    if constexpr (N == 4) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void copies_but() {
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
 // Sums v[0..C) over the warp's lanes, C = 8, 16 or a multiple of 16: each lane ends with the sums of the
@@ -411,69 +428,71 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
             // the last copies have arrived before this CTA ends: every slot is waited for by its reader
         } else if (warp == S::kKeyWarp) {
             // ---- the keys of each tile, four a lane: whether there is one, and e4m3's scales ----
+            // Four neighbours lie in one page where 4 divides the page size; their scales are then 16 bytes (if the
+            // tensors start on such a boundary).  This warp's own instructions bound short tiles: with a page, two
+            // addresses and two loads for every key a turn took 1900 cycles.
+            const bool four = c.page_size % 4 == 0 && (!E4M3 || ((reinterpret_cast<uintptr_t>(c.k_scale) | reinterpret_cast<uintptr_t>(c.v_scale)) & 15) == 0);
             int tile_no = 0;
 #pragma unroll 1
             while (w.next(a, &st)) {
                 const int kv = w.unit / a.row_tiles;
                 const int32_t* table = c.pages + w.b * c.pages_stride;
-                int page[4];
-                [[maybe_unused]] float ks[4], vs[4];
-                auto look = [&](int tile, int (&to)[4]) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int pos = tile * kTile + lane + 32 * i;
-                        to[i] = tile < w.t1 && pos < w.keys ? load_now(table + page_of(pos, c.div_mul, c.div_shift)) : -1;
-                    }
+                auto look = [&](int tile, int pos) {
+                    return tile < w.t1 && pos < w.keys ? load_now(table + page_of(pos, c.div_mul, c.div_shift)) : -1;
                 };
-                auto fetch = [&](int tile, const int (&from)[4], float (&k)[4], float (&v)[4]) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int pos = tile * kTile + lane + 32 * i;
-                        k[i] = v[i] = 1.f;
-                        if (static_cast<unsigned>(from[i]) < static_cast<unsigned>(c.n_pages)) {
-                            const int slot = pos - static_cast<int>(page_of(pos, c.div_mul, c.div_shift)) * c.page_size;
-                            const int64_t at = static_cast<int64_t>(from[i]) * (c.heads * c.page_size) + (kv * c.page_size + slot);
-                            k[i] = load_now(c.k_scale + at);
-                            v[i] = load_now(c.v_scale + at);
-                        }
-                    }
+                auto exists = [&](int page) { return static_cast<unsigned>(page) < static_cast<unsigned>(c.n_pages); };
+                auto scales_at = [&](int page, int pos) {
+                    const int slot = pos - static_cast<int>(page_of(pos, c.div_mul, c.div_shift)) * c.page_size;
+                    return static_cast<int64_t>(page) * (c.heads * c.page_size) + (kv * c.page_size + slot);
                 };
-                // Scales are loaded one tile ahead and pages two, into two sets of registers in turn: a copy from one to
-                // the other would wait for the loads.
-                auto turn = [&](int tile, int (&page)[4], float (&ks)[4], float (&vs)[4], int (&page2)[4], float (&ks2)[4],
-                                float (&vs2)[4]) {
-                    if constexpr (E4M3) fetch(tile + 1, page2, ks2, vs2);
+                // e4m3: a tile's scales are asked for (straight into shared memory) two turns before they are handed on,
+                // and the pages two turns before that.
+                constexpr int kLate = E4M3 ? 2 : 0;
+                auto turn = [&](int tile, int& page) {
                     const int at = tile_no & 3;
-                    if (tile_no >= 4) wait_for(&col.key_empty[at], (tile_no >> 2) - 1, &col.dead);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int key = lane + 32 * i;
-                        const bool there = static_cast<unsigned>(page[i]) < static_cast<unsigned>(c.n_pages);
-                        if constexpr (E4M3) {
-                            // (lg2.approx is 2^-22 off at most: as much as the weight's own exponential)
-                            const float v = fmaxf(vs[i], 1e-37f);
-                            col.key_log[at][key] = there ? __log2f(v) : -INFINITY;
-                            col.key_scale[at][key] = there ? ks[i] * a.scale2 : 0.f;
-                            col.key_inverse[at][key] = __frcp_rn(v);
+                    if (tile < w.t1) {
+                        if (tile_no >= 4) wait_for(&col.key_empty[at], (tile_no >> 2) - 1, &col.dead);
+                        const int pos = tile * kTile + 4 * lane;
+                        if (four) {
+                            const int there = exists(page) ? w.keys - pos : 0;
+                            if (E4M3 && there > 0) {
+                                const int64_t from = scales_at(page, pos);
+                                copy_words<4>(&col.key_scale[at][4 * lane], c.k_scale + from);
+                                copy_words<4>(&col.value_scale[at][4 * lane], c.v_scale + from);
+                            }
+                            *reinterpret_cast<float4*>(&col.key[at][4 * lane]) =
+                                make_float4(there > 0 ? 0.f : -INFINITY, there > 1 ? 0.f : -INFINITY, there > 2 ? 0.f : -INFINITY,
+                                            there > 3 ? 0.f : -INFINITY);
+                            page = look(tile + 2, pos + 2 * kTile);
                         } else {
-                            col.key_log[at][key] = there ? 0.f : -INFINITY;
+#pragma unroll 1
+                            for (int i = 0; i < 4; ++i) {
+                                const int pg = look(tile, pos + i);
+                                if (E4M3 && exists(pg)) {
+                                    const int64_t from = scales_at(pg, pos + i);
+                                    copy_words<1>(&col.key_scale[at][4 * lane + i], c.k_scale + from);
+                                    copy_words<1>(&col.value_scale[at][4 * lane + i], c.v_scale + from);
+                                }
+                                col.key[at][4 * lane + i] = exists(pg) ? 0.f : -INFINITY;
+                            }
                         }
                     }
-                    bar_arrive(5 + at, 160);             // for the one half of the columns, and for the other
-                    bar_arrive(9 + at, 160);
-                    look(tile + 2, page);
+                    if constexpr (E4M3) copies_but<kLate>();
+                    if (tile - kLate >= w.t0) {
+                        const int on = (tile_no - kLate) & 3;
+                        bar_arrive(5 + on, 160);         // for the one half of the columns, and for the other
+                        bar_arrive(9 + on, 160);
+                    }
                     ++tile_no;
                 };
-                int page_b[4];
-                [[maybe_unused]] float ks_b[4], vs_b[4];
-                look(w.t0, page);
-                look(w.t0 + 1, page_b);
-                if constexpr (E4M3) fetch(w.t0, page, ks, vs);
+                // two registers in turn: a copy from one to the other would wait for the load
+                int page = look(w.t0, w.t0 * kTile + 4 * lane), page_b = look(w.t0 + 1, (w.t0 + 1) * kTile + 4 * lane);
 #pragma unroll 1
-                for (int tile = w.t0; tile < w.t1; tile += 2) {
-                    turn(tile, page, ks, vs, page_b, ks_b, vs_b);
-                    if (tile + 1 < w.t1) turn(tile + 1, page_b, ks_b, vs_b, page, ks, vs);
+                for (int tile = w.t0; tile < w.t1 + kLate; tile += 2) {
+                    turn(tile, page);
+                    if (tile + 1 < w.t1 + kLate) turn(tile + 1, page_b);
                 }
+                tile_no -= kLate;
                 w.step(a);
             }
         } else if (warp == S::kMmaWarp) {
@@ -697,12 +716,15 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 // this thread's key: the factor of its scores, log2 of its values' scale (-inf: no key) and its inverse
                 const int at = tile_no & 3;
                 bar_sync(5 + 4 * grp + at, 160);
-                const float g = col.key_log[at][j];
-                float f = f0;
+                float g = col.key[at][j], f = f0;
                 [[maybe_unused]] float inv = 1.f;
                 if constexpr (E4M3) {
-                    f = col.key_scale[at][j] * back;
-                    inv = col.key_inverse[at][j];
+                    // (where there is no key nothing was loaded, or what lies past the end; the logarithm is 2^-22 off
+                    // at most, as much as the weight's own exponential, and the reciprocal one unit)
+                    const float v = g == 0.f ? fmaxf(col.value_scale[at][j], 1e-37f) : 1.f;
+                    f = g == 0.f ? col.key_scale[at][j] * a.scale2 * back : 0.f;
+                    g += __log2f(v);
+                    inv = reciprocal(v);
                 }
                 __syncwarp();
                 mbar_arrive_if(&col.key_empty[at], lane == 0);
