@@ -715,6 +715,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 const bool masked = tile * kTile + kTile - 1 > seen_by_all;
                 // this thread's key: the factor of its scores, log2 of its values' scale (-inf: no key) and its inverse
                 const int at = tile_no & 3;
+                const bool scored = over(&col.s_full[tile_no & 1], tile_no >> 1);       // (asked early: see above)
                 bar_sync(5 + 4 * grp + at, 160);
                 float g = col.key[at][j], f = f0;
                 [[maybe_unused]] float inv = 1.f;
@@ -760,7 +761,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                             if (pos > col.limit[c0 + ch * CH + i]) x[i] = -INFINITY;
                     }
                 };
-                wait_for(&col.s_full[tile_no & 1], tile_no >> 1, &col.dead);
+                wait_more(scored, &col.s_full[tile_no & 1], tile_no >> 1, &col.dead);
                 tmem_after_sync();
                 bool up = E4M3 && !settled;
                 if (!E4M3 && !settled) {
@@ -886,7 +887,6 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 // tile_no - 2, which was issued before the first one of tile_no.
                 if (S::kWeightTiles == 1 && tile_no > 0) values_done(tile_no - 1);
                 weights();
-                if (NCH == 1) sum(0);
                 if constexpr (!E4M3) {
                     // what the pages hold past the end is not used: zeros, in the values' tile
                     if (tile * kTile + kTile > w.keys) {
@@ -903,6 +903,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 tmem_before_sync();
                 __syncwarp();
                 mbar_arrive_if(&col.p_full[tile_no % S::kWeightTiles], lane == 0);
+                if (NCH == 1) sum(0);
             }
             // the sums over the keys
             {
