@@ -90,6 +90,12 @@ struct Shape {
     static constexpr int kMost = E4M3 ? (kRoom - 3 * kStage) / kSlot : kRoom / kSlot;
     static constexpr int kSlots = kMost > (E4M3 ? 6 : 8) ? (E4M3 ? 6 : 8) : kMost < 2 ? 2 : kMost;
     static constexpr int kStages = E4M3 ? ((kRoom - kSlots * kSlot) / kStage < 7 ? (kRoom - kSlots * kSlot) / kStage : 7) : 0;
+    // Keys and values take the slots in turn, so in an odd ring a slot is both's.  Two warps that copy on their own could
+    // then ask a slot's barrier for a phase while it is two behind, and the parity of that answers at once: of three
+    // slots, the values of tile 3 would overwrite those of tile 0.  There one warp copies both, in order (as fast: heads
+    // of 128, 25 tokens a step 235 us, and of 256, one token 248 us, 32 sequences of 8192 tokens).  The rings of codes
+    // are read in order by one group of warps and may be odd.
+    static constexpr bool kOneCopyWarp = !E4M3 && kSlots % 2 == 1;
     static constexpr int kBlocks = DP == 256 ? 2 : 1;          // of 128 rows of O^T
     static constexpr int kCols = 2 * NT + kBlocks * kWeights;
     static constexpr int kTmem = kCols <= 64 ? 64 : kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
@@ -367,14 +373,13 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
         // e4m3: 16 warps start with 128 registers a thread; the softmax takes what the others leave:
         // 256 * 176 + 128 * 88 + 128 * 64 = 64512 of 65536
         if constexpr (E4M3) fewer_registers<64>();
-        if (warp == S::kCopyWarp || warp == S::kCopyWarp + 1) {
+        if (warp == S::kCopyWarp || (!S::kOneCopyWarp && warp == S::kCopyWarp + 1)) {
             // ---- copies: one warp the tiles of keys, one those of values; a box (positions of one page) a lane ----
             constexpr int kDepth = E4M3 ? S::kStages : S::kSlots;
             uint64_t* const arrived = E4M3 ? col.stage_full : col.full;
             uint64_t* const left = E4M3 ? col.stage_empty : col.empty;
             const int boxes = kTile / a.box;                               // of a tile, 1..128
-            const int kv = warp - S::kCopyWarp;
-            const CUtensorMap* map = kv ? &v_map : &k_map;
+            int kv = warp - S::kCopyWarp;
             int e = kv;                                                    // entries of the ring: keys and values in turn
 #pragma unroll 1
             while (w.next(a, &st)) {
@@ -390,6 +395,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 auto turn = [&](int tile, int& page) {
                     // boxes that hold a position below the sequence's end
                     const int full = max(0, min(boxes, (w.keys - tile * kTile + a.box - 1) / a.box));
+                    const CUtensorMap* map = kv ? &v_map : &k_map;
                     const int at = e % kDepth;
                     if (e >= kDepth) wait_for(&left[at], e / kDepth - 1, &col.dead);
                     if (lane == 0) mbar_arrive_expect_tx(&arrived[at], full * a.box * (E4M3 ? a.pitch : S::kPanels * 128));
@@ -414,14 +420,22 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                         }
                     }
                     __syncwarp();
-                    page = look(tile + 2, lane);
-                    e += 2;
+                    if (!S::kOneCopyWarp || kv) page = look(tile + 2, lane);
+                    e += S::kOneCopyWarp ? 1 : 2;
+                };
+                auto both = [&](int tile, int& page) {
+                    turn(tile, page);
+                    if constexpr (S::kOneCopyWarp) {
+                        kv = 1;
+                        turn(tile, page);
+                        kv = 0;
+                    }
                 };
                 int page = look(w.t0, lane), page_b = look(w.t0 + 1, lane);
 #pragma unroll 1
                 for (int tile = w.t0; tile < w.t1; tile += 2) {
-                    turn(tile, page);
-                    if (tile + 1 < w.t1) turn(tile + 1, page_b);
+                    both(tile, page);
+                    if (tile + 1 < w.t1) both(tile + 1, page_b);
                 }
                 w.step(a);
             }

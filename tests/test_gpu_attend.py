@@ -67,6 +67,20 @@ def test_attend(lib, case, dtype, layout):
     _check(out, lse, attend64(c, q, L, d, D ** -0.5, H))
 
 
+# n, q heads a key/value head: 16, 32, 52, 85 and 99 query rows
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("D,n,G", [(D, n, G) for D in (64, 128, 256) for n, G in ((4, 4), (8, 4), (13, 4), (17, 5), (33, 3))
+                                   if D < 256 or n < 33])
+def test_many_tiles_a_cta(lib, D, n, G, dtype):
+    """Far more tiles of keys than the GPU has SMs: every ring comes round several times."""
+    L, H = [3300, 3171, 2900, 3500], 16
+    c = Cache(lib, 4, 3600, H, D, 64, dtype, lens=[a + n - 1 for a in L], seed=8)
+    q = _queries(4, n, H * G, D)
+    out, lse, status = _run(lib, c, q, L, None)
+    assert status == [0] * 4
+    _check(out, lse, attend64(c, q, L, [n - 1] * 4, D ** -0.5, H))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
 def test_many_short_sequences(lib, dtype):
     """More units of work than the GPU has SMs, empty sequences among them; twice on one workspace."""
