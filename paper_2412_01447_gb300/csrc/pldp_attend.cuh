@@ -235,7 +235,7 @@ __device__ __forceinline__ void copies_but() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// Sums v[0..C) over the warp's lanes, C = 8, 16 or a multiple of 16: each lane ends with the sums of the
+// Sums v[0..C) over the warp's lanes, C a multiple of 8: each lane ends with the sums of the
 // columns from the returned one on, in v[0..]; `lanes` neighbouring lanes hold the same.
 template <int C>
 struct ColumnSums {
@@ -1112,6 +1112,7 @@ cudaError_t launch_columns(const AttendArgs& a, const Maps& m, int nt, int ctas,
     if (nt == 16) return launch<16, DP, E4M3>(a, m, ctas, s);
     if (nt == 32) return launch<32, DP, E4M3>(a, m, ctas, s);
     if constexpr (DP <= 128) {
+        if (nt == 48) return launch<48, DP, E4M3>(a, m, ctas, s);
         if (nt == 64) return launch<64, DP, E4M3>(a, m, ctas, s);
         if (nt == 96) return launch<96, DP, E4M3>(a, m, ctas, s);
         return launch<128, DP, E4M3>(a, m, ctas, s);
