@@ -604,6 +604,11 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
             constexpr int kRowChunks = DP / 16, kRows = kConvertThreads / kRowChunks, kTurns = kTile / kRows;
             const int chunk = t % kRowChunks, row0 = t / kRowChunks;
             const bool in = chunk * 16 < D;
+            // where this thread's pieces of a tile lie: kRows rows apart, a multiple of 8, so all with the same swizzle
+            static_assert(kRows % 8 == 0 && kTurns % 4 == 0, "rows");
+            const int first = row0 * a.pitch + chunk * 16, step = kRows * a.pitch;
+            const int line = (chunk >> 2) * (kTile * 128) + row0 * 128;
+            const int low = line + ((((chunk & 3) * 2) ^ (row0 & 7)) << 4), high = low ^ 16;
             int e = 0;
 #pragma unroll 1
             while (w.next(a, &st)) {
@@ -613,24 +618,35 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
 #pragma unroll 1
                     for (int kv = 0; kv < 2; ++kv, ++e) {
                         const int slot = e % S::kSlots, stage = e % S::kStages;
-                        const uint8_t* from = stages + stage * S::kStage + row0 * a.pitch + chunk * 16;
-                        uint8_t* to = ring + slot * S::kSlot + (chunk >> 2) * (kTile * 128);
-                        const int piece = (chunk & 3) * 2;
+                        const uint8_t* from = stages + stage * S::kStage + first;
+                        uint8_t* const to = ring + slot * S::kSlot;
                         const bool codes = over(&col.stage_full[stage], e / S::kStages);
                         const bool room = e < S::kSlots || over(&col.empty[slot], e / S::kSlots - 1);
                         wait_more(codes, &col.stage_full[stage], e / S::kStages, &col.dead);
                         wait_more(room, &col.empty[slot], e / S::kSlots - 1, &col.dead);
                         if (in) {
+                            constexpr int kAtOnce = kTurns < 8 ? kTurns : 8;
+#pragma unroll 1
+                            for (int turn = 0; turn < kTurns; turn += kAtOnce) {
+                                uint4 x[kAtOnce];
 #pragma unroll
-                            for (int i = 0; i < kTurns; ++i) {
-                                const int row = row0 + i * kRows;
-                                uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                                if (row < rows) x = *reinterpret_cast<const uint4*>(from + i * kRows * a.pitch);
-                                uint8_t* line = to + row * 128;
-                                const uint2 h0 = four_codes(x.x), h1 = four_codes(x.y), h2 = four_codes(x.z), h3 = four_codes(x.w);
-                                *reinterpret_cast<uint4*>(line + ((piece ^ (row & 7)) << 4)) = make_uint4(h0.x, h0.y, h1.x, h1.y);
-                                *reinterpret_cast<uint4*>(line + (((piece + 1) ^ (row & 7)) << 4)) = make_uint4(h2.x, h2.y, h3.x, h3.y);
+                                for (int i = 0; i < kAtOnce; ++i, from += step) x[i] = *reinterpret_cast<const uint4*>(from);
+#pragma unroll
+                                for (int i = 0; i < kAtOnce; ++i) {
+                                    const uint2 h0 = four_codes(x[i].x), h1 = four_codes(x[i].y), h2 = four_codes(x[i].z), h3 = four_codes(x[i].w);
+                                    const int at = (turn + i) * (kRows * 128);
+                                    *reinterpret_cast<uint4*>(to + low + at) = make_uint4(h0.x, h0.y, h1.x, h1.y);
+                                    *reinterpret_cast<uint4*>(to + high + at) = make_uint4(h2.x, h2.y, h3.x, h3.y);
+                                }
                             }
+                            // past the end a stage holds anything: zeros, in the sequence's last tile
+                            if (rows < kTile)
+#pragma unroll 1
+                                for (int i = 0; i < kTurns; ++i)
+                                    if (row0 + i * kRows >= rows) {
+                                        *reinterpret_cast<uint4*>(to + low + i * (kRows * 128)) = make_uint4(0u, 0u, 0u, 0u);
+                                        *reinterpret_cast<uint4*>(to + high + i * (kRows * 128)) = make_uint4(0u, 0u, 0u, 0u);
+                                    }
                         }
                         fence_smem_async();
                         __syncwarp();
