@@ -23,14 +23,17 @@
  * and pldp_verify_sample_draft run 4 (greedy or by sampling) for the current step
  * and then 1-3 for the next step.  Offline:
  * pldp_rank_hidden_avg (App. B.2) and pldp_identify_heads / pldp_top_heads
- * (Sec. 4.2.1).
+ * (Sec. 4.2.1).  Around the target model's forward pass of a step, over a paged cache:
+ * pldp_cache_append, pldp_attend_cache, pldp_rank_cache (2 from the cache), pldp_cache_read,
+ * and pldp_token_logprobs on its logits.
  *
  * Conventions shared by every call
  *  - Every pointer argument is a DEVICE pointer owned by the caller (the
  *    attention rows A of the ranking calls may also be device-addressable
  *    page-locked host memory, read in place); the
  *    library allocates nothing and keeps no state between calls, except the
- *    caller-provided verification workspace described at pldp_verify_greedy,
+ *    caller-provided verification workspace described at pldp_verify_greedy
+ *    (and that of pldp_attend_cache, which calls leave zeroed where that matters),
  *    the caller-provided token index that the indexed drafting calls keep up
  *    to date, and the fixed scratch area of pldp_verify_greedy_noalloc.
  *  - All work is enqueued asynchronously on `stream` (a cudaStream_t; NULL is
@@ -648,7 +651,7 @@ typedef struct {
  *   queries and keys   x <- x * rsqrt(mean(x^2) + eps) * norm     (q_norm / k_norm not NULL)
  *                      (a, b) <- (a cos - b sin, b cos + a sin)   (cos not NULL)
  *   q_out <- bf16(q);  the cache's keys and values <- k, v rounded to bf16, or in a
- *   PLDP_E4M3 cache scale = max|x| / 448 (1 for a vector of zeros), code = x / scale.
+ *   PLDP_E4M3 cache scale = max(max|x| / 448, 1e-30) (1 for a vector of zeros), code = x / scale.
  *
  *  q, k, v    dtype (PLDP_F32 or PLDP_BF16): [B, n, q_heads or cache.heads, head_dim]
  *             with strides of their own (sequence, token, head; elements), 16-byte
@@ -732,8 +735,10 @@ PLDP_API pldp_status pldp_cache_read(const pldp_cache_read_args* args, void* str
  *  out        bf16 [B, n, q_heads, head_dim] with strides, as q.
  *  lse        float [B, n, q_heads], contiguous, or NULL.
  *  workspace  pldp_attend_workspace_size bytes, 256-byte aligned, zeroed once before
- *             first use (every call leaves it zeroed where that matters).
- *  status     uint32 [B] or NULL.
+ *             first use (every call leaves it zeroed where that matters; not one that
+ *             sets TIMEOUT: zero it again).
+ *  status     uint32 [B] or NULL.  TIMEOUT: a wait inside the kernel ran out; the call's
+ *             results are none.
  * Rows with nothing to attend to (tokens past draft_len, sequences skipped, positions
  * past the capacity) are written as zeros, their lse as -INFINITY.  Keys and values
  * past a sequence's last new token are never used, whatever they hold; those of its new
@@ -811,7 +816,9 @@ PLDP_API pldp_status pldp_rank_cache(const pldp_rank_cache_args* args, void* str
  * `rows` rows of logits (a step's B * (K+1), say) at temperature T: x = logits / T,
  *   lse = ln sum_v exp(x_v),  logprob = x_token - lse,  entropy = lse - sum_v p_v x_v.
  *
- *  logits     dtype [rows, V], contiguous.  -INFINITY is allowed (a masked token: p = 0).
+ *  logits     dtype [rows, V], contiguous, aligned to its elements, rows below 2^31 and
+ *             V below 2^31 - 4096.
+ *             -INFINITY is allowed (a masked token: p = 0).
  *  tokens     int32 [rows], or NULL (no logprob); outside [0, V): logprob -INFINITY.
  *  logprob, entropy   float [rows] out or NULL.
  *  top        alternatives wanted, 0..32 and <= V: top_id int32 [rows, top] and top_logprob
