@@ -20,6 +20,11 @@ with the token index of ``pldp_index_build``), ``pldp_verify_greedy_draft`` and
 step's draft).  Also ``pldp_rank_hidden_avg``
 (App. B.2) and ``pldp_identify_heads`` / ``pldp_top_heads`` (Sec. 4.2.1).
 
+Around the target model's forward pass over x_t and the draft, on a paged cache
+(class ``pldp_cache``): ``pldp_cache_append``, ``pldp_attend_cache``,
+``pldp_rank_cache`` (Eq. 2 from the cache), ``pldp_cache_read``; and
+``pldp_token_logprobs`` on its logits.
+
 The marshalling of the calls a decode step makes is native as well
 (``csrc/host_calls.cpp``), with the Python below as its wording of errors.
 
