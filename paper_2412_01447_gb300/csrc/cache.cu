@@ -118,16 +118,19 @@ struct Raw {                            // eight elements as they are in memory
 #pragma unroll
         for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) x[i] = *(reinterpret_cast<const uint4*>(p) + i);
     }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) x[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
     __device__ __forceinline__ void unpack(float (&y)[8]) const { load8(reinterpret_cast<const T*>(x), y); }
 };
 
-// A vector (a query, key or value head of one token) is GS lanes', eight elements a lane; a CTA takes a token, its
-// vectors kAppendThreads / GS at a time (or several tokens of fewer vectors), the next one's elements on their way
-// while one is worked on, and then its next token.  Instructions are what bounds it (some 240 a vector and warp), so
-// what a token's vectors share (its position, its page, the rotation's cosines and sines of this lane's elements) is
-// worked out once a token.
-// 4 x 4095 tokens of 48 heads of 128, bf16 to e4m3, with the read of the last positions behind it: 137 us (428 MB,
-// 3.1 TB/s); 1 x 11 tokens, fp32 to bf16: 7 us, two launches' latency.
+// A vector (a query, key or value head of one token) is GS lanes', eight elements a lane.  Of many tokens a quarter of a
+// CTA takes one, its vectors in turn, the next one's elements on their way while one is worked on, and then its next
+// token.  Instructions are what bounds it, so what a token's vectors share (its position, its page, the rotation's
+// cosines and sines of this lane's elements) is worked out once a token.
+// 4 x 4095 tokens of 48 heads of 128, bf16 to e4m3, with the read of the last positions behind it: 110 us (428 MB,
+// 3.9 TB/s); 1 x 11 tokens, fp32 to bf16: 7 us, two launches' latency.
 template <typename T, int GS, bool E4M3>
 __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_kernel(const AppendArgs a) {
     pdl_enter();
@@ -203,73 +206,97 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
         int64_t scale_at;
         const int64_t off = locate(c, c.pages + b * c.pages_stride, pos, scale_at);
         if (off < 0 && first == 0 && at == 0 && a.status) atomicOr(a.status + b, PLDP_ST_PAGE);
-        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.q_out) + (b * a.os.seq + i * a.os.tok + e0);
-#pragma unroll 1
-        for (int h = first, turn = 0; h < total; h += step, turn ^= 1) {
-            float y[8];
+        auto unpack = [&](float (&y)[8]) {
             if (live) {
                 next.unpack(y);
-                if (h + step < total) next.load(source(h + step));
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) y[j] = 0.f;
             }
-            const int kind = h < k_first ? 0 : h < v_first ? 1 : 2;
-            const T* norm = static_cast<const T*>(kind == 0 ? a.q_norm : kind == 1 ? a.k_norm : nullptr);
-            if (norm) {
-                float w[8], sum = 0.f;
+        };
+        auto normed = [&](float (&y)[8], const Raw<T>& norm) {
+            float w[8], sum = 0.f;
+            norm.unpack(w);
+            uint64_t two = 0;                              // (two elements an instruction)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] = 0.f;
-                if (live) load8(norm + e0, w);
-                uint64_t two = 0;                          // (two elements an instruction)
+            for (int j = 0; j < 8; j += 2) two = fma_f32x2(pack_f32x2(y[j], y[j + 1]), pack_f32x2(y[j], y[j + 1]), two);
+            sum = lo_f32(two) + hi_f32(two);
 #pragma unroll
-                for (int j = 0; j < 8; j += 2) two = fma_f32x2(pack_f32x2(y[j], y[j + 1]), pack_f32x2(y[j], y[j + 1]), two);
-                sum = lo_f32(two) + hi_f32(two);
+            for (int o = GS / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(mates, sum, o, GS);
+            const float r = rsqrtf(fmaf(sum, a.inverse_dim, a.eps));
+            const uint64_t r2 = pack_f32x2(r, r);
 #pragma unroll
-                for (int o = GS / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(mates, sum, o, GS);
-                const float r = rsqrtf(fmaf(sum, a.inverse_dim, a.eps));
-                const uint64_t r2 = pack_f32x2(r, r);
+            for (int j = 0; j < 8; j += 2) {
+                const uint64_t z = fma_f32x2(fma_f32x2(pack_f32x2(y[j], y[j + 1]), r2, 0ull), pack_f32x2(w[j], w[j + 1]), 0ull);
+                y[j] = lo_f32(z), y[j + 1] = hi_f32(z);
+            }
+        };
+        auto rotated = [&](float (&y)[8], int turn) {
+            if (a.interleaved) {
 #pragma unroll
                 for (int j = 0; j < 8; j += 2) {
-                    const uint64_t z = fma_f32x2(fma_f32x2(pack_f32x2(y[j], y[j + 1]), r2, 0ull), pack_f32x2(w[j], w[j + 1]), 0ull);
-                    y[j] = lo_f32(z), y[j + 1] = hi_f32(z);
+                    const float p = y[j];
+                    y[j] = p * cs[j] + y[j + 1] * sn[j];
+                    y[j + 1] = y[j + 1] * cs[j + 1] + p * sn[j + 1];
                 }
-            }
-            if (a.rot && kind < 2) {
-                if (a.interleaved) {
-#pragma unroll
-                    for (int j = 0; j < 8; j += 2) {
-                        const float p = y[j];
-                        y[j] = p * cs[j] + y[j + 1] * sn[j];
-                        y[j + 1] = y[j + 1] * cs[j + 1] + p * sn[j + 1];
-                    }
+            } else {
+                float* row = stage[turn][g];
+                *reinterpret_cast<float4*>(row + e0) = make_float4(y[0], y[1], y[2], y[3]);
+                *reinterpret_cast<float4*>(row + e0 + 4) = make_float4(y[4], y[5], y[6], y[7]);
+                __syncwarp(mates);
+                if (alike) {
+                    const float4 lo = *reinterpret_cast<const float4*>(row + partner), hi = *reinterpret_cast<const float4*>(row + partner + 4);
+                    y[0] = y[0] * cs[0] + lo.x * sn[0], y[1] = y[1] * cs[1] + lo.y * sn[1];
+                    y[2] = y[2] * cs[2] + lo.z * sn[2], y[3] = y[3] * cs[3] + lo.w * sn[3];
+                    y[4] = y[4] * cs[4] + hi.x * sn[4], y[5] = y[5] * cs[5] + hi.y * sn[5];
+                    y[6] = y[6] * cs[6] + hi.z * sn[6], y[7] = y[7] * cs[7] + hi.w * sn[7];
                 } else {
-                    float* row = stage[turn][g];
-                    *reinterpret_cast<float4*>(row + e0) = make_float4(y[0], y[1], y[2], y[3]);
-                    *reinterpret_cast<float4*>(row + e0 + 4) = make_float4(y[4], y[5], y[6], y[7]);
-                    __syncwarp(mates);
-                    if (alike) {
-                        const float4 lo = *reinterpret_cast<const float4*>(row + partner), hi = *reinterpret_cast<const float4*>(row + partner + 4);
-                        y[0] = y[0] * cs[0] + lo.x * sn[0], y[1] = y[1] * cs[1] + lo.y * sn[1];
-                        y[2] = y[2] * cs[2] + lo.z * sn[2], y[3] = y[3] * cs[3] + lo.w * sn[3];
-                        y[4] = y[4] * cs[4] + hi.x * sn[4], y[5] = y[5] * cs[5] + hi.y * sn[5];
-                        y[6] = y[6] * cs[6] + hi.z * sn[6], y[7] = y[7] * cs[7] + hi.w * sn[7];
-                    } else {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const int e = e0 + j;
-                            if (e < a.rot) y[j] = y[j] * cs[j] + row[e < half ? e + half : e - half] * sn[j];
-                        }
+                    for (int j = 0; j < 8; ++j) {
+                        const int e = e0 + j;
+                        if (e < a.rot) y[j] = y[j] * cs[j] + row[e < half ? e + half : e - half] * sn[j];
                     }
                 }
             }
-            if (kind == 0) {
-                if (live) *reinterpret_cast<uint4*>(out + h * a.os.head) = bf16_8(y);
-                continue;
+        };
+        // the queries, most of the vectors: nothing in their loop depends on which one it is
+        int h = first, turn = 0;
+        {
+            Raw<T> norm;
+            norm.clear();
+            if (a.q_norm && live) norm.load(static_cast<const T*>(a.q_norm) + e0);
+            const T* from = q + h * a.qs.head;
+            const int64_t from_step = step * a.qs.head, to_step = step * a.os.head;
+            __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.q_out) + (b * a.os.seq + i * a.os.tok + h * a.os.head + e0);
+#pragma unroll 1
+            for (; h < k_first; h += step, turn ^= 1, to += to_step) {
+                float y[8];
+                unpack(y);
+                from += from_step;
+                if (live && h + step < total) next.load(h + step < k_first ? from : source(h + step));
+                if (a.q_norm) normed(y, norm);
+                if (a.rot) rotated(y, turn);
+                if (live) *reinterpret_cast<uint4*>(to) = bf16_8(y);
+            }
+        }
+#pragma unroll 1
+        for (; h < total; h += step, turn ^= 1) {
+            float y[8];
+            unpack(y);
+            if (live && h + step < total) next.load(source(h + step));
+            const bool key = h < v_first;
+            if (key) {
+                if (a.k_norm) {
+                    Raw<T> norm;
+                    norm.clear();
+                    if (live) norm.load(static_cast<const T*>(a.k_norm) + e0);
+                    normed(y, norm);
+                }
+                if (a.rot) rotated(y, turn);
             }
             if (off < 0) continue;
-            const int head = kind == 1 ? h - k_first : h - v_first;
-            uint8_t* dst = (kind == 1 ? c.k : c.v) + off + head * c.head_stride;
+            const int head = key ? h - k_first : h - v_first;
+            uint8_t* dst = (key ? c.k : c.v) + off + head * c.head_stride;
             if constexpr (E4M3) {
                 float m = 0.f;
 #pragma unroll
@@ -282,7 +309,7 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
 #pragma unroll
                     for (int j = 0; j < 8; ++j) y[j] *= inverse;
                     *reinterpret_cast<uint2*>(dst + e0) = make_uint2(e4m3_quad(y[0], y[1], y[2], y[3]), e4m3_quad(y[4], y[5], y[6], y[7]));
-                    if (at == 0) (kind == 1 ? c.k_scale : c.v_scale)[scale_at + static_cast<int64_t>(head) * c.page_size] = scale;
+                    if (at == 0) (key ? c.k_scale : c.v_scale)[scale_at + static_cast<int64_t>(head) * c.page_size] = scale;
                 }
             } else if (live) {
                 *reinterpret_cast<uint4*>(dst + 2 * e0) = bf16_8(y);
@@ -295,12 +322,21 @@ template <typename T, int GS, bool E4M3>
 cudaError_t launch_append_group(AppendArgs a, cudaStream_t s) {
     // few tokens: a token's vectors over as many CTAs as take them at once (1 x 11 tokens of 48: 6.5 us with the read
     // behind it, 7.5 us with one CTA a token)
-    const uint32_t most = kAppendBlocks * sm_count(), groups = kAppendThreads / GS, total = a.q_heads + 2 * a.c.heads;
+    constexpr uint32_t groups = kAppendThreads / GS;
+    const uint32_t most = kAppendBlocks * sm_count(), total = a.q_heads + 2 * a.c.heads;
     const uint32_t turns = (total + groups - 1) / groups;
     a.share = static_cast<int>(total < groups ? total : groups);
     a.at_once = groups / a.share;
-    const uint32_t ctas = (a.tokens + a.at_once - 1) / a.at_once;
+    uint32_t ctas = (a.tokens + a.at_once - 1) / a.at_once;
     const bool few = static_cast<uint64_t>(ctas) * turns <= most;
+    // otherwise a quarter of a CTA a token, which then works out a token's common part less often: 4 x 4095 tokens of 48
+    // vectors 133 -> 110 us (a half or an eighth 110, 112), of shorter ones (64 elements) 104 -> 67, 64 x 17 21 -> 18
+    constexpr uint32_t kMany = groups / 4;
+    if (!few && total > kMany) {
+        a.share = kMany;
+        a.at_once = groups / a.share;
+        ctas = (a.tokens + a.at_once - 1) / a.at_once;
+    }
     return launch_pdl(cache_append_kernel<T, GS, E4M3>, dim3(ctas < most ? ctas : most, few ? turns : 1), dim3(kAppendThreads), 0, s, 0, a);
 }
 template <typename T, bool E4M3>

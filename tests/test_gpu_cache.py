@@ -81,6 +81,23 @@ def test_append(lib, case):
         assert same.all()
 
 
+# more tokens than the GPU takes at once
+MANY = [
+    (3, 701, 5, 3, 128, 16, "bf16", "e4m3", "head", 64, True, True),
+    (3, 701, 5, 3, 80, 24, "f32", "bf16", "token", 80, False, True),
+    (5, 600, 9, 3, 64, 64, "bf16", "e4m3", "token", 64, False, True),
+    (5, 600, 2, 1, 64, 64, "f32", "e4m3", "token", 64, False, False),
+    (3, 450, 3, 1, 256, 7, "bf16", "bf16", "head", 34, True, True),
+    (40, 17, 33, 11, 112, 128, "f32", "e4m3", "head", 112, False, True),
+    (900, 3, 7, 1, 16, 1, "bf16", "e4m3", "token", 16, True, False),
+]
+
+
+@pytest.mark.parametrize("case", MANY)
+def test_append_many_tokens(lib, case):
+    test_append(lib, case)
+
+
 def test_append_in_place_and_default_drafts(lib):
     """q_out may be q; without draft_len every sequence has n tokens."""
     c = Cache(lib, 2, 32, 2, 64, 16, lens=[9, 20], fill=False)
