@@ -17,7 +17,8 @@ namespace {
 //    those are read again (4% of a row of 128256 bf16 for k = 20).
 //
 // Bound by reading the logits, then by the second pass's chain of a row (its units' sums, k chunks, their elements).
-// 1664 rows of 128256 bf16 (427 MB), k = 20, L2 flushed: 89 us, 4.8 TB/s; 11 rows of 32000 fp32, k = 5: 6.1 us.
+// 1664 rows of 128256 bf16 (427 MB), k = 20, L2 flushed: 86 us, 5.0 TB/s (the pass 72); 11 rows of
+// 32000 fp32, k = 5: 5.5 us.
 constexpr int kThreads = 256, kWarps = kThreads / 32, kLoads = 4;
 constexpr int kBlocksPerSm = 5, kWaves = 11;
 constexpr int kMaxTop = 32;
@@ -226,13 +227,15 @@ __device__ __noinline__ unsigned long long best_in_turn(const T* row, const floa
 }
 
 constexpr int kFinishThreads = 128, kFinishWarps = kFinishThreads / 32;
+constexpr int kFinishBlocks = 12;          // 12 x 152 rows at once: 1664 in one go (86.3 us; 89.2 with 9, in two)
+static_assert(kMaxTop * kLoads <= kFinishThreads, "a chunk a thread");
 constexpr int kChunkList = 64, kElementList = 256;    // chunks and elements that a row's alternatives are picked from
 
 // One CTA a row.  The k-th largest of the threads' own largest chunk maxima is a value that k elements reach: the
 // chunks that reach it (k, or a few more) are read again, the elements that reach it counted against one
 // another for their places.  Rows that have more of either (few distinct values) take them in turn.
 template <typename T, bool CUT>
-__global__ void __launch_bounds__(kFinishThreads) logprob_finish_kernel(const T* __restrict__ logits, const LogprobArgs a) {
+__global__ void __launch_bounds__(kFinishThreads, kFinishBlocks) logprob_finish_kernel(const T* __restrict__ logits, const LogprobArgs a) {
     pdl_enter();
     constexpr int VW = 16 / sizeof(T), CE = 32 * VW;
     __shared__ __align__(16) uint32_t maxima_of[kFinishThreads];
@@ -253,8 +256,15 @@ __global__ void __launch_bounds__(kFinishThreads) logprob_finish_kernel(const T*
         const int token = __ldg(a.tokens + r);
         if (token >= 0 && token < static_cast<int>(a.V)) at_token = to_f32(row[token]);
     }
-    float own = -INFINITY;
-    for (uint32_t ch = tid; ch < chunks; ch += kFinishThreads) own = fmaxf(own, __ldcg(chunk_max + ch));
+    // a thread's first unit stays in registers: rows of up to 128 units are read once
+    auto top_of = [](const float4& t) { return fmaxf(fmaxf(t.x, t.y), fmaxf(t.z, t.w)); };
+    float4 mine = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    float2 mine_sums = make_float2(0.f, 0.f);
+    if (tid < a.units) mine = __ldcg(maxima + tid), mine_sums = __ldcg(sums + tid);
+    float own = top_of(mine);
+    // (of few units a chunk each: `top` threads have to have one)
+    if (a.units <= kMaxTop) own = tid < chunks ? __ldcg(chunk_max + tid) : -INFINITY;
+    for (uint32_t k = tid + kFinishThreads; k < a.units; k += kFinishThreads) own = fmaxf(own, top_of(__ldcg(maxima + k)));
     // (a float's order, its last seven bits given up for the thread's: all different, lower threads first)
     const uint32_t own_key = (ordered_key(own) & ~127u) | (127u - tid);
     maxima_of[tid] = own_key;
@@ -267,16 +277,17 @@ __global__ void __launch_bounds__(kFinishThreads) logprob_finish_kernel(const T*
     __syncthreads();
     const float M = fmaxf(fmaxf(part[0][0], part[0][1]), fmaxf(part[0][2], part[0][3]));
     float L = 0.f, U = 0.f;
-    if (M > -INFINITY)
-        for (uint32_t k = tid; k < a.units; k += kFinishThreads) {
-            const float2 s = __ldcg(sums + k);
-            const float4 t = __ldcg(maxima + k);
-            const float d = fmaxf((fmaxf(fmaxf(t.x, t.y), fmaxf(t.z, t.w)) - M) * a.c, -1000.f), by = ex2(d);
+    if (M > -INFINITY) {
+        auto add = [&](const float4& t, const float2& s) {
+            const float d = fmaxf((top_of(t) - M) * a.c, -1000.f), by = ex2(d);
             if (s.x != 0.f) {
                 L = fmaf(s.x, by, L);
                 U = fmaf(s.y + s.x * d, by, U);
             }
-        }
+        };
+        add(mine, mine_sums);
+        for (uint32_t k = tid + kFinishThreads; k < a.units; k += kFinishThreads) add(__ldcg(maxima + k), __ldcg(sums + k));
+    }
     L = warp_sum(L);
     U = warp_sum(U);
     if (lane == 0) part[1][warp] = L, part[2][warp] = U;
@@ -305,11 +316,19 @@ __global__ void __launch_bounds__(kFinishThreads) logprob_finish_kernel(const T*
     }
     if (a.top == 0) return;
     const float reach = floor_value;
-    for (uint32_t ch = tid; ch < chunks; ch += kFinishThreads)
-        if (__ldcg(chunk_max + ch) >= reach) {
+    auto pick = [&](float top, uint32_t ch) {
+        if (top >= reach) {
             const int at = atomicAdd(&chunk_count, 1);
             if (at < kChunkList) list[at] = ch;
         }
+    };
+    for (uint32_t k = tid; k < a.units; k += kFinishThreads) {
+        const float4 t = k == tid ? mine : __ldcg(maxima + k);
+        pick(t.x, 4 * k);
+        pick(t.y, 4 * k + 1);
+        pick(t.z, 4 * k + 2);
+        pick(t.w, 4 * k + 3);
+    }
     __syncthreads();
     const uint32_t head = CUT ? head_of<T>(a, r) : 0u;
     const int n = chunk_count;
