@@ -75,7 +75,7 @@ namespace {
 // Bound by memory where a tile is large: 2 x 131072 keys of 8 heads of 128, bf16, one token: 141..145 us (0.95..0.98
 // of the measured copy rate); 64 x 16384, 17 tokens, 5 query heads a head: 502..517 us (0.93..0.95).  Short
 // tiles are bound by the warps' own work, 0.95 us a tile of 128 keys of 64 elements in e4m3 with up to 16
-// columns (the conversion), 1.3 us with 48 (the softmax): 32 x 8192 keys, 8 heads, 11 tokens: 106 us (2.1 TB/s).
+// columns (the conversion), 1.3 us with 48 (the softmax): 32 x 8192 keys, 8 heads, 11 tokens: 106..109 us (2.0 TB/s).
 // ---------------------------------------------------------------------------
 constexpr int kSoftmaxThreads = 256, kConvertThreads = 128;
 constexpr int kMaxShared = 232448;        // bytes a CTA, static and dynamic
