@@ -129,8 +129,8 @@ struct Raw {                            // eight elements as they are in memory
 // CTA takes one, its vectors in turn, the next one's elements on their way while one is worked on, and then its next
 // token.  Instructions are what bounds it, so what a token's vectors share (its position, its page, the rotation's
 // cosines and sines of this lane's elements) is worked out once a token.
-// 4 x 4095 tokens of 48 heads of 128, bf16 to e4m3, with the read of the last positions behind it: 110 us (428 MB,
-// 3.9 TB/s); 1 x 11 tokens, fp32 to bf16: 7 us, two launches' latency.
+// 4 x 4095 tokens of 48 heads of 128, bf16 to e4m3, with the read of the last positions behind it: 99 us (428 MB,
+// 4.3 TB/s); 1 x 11 tokens, fp32 to bf16: 5.3 us, two launches' latency.
 template <typename T, int GS, bool E4M3>
 __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_kernel(const AppendArgs a) {
     pdl_enter();
@@ -320,8 +320,8 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
 
 template <typename T, int GS, bool E4M3>
 cudaError_t launch_append_group(AppendArgs a, cudaStream_t s) {
-    // few tokens: a token's vectors over as many CTAs as take them at once (1 x 11 tokens of 48: 6.5 us with the read
-    // behind it, 7.5 us with one CTA a token)
+    // few tokens: a token's vectors over as many CTAs as take them at once (1 x 11 tokens of 48: 1 us less than with
+    // one CTA a token)
     constexpr uint32_t groups = kAppendThreads / GS;
     const uint32_t most = kAppendBlocks * sm_count(), total = a.q_heads + 2 * a.c.heads;
     const uint32_t turns = (total + groups - 1) / groups;
@@ -330,7 +330,7 @@ cudaError_t launch_append_group(AppendArgs a, cudaStream_t s) {
     uint32_t ctas = (a.tokens + a.at_once - 1) / a.at_once;
     const bool few = static_cast<uint64_t>(ctas) * turns <= most;
     // otherwise a quarter of a CTA a token, which then works out a token's common part less often: 4 x 4095 tokens of 48
-    // vectors 133 -> 110 us (a half or an eighth 110, 112), of shorter ones (64 elements) 104 -> 67, 64 x 17 21 -> 18
+    // vectors 23 us less (a half 23, an eighth 21), of shorter ones (64 elements) 37, 64 x 17 tokens 3
     constexpr uint32_t kMany = groups / 4;
     if (!few && total > kMany) {
         a.share = kMany;
@@ -360,18 +360,46 @@ struct ReadArgs {
 
 constexpr int kReadThreads = 256;
 
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) { *reinterpret_cast<uint4*>(p) = bf16_8(x); }
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
-    *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
-}
 __device__ __forceinline__ float2 e4m3_two(uint32_t codes) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(codes), __NV_E4M3);
     return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
-// One thread takes 16 bytes of one vector of keys and the same of values.  Bound by memory: 8 x 4096 positions of
-// 8 heads of 128, e4m3 to bf16, 159 MB in 33.5 us (4.7 TB/s).
+// The elements (8 of bf16, 4 of fp32) that 16 bytes of output hold, from the cache's.
+template <bool E4M3>
+struct Piece;
+template <>
+struct Piece<false> {
+    uint4 x = make_uint4(0u, 0u, 0u, 0u);
+    __device__ __forceinline__ void load(const uint8_t* p, const __nv_bfloat16*) { x = ld_stream16(p); }
+    __device__ __forceinline__ void load(const uint8_t* p, const float*) {
+        const uint2 y = __ldcs(reinterpret_cast<const uint2*>(p));
+        x.x = y.x, x.y = y.y;
+    }
+    __device__ __forceinline__ void store(__nv_bfloat16* p, float) const { *reinterpret_cast<uint4*>(p) = x; }
+    __device__ __forceinline__ void store(float* p, float) const {
+        *reinterpret_cast<uint4*>(p) = make_uint4(x.x << 16, x.x & 0xFFFF0000u, x.y << 16, x.y & 0xFFFF0000u);
+    }
+};
+template <>
+struct Piece<true> {
+    uint2 x = make_uint2(0u, 0u);
+    __device__ __forceinline__ void load(const uint8_t* p, const __nv_bfloat16*) { x = __ldcs(reinterpret_cast<const uint2*>(p)); }
+    __device__ __forceinline__ void load(const uint8_t* p, const float*) { x.x = __ldcs(reinterpret_cast<const unsigned int*>(p)); }
+    __device__ __forceinline__ void store(__nv_bfloat16* p, float scale) const {
+        const float2 a = e4m3_two(x.x & 0xFFFFu), b = e4m3_two(x.x >> 16), c = e4m3_two(x.y & 0xFFFFu), d = e4m3_two(x.y >> 16);
+        *reinterpret_cast<uint4*>(p) = make_uint4(bf16_pair(a.x * scale, a.y * scale), bf16_pair(b.x * scale, b.y * scale),
+                                                  bf16_pair(c.x * scale, c.y * scale), bf16_pair(d.x * scale, d.y * scale));
+    }
+    __device__ __forceinline__ void store(float* p, float scale) const {
+        const float2 a = e4m3_two(x.x & 0xFFFFu), b = e4m3_two(x.x >> 16);
+        *reinterpret_cast<float4*>(p) = make_float4(a.x * scale, a.y * scale, b.x * scale, b.y * scale);
+    }
+};
+
+// One thread takes 16 bytes of output of one vector of keys and the same of values, so that neighbours write side by
+// side, and steps from piece to piece without divisions.  Bound by memory: 8 x 4096 positions of 8 heads of 128, e4m3
+// to bf16, 159 MB in 28.6 us (5.6 TB/s); 33.5 with 16 bytes of codes a thread and two divisions a piece.
 template <typename O, bool E4M3>
 __global__ void __launch_bounds__(kReadThreads) cache_read_kernel(const ReadArgs a) {
     pdl_enter();
@@ -392,45 +420,36 @@ __global__ void __launch_bounds__(kReadThreads) cache_read_kernel(const ReadArgs
     }
     if (blockIdx.x == 0 && threadIdx.x == 0 && st && a.status) atomicOr(a.status + b, st);
     const int lo = blockIdx.x * a.per, hi = min(lo + a.per, count);
-    const uint32_t chunks = c.vec_bytes / 16, row = chunks * c.heads;
-    const uint32_t items = hi > lo ? static_cast<uint32_t>(hi - lo) * row : 0u;
+    constexpr int kElements = 16 / sizeof(O), kBytes = kElements * (E4M3 ? 1 : 2);
+    const uint32_t rows = hi > lo ? hi - lo : 0, heads = c.heads, chunks = static_cast<uint32_t>(c.head_dim) / kElements;
     const int32_t* table = c.pages + b * c.pages_stride;
-    for (uint32_t t = threadIdx.x; t < items; t += kReadThreads) {
-        const uint32_t r = t / row, in = t - r * row, head = in / chunks, ch = in - head * chunks;
+    // this thread's piece (position, head, chunk), and from one to its next
+    uint32_t ch = threadIdx.x % chunks, r = threadIdx.x / chunks, head = r % heads;
+    r /= heads;
+    const uint32_t ch_step = kReadThreads % chunks, vectors = kReadThreads / chunks, head_step = vectors % heads, r_step = vectors / heads;
+    while (r < rows) {
         const int i = lo + static_cast<int>(r);
         int64_t scale_at;
         const int64_t off = locate(c, table, first + i, scale_at);
-        if (off < 0 && in == 0 && a.status) atomicOr(a.status + b, PLDP_ST_PAGE);
-        const int64_t to = b * a.os.seq + i * a.os.tok + head * a.os.head + ch * (E4M3 ? 16 : 8);
+        if (off < 0 && head == 0 && ch == 0 && a.status) atomicOr(a.status + b, PLDP_ST_PAGE);
+        const int64_t from = off + head * c.head_stride + ch * kBytes;
+        const int64_t to = b * a.os.seq + i * a.os.tok + head * a.os.head + ch * kElements;
+        Piece<E4M3> x[2];
+        float scale[2] = {0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            if (off < 0 || !(w ? a.v_out : a.k_out)) continue;
+            x[w].load((w ? c.v : c.k) + from, static_cast<const O*>(nullptr));
+            if constexpr (E4M3) scale[w] = __ldg((w ? c.v_scale : c.k_scale) + scale_at + static_cast<int64_t>(head) * c.page_size);
+        }
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
             O* out = static_cast<O*>(w ? a.v_out : a.k_out);
-            if (!out) continue;
-            uint4 raw = make_uint4(0u, 0u, 0u, 0u);
-            if (off >= 0) raw = ld_stream16((w ? c.v : c.k) + off + head * c.head_stride + ch * 16);
-            if constexpr (E4M3) {
-                const float scale =
-                    off >= 0 ? __ldg((w ? c.v_scale : c.k_scale) + scale_at + static_cast<int64_t>(head) * c.page_size) : 0.f;
-                const uint32_t q[4] = {raw.x, raw.y, raw.z, raw.w};
-                float x[8];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float2 lo2 = e4m3_two(q[k] & 0xFFFFu), hi2 = e4m3_two(q[k] >> 16);
-                    const int j = (k & 1) * 4;
-                    x[j] = lo2.x * scale, x[j + 1] = lo2.y * scale, x[j + 2] = hi2.x * scale, x[j + 3] = hi2.y * scale;
-                    if (k & 1) store8(out + to + (k >> 1) * 8, x);
-                }
-            } else {
-                const uint32_t q[4] = {raw.x, raw.y, raw.z, raw.w};
-                float x[8];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    x[2 * k] = __uint_as_float(q[k] << 16);
-                    x[2 * k + 1] = __uint_as_float(q[k] & 0xFFFF0000u);
-                }
-                store8(out + to, x);
-            }
+            if (out) x[w].store(out + to, scale[w]);
         }
+        ch += ch_step, head += head_step, r += r_step;
+        if (ch >= chunks) ch -= chunks, ++head;
+        if (head >= heads) head -= heads, ++r;
     }
 }
 
@@ -513,9 +532,11 @@ PLDP_API pldp_status pldp_cache_read(const pldp_cache_read_args* p, void* stream
     a.os = strides_of(p->out_strides);
     a.status = p->status;
     a.n = p->n;
-    // about four 16-byte pieces a thread, at least one position a CTA
-    const int row = a.c.vec_bytes / 16 * a.c.heads;
-    a.per = 4 * kReadThreads / row;
+    // about four pieces a thread (159 MB: 28.6 us; eight 31.0, two 29.8, one 35.5), at least one position a CTA; one a
+    // thread where that leaves SMs without a CTA (an append of 11 tokens and their read: 5.3 us; four 6.2)
+    const int row = a.c.head_dim * (p->dtype == PLDP_F32 ? 4 : 2) / 16 * a.c.heads;
+    const bool few = static_cast<int64_t>(p->n) * p->B * row < static_cast<int64_t>(4 * kReadThreads) * sm_count();
+    a.per = (few ? 1 : 4) * kReadThreads / row;
     if (a.per < 1) a.per = 1;
     const dim3 grid((p->n + a.per - 1) / a.per, p->B);
     auto s = static_cast<cudaStream_t>(stream);
