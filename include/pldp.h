@@ -736,7 +736,8 @@ PLDP_API pldp_status pldp_cache_read(const pldp_cache_read_args* args, void* str
  *  lse        float [B, n, q_heads], contiguous, or NULL.
  *  workspace  pldp_attend_workspace_size bytes, 256-byte aligned, zeroed once before
  *             first use (every call leaves it zeroed where that matters; not one that
- *             sets TIMEOUT: zero it again).
+ *             sets TIMEOUT: zero it again).  Calls of different shapes may share one of the
+ *             largest size; calls that may run concurrently need separate ones.
  *  status     uint32 [B] or NULL.  TIMEOUT: a wait inside the kernel ran out; the call's
  *             results are none.
  * Rows with nothing to attend to (tokens past draft_len, sequences skipped, positions

@@ -917,7 +917,8 @@ def pldp_attend_cache(cache, q, seq_len, out, workspace, draft_len=None, lse=Non
     """Attention of a step's tokens (x_t and the draft, appended before) over the cache.  q and
     out bfloat16 [B, n, q_heads, head_dim]; lse float32 [B, n, q_heads] (optional); scale default
     1/sqrt(head_dim).  workspace: uint8 CUDA tensor of pldp_attend_workspace_size(B, n, q_heads,
-    heads, head_dim) bytes, zeroed once before first use."""
+    heads, head_dim) bytes, zeroed once before first use; one of the largest size does for calls of
+    any shapes that follow one another."""
     if _calls is not None and type(cache) is pldp_cache and _done("pldp_attend_cache", _calls.attend_cache(
             cache.address, cache.B, q, seq_len, out, workspace, draft_len, lse, scale, status, stream)):
         return

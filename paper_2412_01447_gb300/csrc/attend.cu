@@ -17,15 +17,14 @@ int columns_of(int rows, int head_dim) {
 }
 int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
-struct Space {
-    size_t tickets, parts;   // bytes
-};
-Space space_of(int64_t B, int64_t n, int64_t q_heads, int64_t heads, int head_dim) {
+// The workspace: a ticket for each CTA, at a place that no shape moves, so that calls of any shapes find them zeroed;
+// then the parts, which need not be.
+constexpr size_t kTicketBytes = 1024;
+static_assert(kMaxCtas * sizeof(uint32_t) <= kTicketBytes, "tickets");
+size_t space_of(int64_t n, int64_t q_heads, int64_t heads, int head_dim) {
     const int64_t rows = n * (q_heads / heads);
     const int nt = columns_of(rows > 128 ? 128 : static_cast<int>(rows), head_dim);
-    const int64_t units = B * heads * ((rows + nt - 1) / nt);
-    return {static_cast<size_t>((units * 4 + 255) / 256 * 256),
-            static_cast<size_t>(2 * kMaxCtas) * nt * (padded_dim(head_dim) + 2) * sizeof(float)};
+    return kTicketBytes + static_cast<size_t>(2 * kMaxCtas) * nt * (padded_dim(head_dim) + 2) * sizeof(float);
 }
 
 // The pool as a tensor of (element, position, head, page), its middle dimensions by ascending
@@ -66,8 +65,7 @@ extern "C" {
 
 PLDP_API size_t pldp_attend_workspace_size(int B, int n, int q_heads, int heads, int head_dim) {
     if (B < 0 || n < 1 || q_heads < 1 || heads < 1 || q_heads % heads || head_dim < 1) return 0;
-    const Space sp = space_of(B, n, q_heads, heads, head_dim);
-    return (sp.tickets + sp.parts + 255) / 256 * 256;
+    return (space_of(n, q_heads, heads, head_dim) + 255) / 256 * 256;
 }
 
 PLDP_API pldp_status pldp_attend_cache(const pldp_attend_args* p, void* stream) {
@@ -104,9 +102,8 @@ PLDP_API pldp_status pldp_attend_cache(const pldp_attend_args* p, void* stream) 
     a.scale2 = p->scale * 1.4426950408889634f;
     const int nt = columns_of(static_cast<int>(rows), p->cache.head_dim);
     a.row_tiles = static_cast<int>((rows + nt - 1) / nt);
-    const Space sp = space_of(p->B, p->n, p->q_heads, p->cache.heads, p->cache.head_dim);
     a.tickets = static_cast<uint32_t*>(p->workspace);
-    a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(p->workspace) + sp.tickets);
+    a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(p->workspace) + kTicketBytes);
     const int64_t most = static_cast<int64_t>(p->B) * p->cache.heads * a.row_tiles * ((a.c.capacity + int64_t(kTile) - 1) / kTile);
     int ctas = sm_count() < kMaxCtas ? sm_count() : kMaxCtas;
     if (most < ctas) ctas = static_cast<int>(most);

@@ -64,7 +64,7 @@ namespace {
 // The keys of all sequences and heads form one list of tiles, cut into equal parts, one a CTA
 // (one a SM), so that ragged lengths and few long sequences keep every SM reading to the end.
 // What a CTA holds of a unit (sequence, head, rows) that others share goes to the workspace, and
-// the last of them joins the parts in order.
+// the last of them, by the ticket of the CTA in which the unit begins, joins the parts in order.
 //
 // Warps: 8 for the softmax (a key a thread, half of the columns each four), one that issues the matrix
 // instructions, two that copy (tensor copies, one a page's positions: keys, values), one that looks the
@@ -1026,7 +1026,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 bar_sync(4, kSoftmaxThreads);
                 if (tid == 0) {
                     // after all that the barrier has seen written, before what the others wrote is read
-                    uint32_t* ticket = a.tickets + static_cast<int64_t>(w.b) * units + w.unit;
+                    uint32_t* ticket = a.tickets + c_first;      // (of the units that begin there it is the only one cut)
                     uint32_t before;
                     asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(ticket) : "memory");
                     const bool is_last = before == static_cast<uint32_t>(c_last - c_first);
