@@ -148,6 +148,9 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
     // where this lane's partners in the rotation are, when its eight elements rotate alike (or not at all)
     const bool alike = a.interleaved || (half & 7) == 0;
     const int partner = e0 < half ? e0 + half : e0 < a.rot ? e0 - half : e0;
+    // The stage's two places, in turn from one rotated vector to the next, over the end of a token as well: the one barrier
+    // between a place's write and its reads then also lies between those reads and the write after next.
+    int turn = 0;
 #pragma unroll 1
     for (uint32_t token = blockIdx.x * a.at_once + sub; token < a.tokens; token += gridDim.x * a.at_once) {
         const int b = token / static_cast<uint32_t>(a.n), i = token - b * a.n;
@@ -231,7 +234,7 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
                 y[j] = lo_f32(z), y[j + 1] = hi_f32(z);
             }
         };
-        auto rotated = [&](float (&y)[8], int turn) {
+        auto rotated = [&](float (&y)[8]) {
             if (a.interleaved) {
 #pragma unroll
                 for (int j = 0; j < 8; j += 2) {
@@ -241,6 +244,7 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
                 }
             } else {
                 float* row = stage[turn][g];
+                turn ^= 1;
                 *reinterpret_cast<float4*>(row + e0) = make_float4(y[0], y[1], y[2], y[3]);
                 *reinterpret_cast<float4*>(row + e0 + 4) = make_float4(y[4], y[5], y[6], y[7]);
                 __syncwarp(mates);
@@ -260,7 +264,7 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
             }
         };
         // the queries, most of the vectors: nothing in their loop depends on which one it is
-        int h = first, turn = 0;
+        int h = first;
         {
             Raw<T> norm;
             norm.clear();
@@ -269,18 +273,18 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
             const int64_t from_step = step * a.qs.head, to_step = step * a.os.head;
             __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.q_out) + (b * a.os.seq + i * a.os.tok + h * a.os.head + e0);
 #pragma unroll 1
-            for (; h < k_first; h += step, turn ^= 1, to += to_step) {
+            for (; h < k_first; h += step, to += to_step) {
                 float y[8];
                 unpack(y);
                 from += from_step;
                 if (live && h + step < total) next.load(h + step < k_first ? from : source(h + step));
                 if (a.q_norm) normed(y, norm);
-                if (a.rot) rotated(y, turn);
+                if (a.rot) rotated(y);
                 if (live) *reinterpret_cast<uint4*>(to) = bf16_8(y);
             }
         }
 #pragma unroll 1
-        for (; h < total; h += step, turn ^= 1) {
+        for (; h < total; h += step) {
             float y[8];
             unpack(y);
             if (live && h + step < total) next.load(source(h + step));
@@ -292,7 +296,7 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
                     if (live) norm.load(static_cast<const T*>(a.k_norm) + e0);
                     normed(y, norm);
                 }
-                if (a.rot) rotated(y, turn);
+                if (a.rot) rotated(y);
             }
             if (off < 0) continue;
             const int head = key ? h - k_first : h - v_first;
