@@ -776,14 +776,16 @@ PLDP_API size_t pldp_attend_workspace_size(int B, int n, int q_heads, int heads,
  *
  *  q, q_heads, q_strides, scale, lse   of the step's pldp_attend_cache (lse [B, n, q_heads]).
  *  row        int32 [B] (accept_len), or NULL for row 0; outside [0, n): ROW_INDEX, no
- *             result.
+ *             result (scores of -INFINITY, best_pos -1).
  *  kv_len     int32 [B] (kv_keep_len), 0..capacity (else SEQ_LEN, no result): candidates
- *             outside [0, kv_len) score -INFINITY and are never chosen.
+ *             outside [0, kv_len) score -INFINITY and are never chosen, with accumulate too.
  *  heads      int32 [n_sel], or NULL for all q_heads (n_sel ignored): the selected query heads;
  *             entries outside [0, q_heads) are ignored and set ROW_INDEX.
  *             n_sel * head_dim <= 49152.
  *  accumulate not 0: scores holds those of other layers, and a candidate's score is
- *             the larger of both (MAX) or their sum (SUM): call layer by layer.
+ *             the larger of both (MAX) or their sum (SUM): call layer by layer.  A
+ *             candidate that this layer has no score for (PAGE, or no entry of heads is a
+ *             head) keeps theirs; without accumulate it scores -INFINITY.
  *  cand_pos, cand_count, C_cap   as written by pldp_find_candidates.
  *  scores     float [B, C_cap] out, or NULL (not with accumulate).
  *  best_pos, best_score, status  as pldp_rank_attention; ties go to the smaller j.

@@ -34,6 +34,7 @@ constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kChunk = 64;           // candidates looked up at once
 constexpr int kParts = 1024;         // scores of (candidate, key/value head) held
 constexpr int kInFlight = 4;
+constexpr int64_t kNoCandidate = -2;   // in the place of a key's offset (locate()'s -1 is a missing page)
 
 // Elements that 16 bytes hold, as floats, times q and added up.
 template <bool E4M3>
@@ -162,7 +163,7 @@ __global__ void __launch_bounds__(kThreads) rank_cache_kernel(const RankArgs a) 
         for (int t = threadIdx.x; t < here; t += kThreads) {
             const int j = __ldg(a.cand_pos + static_cast<int64_t>(b) * a.C_cap + rank + (i0 + t) * S);
             pos[t] = j;
-            off[t] = -1;
+            off[t] = kNoCandidate;
             if (ok && j >= 0 && j < len) {
                 off[t] = locate(c, table, j, scale_at[t]);
                 if (off[t] < 0 && a.status) atomicOr(a.status + b, PLDP_ST_PAGE);
@@ -205,11 +206,13 @@ __global__ void __launch_bounds__(kThreads) rank_cache_kernel(const RankArgs a) 
         __syncthreads();
         for (int t = threadIdx.x; t < here; t += kThreads) {
             float* out = a.scores ? a.scores + static_cast<int64_t>(b) * a.C_cap + rank + (i0 + t) * S : nullptr;
-            const bool live = off[t] >= 0;
+            // A candidate without a page, or where no selected head is one, has no score of this layer: that of the
+            // others stands.  One outside the context, or of a sequence that is refused, has none at all.
+            const bool live = off[t] >= 0 && n_groups > 0;
             float score = live && a.sum ? 0.f : -INFINITY;
             if (live)
                 for (int k = 0; k < n_groups; ++k) score = a.sum ? score + part[t * n_groups + k] : fmaxf(score, part[t * n_groups + k]);
-            if (a.accumulate) {
+            if (a.accumulate && off[t] != kNoCandidate) {
                 const float before = *out;
                 score = live ? (a.sum ? before + score : fmaxf(before, score)) : before;
             }
