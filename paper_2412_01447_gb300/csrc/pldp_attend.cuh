@@ -12,6 +12,11 @@ namespace pldp {
 
 constexpr int kTile = 128;                // keys a tile
 constexpr int kMaxCtas = 192;             // parts of the list at most
+#ifdef PLDP_TEST_STUCK_SCORES
+constexpr uint32_t kPolls = 1u << 12;     // test build: a short bound on every wait
+#else
+constexpr uint32_t kPolls = kMbarPolls;
+#endif
 
 struct AttendArgs {
     CacheView c;
@@ -127,9 +132,13 @@ struct Columns {
     alignas(16) float key[4][kTile], key_scale[E4M3 ? 4 : 1][E4M3 ? kTile : 4], value_scale[E4M3 ? 4 : 1][E4M3 ? kTile : 4];
     int limit[NT];                  // last position that the row sees
     int seen[NT];                   // whether m has been set
-    uint64_t full[8], empty[8], stage_full[8], stage_empty[8], s_full[2], p_full[2], pv_done[2], q_full, key_empty[4];
+    uint64_t full[8], empty[8], stage_full[8], stage_empty[8], s_full[2], p_full[2], pv_done[2], q_full, key_empty[4], drained;
+#ifdef PLDP_TEST_STUCK_SCORES
+    uint64_t never;                 // test build: a barrier that nothing arrives on
+#endif
     uint32_t tmem, amax;
     int dead, last;
+    int ended[2];                   // entries of the ring that the copy warps have come to
     int b, unit, tile;              // where this CTA's part of the list starts
     long long at, count;            // its first tile in the list, tiles in it
     long long each, extra;          // tiles a CTA, and CTAs that have one more
@@ -139,7 +148,9 @@ struct Columns {
 // Whether a phase is over; the answer takes some 120 cycles, which other questions and work can share.
 __device__ __forceinline__ bool over(uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity & 1u, 1); }
 // Waits, with a limit; after one has run out no wait of this CTA blocks for long any more, and its results
-// are marked as none.
+// are marked as none.  From then on a role may be ahead of the others, so no copy starts any more (its place may be in
+// use), the warp of keys still waits for the softmax, which meets it at barriers without a limit, and what is in flight is
+// waited for before the CTA ends.
 __device__ __forceinline__ void wait_more(bool done, uint64_t* bar, uint32_t parity, int* dead) {
     // (one statement: the loop as C++ came to a hundred instructions at each of its places)
     asm volatile(
@@ -158,7 +169,7 @@ __device__ __forceinline__ void wait_more(bool done, uint64_t* bar, uint32_t par
         "@p bra AGAIN;\n\t"
         "st.volatile.shared.u32 [%3], 1;\n\t"
         "DONE:\n\t}" ::"r"(static_cast<uint32_t>(done)),
-        "r"(smem_u32(bar)), "r"(parity & 1u), "r"(smem_u32(dead)), "n"(kMbarPolls)
+        "r"(smem_u32(bar)), "r"(parity & 1u), "r"(smem_u32(dead)), "n"(kPolls)
         : "memory");
 }
 __device__ __forceinline__ void wait_for(uint64_t* bar, uint32_t parity, int* dead) {
@@ -310,6 +321,10 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
         mbar_init(&col.pv_done[0], 1);
         mbar_init(&col.pv_done[1], 1);
         mbar_init(&col.q_full, kSoftmaxThreads / 32);
+        mbar_init(&col.drained, 1);
+#ifdef PLDP_TEST_STUCK_SCORES
+        mbar_init(&col.never, 1);
+#endif
         fence_mbar_init();
         col.dead = 0;
     }
@@ -392,8 +407,10 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
             const int boxes = kTile / a.box;                               // of a tile, 1..128
             int kv = warp - S::kCopyWarp;
             int e = kv;                                                    // entries of the ring: keys and values in turn
+            constexpr int kStep = S::kOneCopyWarp ? 1 : 2;
+            bool on = true;                                                // no wait has run out
 #pragma unroll 1
-            while (w.next(a, &st)) {
+            while (on && w.next(a, &st)) {
                 if (kv == 0 && w.t0 == 0 && w.unit == 0 && lane == 0 && st && a.status) atomicOr(a.status + w.b, st);
                 const int head = w.unit / a.row_tiles;
                 const int32_t* table = c.pages + w.b * c.pages_stride;
@@ -409,6 +426,8 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                     const CUtensorMap* map = kv ? &v_map : &k_map;
                     const int at = e % kDepth;
                     if (e >= kDepth) wait_for(&left[at], e / kDepth - 1, &col.dead);
+                    on = !__any_sync(0xFFFFFFFFu, *static_cast<volatile int*>(&col.dead));
+                    if (!on) return;
                     if (lane == 0) mbar_arrive_expect_tx(&arrived[at], full * a.box * (E4M3 ? a.pitch : S::kPanels * 128));
                     __syncwarp();
                     uint8_t* dst = E4M3 ? stages + at * S::kStage : ring + at * S::kSlot;
@@ -432,11 +451,12 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                     }
                     __syncwarp();
                     if (!S::kOneCopyWarp || kv) page = look(tile + 2, lane);
-                    e += S::kOneCopyWarp ? 1 : 2;
+                    e += kStep;
                 };
                 auto both = [&](int tile, int& page) {
                     turn(tile, page);
                     if constexpr (S::kOneCopyWarp) {
+                        if (!on) return;
                         kv = 1;
                         turn(tile, page);
                         kv = 0;
@@ -444,13 +464,24 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 };
                 int page = look(w.t0, lane), page_b = look(w.t0 + 1, lane);
 #pragma unroll 1
-                for (int tile = w.t0; tile < w.t1; tile += 2) {
+                for (int tile = w.t0; on && tile < w.t1; tile += 2) {
                     both(tile, page);
-                    if (tile + 1 < w.t1) both(tile + 1, page_b);
+                    if (on && tile + 1 < w.t1) both(tile + 1, page_b);
                 }
                 w.step(a);
             }
-            // the last copies have arrived before this CTA ends: every slot is waited for by its reader
+            // The last copy into each place arrives before this CTA ends, whether or not its reader has waited for it: the
+            // last entry of either warp there, by the parity of its turn.
+            if (lane == 0) col.ended[warp - S::kCopyWarp] = e;
+            if constexpr (S::kOneCopyWarp) __syncwarp();
+            else bar_sync(13, 64);
+            if (warp == S::kCopyWarp && lane < kDepth) {
+                const int ended[2] = {col.ended[0], S::kOneCopyWarp ? col.ended[0] : col.ended[1]};   // (each warp's next one)
+                const int top = max(ended[0], ended[1]) - 1;
+                int x = top - (top - lane + kDepth) % kDepth;
+                while (x >= 0 && x >= ended[x & 1]) x -= kDepth;
+                if (x >= 0) mbar_wait(&arrived[lane], (x / kDepth) & 1, kMbarPolls);
+            }
         } else if (warp == S::kKeyWarp) {
             // ---- the keys of each tile, four a lane: whether there is one, and e4m3's scales ----
             // Four neighbours lie in one page where 4 divides the page size; their scales are then 16 bytes (if the
@@ -477,7 +508,11 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 auto turn = [&](int tile, int& page) {
                     const int at = tile_no & 3;
                     if (tile < w.t1) {
-                        if (tile_no >= 4) wait_for(&col.key_empty[at], (tile_no >> 2) - 1, &col.dead);
+                        if (tile_no >= 4 && !over(&col.key_empty[at], (tile_no >> 2) - 1)) {
+                            wait_more(false, &col.key_empty[at], (tile_no >> 2) - 1, &col.dead);
+                            // ahead of the softmax this warp would arrive on a barrier before they have left it
+                            if (*static_cast<volatile int*>(&col.dead)) mbar_wait(&col.key_empty[at], ((tile_no >> 2) - 1) & 1, kMbarPolls);
+                        }
                         const int pos = tile * kTile + 4 * lane;
                         if (four) {
                             const int there = exists(page) ? w.keys - pos : 0;
@@ -537,7 +572,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 uint32_t polls = 0;
 #pragma unroll 1
                 while (!__all_sync(0xFFFFFFFFu, done)) {
-                    if (++polls >= kMbarPolls || *static_cast<volatile int*>(&col.dead)) {
+                    if (++polls >= kPolls || *static_cast<volatile int*>(&col.dead)) {
                         *static_cast<volatile int*>(&col.dead) = 1;
                         break;
                     }
@@ -607,6 +642,9 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 ++segment;
                 w.step(a);
             }
+            // nothing reads shared memory or writes tensor memory any more when they are given back
+            mma_commit(&col.drained, lead);
+            mbar_wait(&col.drained, 0, kMbarPolls);
         }
     } else if (E4M3 && warp >= 8) {
         // ---- e4m3: the codes of a tile of keys or values to f16, 16 at a time ----
@@ -803,6 +841,9 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                             if (pos > col.limit[c0 + ch * CH + i]) x[i] = -INFINITY;
                     }
                 };
+#ifdef PLDP_TEST_STUCK_SCORES
+                wait_for(&col.never, 0, &col.dead);
+#endif
                 wait_more(scored, &col.s_full[tile_no & 1], tile_no >> 1, &col.dead);
                 tmem_after_sync();
                 bool up = E4M3 && !settled;
