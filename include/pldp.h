@@ -625,7 +625,9 @@ PLDP_API pldp_status pldp_top_heads(const uint32_t* counts, int R, int k, int32_
  *             strides multiples of 16 bytes.
  *  dtype      PLDP_BF16, or PLDP_E4M3: 8-bit codes (4 exponent and 3 mantissa bits,
  *             largest 448) and one fp32 scale for each vector,
- *             value = code * scale, scales > 0 and finite.
+ *             value = code * scale, scales finite and 2^-80 (8.3e-25) or more.  A vector of
+ *             zeros should have that smallest scale: attention's weights round relative to
+ *             the largest of weight * scale.
  *  k_scale, v_scale   float [n_pages, heads, page_size], contiguous (PLDP_E4M3; else NULL).
  *  n_pages, page_size  >= 1, any size; max_pages * page_size < 2^31.
  *  heads      key/value heads, 1..1024; head_dim a multiple of 16, 16..256.
@@ -651,7 +653,7 @@ typedef struct {
  *   queries and keys   x <- x * rsqrt(mean(x^2) + eps) * norm     (q_norm / k_norm not NULL)
  *                      (a, b) <- (a cos - b sin, b cos + a sin)   (cos not NULL)
  *   q_out <- bf16(q);  the cache's keys and values <- k, v rounded to bf16, or in a
- *   PLDP_E4M3 cache scale = max(max|x| / 448, 1e-30) (1 for a vector of zeros), code = x / scale.
+ *   PLDP_E4M3 cache scale = max(max|x| / 448, 2^-80), code = x / scale.
  *
  *  q, k, v    dtype (PLDP_F32 or PLDP_BF16): [B, n, q_heads or cache.heads, head_dim]
  *             with strides of their own (sequence, token, head; elements), 16-byte

@@ -307,8 +307,7 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
                 for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(y[j]));
 #pragma unroll
                 for (int o = GS / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(mates, m, o, GS));
-                // (a vector below 1e-28 throughout is held as if it were that large)
-                const float scale = m > 0.f ? fmaxf(m * (1.f / 448.f), 1e-30f) : 1.f, inverse = __fdividef(1.f, scale);
+                const float scale = fmaxf(m * (1.f / 448.f), kLeastScale), inverse = __fdividef(1.f, scale);
                 if (live) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) y[j] *= inverse;

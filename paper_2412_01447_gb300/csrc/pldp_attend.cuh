@@ -802,7 +802,7 @@ attend_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap k_map, con
                 if constexpr (E4M3) {
                     // (where there is no key nothing was loaded, or what lies past the end; the logarithm is 2^-22 off
                     // at most, as much as the weight's own exponential, and the reciprocal one unit)
-                    const float v = g == 0.f ? fmaxf(col.value_scale[at][j], 1e-37f) : 1.f;
+                    const float v = g == 0.f ? fmaxf(col.value_scale[at][j], kLeastScale) : 1.f;
                     f = g == 0.f ? col.key_scale[at][j] * a.scale2 * back : 0.f;
                     g += __log2f(v);
                     inv = reciprocal(v);

@@ -6,6 +6,10 @@
 namespace pldp {
 
 constexpr int kMaxHeadDim = 256;
+// The smallest scale of an e4m3 vector, which vectors of zeros have as well.  Attention rounds weights relative to the
+// largest of weight x scale, so a value of zeros must not count as if it were large; and its sums hold weight / scale up to
+// 2^15 2^80 for each of 2^31 keys, which is below 2^127.
+constexpr float kLeastScale = 0x1p-80f;
 
 // One cache.  Offsets and strides in bytes; positions are below 2^31.
 struct CacheView {
