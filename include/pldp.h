@@ -653,7 +653,8 @@ typedef struct {
  *   queries and keys   x <- x * rsqrt(mean(x^2) + eps) * norm     (q_norm / k_norm not NULL)
  *                      (a, b) <- (a cos - b sin, b cos + a sin)   (cos not NULL)
  *   q_out <- bf16(q);  the cache's keys and values <- k, v rounded to bf16, or in a
- *   PLDP_E4M3 cache scale = max(max|x| / 448, 2^-80), code = x / scale.
+ *   PLDP_E4M3 cache scale = max(max|x| * (1/448), 2^-80), code = x / scale (in fp32,
+ *   rounded to the nearest code).
  *
  *  q, k, v    dtype (PLDP_F32 or PLDP_BF16): [B, n, q_heads or cache.heads, head_dim]
  *             with strides of their own (sequence, token, head; elements), 16-byte

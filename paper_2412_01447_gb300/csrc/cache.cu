@@ -307,10 +307,17 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
                 for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(y[j]));
 #pragma unroll
                 for (int o = GS / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(mates, m, o, GS));
-                const float scale = fmaxf(m * (1.f / 448.f), kLeastScale), inverse = __fdividef(1.f, scale);
+                // Codes are quotients as 32-bit division rounds them, on which ties between codes depend: a product with the inverse,
+                // put right by its remainder (Markstein 1990), two elements an instruction.
+                const float scale = fmaxf(m * (1.f / 448.f), kLeastScale), inverse = 1.f / scale;
                 if (live) {
+                    const uint64_t by = pack_f32x2(inverse, inverse), less = pack_f32x2(-scale, -scale);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) y[j] *= inverse;
+                    for (int j = 0; j < 8; j += 2) {
+                        const uint64_t x = pack_f32x2(y[j], y[j + 1]), first = fma_f32x2(x, by, 0ull);
+                        const uint64_t z = fma_f32x2(fma_f32x2(first, less, x), by, first);
+                        y[j] = lo_f32(z), y[j + 1] = hi_f32(z);
+                    }
                     *reinterpret_cast<uint2*>(dst + e0) = make_uint2(e4m3_quad(y[0], y[1], y[2], y[3]), e4m3_quad(y[4], y[5], y[6], y[7]));
                     if (at == 0) (key ? c.k_scale : c.v_scale)[scale_at + static_cast<int64_t>(head) * c.page_size] = scale;
                 }
