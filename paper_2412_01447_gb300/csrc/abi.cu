@@ -19,11 +19,10 @@ pldp_status fail(pldp_status code, const char* fmt, ...) {
     return code;
 }
 
-pldp_status check_launch(const char* what) {
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess)
-        return fail(PLDP_ERR_CUDA, "%s: launch failed: %s", what, cudaGetErrorString(e));
-    return PLDP_OK;
+pldp_status launched(const char* what, cudaError_t e) {
+    if (e == cudaSuccess) return PLDP_OK;
+    cudaGetLastError();                               // reported here, and by no later call
+    return fail(PLDP_ERR_CUDA, "%s: launch failed: %s", what, cudaGetErrorString(e));
 }
 
 int sm_count() {

@@ -119,8 +119,7 @@ PLDP_API pldp_status pldp_attend_cache(const pldp_attend_args* p, void* stream) 
     a.head_first = head_first;
     auto s = static_cast<cudaStream_t>(stream);
     const cudaError_t e = e4m3 ? launch_attend_e4m3(a, maps, nt, ctas, s) : launch_attend_bf16(a, maps, nt, ctas, s);
-    if (e != cudaSuccess) return fail(PLDP_ERR_CUDA, "%s: launch failed: %s", fn, cudaGetErrorString(e));
-    return check_launch(fn);
+    return launched(fn, e);
 }
 
 }  // extern "C"

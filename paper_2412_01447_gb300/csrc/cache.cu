@@ -518,8 +518,7 @@ PLDP_API pldp_status pldp_cache_append(const pldp_cache_append_args* p, void* st
     cudaError_t e;
     if (p->dtype == PLDP_F32) e = q8 ? launch_append<float, true>(a, s) : launch_append<float, false>(a, s);
     else e = q8 ? launch_append<__nv_bfloat16, true>(a, s) : launch_append<__nv_bfloat16, false>(a, s);
-    if (e != cudaSuccess) return fail(PLDP_ERR_CUDA, "%s: launch failed: %s", fn, cudaGetErrorString(e));
-    return check_launch(fn);
+    return launched(fn, e);
 }
 
 PLDP_API pldp_status pldp_cache_read(const pldp_cache_read_args* p, void* stream) {
@@ -558,8 +557,7 @@ PLDP_API pldp_status pldp_cache_read(const pldp_cache_read_args* p, void* stream
     else
         e = q8 ? launch_pdl(cache_read_kernel<__nv_bfloat16, true>, grid, dim3(kReadThreads), 0, s, 0, a)
                : launch_pdl(cache_read_kernel<__nv_bfloat16, false>, grid, dim3(kReadThreads), 0, s, 0, a);
-    if (e != cudaSuccess) return fail(PLDP_ERR_CUDA, "%s: launch failed: %s", fn, cudaGetErrorString(e));
-    return check_launch(fn);
+    return launched(fn, e);
 }
 
 }  // extern "C"

@@ -452,8 +452,7 @@ PLDP_API pldp_status pldp_token_logprobs(const void* logits, pldp_dtype dtype, i
     cudaError_t e;
     if (dtype == PLDP_F32) e = cut ? launch<float, true>(logits, a, s) : launch<float, false>(logits, a, s);
     else e = cut ? launch<__nv_bfloat16, true>(logits, a, s) : launch<__nv_bfloat16, false>(logits, a, s);
-    if (e != cudaSuccess) return fail(PLDP_ERR_CUDA, "%s: launch failed: %s", fn, cudaGetErrorString(e));
-    return check_launch(fn);
+    return launched(fn, e);
 }
 
 }  // extern "C"

@@ -16,7 +16,7 @@ namespace cg = cooperative_groups;
 // host-side error reporting (defined in abi.cu)
 // ---------------------------------------------------------------------------
 pldp_status fail(pldp_status code, const char* fmt, ...);
-pldp_status check_launch(const char* what);
+pldp_status launched(const char* what, cudaError_t e);  // what a launch answered, as a status
 int sm_count();  // SMs of the current device
 // CTAs of `kernel` that fit on the whole current device at once (cached).
 int resident_blocks(const void* kernel, int threads, size_t smem);

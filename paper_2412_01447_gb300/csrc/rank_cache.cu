@@ -302,6 +302,5 @@ extern "C" PLDP_API pldp_status pldp_rank_cache(const pldp_rank_cache_args* p, v
     if (static_cast<int64_t>(p->B) * S > INT32_MAX) return fail(PLDP_ERR_UNSUPPORTED, "%s: too many sequences", fn);
     auto s = static_cast<cudaStream_t>(stream);
     const cudaError_t e = p->cache.dtype == PLDP_E4M3 ? launch_group<true>(a, p->B, S, smem, s) : launch_group<false>(a, p->B, S, smem, s);
-    if (e != cudaSuccess) return fail(PLDP_ERR_CUDA, "%s: launch failed: %s", fn, cudaGetErrorString(e));
-    return check_launch(fn);
+    return launched(fn, e);
 }
