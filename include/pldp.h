@@ -629,7 +629,8 @@ PLDP_API pldp_status pldp_top_heads(const uint32_t* counts, int R, int k, int32_
  *             zeros should have that smallest scale: attention's weights round relative to
  *             the largest of weight * scale.
  *  k_scale, v_scale   float [n_pages, heads, page_size], contiguous (PLDP_E4M3; else NULL).
- *  n_pages, page_size  >= 1, any size; max_pages * page_size < 2^31.
+ *  n_pages, page_size  >= 1, any size; max_pages * page_size < 2^31 (pldp_attend_cache:
+ *             <= 2^31 - 4096).
  *  heads      key/value heads, 1..1024; head_dim a multiple of 16, 16..256.
  *  pages      int32 [B, pages_stride]: the page of each page_size positions, max_pages
  *             entries a sequence.  An entry outside [0, n_pages) sets PAGE: its

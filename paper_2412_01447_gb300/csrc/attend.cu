@@ -77,6 +77,9 @@ PLDP_API pldp_status pldp_attend_cache(const pldp_attend_args* p, void* stream) 
     AttendArgs a = {};
     pldp_status st = cache_view(fn, p->cache, p->B, &a.c);
     if (st != PLDP_OK) return st;
+    // (tiles are counted past the last position)
+    if (a.c.capacity > INT32_MAX - 4095)
+        return fail(PLDP_ERR_UNSUPPORTED, "%s: more than 2^31 - 4096 positions a sequence", fn);
     if (p->q_heads % p->cache.heads)
         return fail(PLDP_ERR_INVALID_ARG, "%s: q_heads must be a multiple of the cache's heads", fn);
     const int64_t rows = static_cast<int64_t>(p->n) * (p->q_heads / p->cache.heads);
