@@ -429,9 +429,9 @@ __global__ void __launch_bounds__(kReadThreads) cache_read_kernel(const ReadArgs
         count = c.capacity - first;
     }
     if (blockIdx.x == 0 && threadIdx.x == 0 && st && a.status) atomicOr(a.status + b, st);
-    const int lo = blockIdx.x * a.per, hi = min(lo + a.per, count);
+    const int lo = blockIdx.x * a.per;                  // below n
     constexpr int kElements = 16 / sizeof(O), kBytes = kElements * (E4M3 ? 1 : 2);
-    const uint32_t rows = hi > lo ? hi - lo : 0, heads = c.heads, chunks = static_cast<uint32_t>(c.head_dim) / kElements;
+    const uint32_t rows = lo < count ? min(a.per, count - lo) : 0, heads = c.heads, chunks = static_cast<uint32_t>(c.head_dim) / kElements;
     const int32_t* table = c.pages + b * c.pages_stride;
     // this thread's piece (position, head, chunk), and from one to its next
     uint32_t ch = threadIdx.x % chunks, r = threadIdx.x / chunks, head = r % heads;
@@ -547,7 +547,7 @@ PLDP_API pldp_status pldp_cache_read(const pldp_cache_read_args* p, void* stream
     const bool few = static_cast<int64_t>(p->n) * p->B * row < static_cast<int64_t>(4 * kReadThreads) * sm_count();
     a.per = (few ? 1 : 4) * kReadThreads / row;
     if (a.per < 1) a.per = 1;
-    const dim3 grid((p->n + a.per - 1) / a.per, p->B);
+    const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(p->n) + a.per - 1) / a.per), p->B);
     auto s = static_cast<cudaStream_t>(stream);
     const bool q8 = p->cache.dtype == PLDP_E4M3;
     cudaError_t e;
