@@ -876,6 +876,8 @@ def pldp_cache_append(cache, q, k, v, seq_len, q_out, draft_len=None, q_norm=Non
         if cos is None or sin is None or cos.dim() != 2 or cos.shape != sin.shape:
             raise ValueError("cos and sin must both be [positions, rot/2]")
         a.cos, a.sin = _dense(cos, "cos", torch.float32), _dense(sin, "sin", torch.float32)
+        if cos.numel() == 0:                             # an empty tensor's null pointer would mean no rotation
+            raise PldpError("pldp_cache_append", PLDP_ERR_INVALID_ARG, "rot must be even, 2..head_dim, and rot_rows >= 1")
         a.rot_rows, a.rot = cos.shape[0], 2 * cos.shape[1]
     a.interleaved = int(bool(interleaved))
     a.seq_len = _dense(seq_len, "seq_len", torch.int32, n=B)

@@ -697,7 +697,7 @@ PLDP_CALL(cache_append) {
     if (v[11] != Py_None || v[12] != Py_None) {
         const at::Tensor *c = a.tensor(v[11]), *s = a.tensor(v[12]);
         if (!c || !s || c->dim() != 2 || s->dim() != 2 || c->size(0) != s->size(0) || c->size(1) != s->size(1) ||
-            c->size(1) > INT32_MAX / 2)
+            c->size(1) > INT32_MAX / 2 || c->numel() == 0)
             Py_RETURN_NONE;
         p.cos = a.floats(v[11], -1);
         p.sin = a.floats(v[12], -1);
