@@ -1,4 +1,5 @@
 // Log probabilities of tokens, entropy and alternatives: pldp_token_logprobs.
+#include <float.h>
 #include <math.h>
 
 #include "pldp_internal.cuh"
@@ -447,7 +448,7 @@ PLDP_API pldp_status pldp_token_logprobs(const void* logits, pldp_dtype dtype, i
     a.units = static_cast<uint32_t>(units_of(V, es, cut));
     a.maxima = static_cast<float4*>(workspace);
     a.sums = reinterpret_cast<float2*>(a.maxima + rows * a.units);
-    a.c = 1.4426950408889634f / temperature;
+    a.c = fminf(1.4426950408889634f / temperature, FLT_MAX);       // (infinity would make the maximum's own exponent 0 * inf)
     auto s = static_cast<cudaStream_t>(stream);
     cudaError_t e;
     if (dtype == PLDP_F32) e = cut ? launch<float, true>(logits, a, s) : launch<float, false>(logits, a, s);
