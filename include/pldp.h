@@ -825,7 +825,8 @@ PLDP_API pldp_status pldp_rank_cache(const pldp_rank_cache_args* args, void* str
  *
  *  logits     dtype [rows, V], contiguous, aligned to its elements, rows below 2^31 and
  *             V below 2^31 - 4096.
- *             -INFINITY is allowed (a masked token: p = 0).
+ *             -INFINITY is allowed (a masked token: p = 0).  A row with NaN or +INFINITY has no
+ *             probabilities; its alternatives are tokens all the same.
  *  tokens     int32 [rows], or NULL (no logprob); outside [0, V): logprob -INFINITY.
  *  logprob, entropy   float [rows] out or NULL.
  *  top        alternatives wanted, 0..32 and <= V: top_id int32 [rows, top] and top_logprob

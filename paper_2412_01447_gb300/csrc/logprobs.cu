@@ -370,7 +370,7 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishBlocks) logprob_finish_
             a.top_logprob[r * a.top + place] = x > -INFINITY ? ((x - M) * a.c - log_l) * kLn2 : -INFINITY;
         }
     };
-    if (n <= kChunkList && m <= kElementList) {
+    if (n <= kChunkList && m <= kElementList && m >= a.top) {       // (fewer reach it only where logits are NaN)
         // (the order in which they came into the list does not matter: the keys are all different)
         for (int i = tid; i < m; i += kFinishThreads) {
             const unsigned long long key = elements[i];
