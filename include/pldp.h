@@ -736,7 +736,7 @@ PLDP_API pldp_status pldp_cache_read(const pldp_cache_read_args* args, void* str
  *  q_heads    a multiple of cache.heads.
  *  seq_len, draft_len   as pldp_cache_append (the capacity is max_pages * page_size).
  *  scale      finite; 1/sqrt(head_dim) as a rule.
- *  out        bf16 [B, n, q_heads, head_dim] with strides, as q.
+ *  out        bf16 [B, n, q_heads, head_dim] with strides, as q; it must not overlap q.
  *  lse        float [B, n, q_heads], contiguous, or NULL.
  *  workspace  pldp_attend_workspace_size bytes, 256-byte aligned, zeroed once before
  *             first use (every call leaves it zeroed where that matters; not one that
@@ -747,8 +747,12 @@ PLDP_API pldp_status pldp_cache_read(const pldp_cache_read_args* args, void* str
  * Rows with nothing to attend to (tokens past draft_len, sequences skipped, positions
  * past the capacity) are written as zeros, their lse as -INFINITY.  Keys and values
  * past a sequence's last new token are never used, whatever they hold; those of its new
- * tokens must be finite for all of its rows.  Sums and the running maximum are held in
- * fp32; results are the same for the same inputs, however the work is scheduled.
+ * tokens must be finite for all of its rows, and a bf16 cache's values below 2^32 in size.
+ * Sums and the running maximum are held in fp32; each weight exp(s_j - lse) is rounded on
+ * its way into the products, by up to 2^-17 of it over a bf16 cache and 2^-11 over an e4m3
+ * one; results are the same for the same inputs, however the work is scheduled.
+ * A step's rows are what this is made for: of a prompt every 128 rows go through all of
+ * their sequence's keys.
  */
 typedef struct {
     pldp_cache cache;
@@ -833,7 +837,7 @@ PLDP_API pldp_status pldp_rank_cache(const pldp_rank_cache_args* args, void* str
  *             float [rows, top], by descending logit, ties to the lower index (either
  *             may be NULL).
  *  workspace  pldp_token_logprobs_workspace_size bytes, 16-byte aligned; need not be
- *             cleared.
+ *             cleared.  Calls that may run concurrently need separate ones.
  * A row of -INFINITY throughout: logprob -INFINITY, entropy 0, top_id 0, 1, ... with
  * -INFINITY.
  */

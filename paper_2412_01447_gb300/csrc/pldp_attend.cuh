@@ -62,7 +62,7 @@ namespace {
 // Weights are rounded to 16 bits for the second product: in a bf16 cache as a sum of two bf16
 // (2^-17 of the weight; one alone would add as much error as the result's own rounding), the second
 // ones as NT more columns, which cost the product little beside reading V^T; in an
-// e4m3 cache as f16 (2^-12), in which the codes, at most 448, are exact as well.  The scales of an
+// e4m3 cache as f16 (2^-11), in which the codes, at most 448, are exact as well.  The scales of an
 // e4m3 cache never touch its codes: k's multiplies the key's scores, v's goes into the exponent
 // (w = vs 2^(x - m), m the maximum of x + log2 vs) and is divided out of the sums.
 //
@@ -77,10 +77,12 @@ namespace {
 // one that is over takes some 120 cycles, so waits are asked together or ahead, and code is kept short:
 // all of these loops share one instruction cache.
 //
-// Bound by memory where a tile is large: 2 x 131072 keys of 8 heads of 128, bf16, one token: 141..145 us (0.95..0.98
+// Bound by memory where a tile is large: 2 x 131072 keys of 8 heads of 128, bf16, one token: 141..146 us (0.95..0.98
 // of the measured copy rate); 64 x 16384, 17 tokens, 5 query heads a head: 502..517 us (0.93..0.95).  Short
 // tiles are bound by the warps' own work, 0.95 us a tile of 128 keys of 64 elements in e4m3 with up to 16
 // columns (the conversion), 1.3 us with 48 (the softmax): 32 x 8192 keys, 8 heads, 11 tokens: 106..109 us (2.0 TB/s).
+// Of a prompt every tile of rows walks all of its sequence's keys, those that it sees none of too: 4 x 4095 tokens, 32 query
+// heads, bf16: 2.2 ms (209 of 1922 TFLOP/s for what the mask leaves).
 // ---------------------------------------------------------------------------
 constexpr int kSoftmaxThreads = 256, kConvertThreads = 128;
 constexpr int kMaxShared = 232448;        // bytes a CTA, static and dynamic

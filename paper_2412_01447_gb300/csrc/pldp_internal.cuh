@@ -191,7 +191,7 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, uint32
     return false;
 }
 
-constexpr uint32_t kMbarPolls = 1u << 22;   // each try_wait may suspend; ~tens of ms bound
+constexpr uint32_t kMbarPolls = 1u << 22;   // a poll that fails takes some 4 us (it suspends): a limit of 16 s
 
 // ---------------------------------------------------------------------------
 // Programmatic dependent launch.  Kernels of a step are launched so that the
