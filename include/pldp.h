@@ -25,7 +25,10 @@
  * pldp_rank_hidden_avg (App. B.2) and pldp_identify_heads / pldp_top_heads
  * (Sec. 4.2.1).  Around the target model's forward pass of a step, over a paged cache:
  * pldp_cache_append, pldp_attend_cache, pldp_rank_cache (2 from the cache), pldp_cache_read,
- * and pldp_token_logprobs on its logits.
+ * and pldp_token_logprobs on its logits.  Before the steps, and between them: prompts of
+ * different lengths packed into the cache (pldp_cache_append_prompt, pldp_attend_prompt), and
+ * its pages given out, shared and given back on the device (pldp_pages_reserve, pldp_pages_fork,
+ * pldp_pages_free, pldp_pages_compact, pldp_cache_copy_pages).
  *
  * Conventions shared by every call
  *  - Every pointer argument is a DEVICE pointer owned by the caller (the
@@ -752,7 +755,7 @@ PLDP_API pldp_status pldp_cache_read(const pldp_cache_read_args* args, void* str
  * its way into the products, by up to 2^-17 of it over a bf16 cache and 2^-11 over an e4m3
  * one; results are the same for the same inputs, however the work is scheduled.
  * A step's rows are what this is made for: of a prompt every 128 rows go through all of
- * their sequence's keys.
+ * their sequence's keys (pldp_attend_prompt: those that they see).
  */
 typedef struct {
     pldp_cache cache;
@@ -848,6 +851,191 @@ PLDP_API pldp_status pldp_token_logprobs(const void* logits, pldp_dtype dtype, i
                                          size_t workspace_bytes, void* stream);
 
 PLDP_API size_t pldp_token_logprobs_workspace_size(int64_t rows, int V);
+
+/* ---------------------------------------------------------------------------
+ * Prompts: sequences of different lengths, packed
+ * ---------------------------------------------------------------------------
+ * The tokens of B prompts (or chunks of prompts) behind one another, without padding: those of
+ * sequence b are rows rows[b] .. rows[b+1]-1, its row rows[b]+i stands at position start[b]+i.
+ *
+ *  R          rows of the tensors, >= 0 and below 2^31 - 256; rows behind rows[B] (or before
+ *             rows[0]) belong to no sequence: nothing of them is used, nothing is written there.
+ *  rows       int32 [B+1], ascending, 0 <= rows[b] <= rows[b+1] <= R; a sequence may have no
+ *             rows.  Where a pair descends or leaves [0, R]: SEQ_LEN, that sequence is skipped
+ *             (rows that two sequences then claim are one of theirs).
+ *  start      int32 [B], or NULL for 0; outside [0, capacity]: SEQ_LEN, skipped.  Tokens at
+ *             or past the capacity: CAPACITY, they take no part.
+ */
+
+/*
+ * pldp_cache_append of packed tokens: the same arithmetic and results, and the same arguments,
+ * without draft_len; q, k, v and q_out are [R, heads, head_dim] with strides (token, head).
+ * The capacity is max_pages * page_size, and rot_rows where that is less.  B and R below 2^31.
+ */
+typedef struct {
+    pldp_cache cache;
+    const void* q;
+    const void* k;
+    const void* v;
+    pldp_dtype dtype;
+    int B, R, q_heads;
+    int64_t q_strides[2], k_strides[2], v_strides[2]; /* token, head */
+    const void* q_norm;
+    const void* k_norm;
+    float eps;
+    const float* cos;
+    const float* sin;
+    int rot, interleaved;
+    int64_t rot_rows;
+    const int32_t* rows;
+    const int32_t* start;
+    void* q_out;
+    int64_t q_out_strides[2];
+    uint32_t* status;
+} pldp_cache_append_prompt_args;
+
+PLDP_API pldp_status pldp_cache_append_prompt(const pldp_cache_append_prompt_args* args, void* stream);
+
+/*
+ * Causal attention of packed prompts over the cache (their own keys and values included:
+ * append first).  The row of sequence b at position p, query head h, with kv head
+ * h / (q_heads / cache.heads):
+ *   s_j   = scale * q . k_j   for positions j = 0 .. p
+ *   out   = sum_j exp(s_j - lse) v_j,   lse = ln sum_j exp(s_j)
+ * so a prompt's prefix may be in the cache already (a shared one, or earlier chunks).
+ *
+ *  q          bf16 [R, q_heads, head_dim] with strides (token, head), 16-byte aligned,
+ *             strides multiples of 16 bytes.
+ *  q_heads    a multiple of cache.heads.
+ *  scale      finite; 1/sqrt(head_dim) as a rule.
+ *  out        bf16 [R, q_heads, head_dim] with strides, as q; it must not overlap q.
+ *  lse        float [R, q_heads], contiguous, or NULL (pldp_rank_cache takes that of one
+ *             sequence's rows, the last of them its row).
+ *  workspace  pldp_attend_prompt_workspace_size bytes, 256-byte aligned; need not be cleared.
+ *             Calls of any shapes may share one of the largest size; calls that may run
+ *             concurrently need separate ones.
+ *  status     uint32 [B] or NULL.  TIMEOUT: a wait inside the kernel ran out; the call's
+ *             results are none.
+ * Rows of a sequence with nothing to attend to (skipped, past the capacity, no page holds any
+ * of their positions) are written as zeros, their lse as -INFINITY; of a sequence whose rows
+ * are not within [0, R] nothing is written.  Keys and values past a sequence's last row are never
+ * used, whatever they hold; those before it must be finite, and a bf16 cache's values below 2^32
+ * in size.  Sums and the running maximum are held in fp32; each weight exp(s_j - lse) is rounded
+ * on its way into the product with the values, by up to 2^-8 of it over a bf16 cache and 2^-11 over an
+ * e4m3 one (there small ones by up to 2^-32 of the largest weight * v_scale of the row); results
+ * are the same for the same inputs, however the work is scheduled.
+ */
+typedef struct {
+    pldp_cache cache;
+    const void* q;
+    int B, R, q_heads;
+    int64_t q_strides[2];
+    const int32_t* rows;
+    const int32_t* start;
+    float scale;
+    void* out;
+    int64_t out_strides[2];
+    float* lse;
+    uint32_t* status;
+    void* workspace;
+    size_t workspace_bytes;
+} pldp_attend_prompt_args;
+
+PLDP_API pldp_status pldp_attend_prompt(const pldp_attend_prompt_args* args, void* stream);
+
+/* Bytes of workspace pldp_attend_prompt needs on the current device, whatever B and R (0 if invalid). */
+PLDP_API size_t pldp_attend_prompt_workspace_size(int q_heads, int heads, int head_dim);
+
+/* ---------------------------------------------------------------------------
+ * The pages of a cache
+ * ---------------------------------------------------------------------------
+ * Verification moves seq_len on the device, so the pages of the next step are given out there too:
+ * these calls keep a page table (one for all layers: page p is page p of each layer's pool) and
+ * the number of its entries that hold each page.  Pages that several sequences hold (a common
+ * prompt) are shared until one of them writes.
+ *
+ *  pages      int32 [B, pages_stride], max_pages entries a row: the table that pldp_cache
+ *             reads.  An entry outside [0, n_pages) holds no page; the calls write -1.
+ *  refs       int32 [n_pages]: the entries that hold each page, 0 for a free one.  Start
+ *             with a table of -1 and refs of 0, or with both as they belong together; a caller that
+ *             adds 1 to a page's keeps it from being given out or written.
+ *  B          rows, 0..65535 (else PLDP_ERR_UNSUPPORTED).  max_pages * page_size < 2^31,
+ *             n_pages <= 2^31 - 4096.
+ * Whatever refs holds, no call writes outside these arrays; results are the ones described
+ * where refs is as described.  Calls on one table follow one another (one stream, or ordered ones).
+ */
+typedef struct {
+    int32_t* pages;
+    int64_t pages_stride;
+    int B, max_pages, page_size;
+    int32_t* refs;
+    int n_pages;
+} pldp_page_table;
+
+/* Bytes of workspace pldp_pages_reserve and pldp_pages_compact need for a table (0 if invalid);
+ * 16-byte aligned, need not be cleared. */
+PLDP_API size_t pldp_pages_workspace_size(int B, int max_pages, int n_pages);
+
+/*
+ * Makes positions start[b] .. start[b]+count[b]-1 of every sequence ones that may be written:
+ * entries in that range that hold no page, or one that others hold too (refs above 1 before the
+ * call), get free pages, the lowest ones, in order of sequence and position.
+ * A sequence gets all of the pages that it needs or, where it and those before it need more than
+ * there are, none: CAPACITY, its entries stay as they are and it must not be written.
+ *
+ *  start      int32 [B] (kv_keep_len of a step: x_t's position).
+ *  count      int32 [B], or NULL for n (K+1).  0: nothing to do.
+ *  n          the largest count, >= 0.  A negative start, or a count outside [0, n]: SEQ_LEN, nothing done.
+ *             A range that passes max_pages * page_size: CAPACITY, nothing done.
+ *  copies     int32 [B, 2] out: the page that pldp_cache_copy_pages has to copy, and where to
+ *             (the one in which start lies, if it was shared and start is not its first
+ *             position), or -1, -1.
+ *  status     uint32 [B] or NULL.
+ */
+PLDP_API pldp_status pldp_pages_reserve(const pldp_page_table* table, const int32_t* start, const int32_t* count, int n,
+                                        int32_t* copies, uint32_t* status, void* workspace, size_t workspace_bytes,
+                                        void* stream);
+
+/*
+ * Row b becomes the first entries of row parent[b], those that hold its positions 0..len[b]-1,
+ * which both hold from then on; what row b held before is given back.
+ *
+ *  parent     int32 [B]; -1 or b itself: row b stays as it is.  Outside [-1, B), or a row
+ *             that has another row as its parent itself: ROW_INDEX, row b stays as it is.
+ *  len        int32 [B]; negative or past max_pages * page_size: SEQ_LEN, row b stays as it is.
+ *  status     uint32 [B] or NULL.
+ */
+PLDP_API pldp_status pldp_pages_fork(const pldp_page_table* table, const int32_t* parent, const int32_t* len,
+                                     uint32_t* status, void* stream);
+
+/*
+ * Gives back the entries past those that hold positions 0..keep_len[b]-1 (0: all of a sequence that
+ * has ended); a negative keep_len[b] leaves row b as it is.
+ */
+PLDP_API pldp_status pldp_pages_free(const pldp_page_table* table, const int32_t* keep_len, void* stream);
+
+/*
+ * Moves the held pages to the front of the pool: the highest one to the lowest free one, and so
+ * on, until the held ones are 0..U-1.  The table and refs are changed here, the contents follow with
+ * pldp_cache_copy_pages (in every layer) before the next use.
+ *
+ *  copies     int32 [copies_cap, 2] out, copies_cap >= n_pages / 2: from, to.
+ *  n_copies   int32 [1] out.
+ *  used       int32 [1] out, or NULL: U.
+ */
+PLDP_API pldp_status pldp_pages_compact(const pldp_page_table* table, int32_t* copies, int copies_cap, int32_t* n_copies,
+                                        int32_t* used, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Copies whole pages of one layer's keys and values (and scales): copies[i][0] to copies[i][1].
+ *
+ *  copies     int32 [n, 2]; a pair with an entry outside [0, n_pages), or with twice the same, is skipped.
+ *  n_copies   int32 [1], or NULL for n: pairs 0..min(n, n_copies)-1.
+ * No page may be written by one pair and read or written by another (in the lists of the calls above
+ * none is): its contents are then those of any of them.
+ */
+PLDP_API pldp_status pldp_cache_copy_pages(const pldp_cache* cache, const int32_t* copies, int n, const int32_t* n_copies,
+                                           void* stream);
 
 /* Message describing the last failed call on this host thread ("" if none). */
 PLDP_API const char* pldp_last_error(void);

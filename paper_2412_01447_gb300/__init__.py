@@ -23,7 +23,10 @@ step's draft).  Also ``pldp_rank_hidden_avg``
 Around the target model's forward pass over x_t and the draft, on a paged cache
 (class ``pldp_cache``): ``pldp_cache_append``, ``pldp_attend_cache``,
 ``pldp_rank_cache`` (Eq. 2 from the cache), ``pldp_cache_read``; and
-``pldp_token_logprobs`` on its logits.
+``pldp_token_logprobs`` on its logits.  Prompts of different lengths, packed:
+``pldp_cache_append_prompt``, ``pldp_attend_prompt``.  The cache's pages (class
+``pldp_page_table``): ``pldp_pages_reserve``, ``pldp_pages_fork``, ``pldp_pages_free``,
+``pldp_pages_compact``, ``pldp_cache_copy_pages``.
 
 The marshalling of the calls a decode step makes is native as well
 (``csrc/host_calls.cpp``), with the Python below as its wording of errors.
@@ -61,6 +64,9 @@ __all__ = [
     "pldp_cache", "pldp_cache_args", "pldp_cache_append", "pldp_cache_append_args", "pldp_cache_read",
     "pldp_cache_read_args", "pldp_attend_cache", "pldp_attend_args", "pldp_attend_workspace_size",
     "pldp_rank_cache", "pldp_rank_cache_args", "pldp_token_logprobs", "pldp_token_logprobs_workspace_size",
+    "pldp_cache_append_prompt", "pldp_cache_append_prompt_args", "pldp_attend_prompt", "pldp_attend_prompt_args",
+    "pldp_attend_prompt_workspace_size", "pldp_page_table", "pldp_page_table_args", "pldp_pages_workspace_size",
+    "pldp_pages_reserve", "pldp_pages_fork", "pldp_pages_free", "pldp_pages_compact", "pldp_cache_copy_pages",
     "pldp_version", "pldp_last_error",
 ]
 
@@ -198,6 +204,40 @@ class pldp_rank_cache_args(ctypes.Structure):
     ]
 
 
+_ROW_STRIDES = ctypes.c_int64 * 2
+
+
+class pldp_cache_append_prompt_args(ctypes.Structure):
+    """Mirror of the C argument block of pldp_cache_append_prompt (include/pldp.h)."""
+    _fields_ = [
+        ("cache", pldp_cache_args), ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("dtype", ctypes.c_int), ("B", ctypes.c_int), ("R", ctypes.c_int), ("q_heads", ctypes.c_int),
+        ("q_strides", _ROW_STRIDES), ("k_strides", _ROW_STRIDES), ("v_strides", _ROW_STRIDES),
+        ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p), ("eps", ctypes.c_float),
+        ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("rot", ctypes.c_int), ("interleaved", ctypes.c_int),
+        ("rot_rows", ctypes.c_int64), ("rows", ctypes.c_void_p), ("start", ctypes.c_void_p),
+        ("q_out", ctypes.c_void_p), ("q_out_strides", _ROW_STRIDES), ("status", ctypes.c_void_p),
+    ]
+
+
+class pldp_attend_prompt_args(ctypes.Structure):
+    """Mirror of the C argument block of pldp_attend_prompt (include/pldp.h)."""
+    _fields_ = [
+        ("cache", pldp_cache_args), ("q", ctypes.c_void_p), ("B", ctypes.c_int), ("R", ctypes.c_int),
+        ("q_heads", ctypes.c_int), ("q_strides", _ROW_STRIDES), ("rows", ctypes.c_void_p), ("start", ctypes.c_void_p),
+        ("scale", ctypes.c_float), ("out", ctypes.c_void_p), ("out_strides", _ROW_STRIDES), ("lse", ctypes.c_void_p),
+        ("status", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class pldp_page_table_args(ctypes.Structure):
+    """Mirror of the C description of a page table, pldp_page_table (include/pldp.h)."""
+    _fields_ = [
+        ("pages", ctypes.c_void_p), ("pages_stride", ctypes.c_int64), ("B", ctypes.c_int), ("max_pages", ctypes.c_int),
+        ("page_size", ctypes.c_int), ("refs", ctypes.c_void_p), ("n_pages", ctypes.c_int),
+    ]
+
+
 def library_path() -> str:
     return _build.LIB
 
@@ -293,7 +333,9 @@ def _load():
             lib.pldp_verify_sample_workspace_size.argtypes = [i32, i32, i32, i32]
             lib.pldp_verify_sample_workspace_size.restype = sz
             for f, block in (("pldp_cache_append", pldp_cache_append_args), ("pldp_cache_read", pldp_cache_read_args),
-                             ("pldp_attend_cache", pldp_attend_args), ("pldp_rank_cache", pldp_rank_cache_args)):
+                             ("pldp_attend_cache", pldp_attend_args), ("pldp_rank_cache", pldp_rank_cache_args),
+                             ("pldp_cache_append_prompt", pldp_cache_append_prompt_args),
+                             ("pldp_attend_prompt", pldp_attend_prompt_args)):
                 getattr(lib, f).argtypes = [ctypes.POINTER(block), P]
                 getattr(lib, f).restype = ctypes.c_int
             lib.pldp_attend_workspace_size.argtypes = [i32, i32, i32, i32, i32]
@@ -302,6 +344,18 @@ def _load():
             lib.pldp_token_logprobs.restype = ctypes.c_int
             lib.pldp_token_logprobs_workspace_size.argtypes = [i64, i32]
             lib.pldp_token_logprobs_workspace_size.restype = sz
+            lib.pldp_attend_prompt_workspace_size.argtypes = [i32, i32, i32]
+            lib.pldp_attend_prompt_workspace_size.restype = sz
+            table = ctypes.POINTER(pldp_page_table_args)
+            lib.pldp_pages_workspace_size.argtypes = [i32, i32, i32]
+            lib.pldp_pages_workspace_size.restype = sz
+            lib.pldp_pages_reserve.argtypes = [table, P, P, i32, P, P, P, sz, P]
+            lib.pldp_pages_fork.argtypes = [table, P, P, P, P]
+            lib.pldp_pages_free.argtypes = [table, P, P]
+            lib.pldp_pages_compact.argtypes = [table, P, i32, P, P, P, sz, P]
+            lib.pldp_cache_copy_pages.argtypes = [ctypes.POINTER(pldp_cache_args), P, i32, P, P]
+            for f in ("pldp_pages_reserve", "pldp_pages_fork", "pldp_pages_free", "pldp_pages_compact", "pldp_cache_copy_pages"):
+                getattr(lib, f).restype = ctypes.c_int
             lib.pldp_last_error.argtypes = []
             lib.pldp_last_error.restype = ctypes.c_char_p
             lib.pldp_version.argtypes = []
@@ -1013,6 +1067,180 @@ def pldp_token_logprobs(logits, tokens, logprob, workspace, entropy=None, top_id
         _dense(top_id, "top_id", torch.int32, allow_none=True, n=rows * top),
         _dense(top_logprob, "top_logprob", torch.float32, allow_none=True, n=rows * top),
         _dense(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+# ----------------------------------------------------------------------------
+# prompts, packed
+# ----------------------------------------------------------------------------
+def _packed(t, name, shape, dtypes):
+    """A [rows, heads, head_dim] tensor of `shape` (None: any) with unit inner stride; returns
+    (pointer, its two strides)."""
+    p = _dev(t, name)
+    if t.dim() != 3 or t.stride(2) != 1 or t.dtype not in dtypes:
+        raise ValueError(f"{name} must be [rows, heads, head_dim] of {' or '.join(map(str, dtypes))} with unit inner stride")
+    if any(w is not None and w != g for w, g in zip(shape, t.shape)):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, the call needs {shape}")
+    return p, _ROW_STRIDES(*t.stride()[:2])
+
+
+def _sequences(cache, rows, q):
+    """The number of sequences of `rows`, and the cache's description."""
+    p = _dense(rows, "rows", torch.int32)
+    if rows.dim() != 1 or rows.numel() < 1:
+        raise ValueError("rows must be [B + 1]")
+    args = _step_cache(cache, rows.numel() - 1)
+    if q.shape[2] != cache.head_dim:
+        raise ValueError(f"q has head_dim {q.shape[2]}, the cache {cache.head_dim}")
+    return p, rows.numel() - 1, args
+
+
+def pldp_cache_append_prompt(cache, q, k, v, rows, q_out, start=None, q_norm=None, k_norm=None, eps=1e-6, cos=None, sin=None,
+                             interleaved=False, status=None, stream=None):
+    """pldp_cache_append of prompts packed behind one another: rows rows[b] .. rows[b+1]-1 (int32
+    [B + 1]) of q [rows, q_heads, head_dim] and of k and v [rows, heads, head_dim] are sequence b's
+    tokens at positions start[b] (int32 [B], None: 0) and on.  Other arguments as pldp_cache_append."""
+    kinds = (torch.float32, torch.bfloat16)
+    a = pldp_cache_append_prompt_args()
+    a.q, a.q_strides = _packed(q, "q", (None,) * 3, kinds)
+    R, Hq, D = q.shape
+    a.rows, a.B, a.cache = _sequences(cache, rows, q)
+    a.k, a.k_strides = _packed(k, "k", (R, cache.heads, D), (q.dtype,))
+    a.v, a.v_strides = _packed(v, "v", (R, cache.heads, D), (q.dtype,))
+    a.q_out, a.q_out_strides = _packed(q_out, "q_out", (R, Hq, D), (torch.bfloat16,))
+    a.dtype, a.R, a.q_heads, a.eps = _code(q.dtype), R, Hq, float(eps)
+    a.q_norm = _dense(q_norm, "q_norm", q.dtype, allow_none=True, n=D)
+    a.k_norm = _dense(k_norm, "k_norm", q.dtype, allow_none=True, n=D)
+    if cos is not None or sin is not None:
+        if cos is None or sin is None or cos.dim() != 2 or cos.shape != sin.shape:
+            raise ValueError("cos and sin must both be [positions, rot/2]")
+        a.cos, a.sin = _dense(cos, "cos", torch.float32), _dense(sin, "sin", torch.float32)
+        if cos.numel() == 0:                             # an empty tensor's null pointer would mean no rotation
+            raise PldpError("pldp_cache_append_prompt", PLDP_ERR_INVALID_ARG, "rot must be even, 2..head_dim, and rot_rows >= 1")
+        a.rot_rows, a.rot = cos.shape[0], 2 * cos.shape[1]
+    a.interleaved = int(bool(interleaved))
+    a.start = _dense(start, "start", torch.int32, allow_none=True, n=a.B)
+    a.status = _dense(status, "status", _WORD, allow_none=True, n=a.B)
+    _check("pldp_cache_append_prompt", _load().pldp_cache_append_prompt(ctypes.byref(a), _stream(stream)))
+
+
+def pldp_attend_prompt_workspace_size(q_heads, heads, head_dim) -> int:
+    return int(_load().pldp_attend_prompt_workspace_size(q_heads, heads, head_dim))
+
+
+def pldp_attend_prompt(cache, q, rows, out, workspace, start=None, lse=None, scale=None, status=None, stream=None):
+    """Causal attention over the cache of prompts packed behind one another (appended before): rows
+    rows[b] .. rows[b+1]-1 (int32 [B + 1]) of q and out, bfloat16 [rows, q_heads, head_dim], are
+    sequence b's tokens at positions start[b] (int32 [B], None: 0) and on, behind whatever the cache
+    holds of it before.  lse float32 [rows, q_heads] (optional); scale default 1/sqrt(head_dim).
+    workspace: uint8 CUDA tensor of pldp_attend_prompt_workspace_size(q_heads, heads, head_dim)
+    bytes, 256-byte aligned; calls of any lengths that follow one another may share it."""
+    a = pldp_attend_prompt_args()
+    a.q, a.q_strides = _packed(q, "q", (None,) * 3, (torch.bfloat16,))
+    R, Hq, D = q.shape
+    a.rows, a.B, a.cache = _sequences(cache, rows, q)
+    a.out, a.out_strides = _packed(out, "out", (R, Hq, D), (torch.bfloat16,))
+    a.R, a.q_heads = R, Hq
+    a.scale = D ** -0.5 if scale is None else float(scale)
+    a.start = _dense(start, "start", torch.int32, allow_none=True, n=a.B)
+    a.lse = _dense(lse, "lse", torch.float32, allow_none=True, n=R * Hq)
+    a.status = _dense(status, "status", _WORD, allow_none=True, n=a.B)
+    a.workspace = _dense(workspace, "workspace")
+    a.workspace_bytes = workspace.numel() * workspace.element_size()
+    _check("pldp_attend_prompt", _load().pldp_attend_prompt(ctypes.byref(a), _stream(stream)))
+
+
+# ----------------------------------------------------------------------------
+# the pages of a cache
+# ----------------------------------------------------------------------------
+class pldp_page_table:
+    """The page table of a cache (one for all layers) with the number of entries that hold each
+    page: the description of pldp_page_table in include/pldp.h, made and checked once (it keeps
+    the tensors alive).
+
+    pages       int32 [B, max_pages], rows may be strided; -1: no page.
+    refs        int32 [n_pages], contiguous.
+    page_size   positions of a page.
+    """
+
+    def __init__(self, pages, refs, page_size):
+        p, stride, max_pages = _rows(pages, "pages")
+        a = self.args = pldp_page_table_args()
+        a.pages, a.pages_stride, a.B, a.max_pages, a.page_size = p, stride, pages.shape[0], max_pages, int(page_size)
+        if not isinstance(refs, torch.Tensor) or refs.dim() != 1:
+            raise ValueError("refs must be an int32 CUDA tensor [n_pages]")
+        a.refs, a.n_pages = _dense(refs, "refs", torch.int32), refs.numel()
+        self.B, self.max_pages, self.page_size, self.n_pages = a.B, max_pages, int(page_size), a.n_pages
+        self.address = ctypes.addressof(a)                   # for the native calls
+        self.tensors = (pages, refs)
+
+
+def _table(table):
+    if not isinstance(table, pldp_page_table):
+        raise ValueError("table must be a pldp_page_table")
+    return ctypes.byref(table.args)
+
+
+def _pairs(copies, name="copies", n=None):
+    """int32 [n, 2], contiguous: (pointer, n)."""
+    p = _dense(copies, name, torch.int32)
+    if copies.dim() != 2 or copies.shape[1] != 2 or (n is not None and copies.shape[0] != n):
+        raise ValueError(f"{name} must be [{'n' if n is None else n}, 2]")
+    return p, copies.shape[0]
+
+
+def pldp_pages_workspace_size(table) -> int:
+    _table(table)
+    return int(_load().pldp_pages_workspace_size(table.B, table.max_pages, table.n_pages))
+
+
+def pldp_pages_reserve(table, start, copies, workspace, n, count=None, status=None, stream=None):
+    """Makes positions start[b] .. start[b]+count[b]-1 (int32 [B]; count None: n, which is the most)
+    of every sequence ones that may be written: the lowest free pages for those that have none, and
+    for pages that others hold too.  copies int32 [B, 2]: the page that pldp_cache_copy_pages then has
+    to copy in every layer, and where to.  workspace: uint8 CUDA tensor of
+    pldp_pages_workspace_size(table) bytes."""
+    t = _table(table)
+    _check("pldp_pages_reserve", _load().pldp_pages_reserve(
+        t, _dense(start, "start", torch.int32, n=table.B), _dense(count, "count", torch.int32, allow_none=True, n=table.B), int(n),
+        _pairs(copies, n=table.B)[0], _dense(status, "status", _WORD, allow_none=True, n=table.B), _dense(workspace, "workspace"),
+        workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def pldp_pages_fork(table, parent, len, status=None, stream=None):
+    """Row b of the table becomes those of row parent[b]'s entries that hold its first len[b]
+    positions, shared with it (int32 [B]; parent -1: the row stays as it is)."""
+    t = _table(table)
+    _check("pldp_pages_fork", _load().pldp_pages_fork(
+        t, _dense(parent, "parent", torch.int32, n=table.B), _dense(len, "len", torch.int32, n=table.B),
+        _dense(status, "status", _WORD, allow_none=True, n=table.B), _stream(stream)))
+
+
+def pldp_pages_free(table, keep_len, stream=None):
+    """Gives back the pages past each sequence's first keep_len[b] positions (int32 [B]; 0: all of
+    them, negative: none)."""
+    t = _table(table)
+    _check("pldp_pages_free", _load().pldp_pages_free(t, _dense(keep_len, "keep_len", torch.int32, n=table.B), _stream(stream)))
+
+
+def pldp_pages_compact(table, copies, n_copies, workspace, used=None, stream=None):
+    """Moves the held pages to the front of the pool in the table and refs; copies int32 [at least
+    n_pages // 2, 2] and n_copies int32 [1] are what pldp_cache_copy_pages then has to copy in every
+    layer, used (int32 [1], optional) the number of held pages."""
+    t = _table(table)
+    p, cap = _pairs(copies)
+    _check("pldp_pages_compact", _load().pldp_pages_compact(
+        t, p, cap, _dense(n_copies, "n_copies", torch.int32, n=1), _dense(used, "used", torch.int32, allow_none=True, n=1),
+        _dense(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def pldp_cache_copy_pages(cache, copies, n_copies=None, stream=None):
+    """Copies pages of one layer's cache, copies[i, 0] to copies[i, 1] (int32 [n, 2]; pairs with an
+    entry that is no page are skipped), the first n_copies[0] pairs (int32 [1], None: all)."""
+    if not isinstance(cache, pldp_cache):
+        raise ValueError("cache must be a pldp_cache")
+    p, n = _pairs(copies)
+    _check("pldp_cache_copy_pages", _load().pldp_cache_copy_pages(
+        ctypes.byref(cache.args), p, n, _dense(n_copies, "n_copies", torch.int32, allow_none=True, n=1), _stream(stream)))
 
 
 def pldp_version() -> int:

@@ -27,6 +27,8 @@ size_t space_of(int64_t n, int64_t q_heads, int64_t heads, int head_dim) {
     return kTicketBytes + static_cast<size_t>(2 * kMaxCtas) * nt * (padded_dim(head_dim) + 2) * sizeof(float);
 }
 
+}  // namespace
+
 // The pool as a tensor of (element, position, head, page), its middle dimensions by ascending
 // stride, copied in boxes of `box` positions of one head of one page: 64 elements of bf16, swizzled as the
 // matrix instructions read them, or a whole vector of codes.
@@ -56,7 +58,6 @@ bool pool_map(CUtensorMap* map, void* base, const CacheView& c, bool e4m3, int b
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-}  // namespace
 }  // namespace pldp
 
 using namespace pldp;

@@ -1,4 +1,4 @@
-// The paged cache around a step: pldp_cache_append and pldp_cache_read.
+// The paged cache around a step and of prompts: pldp_cache_append, pldp_cache_append_prompt and pldp_cache_read.
 #include <cuda_fp8.h>
 #include <math.h>
 
@@ -75,8 +75,9 @@ struct AppendArgs {
     Strides qs, ks, vs, os;
     const float *cos, *sin;
     const int32_t *seq_len, *draft_len;
+    const int32_t *rows, *start;        // of packed tokens, in place of the two above
     uint32_t* status;
-    int n, q_heads, rot, interleaved, capacity;
+    int B, n, q_heads, rot, interleaved, capacity;
     uint32_t tokens, at_once;           // tokens in all, and a CTA's at a time
     int share;                          // groups of lanes a token
     float eps, inverse_dim;
@@ -131,9 +132,17 @@ struct Raw {                            // eight elements as they are in memory
 // cosines and sines of this lane's elements) is worked out once a token.
 // 4 x 4095 tokens of 48 heads of 128, bf16 to e4m3, with the read of the last positions behind it: 99 us (428 MB,
 // 4.3 TB/s); 1 x 11 tokens, fp32 to bf16: 5.3 us, two launches' latency.
-template <typename T, int GS, bool E4M3>
+// PACKED: prompts of different lengths behind one another; a token looks its sequence up (its CTA's last one, or by
+// bisection), and the first CTA tells what is wrong with the sequences.
+template <typename T, int GS, bool E4M3, bool PACKED>
 __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_kernel(const AppendArgs a) {
     pdl_enter();
+    if (PACKED && a.status && blockIdx.x == 0 && blockIdx.y == 0)
+        for (int b = threadIdx.x; b < a.B; b += kAppendThreads) {
+            uint32_t st;
+            packed_rows(a.rows, a.start, b, static_cast<int>(a.tokens), a.capacity, st);
+            if (st) atomicOr(a.status + b, st);
+        }
     constexpr int kGroups = kAppendThreads / GS;
     __shared__ __align__(16) float stage[2][kGroups][GS * 8];
     const CacheView& c = a.c;
@@ -151,9 +160,17 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
     // The stage's two places, in turn from one rotated vector to the next, over the end of a token as well: the one barrier
     // between a place's write and its reads then also lies between those reads and the write after next.
     int turn = 0;
+    [[maybe_unused]] int in = 0;                       // the last packed token's sequence
 #pragma unroll 1
     for (uint32_t token = blockIdx.x * a.at_once + sub; token < a.tokens; token += gridDim.x * a.at_once) {
-        const int b = token / static_cast<uint32_t>(a.n), i = token - b * a.n;
+        int b, i;
+        if constexpr (PACKED) {
+            // (strides of one sequence: i counts from the first row of all)
+            in = sequence_of(a.rows, a.B, static_cast<int>(token), in);
+            b = 0, i = token;
+        } else {
+            b = token / static_cast<uint32_t>(a.n), i = token - b * a.n;
+        }
         const T* q = static_cast<const T*>(a.q) + (b * a.qs.seq + i * a.qs.tok + e0);
         const T* k = static_cast<const T*>(a.k) + (b * a.ks.seq + i * a.ks.tok + e0);
         const T* v = static_cast<const T*>(a.v) + (b * a.vs.seq + i * a.vs.tok + e0);
@@ -162,11 +179,19 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
         };
         Raw<T> next;
         if (first < total && live) next.load(source(first));
-        uint32_t st;
-        const StepTokens tk = step_tokens(a.seq_len, a.draft_len, b, a.n, a.capacity, st);
-        if (i == 0 && first == 0 && at == 0 && st && a.status) atomicOr(a.status + b, st);
-        if (i >= tk.count) continue;
-        const int pos = tk.first + i;
+        int pos, seq;
+        if constexpr (PACKED) {
+            uint32_t st;
+            const PackedRows pr = packed_rows(a.rows, a.start, in, static_cast<int>(a.tokens), a.capacity, st);
+            if (i < pr.row || i - pr.row >= pr.count) continue;
+            pos = pr.first + (i - pr.row), seq = in;
+        } else {
+            uint32_t st;
+            const StepTokens tk = step_tokens(a.seq_len, a.draft_len, b, a.n, a.capacity, st);
+            if (i == 0 && first == 0 && at == 0 && st && a.status) atomicOr(a.status + b, st);
+            if (i >= tk.count) continue;
+            pos = tk.first + i, seq = b;
+        }
         // y' = y cs + partner sn; an element that does not rotate is its own partner, cs = 1, sn = 0
         float cs[8], sn[8];
         {
@@ -207,8 +232,8 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
             }
         }
         int64_t scale_at;
-        const int64_t off = locate(c, c.pages + b * c.pages_stride, pos, scale_at);
-        if (off < 0 && first == 0 && at == 0 && a.status) atomicOr(a.status + b, PLDP_ST_PAGE);
+        const int64_t off = locate(c, c.pages + seq * c.pages_stride, pos, scale_at);
+        if (off < 0 && first == 0 && at == 0 && a.status) atomicOr(a.status + seq, PLDP_ST_PAGE);
         auto unpack = [&](float (&y)[8]) {
             if (live) {
                 next.unpack(y);
@@ -328,7 +353,7 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
     }
 }
 
-template <typename T, int GS, bool E4M3>
+template <typename T, int GS, bool E4M3, bool PACKED>
 cudaError_t launch_append_group(AppendArgs a, cudaStream_t s) {
     // few tokens: a token's vectors over as many CTAs as take them at once (1 x 11 tokens of 48: 1 us less than with
     // one CTA a token)
@@ -347,13 +372,20 @@ cudaError_t launch_append_group(AppendArgs a, cudaStream_t s) {
         a.at_once = groups / a.share;
         ctas = (a.tokens + a.at_once - 1) / a.at_once;
     }
-    return launch_pdl(cache_append_kernel<T, GS, E4M3>, dim3(ctas < most ? ctas : most, few ? turns : 1), dim3(kAppendThreads), 0, s, 0, a);
+    if (PACKED && ctas == 0) ctas = 1;                  // (for the status)
+    return launch_pdl(cache_append_kernel<T, GS, E4M3, PACKED>, dim3(ctas < most ? ctas : most, few ? turns : 1), dim3(kAppendThreads), 0, s,
+                      0, a);
 }
-template <typename T, bool E4M3>
-cudaError_t launch_append(const AppendArgs& a, cudaStream_t s) {
-    if (a.c.head_dim <= 64) return launch_append_group<T, 8, E4M3>(a, s);
-    if (a.c.head_dim <= 128) return launch_append_group<T, 16, E4M3>(a, s);
-    return launch_append_group<T, 32, E4M3>(a, s);
+template <typename T, bool E4M3, bool PACKED>
+cudaError_t launch_append_heads(const AppendArgs& a, cudaStream_t s) {
+    if (a.c.head_dim <= 64) return launch_append_group<T, 8, E4M3, PACKED>(a, s);
+    if (a.c.head_dim <= 128) return launch_append_group<T, 16, E4M3, PACKED>(a, s);
+    return launch_append_group<T, 32, E4M3, PACKED>(a, s);
+}
+template <bool PACKED>
+cudaError_t launch_append(const AppendArgs& a, pldp_dtype dtype, bool e4m3, cudaStream_t s) {
+    if (dtype == PLDP_F32) return e4m3 ? launch_append_heads<float, true, PACKED>(a, s) : launch_append_heads<float, false, PACKED>(a, s);
+    return e4m3 ? launch_append_heads<__nv_bfloat16, true, PACKED>(a, s) : launch_append_heads<__nv_bfloat16, false, PACKED>(a, s);
 }
 
 // ---------------------------------------------------------------------------
@@ -464,6 +496,48 @@ __global__ void __launch_bounds__(kReadThreads) cache_read_kernel(const ReadArgs
 }
 
 Strides strides_of(const int64_t (&s)[3]) { return {s[0], s[1], s[2]}; }
+Strides packed_strides(const int64_t (&s)[2]) { return {0, s[0], s[1]}; }
+
+// What the two forms of append have in common: the checks without tensors ...
+template <typename Args>
+pldp_status append_form(const char* fn, const Args& p, AppendArgs* a) {
+    if (p.dtype != PLDP_F32 && p.dtype != PLDP_BF16)
+        return fail(PLDP_ERR_UNSUPPORTED, "%s: dtype %d", fn, static_cast<int>(p.dtype));
+    if (p.q_heads > 65536) return fail(PLDP_ERR_UNSUPPORTED, "%s: more than 65536 query heads", fn);
+    const pldp_status st = cache_view(fn, p.cache, p.B, &a->c);
+    if (st != PLDP_OK) return st;
+    if ((p.cos == nullptr) != (p.sin == nullptr)) return fail(PLDP_ERR_INVALID_ARG, "%s: cos and sin go together", fn);
+    if (p.cos && (p.rot < 2 || p.rot > p.cache.head_dim || p.rot % 2 || p.rot_rows < 1))
+        return fail(PLDP_ERR_INVALID_ARG, "%s: rot must be even, 2..head_dim, and rot_rows >= 1", fn);
+    if (!(p.eps >= 0.f) || !isfinite(p.eps)) return fail(PLDP_ERR_INVALID_ARG, "%s: eps must be finite and >= 0", fn);
+    return PLDP_OK;
+}
+// ... and, with the strides in `a`, those of the tensors, and what the kernel takes of them.
+template <typename Args>
+pldp_status append_tensors(const char* fn, const Args& p, AppendArgs* a) {
+    const size_t es = p.dtype == PLDP_F32 ? 4 : 2;
+    const struct { const char* name; const void* at; const Strides& s; size_t es; } tensors[] = {
+        {"q", p.q, a->qs, es}, {"k", p.k, a->ks, es}, {"v", p.v, a->vs, es}, {"q_out", p.q_out, a->os, 2}};
+    for (const auto& t : tensors) {
+        const int64_t strides[3] = {t.s.seq, t.s.tok, t.s.head};
+        const pldp_status st = check_rows(fn, t.name, t.at, strides, t.es);
+        if (st != PLDP_OK) return st;
+    }
+    if (!aligned16(p.q_norm) || !aligned16(p.k_norm) || !aligned16(p.cos) || !aligned16(p.sin))
+        return fail(PLDP_ERR_INVALID_ARG, "%s: norms, cos and sin must be 16-byte aligned", fn);
+    a->q = p.q, a->k = p.k, a->v = p.v;
+    a->q_norm = p.q_norm, a->k_norm = p.k_norm;
+    a->q_out = p.q_out;
+    a->cos = p.cos, a->sin = p.sin;
+    a->status = p.status;
+    a->B = p.B, a->q_heads = p.q_heads;
+    a->rot = p.cos ? p.rot : 0, a->interleaved = p.interleaved != 0;
+    a->capacity = a->c.capacity;
+    if (p.cos && p.rot_rows < a->capacity) a->capacity = static_cast<int>(p.rot_rows);
+    a->eps = p.eps;
+    a->inverse_dim = 1.f / p.cache.head_dim;
+    return PLDP_OK;
+}
 
 }  // namespace
 }  // namespace pldp
@@ -477,48 +551,40 @@ PLDP_API pldp_status pldp_cache_append(const pldp_cache_append_args* p, void* st
     if (!p) return fail(PLDP_ERR_INVALID_ARG, "%s: null argument block", fn);
     if (p->B < 0 || p->n < 1 || p->q_heads < 1)
         return fail(PLDP_ERR_INVALID_ARG, "%s: B < 0, n < 1 or q_heads < 1", fn);
-    if (p->dtype != PLDP_F32 && p->dtype != PLDP_BF16)
-        return fail(PLDP_ERR_UNSUPPORTED, "%s: dtype %d", fn, static_cast<int>(p->dtype));
-    if (p->q_heads > 65536) return fail(PLDP_ERR_UNSUPPORTED, "%s: more than 65536 query heads", fn);
     AppendArgs a = {};
-    pldp_status st = cache_view(fn, p->cache, p->B, &a.c);
+    pldp_status st = append_form(fn, *p, &a);
     if (st != PLDP_OK) return st;
-    if ((p->cos == nullptr) != (p->sin == nullptr)) return fail(PLDP_ERR_INVALID_ARG, "%s: cos and sin go together", fn);
-    if (p->cos && (p->rot < 2 || p->rot > p->cache.head_dim || p->rot % 2 || p->rot_rows < 1))
-        return fail(PLDP_ERR_INVALID_ARG, "%s: rot must be even, 2..head_dim, and rot_rows >= 1", fn);
-    if (!(p->eps >= 0.f) || !isfinite(p->eps)) return fail(PLDP_ERR_INVALID_ARG, "%s: eps must be finite and >= 0", fn);
     if (static_cast<int64_t>(p->B) * p->n > INT32_MAX)
         return fail(PLDP_ERR_UNSUPPORTED, "%s: B * n must be below 2^31", fn);
     if (p->B == 0) return PLDP_OK;
     if (!p->q || !p->k || !p->v || !p->q_out || !p->seq_len) return fail(PLDP_ERR_INVALID_ARG, "%s: null pointer", fn);
-    const size_t es = p->dtype == PLDP_F32 ? 4 : 2;
-    if ((st = check_rows(fn, "q", p->q, p->q_strides, es)) != PLDP_OK) return st;
-    if ((st = check_rows(fn, "k", p->k, p->k_strides, es)) != PLDP_OK) return st;
-    if ((st = check_rows(fn, "v", p->v, p->v_strides, es)) != PLDP_OK) return st;
-    if ((st = check_rows(fn, "q_out", p->q_out, p->q_out_strides, 2)) != PLDP_OK) return st;
-    if (!aligned16(p->q_norm) || !aligned16(p->k_norm) || !aligned16(p->cos) || !aligned16(p->sin))
-        return fail(PLDP_ERR_INVALID_ARG, "%s: norms, cos and sin must be 16-byte aligned", fn);
-    a.q = p->q, a.k = p->k, a.v = p->v;
-    a.q_norm = p->q_norm, a.k_norm = p->k_norm;
-    a.q_out = p->q_out;
     a.qs = strides_of(p->q_strides), a.ks = strides_of(p->k_strides), a.vs = strides_of(p->v_strides);
     a.os = strides_of(p->q_out_strides);
-    a.cos = p->cos, a.sin = p->sin;
+    if ((st = append_tensors(fn, *p, &a)) != PLDP_OK) return st;
     a.seq_len = p->seq_len, a.draft_len = p->draft_len;
-    a.status = p->status;
-    a.n = p->n, a.q_heads = p->q_heads;
-    a.rot = p->cos ? p->rot : 0, a.interleaved = p->interleaved != 0;
-    a.capacity = a.c.capacity;
-    if (p->cos && p->rot_rows < a.capacity) a.capacity = static_cast<int>(p->rot_rows);
-    a.eps = p->eps;
+    a.n = p->n;
     a.tokens = p->B * p->n;
-    a.inverse_dim = 1.f / p->cache.head_dim;
-    auto s = static_cast<cudaStream_t>(stream);
-    const bool q8 = p->cache.dtype == PLDP_E4M3;
-    cudaError_t e;
-    if (p->dtype == PLDP_F32) e = q8 ? launch_append<float, true>(a, s) : launch_append<float, false>(a, s);
-    else e = q8 ? launch_append<__nv_bfloat16, true>(a, s) : launch_append<__nv_bfloat16, false>(a, s);
-    return launched(fn, e);
+    return launched(fn, launch_append<false>(a, p->dtype, p->cache.dtype == PLDP_E4M3, static_cast<cudaStream_t>(stream)));
+}
+
+PLDP_API pldp_status pldp_cache_append_prompt(const pldp_cache_append_prompt_args* p, void* stream) {
+    const char* fn = "cache_append_prompt";
+    if (!p) return fail(PLDP_ERR_INVALID_ARG, "%s: null argument block", fn);
+    if (p->B < 0 || p->R < 0 || p->q_heads < 1)
+        return fail(PLDP_ERR_INVALID_ARG, "%s: B < 0, R < 0 or q_heads < 1", fn);
+    AppendArgs a = {};
+    pldp_status st = append_form(fn, *p, &a);
+    if (st != PLDP_OK) return st;
+    if (p->R > INT32_MAX - 256) return fail(PLDP_ERR_UNSUPPORTED, "%s: R must be below 2^31 - 256", fn);
+    if (p->B == 0) return PLDP_OK;
+    if (!p->rows || (p->R > 0 && (!p->q || !p->k || !p->v || !p->q_out)))
+        return fail(PLDP_ERR_INVALID_ARG, "%s: null pointer", fn);
+    a.qs = packed_strides(p->q_strides), a.ks = packed_strides(p->k_strides), a.vs = packed_strides(p->v_strides);
+    a.os = packed_strides(p->q_out_strides);
+    if ((st = append_tensors(fn, *p, &a)) != PLDP_OK) return st;
+    a.rows = p->rows, a.start = p->start;
+    a.tokens = p->R;
+    return launched(fn, launch_append<true>(a, p->dtype, p->cache.dtype == PLDP_E4M3, static_cast<cudaStream_t>(stream)));
 }
 
 PLDP_API pldp_status pldp_cache_read(const pldp_cache_read_args* p, void* stream) {

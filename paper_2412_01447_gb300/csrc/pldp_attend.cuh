@@ -36,6 +36,7 @@ struct AttendArgs {
 struct Maps {
     CUtensorMap k, v;
 };
+bool pool_map(CUtensorMap* map, void* base, const CacheView& c, bool e4m3, int box, int pitch, bool* head_first);
 
 // One launch for nt columns; one translation unit a cache type.
 cudaError_t launch_attend_bf16(const AttendArgs& a, const Maps& m, int nt, int ctas, cudaStream_t s);

@@ -78,4 +78,43 @@ __device__ __forceinline__ StepTokens step_tokens(const int32_t* seq_len, const 
     return {L - 1, count};
 }
 
+// The packed tokens of one sequence.
+struct PackedRows {
+    int row;     // its first one
+    int first;   // the position of that
+    int count;   // tokens with a position below the capacity; 0: nothing to do
+    int given;   // and the rows that it has in all
+};
+__device__ __forceinline__ PackedRows packed_rows(const int32_t* rows, const int32_t* start, int b, int R, int capacity,
+                                                  uint32_t& status) {
+    const int r0 = __ldg(rows + b), r1 = __ldg(rows + b + 1), p = start ? __ldg(start + b) : 0;
+    status = 0;
+    if (r0 < 0 || r1 < r0 || r1 > R) {
+        status = PLDP_ST_SEQ_LEN;
+        return {0, 0, 0, 0};
+    }
+    if (p < 0 || p > capacity) {
+        status = PLDP_ST_SEQ_LEN;
+        return {r0, 0, 0, r1 - r0};
+    }
+    int count = r1 - r0;
+    if (count > capacity - p) {
+        status = PLDP_ST_CAPACITY;
+        count = capacity - p;
+    }
+    return {r0, p, count, r1 - r0};
+}
+
+// The last sequence whose rows start at or before `row` (the first where none does); `hint` is looked at first.
+__device__ __forceinline__ int sequence_of(const int32_t* rows, int B, int row, int hint) {
+    if (__ldg(rows + hint) <= row && row < __ldg(rows + hint + 1)) return hint;
+    int lo = 0, hi = B;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (__ldg(rows + mid) <= row) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
 }  // namespace pldp

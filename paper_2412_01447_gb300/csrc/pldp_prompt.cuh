@@ -1,0 +1,933 @@
+// Causal attention of packed prompts over the paged cache: the kernel of pldp_attend_prompt (prompt.cu).
+#pragma once
+
+#include "pldp_attend.cuh"
+
+namespace pldp {
+
+struct PromptArgs {
+    CacheView c;
+    const __nv_bfloat16* q;
+    __nv_bfloat16* out;
+    int64_t q_tok, q_head, o_tok, o_head;
+    const int32_t *rows, *start;
+    float* lse;
+    uint32_t* status;
+    float* parts;                          // [2 a CTA][Part]
+    struct CutUnit* cuts;                  // [CTAs]
+    int B, R, q_heads, group;
+    int box;                               // as AttendArgs
+    int head_first;
+    int least;                             // tiles a CTA takes at least
+    float scale2;                          // |scale| * log2(e)
+    uint32_t flip;                         // what turns the signs of two queries for a negative scale
+};
+
+// A unit that several CTAs have parts of, written by the CTA in which it begins: what the join needs.
+struct CutUnit {
+    int parts;                             // 0: none
+    int first_cta;
+    int row0, rows;                        // the unit's rows of the sequence and kv head (token * group + head)
+    int row_base, kv;                      // the sequence's first row
+};
+
+// One launch; one translation unit a cache type.
+cudaError_t launch_prompt_bf16(const PromptArgs& a, const Maps& m, int ctas, cudaStream_t s);
+cudaError_t launch_prompt_e4m3(const PromptArgs& a, const Maps& m, int ctas, cudaStream_t s);
+
+__host__ __device__ constexpr int prompt_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
+__host__ __device__ constexpr int prompt_rows(int dp) { return dp == 256 ? 128 : 256; }       // rows of a unit
+// What a part of a unit leaves: per 128 rows the sums [DP / 4][128][4], then the maxima [128] and the weights' sums [128].
+__host__ __device__ constexpr int prompt_part(int dp) { return prompt_rows(dp) * (dp + 2); }
+constexpr int kPromptCtas = 192;           // at most
+
+namespace {
+
+// sum over i < n of floor((a i + b) / m), by the steps of Euclid's algorithm.
+__host__ __device__ inline uint64_t floor_sum(uint64_t n, uint64_t m, uint64_t a, uint64_t b) {
+    uint64_t sum = 0;
+    if (n == 0) return 0;
+    while (true) {
+        if (a >= m) sum += n * (n - 1) / 2 * (a / m), a %= m;
+        if (b >= m) sum += n * (b / m), b %= m;
+        const uint64_t y = a * n + b;
+        if (y < m) return sum;
+        n = y / m, b = y % m;
+        const uint64_t t = m;
+        m = a, a = t;
+    }
+}
+
+// The rows of a sequence and kv head, token * group + head, cut into units of `UR`; unit u sees the keys up to its last
+// row's token, T(u) tiles.  tiles_before: those of the units before u, u up to the number of units.
+struct Units {
+    int64_t N;         // rows
+    int group, start, count;
+};
+__device__ __forceinline__ Units units_of(const PackedRows& p, int group) {
+    return {static_cast<int64_t>(p.count) * group, group, p.first, p.count};
+}
+template <int UR>
+__device__ __forceinline__ int unit_count(const Units& s) { return static_cast<int>((s.N + UR - 1) / UR); }
+template <int UR>
+__device__ __forceinline__ int unit_tiles(const Units& s, int u) {
+    const int64_t end = min(s.N, (static_cast<int64_t>(u) + 1) * UR);
+    return (s.start + static_cast<int>(static_cast<uint32_t>(end - 1) / static_cast<uint32_t>(s.group)) + kTile) / kTile;
+}
+template <int UR>
+__device__ __forceinline__ int64_t tiles_before(const Units& s, int u) {
+    if (u == 0) return 0;
+    const int whole = static_cast<int64_t>(u) * UR > s.N ? u - 1 : u;          // the last unit may have fewer rows
+    const uint64_t m = static_cast<uint64_t>(kTile) * s.group;
+    int64_t n = floor_sum(whole, m, UR, static_cast<uint64_t>(s.start) * s.group + UR - 1 + m);
+    if (whole < u) n += unit_tiles<UR>(s, whole);
+    return n;
+}
+
+template <int DP, bool E4M3>
+struct PromptShape {
+    static constexpr int kQ = DP == 256 ? 1 : 2;               // tiles of 128 rows
+    static constexpr int kRows = kQ * 128;
+    static constexpr int kSoftmaxWarps = 4 * kQ;
+    static constexpr int kConvertWarps = E4M3 ? 4 : 0;
+    // warps: softmax, matrix instructions, copies, keys' scales, queries, conversion
+    static constexpr int kMmaWarp = kSoftmaxWarps, kCopyWarp = kMmaWarp + 1, kKeyWarp = kMmaWarp + 2, kQueryWarp = kMmaWarp + 3;
+    static constexpr int kConvertWarp = kMmaWarp + 4;
+    static constexpr int kThreads = (kSoftmaxWarps + 4 + kConvertWarps) * 32;
+    static constexpr int kPanels = DP / 64;
+    static constexpr int kSlot = kPanels * kTile * 128;
+    static constexpr int kQBytes = kQ * kPanels * 128 * 128;
+    static constexpr int kStatic = E4M3 ? 10240 : 2048;        // PromptShared
+    static constexpr int kMost = (kMaxShared - 1024 - kStatic - kQBytes) / kSlot;
+    static constexpr int kSlots = kMost > 6 ? 6 : kMost;
+    static constexpr int kBytes = kQBytes + kSlots * kSlot + 1024;
+    static constexpr int kO = 256;                             // column of the first sums
+    // 384 threads start with 168 registers each (512: 128); the softmax takes what the others leave
+    static constexpr int kSoftmaxRegs = E4M3 ? 168 : 208, kOtherRegs = E4M3 ? 56 : 88, kConvertRegs = 112;
+    static_assert(kSlots >= 2 && kBytes + kStatic <= kMaxShared, "shared memory");
+};
+
+constexpr int kAhead = 8;                  // tiles whose holes are kept (more than the ring of keys holds)
+
+template <bool E4M3>
+struct PromptShared {
+    alignas(16) float key_factor[E4M3 ? 4 : 1][E4M3 ? kTile : 4], key_log[E4M3 ? 4 : 1][E4M3 ? kTile : 4], key_inverse[E4M3 ? 4 : 1][E4M3 ? kTile : 4];
+    float back[E4M3 ? 2 : 1][E4M3 ? 256 : 1];
+    uint8_t live[kAhead][kTile];           // whether a page holds the key; looked at where `holes` is set
+    int holes[kAhead];
+    uint64_t full[8], empty[8], s_full[2], p_full[2], pv_done[2], q_full[2], q_empty[2], tail, drained,
+        key_full[4], key_empty[4];
+    uint32_t tmem;
+    int dead, zeros;
+    long long warp_sum[20];
+    long long total;
+    // where this CTA's part of the list starts
+    int b, kv, unit, tile;
+    long long at, count, each, extra;
+};
+
+// The CTA's part of the list, unit by unit: sequences, their kv heads, the units of one of those.
+template <int UR>
+struct PromptWalk {
+    int b, kv, unit, t0;
+    long long at, left;
+    // the unit's
+    PackedRows p;
+    Units s;
+    int units, T, t1;
+    int64_t r0;
+    int rows;          // below UR only in the last unit
+    int end;           // positions from here on are not the sequence's
+
+    __device__ __forceinline__ bool next(const PromptArgs& a) {
+        if (left <= 0) return false;
+        uint32_t st;
+        while (true) {                                           // (sequences without rows hold no tiles)
+            p = packed_rows(a.rows, a.start, b, a.R, a.c.capacity, st);
+            if (p.count > 0) break;
+            ++b;
+        }
+        s = units_of(p, a.group);
+        units = unit_count<UR>(s);
+        T = unit_tiles<UR>(s, unit);
+        t1 = left < T - t0 ? t0 + static_cast<int>(left) : T;
+        r0 = static_cast<int64_t>(unit) * UR;
+        rows = static_cast<int>(min(static_cast<int64_t>(UR), s.N - r0));
+        end = s.start + s.count;
+        return true;
+    }
+    __device__ __forceinline__ void step(const PromptArgs& a) {
+        at += t1 - t0;
+        left -= t1 - t0;
+        t0 = 0;
+        if (++unit == units) {
+            unit = 0;
+            if (++kv == a.c.heads) kv = 0, ++b;
+        }
+    }
+};
+
+// D += A B with A in tensor memory.
+__device__ __forceinline__ void mma_f16_tmem(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t b_hi, uint32_t form, uint32_t accumulate,
+                                             uint32_t lead) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 b;\n\t"
+        "mov.b64 b, {%2, %3};\n\t"
+        "setp.ne.u32 p, %5, 0;\n\t"
+        "setp.ne.u32 q, %6, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}"
+        ::"r"(d), "r"(a), "r"(b_lo), "r"(b_hi), "r"(form), "r"(accumulate), "r"(lead)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t* v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+        ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+          "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
+          "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
+          "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]), "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
+// ---------------------------------------------------------------------------
+// One pass over the keys that a unit sees, 128 at a time.  A unit is 256 (heads above 128 elements: 128) rows of one
+// sequence and key/value head: the rows of all of its query heads, token by token, so short prompts with grouped heads
+// fill the tensor core's 128 rows and only the last tokens' keys are masked.
+//   S [128 rows, 128 keys] = Q K^T       P = 2^(x - m)       O [128 rows, D] += P V
+// S and O of two row tiles stay in tensor memory (512 columns); P, 16 bits a weight, overwrites S and is the second
+// product's operand from there, so only queries, keys and values pass through shared memory.  A thread owns a row: its
+// maximum, sum and rescaling need no other thread.  While one tile of rows is in the softmax, the tensor core works for
+// the other.  The running maximum m of a row moves only when a score passes it by more than 2^64 (2^8 where weights are
+// f16): weights may be large, their rounding is relative.
+//
+// Weights are rounded to bf16 (2^-8 of each) over a bf16 cache, whose values need bf16's range: two terms, as a step's attention takes
+// them, would make the second product, half of the work here, twice as long.  Over an e4m3 cache codes, exact in f16, are
+// converted by warps of their own and weights are f16 (2^-11); k's scales multiply the scores, v's go into the exponent
+// and are divided out of the sums.
+//
+// The tiles of all units form one list, cut into equal parts, one a CTA (one a SM), whatever the lengths are; what
+// a part holds of a unit that others share goes to the workspace, and the join, a kernel behind this one, adds them in order.
+// ---------------------------------------------------------------------------
+template <int DP, bool E4M3>
+__global__ void __launch_bounds__(PromptShape<DP, E4M3>::kThreads, 1)
+prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+    using S = PromptShape<DP, E4M3>;
+    constexpr int UR = S::kRows, NQ = S::kQ, kThreads = S::kThreads;
+    static_assert(sizeof(PromptShared<E4M3>) <= S::kStatic, "shared memory");
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(16) PromptShared<E4M3> sh;
+    uint8_t* ring = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
+    uint8_t* const q_smem = ring + S::kSlots * S::kSlot;
+    const CacheView& c = a.c;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = c.head_dim;
+
+    if (warp == S::kMmaWarp) tmem_alloc(&sh.tmem, 512);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 8; ++i) {
+            mbar_init(&sh.full[i], E4M3 ? S::kConvertWarps : 1);
+            mbar_init(&sh.empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sh.s_full[i], 1);
+            mbar_init(&sh.p_full[i], 4);
+            mbar_init(&sh.pv_done[i], 1);
+            mbar_init(&sh.q_full[i], 1);
+            mbar_init(&sh.q_empty[i], 1);
+        }
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(&sh.key_full[i], 1);
+            mbar_init(&sh.key_empty[i], S::kSoftmaxWarps);
+        }
+        mbar_init(&sh.tail, 1);
+        mbar_init(&sh.drained, 1);
+        fence_mbar_init();
+        sh.dead = 0;
+        sh.zeros = 0;
+    }
+    pdl_enter();
+    __syncthreads();
+
+    // the list: every thread counts the tiles of a strip of sequences
+    {
+        const int strip = (a.B + kThreads - 1) / kThreads;
+        const int lo = min(a.B, static_cast<int>(threadIdx.x) * strip), hi = min(a.B, lo + strip);
+        auto tiles_of = [&](int b) -> long long {
+            uint32_t st;
+            const PackedRows p = packed_rows(a.rows, a.start, b, a.R, c.capacity, st);
+            const Units s = units_of(p, a.group);
+            return c.heads * tiles_before<UR>(s, unit_count<UR>(s));
+        };
+        long long mine = 0;
+#pragma unroll 1
+        for (int b = lo; b < hi; ++b) {
+            uint32_t st;
+            const PackedRows p = packed_rows(a.rows, a.start, b, a.R, c.capacity, st);
+            if (st && blockIdx.x == 0 && a.status) atomicOr(a.status + b, st);
+            if (p.count < p.given) sh.zeros = 1;
+            mine += tiles_of(b);
+        }
+        long long upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long t = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+            if (lane >= o) upto += t;
+        }
+        if (lane == 31) sh.warp_sum[warp] = upto;
+        __syncthreads();
+        long long total = 0;
+#pragma unroll 1
+        for (int w = 0; w < kThreads / 32; ++w) {
+            if (w == warp) upto += total;
+            total += sh.warp_sum[w];
+        }
+        // equal parts; the first `extra` CTAs take one tile more than the others
+        const long long most = (total + a.least - 1) / a.least;
+        const int ctas = static_cast<int>(most < gridDim.x ? most : gridDim.x);
+        const long long each = ctas ? total / ctas : 0, extra = ctas ? total - each * ctas : 0;
+        const long long g0 = each * blockIdx.x + min(static_cast<long long>(blockIdx.x), extra);
+        const long long g1 = g0 + each + (blockIdx.x < extra ? 1 : 0);
+        long long before = upto - mine;
+        if (blockIdx.x < ctas && before <= g0 && g0 < before + mine) {              // one thread's
+            int b = lo;
+#pragma unroll 1
+            for (;; ++b) {
+                const long long t = tiles_of(b);
+                if (g0 < before + t) break;
+                before += t;
+            }
+            uint32_t st;
+            const Units s = units_of(packed_rows(a.rows, a.start, b, a.R, c.capacity, st), a.group);
+            const int units = unit_count<UR>(s);
+            const long long per = tiles_before<UR>(s, units), in = g0 - before;
+            const int kv = static_cast<int>(in / per);
+            const long long x = in - kv * per;
+            int u0 = 0, u1 = units;                                                 // tiles_before(u0) <= x < tiles_before(u1)
+#pragma unroll 1
+            while (u1 - u0 > 1) {
+                const int mid = (u0 + u1) >> 1;
+                if (tiles_before<UR>(s, mid) <= x) u0 = mid;
+                else u1 = mid;
+            }
+            sh.b = b, sh.kv = kv, sh.unit = u0;
+            sh.tile = static_cast<int>(x - tiles_before<UR>(s, u0));
+            sh.at = g0, sh.count = g1 - g0;
+        }
+        if (threadIdx.x == 0) {
+            sh.each = each, sh.extra = extra;
+            if (blockIdx.x >= ctas) sh.count = 0;
+        }
+    }
+    tmem_before_sync();
+    __syncthreads();
+    tmem_after_sync();
+    const uint32_t tmem = sh.tmem;
+    PromptWalk<UR> w;
+    w.b = sh.b, w.kv = sh.kv, w.unit = sh.unit, w.t0 = sh.tile, w.at = sh.at, w.left = sh.count;
+    if (sh.zeros) {
+        // tokens that take no part: their rows, of all heads
+#pragma unroll 1
+        for (int b = 0; b < a.B; ++b) {
+            uint32_t st;
+            const PackedRows p = packed_rows(a.rows, a.start, b, a.R, c.capacity, st);
+            const int64_t heads = a.q_heads, chunks = D / 8, items = (p.given - p.count) * heads * chunks;
+            for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < items; i += static_cast<int64_t>(gridDim.x) * kThreads) {
+                const int64_t vec = i / chunks, row = p.row + p.count + vec / heads, h = vec % heads;
+                *reinterpret_cast<uint4*>(a.out + row * a.o_tok + h * a.o_head + (i - vec * chunks) * 8) = make_uint4(0u, 0u, 0u, 0u);
+                if (i == vec * chunks && a.lse) a.lse[row * heads + h] = -INFINITY;
+            }
+        }
+    }
+
+    if constexpr (NQ == 2) {
+        if (warp < S::kMmaWarp) more_registers<S::kSoftmaxRegs>();
+        else if (warp < S::kConvertWarp) fewer_registers<S::kOtherRegs>();
+        else fewer_registers<S::kConvertRegs>();
+    }
+    if (warp == S::kCopyWarp) {
+        // ---- copies: keys and values in turn, a box (positions of one page) a lane; e4m3: nothing, the converting warps load ----
+        if constexpr (!E4M3) {
+        constexpr int kDepth = S::kSlots;
+        const int boxes = kTile / a.box;
+        int e = 0, tile_no = 0, tails = 0;
+        bool on = true;
+#pragma unroll 1
+        while (on && w.next(a)) {
+            const int32_t* table = c.pages + w.b * c.pages_stride;
+#pragma unroll 1
+            for (int tile = w.t0; on && tile < w.t1; ++tile, ++tile_no) {
+                // boxes that hold a position of the sequence
+                const int full = min(boxes, (w.end - tile * kTile + a.box - 1) / a.box);
+                const bool tail = tile * kTile + kTile > w.end;
+#pragma unroll 1
+                for (int kv = 0; on && kv < 2; ++kv, ++e) {
+                    const CUtensorMap* map = kv ? &v_map : &k_map;
+                    const int at = e % kDepth;
+                    if (e >= kDepth) wait_for(&sh.empty[at], e / kDepth - 1, &sh.dead);
+                    on = !__any_sync(0xFFFFFFFFu, *static_cast<volatile int*>(&sh.dead));
+                    if (!on) break;
+                    uint64_t* const bar = tail && kv ? &sh.tail : &sh.full[at];
+                    if (lane == 0) mbar_arrive_expect_tx(bar, full * a.box * S::kPanels * 128);
+                    __syncwarp();
+                    uint8_t* dst = ring + at * S::kSlot;
+                    bool hole = false;
+#pragma unroll 1
+                    for (int box = lane; box < full; box += 32) {
+                        const int pos = tile * kTile + box * a.box;
+                        const int pg_at = page_of(pos, c.div_mul, c.div_shift), slot = pos - pg_at * c.page_size;
+                        int pg = __ldg(table + pg_at);
+                        if (static_cast<unsigned>(pg) >= static_cast<unsigned>(c.n_pages)) {
+                            pg = c.n_pages;                                // outside the tensor: zeros
+                            hole = true;
+                        }
+                        const int c1 = a.head_first ? w.kv : slot, c2 = a.head_first ? slot : w.kv;
+#pragma unroll 1
+                        for (int p = 0; p < S::kPanels; ++p)
+                            tma_box(dst + p * (kTile * 128) + box * a.box * 128, map, p * 64, c1, c2, pg, bar);
+                    }
+                    if (kv == 0) {
+                        hole = __any_sync(0xFFFFFFFFu, hole);
+                        if (hole) {
+#pragma unroll 1
+                            for (int i = lane; i < kTile; i += 32) {
+                                const int pos = tile * kTile + i;
+                                const int pg = pos < w.end ? __ldg(table + page_of(pos, c.div_mul, c.div_shift)) : 0;
+                                sh.live[tile_no % kAhead][i] = static_cast<unsigned>(pg) < static_cast<unsigned>(c.n_pages);
+                            }
+                            if (lane == 0 && a.status) atomicOr(a.status + w.b, PLDP_ST_PAGE);
+                        }
+                        if (lane == 0) sh.holes[tile_no % kAhead] = hole;
+                    }
+                    if (tail && kv) {
+                        // what the pages hold past the end is not used: zeros, in the values' tile
+                        wait_for(&sh.tail, tails, &sh.dead);
+                        ++tails;
+#pragma unroll 1
+                        for (int r = w.end - tile * kTile; r < kTile; ++r)
+#pragma unroll 1
+                            for (int p = lane; p < 8 * S::kPanels; p += 32)
+                                *reinterpret_cast<uint4*>(dst + (p >> 3) * (kTile * 128) + r * 128 + (p & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                        fence_smem_async();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&sh.full[at]);
+                    }
+                    __syncwarp();
+                }
+            }
+            w.step(a);
+        }
+        // the last copy into each place arrives before this CTA ends, whether or not its reader has waited for it
+        if (lane < kDepth) {
+            const int x = e - 1 - ((e - 1 - lane) % kDepth + kDepth) % kDepth;
+            if (x >= 0) mbar_wait(&sh.full[lane], (x / kDepth) & 1, kMbarPolls);
+        } else if (lane == 31 && tails > 0) {
+            mbar_wait(&sh.tail, (tails - 1) & 1, kMbarPolls);
+        }
+        }
+    } else if (warp == S::kKeyWarp) {
+        // ---- e4m3: the scales of each tile, four keys a lane ----
+        if constexpr (E4M3) {
+            int tile_no = 0;
+#pragma unroll 1
+            while (w.next(a)) {
+                const int32_t* table = c.pages + w.b * c.pages_stride;
+#pragma unroll 1
+                for (int tile = w.t0; tile < w.t1; ++tile, ++tile_no) {
+                    const int at = tile_no & 3;
+                    float f[4], g[4], inv[4];
+                    bool gone[4], hole = false;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int pos = tile * kTile + 4 * lane + i;
+                        f[i] = 0.f, g[i] = 0.f, inv[i] = 1.f;
+                        gone[i] = false;
+                        if (pos < w.end) {
+                            const int pg_at = page_of(pos, c.div_mul, c.div_shift), pg = __ldg(table + pg_at);
+                            gone[i] = static_cast<unsigned>(pg) >= static_cast<unsigned>(c.n_pages);
+                            hole |= gone[i];
+                            if (!gone[i]) {
+                                const int64_t from = (static_cast<int64_t>(pg) * c.heads + w.kv) * c.page_size + (pos - pg_at * c.page_size);
+                                const float v = fmaxf(__ldg(c.v_scale + from), kLeastScale);
+                                // (the logarithm is 2^-22 off at most, as much as the weight's own exponential)
+                                f[i] = __ldg(c.k_scale + from), g[i] = __log2f(v), inv[i] = reciprocal(v);
+                            }
+                        }
+                    }
+                    if (tile_no >= 4) wait_for(&sh.key_empty[at], (tile_no >> 2) - 1, &sh.dead);
+                    *reinterpret_cast<float4*>(&sh.key_factor[at][4 * lane]) = make_float4(f[0], f[1], f[2], f[3]);
+                    *reinterpret_cast<float4*>(&sh.key_log[at][4 * lane]) = make_float4(g[0], g[1], g[2], g[3]);
+                    *reinterpret_cast<float4*>(&sh.key_inverse[at][4 * lane]) = make_float4(inv[0], inv[1], inv[2], inv[3]);
+                    hole = __any_sync(0xFFFFFFFFu, hole);
+                    if (hole) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sh.live[tile_no % kAhead][4 * lane + i] = !gone[i];
+                        if (lane == 0 && a.status) atomicOr(a.status + w.b, PLDP_ST_PAGE);
+                    }
+                    if (lane == 0) sh.holes[tile_no % kAhead] = hole;
+                    __syncwarp();
+                    mbar_arrive_if(&sh.key_full[at], lane == 0);
+                }
+                w.step(a);
+            }
+        }
+    } else if (warp == S::kQueryWarp) {
+        // ---- queries of the next unit, as soon as the last scores of this one are done ----
+        int seg[2] = {0, 0};
+#pragma unroll 1
+        while (w.next(a)) {
+#pragma unroll 1
+            for (int q = 0; q < NQ; ++q) {
+                if (q * 128 >= w.rows) break;
+                if (seg[q] > 0) wait_for(&sh.q_empty[q], seg[q] - 1, &sh.dead);
+                // a lane has a piece of 16 bytes of a row, DP / 8 lanes a row, or all of them several
+                constexpr int kLanes = DP / 8 < 32 ? DP / 8 : 32, kAt = 32 / kLanes, kBatch = 8;
+                const int piece = lane % kLanes;
+                uint8_t* const to = q_smem + q * (S::kPanels * 128 * 128) + (piece >> 3) * (128 * 128);
+#pragma unroll 1
+                for (int row0 = 0; row0 < 128; row0 += kAt * kBatch) {
+                    uint4 x[kBatch];
+#pragma unroll
+                    for (int i = 0; i < kBatch; ++i) {
+                        const int row = row0 + i * kAt + lane / kLanes;
+                        const int64_t r = w.r0 + q * 128 + row;
+                        x[i] = make_uint4(0u, 0u, 0u, 0u);
+                        if (r < w.s.N && piece * 8 < D) {
+                            const uint32_t tok = static_cast<uint32_t>(r) / static_cast<uint32_t>(a.group), h = static_cast<uint32_t>(r) - tok * a.group;
+                            x[i] = *reinterpret_cast<const uint4*>(a.q + (w.p.row + static_cast<int64_t>(tok)) * a.q_tok +
+                                                                   (static_cast<int64_t>(w.kv) * a.group + h) * a.q_head + piece * 8);
+                            x[i].x ^= a.flip, x[i].y ^= a.flip, x[i].z ^= a.flip, x[i].w ^= a.flip;
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < kBatch; ++i) {
+                        const int row = row0 + i * kAt + lane / kLanes;
+                        if constexpr (E4M3) {
+                            // bf16 to f16: the row's largest element to 2^14..2^15 by a power of two
+                            uint32_t v[4] = {x[i].x, x[i].y, x[i].z, x[i].w}, most = 0;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) most = max(most, max((v[k] << 16) & 0x7FFF0000u, v[k] & 0x7FFF0000u));
+#pragma unroll
+                            for (int o = kLanes / 2; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+                            const int ex = static_cast<int>(most >> 23);
+                            const int up = ex == 0 || ex == 255 ? 0 : min(14 - (ex - 127), 120);
+                            const float lift = __uint_as_float(static_cast<uint32_t>(up + 127) << 23);
+                            if (piece == 0) sh.back[seg[q] & 1][q * 128 + row] = __uint_as_float(static_cast<uint32_t>(127 - up) << 23);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                v[k] = pack_f16(__uint_as_float(v[k] << 16) * lift, __uint_as_float(v[k] & 0xFFFF0000u) * lift);
+                            x[i] = make_uint4(v[0], v[1], v[2], v[3]);
+                        }
+                        *reinterpret_cast<uint4*>(to + row * 128 + (((piece & 7) ^ (row & 7)) << 4)) = x[i];
+                    }
+                }
+                fence_smem_async();
+                __syncwarp();
+                mbar_arrive_if(&sh.q_full[q], lane == 0);
+                ++seg[q];
+            }
+            w.step(a);
+        }
+    } else if (warp == S::kMmaWarp) {
+        // ---- matrix instructions ----
+        const uint64_t q_op = smem_operand(smem_u32(q_smem), 16, 1024, swizzle_mode(128));
+        const uint64_t k_op = smem_operand(smem_u32(ring), 16, 1024, swizzle_mode(128));
+        const uint64_t v_op = smem_operand(smem_u32(ring), kTile * 128, 1024, swizzle_mode(128));
+        const uint32_t q_lo = static_cast<uint32_t>(q_op), q_hi = q_op >> 32, k_lo = static_cast<uint32_t>(k_op), k_hi = k_op >> 32;
+        const uint32_t v_lo = static_cast<uint32_t>(v_op), v_hi = v_op >> 32;
+        constexpr uint32_t kScores = mma_form(128, 128, !E4M3, false, false);
+        const uint32_t values = mma_form(128, D, !E4M3, false, true);
+        const uint32_t lead = elect_lane();
+        int e = 0;                                       // entry of the ring
+        int seg[2] = {0, 0}, s_no[2] = {0, 0}, p_no[2] = {0, 0};     // units, scores and weights of each tile of rows so far
+        auto scores = [&](int q, int slot, int at) {     // S of a tile of rows, to place `at`
+            const uint32_t op = k_lo + slot * (S::kSlot / 16), qo = q_lo + q * (S::kPanels * 128 * 128 / 16);
+#pragma unroll
+            for (int s = 0; s < DP / 16; ++s)
+                if (s * 16 < D)
+                    mma_f16(tmem + at * 128, qo + (s >> 2) * (128 * 8) + (s & 3) * 2, q_hi, op + (s >> 2) * (kTile * 8) + (s & 3) * 2, k_hi,
+                            kScores, s > 0, lead);
+            mma_commit(&sh.s_full[at], lead);
+        };
+        auto sums = [&](int q, int slot, int at, bool more) {
+            const uint32_t op = v_lo + slot * (S::kSlot / 16);
+#pragma unroll
+            for (int s = 0; s < kTile / 16; ++s)
+                mma_f16_tmem(tmem + S::kO + q * DP, tmem + at * 128 + s * 8, op + s * 128, v_hi, values, s > 0 || more, lead);
+            mma_commit(&sh.pv_done[q], lead);
+        };
+        auto arrived = [&](int entry) { wait_for(&sh.full[entry % S::kSlots], entry / S::kSlots, &sh.dead); };
+#pragma unroll 1
+        while (w.next(a)) {
+            const int n = w.t1 - w.t0, nq = w.rows > 128 ? 2 : 1;
+            if constexpr (NQ == 2) {
+                // tile i: entry e + 2 i keys, e + 2 i + 1 values
+                arrived(e);
+#pragma unroll 1
+                for (int q = 0; q < nq; ++q) {
+                    wait_for(&sh.q_full[q], seg[q], &sh.dead);
+                    __syncwarp();
+                    tmem_after_sync();
+                    scores(q, e % S::kSlots, q);
+                    if (n == 1) mma_commit(&sh.q_empty[q], lead);
+                }
+                mma_commit(&sh.empty[e % S::kSlots], lead);
+#pragma unroll 1
+                for (int i = 0; i < n; ++i) {
+                    arrived(e + 2 * i + 1);
+                    if (i + 1 < n) arrived(e + 2 * i + 2);
+                    const int v_slot = (e + 2 * i + 1) % S::kSlots, k_slot = (e + 2 * i + 2) % S::kSlots;
+#pragma unroll 1
+                    for (int q = 0; q < nq; ++q) {
+                        wait_for(&sh.p_full[q], p_no[q]++, &sh.dead);
+                        __syncwarp();
+                        tmem_after_sync();
+                        sums(q, v_slot, q, i > 0);
+                        if (i + 1 < n) {
+                            scores(q, k_slot, q);
+                            if (i + 2 == n) mma_commit(&sh.q_empty[q], lead);
+                        }
+                    }
+                    mma_commit(&sh.empty[v_slot], lead);
+                    if (i + 1 < n) mma_commit(&sh.empty[k_slot], lead);
+                }
+            } else {
+                // one tile of rows: the next scores before this tile's weights are waited for, two places in turn
+                wait_for(&sh.q_full[0], seg[0], &sh.dead);
+                arrived(e);
+                __syncwarp();
+                tmem_after_sync();
+                scores(0, e % S::kSlots, s_no[0] & 1);
+                ++s_no[0];
+                if (n == 1) mma_commit(&sh.q_empty[0], lead);
+                mma_commit(&sh.empty[e % S::kSlots], lead);
+#pragma unroll 1
+                for (int i = 0; i < n; ++i) {
+                    const int v_slot = (e + 2 * i + 1) % S::kSlots, k_slot = (e + 2 * i + 2) % S::kSlots;
+                    if (i + 1 < n) {
+                        arrived(e + 2 * i + 2);
+                        __syncwarp();
+                        tmem_after_sync();
+                        scores(0, k_slot, s_no[0] & 1);
+                        ++s_no[0];
+                        if (i + 2 == n) mma_commit(&sh.q_empty[0], lead);
+                        mma_commit(&sh.empty[k_slot], lead);
+                    }
+                    arrived(e + 2 * i + 1);
+                    wait_for(&sh.p_full[p_no[0] & 1], p_no[0] >> 1, &sh.dead);
+                    __syncwarp();
+                    tmem_after_sync();
+                    sums(0, v_slot, p_no[0] & 1, i > 0);
+                    ++p_no[0];
+                    mma_commit(&sh.empty[v_slot], lead);
+                }
+            }
+            ++seg[0];
+            if (nq == 2) ++seg[1];
+            e += 2 * n;
+            w.step(a);
+        }
+        // nothing reads shared memory or writes tensor memory any more when they are given back
+        mma_commit(&sh.drained, lead);
+        mbar_wait(&sh.drained, 0, kMbarPolls);
+    } else if (E4M3 && warp >= S::kConvertWarp) {
+        // ---- e4m3: the codes of a tile of keys or values to f16, 16 at a time, the next tile's on their way ----
+        if constexpr (E4M3) {
+            constexpr int kConvert = S::kConvertWarps * 32;
+            const int t = threadIdx.x - S::kConvertWarp * 32;
+            constexpr int kRowChunks = DP / 16, kStepRows = kConvert / kRowChunks, kTurns = kTile / kStepRows;
+            const int chunk = t % kRowChunks, row0 = t / kRowChunks;
+            const bool in = chunk * 16 < D;
+            static_assert(kStepRows % 8 == 0, "rows");
+            const int line = (chunk >> 2) * (kTile * 128) + row0 * 128;
+            const int low = line + ((((chunk & 3) * 2) ^ (row0 & 7)) << 4), high = low ^ 16;
+            constexpr int kAtOnce = kTurns < 8 ? kTurns : 8, kPasses = kTurns / kAtOnce;
+            int e = 0;
+            // Pieces of the walk in order: pass 0 .. kPasses-1 of the keys, then of the values.
+            PromptWalk<UR> ahead = w;
+            bool more = ahead.next(a);
+            int tile_ahead = ahead.t0, part_ahead = 0;
+            auto fetch = [&](uint4 (&x)[kAtOnce]) {
+                if (!more) return;
+                const int kv = part_ahead / kPasses, turn = part_ahead % kPasses * kAtOnce;
+                const int32_t* table = c.pages + ahead.b * c.pages_stride;
+                const uint8_t* base = (kv ? c.v : c.k) + ahead.kv * c.head_stride + chunk * 16;
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i) {
+                    const int pos = tile_ahead * kTile + row0 + (turn + i) * kStepRows;
+                    x[i] = make_uint4(0u, 0u, 0u, 0u);
+                    if (in && pos < ahead.end) {
+                        const int pg_at = page_of(pos, c.div_mul, c.div_shift), pg = __ldg(table + pg_at);
+                        if (static_cast<unsigned>(pg) < static_cast<unsigned>(c.n_pages))
+                            x[i] = *reinterpret_cast<const uint4*>(base + pg * c.page_stride + (pos - pg_at * c.page_size) * c.pos_stride);
+                    }
+                }
+                if (++part_ahead == 2 * kPasses) {
+                    part_ahead = 0;
+                    if (++tile_ahead == ahead.t1) {
+                        ahead.step(a);
+                        more = ahead.next(a);
+                        tile_ahead = ahead.t0;
+                    }
+                }
+            };
+            auto convert = [&](const uint4 (&x)[kAtOnce], int turn) {
+                uint8_t* const to = ring + e % S::kSlots * S::kSlot;
+                if (turn == 0 && e >= S::kSlots) wait_for(&sh.empty[e % S::kSlots], e / S::kSlots - 1, &sh.dead);
+                if (in)
+#pragma unroll
+                    for (int i = 0; i < kAtOnce; ++i) {
+                        const uint2 h0 = four_codes(x[i].x), h1 = four_codes(x[i].y), h2 = four_codes(x[i].z), h3 = four_codes(x[i].w);
+                        const int at = (turn + i) * (kStepRows * 128);
+                        *reinterpret_cast<uint4*>(to + low + at) = make_uint4(h0.x, h0.y, h1.x, h1.y);
+                        *reinterpret_cast<uint4*>(to + high + at) = make_uint4(h2.x, h2.y, h3.x, h3.y);
+                    }
+                if (turn + kAtOnce == kTurns) {
+                    fence_smem_async();
+                    __syncwarp();
+                    mbar_arrive_if(&sh.full[e % S::kSlots], lane == 0);
+                    ++e;
+                }
+            };
+            uint4 x[kAtOnce], y[kAtOnce];
+            fetch(x);
+            // (the list has an even number of pieces: keys and values)
+            int64_t pieces = w.left * 2 * kPasses;
+            int turn = 0;
+#pragma unroll 1
+            for (; pieces > 0; pieces -= 2) {
+                fetch(y);
+                convert(x, turn);
+                turn = (turn + kAtOnce) % kTurns;
+                fetch(x);
+                convert(y, turn);
+                turn = (turn + kAtOnce) % kTurns;
+            }
+        }
+    } else {
+        // ---- softmax: a row a thread ----
+        const int q = warp >> 2, quad = warp & 3, j = quad * 32 + lane;
+        const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16, my_o = tmem + lanes + S::kO + q * DP;
+        constexpr float kLift = E4M3 ? 7.f : 0.f;       // f16 weights up to 2^15 instead of 2^8: fewer of them vanish
+        constexpr float kRoomUp = E4M3 ? 8.f : 64.f;
+        int tile_no = 0, mine = 0;                      // tiles of this CTA, and those of this warp's rows
+        [[maybe_unused]] int seg = 0;                   // and its units
+        bool cut_here = false;
+#pragma unroll 1
+        while (w.next(a)) {
+            if (q * 128 >= w.rows) {                    // no rows for these warps
+                if constexpr (E4M3)
+#pragma unroll 1
+                    for (int tile = w.t0; tile < w.t1; ++tile, ++tile_no) {
+                        wait_for(&sh.key_full[tile_no & 3], tile_no >> 2, &sh.dead);
+                        __syncwarp();
+                        mbar_arrive_if(&sh.key_empty[tile_no & 3], lane == 0);
+                    }
+                else tile_no += w.t1 - w.t0;
+                w.step(a);
+                continue;
+            }
+            const int64_t r = w.r0 + q * 128 + j;
+            const bool is_row = r < w.s.N;
+            const uint32_t tok = is_row ? static_cast<uint32_t>(r) / static_cast<uint32_t>(a.group) : 0u;
+            const uint32_t head = is_row ? static_cast<uint32_t>(w.kv) * a.group + (static_cast<uint32_t>(r) - tok * a.group) : 0u;
+            const int limit = is_row ? w.s.start + static_cast<int>(tok) : -1;         // last position that the row sees
+            const int seen_by_all = w.s.start + static_cast<int>(static_cast<uint32_t>(w.r0 + q * 128) / static_cast<uint32_t>(a.group));
+            float m = -INFINITY;                        // (of x, in powers of two; less the lift)
+            uint64_t l2 = 0;
+            float f = a.scale2;
+            uint64_t f2 = pack_f32x2(f, f);
+#pragma unroll 1
+            for (int tile = w.t0; tile < w.t1; ++tile, ++tile_no, ++mine) {
+                const int at = NQ == 2 ? q : mine & 1;
+                const uint32_t s_at = tmem + lanes + at * 128;
+                const uint32_t s_turn = NQ == 2 ? mine : mine >> 1;
+                [[maybe_unused]] const int k_at = tile_no & 3;
+                if constexpr (E4M3) wait_for(&sh.key_full[k_at], tile_no >> 2, &sh.dead);
+                wait_for(&sh.s_full[at], s_turn, &sh.dead);
+                __syncwarp();
+                tmem_after_sync();
+                if constexpr (E4M3) {
+                    // (written before the queries were handed to the matrix instructions; asking that barrier itself would
+                    // ask for a phase that may be two behind)
+                    if (tile == w.t0) f = a.scale2 * sh.back[seg & 1][q * 128 + j], f2 = pack_f32x2(f, f);
+                }
+                const bool masked = tile * kTile + kTile - 1 > seen_by_all;
+                const bool holes = sh.holes[tile_no % kAhead];
+                // x of 32 keys
+                auto load = [&](int ch, float (&x)[32]) {
+                    tmem_load(s_at + ch * 32, x);
+                    if constexpr (E4M3) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) {
+                            const float4 kf = *reinterpret_cast<const float4*>(&sh.key_factor[k_at][ch * 32 + i]);
+                            const float4 lg = *reinterpret_cast<const float4*>(&sh.key_log[k_at][ch * 32 + i]);
+                            const uint64_t a0 = fma_f32x2(pack_f32x2(kf.x, kf.y), f2, 0ull), a1 = fma_f32x2(pack_f32x2(kf.z, kf.w), f2, 0ull);
+                            const uint64_t lo = fma_f32x2(pack_f32x2(x[i], x[i + 1]), a0, pack_f32x2(lg.x, lg.y));
+                            const uint64_t hi = fma_f32x2(pack_f32x2(x[i + 2], x[i + 3]), a1, pack_f32x2(lg.z, lg.w));
+                            x[i] = lo_f32(lo), x[i + 1] = hi_f32(lo), x[i + 2] = lo_f32(hi), x[i + 3] = hi_f32(hi);
+                        }
+                    }
+                    if (masked) {
+                        const int most = limit - tile * kTile - ch * 32;              // keys up to here
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (i > most) x[i] = -INFINITY;
+                    }
+                    if (holes) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (!sh.live[tile_no % kAhead][ch * 32 + i]) x[i] = -INFINITY;
+                    }
+                };
+                float top = -INFINITY;
+#pragma unroll
+                for (int ch = 0; ch < 4; ++ch) {
+                    float x[32];
+                    load(ch, x);
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) top = max3(top, x[i], x[i + 1]);
+                }
+                if constexpr (!E4M3) top = top > -INFINITY ? top * f : top;
+                // m moves: at first, or when weights would grow too large
+                const bool up = top > m + kRoomUp || (m == -INFINITY && top > -INFINITY);
+                if (__any_sync(0xFFFFFFFFu, up)) {
+                    float by = 1.f;
+                    if (up) {
+                        by = m == -INFINITY ? 0.f : ex2(m - top);
+                        m = top;
+                    }
+                    l2 = fma_f32x2(l2, pack_f32x2(by, by), 0ull);
+                    if (tile > w.t0) {
+                        wait_for(&sh.pv_done[q], mine - 1, &sh.dead);
+                        __syncwarp();
+                        tmem_after_sync();
+#pragma unroll 1
+                        for (int i = 0; i < DP; i += 8) {
+                            float o[8];
+                            tmem_load(my_o + i, o);
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) o[k] *= by;
+                            tmem_store8(my_o + i, o);
+                        }
+                        tmem_store_wait();
+                    }
+                }
+                const float less = m == -INFINITY ? 0.f : kLift - m;
+                const uint64_t less2 = pack_f32x2(less, less);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t p[32];
+#pragma unroll
+                    for (int ch = 0; ch < 2; ++ch) {
+                        float x[32];
+                        load(2 * half + ch, x);
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            const uint64_t e = E4M3 ? add_f32x2(pack_f32x2(x[i], x[i + 1]), less2) : fma_f32x2(pack_f32x2(x[i], x[i + 1]), f2, less2);
+                            const float p0 = ex2(lo_f32(e)), p1 = ex2(hi_f32(e));
+                            if constexpr (E4M3) {
+                                const float2 inv = *reinterpret_cast<const float2*>(&sh.key_inverse[k_at][(2 * half + ch) * 32 + i]);
+                                l2 = fma_f32x2(pack_f32x2(p0, p1), pack_f32x2(inv.x, inv.y), l2);
+                                p[ch * 16 + i / 2] = pack_f16(p0, p1);
+                            } else {
+                                l2 = add_f32x2(l2, pack_f32x2(p0, p1));
+                                p[ch * 16 + i / 2] = pack_bf16(p0, p1);
+                            }
+                        }
+                    }
+                    tmem_store32(s_at + half * 32, p);
+                }
+                tmem_store_wait();
+                tmem_before_sync();
+                __syncwarp();
+                mbar_arrive_if(&sh.p_full[at], lane == 0);
+                if constexpr (E4M3) mbar_arrive_if(&sh.key_empty[k_at], lane == 0);
+            }
+            // ---- the unit's end ----
+            wait_for(&sh.pv_done[q], mine - 1, &sh.dead);
+            __syncwarp();
+            tmem_after_sync();
+            const float l = lo_f32(l2) + hi_f32(l2);
+            const bool whole = w.t0 == 0 && w.t1 == w.T;
+            if (whole) {
+                const float inverse = l > 0.f ? 1.f / l : 0.f;
+                const int64_t row = w.p.row + static_cast<int64_t>(tok);
+                if (is_row && a.lse) a.lse[row * a.q_heads + head] = l > 0.f ? (log2f(l) + m - kLift) * 0.69314718055994531f : -INFINITY;
+                __nv_bfloat16* out = a.out + row * a.o_tok + head * a.o_head;
+#pragma unroll 1
+                for (int i = 0; i < D; i += 16) {
+                    float o[16];
+                    tmem_load(my_o + i, o);
+                    uint32_t y[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) y[k] = l > 0.f ? pack_bf16(o[2 * k] * inverse, o[2 * k + 1] * inverse) : 0u;
+                    if (is_row) {
+                        *reinterpret_cast<uint4*>(out + i) = make_uint4(y[0], y[1], y[2], y[3]);
+                        *reinterpret_cast<uint4*>(out + i + 8) = make_uint4(y[4], y[5], y[6], y[7]);
+                    }
+                    __syncwarp();
+                }
+            } else {
+                // (which of this CTA's two places: the unit began in another's part, or in this one's)
+                float* part = a.parts + static_cast<int64_t>(2 * blockIdx.x + (w.t0 == 0 ? 1 : 0)) * prompt_part(DP) + q * 128 * (DP + 2);
+#pragma unroll 1
+                for (int i = 0; i < D; i += 16) {
+                    float o[16];
+                    tmem_load(my_o + i, o);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        *reinterpret_cast<float4*>(part + ((i / 4 + k) * 128 + j) * 4) = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+                    __syncwarp();
+                }
+                part[128 * DP + j] = l > 0.f ? m - kLift : -INFINITY;
+                part[128 * DP + 128 + j] = l;
+                if (w.t0 == 0) cut_here = true;
+                if (w.t0 == 0 && threadIdx.x == 0) {
+                    // the CTA that has the unit's last tile
+                    const long long last = w.at + w.T - 1, edge = (sh.each + 1) * sh.extra;
+                    const int c_last = static_cast<int>(last < edge ? last / (sh.each + 1) : sh.extra + (last - edge) / sh.each);
+                    a.cuts[blockIdx.x] = {c_last - static_cast<int>(blockIdx.x) + 1, static_cast<int>(blockIdx.x), static_cast<int>(w.r0), w.rows,
+                                          w.p.row, w.kv};
+                }
+            }
+            if (sh.dead && j == 0 && a.status) atomicOr(a.status + w.b, PLDP_ST_TIMEOUT);
+            tmem_before_sync();
+            ++seg;
+            w.step(a);
+        }
+        if (threadIdx.x == 0 && !cut_here) a.cuts[blockIdx.x].parts = 0;
+    }
+    tmem_before_sync();
+    __syncthreads();
+    if (warp == S::kMmaWarp) {
+        tmem_after_sync();
+        tmem_free(tmem, 512);
+    }
+}
+
+template <int DP, bool E4M3>
+cudaError_t launch_prompt(const PromptArgs& a, const Maps& m, int ctas, cudaStream_t s) {
+    using Shape = PromptShape<DP, E4M3>;
+    const cudaError_t e = cudaFuncSetAttribute(prompt_kernel<DP, E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::kBytes);
+    if (e != cudaSuccess) return e;
+    // what the warps take must be what the block was launched with: more would be waited for without end
+    static const int regs = [] {
+        cudaFuncAttributes attr;
+        return cudaFuncGetAttributes(&attr, prompt_kernel<DP, E4M3>) == cudaSuccess ? attr.numRegs : 0;
+    }();
+    constexpr int kSplit = (Shape::kSoftmaxWarps * Shape::kSoftmaxRegs + 4 * Shape::kOtherRegs + Shape::kConvertWarps * Shape::kConvertRegs) * 32;
+    if (Shape::kQ == 2 && regs * Shape::kThreads < kSplit) return cudaErrorLaunchOutOfResources;
+    return launch_pdl(prompt_kernel<DP, E4M3>, dim3(ctas), dim3(Shape::kThreads), Shape::kBytes, s, 0, a, m.k, m.v);
+}
+template <bool E4M3>
+cudaError_t launch_prompt_dims(const PromptArgs& a, const Maps& m, int ctas, cudaStream_t s) {
+    const int dp = prompt_dim(a.c.head_dim);
+    return dp == 64 ? launch_prompt<64, E4M3>(a, m, ctas, s) : dp == 128 ? launch_prompt<128, E4M3>(a, m, ctas, s) : launch_prompt<256, E4M3>(a, m, ctas, s);
+}
+
+}  // namespace
+}  // namespace pldp
