@@ -16,9 +16,9 @@ struct PromptArgs {
     float* parts;                          // [2 a CTA][Part]
     struct CutUnit* cuts;                  // [CTAs]
     int B, R, q_heads, group;
-    int box;                               // as AttendArgs
+    int box, pitch;                        // as AttendArgs
     int head_first;
-    int least;                             // tiles a CTA takes at least
+    int least;                             // of the list a CTA takes at least
     float scale2;                          // |scale| * log2(e)
     uint32_t flip;                         // what turns the signs of two queries for a negative scale
 };
@@ -83,6 +83,22 @@ __device__ __forceinline__ int64_t tiles_before(const Units& s, int u) {
     if (whole < u) n += unit_tiles<UR>(s, whole);
     return n;
 }
+// What a unit costs beside its tiles, in tiles: its queries' way in, the first scores' and the last weights' latency, its
+// results' way out.  The list counts it, so that a part of many short units is not the last to end.
+constexpr int kUnitCost = 3;
+template <int UR>
+__device__ __forceinline__ int64_t cost_before(const Units& s, int u) { return tiles_before<UR>(s, u) + static_cast<int64_t>(u) * kUnitCost; }
+// The unit that holds place x of the list of one kv head: cost_before(u) <= x < cost_before(u + 1).
+template <int UR>
+__device__ __forceinline__ int unit_at(const Units& s, int units, int64_t x) {
+    // tiles grow linearly from unit to unit: the root of their sum, and from there to the unit itself
+    const float a2 = UR / (2.f * kTile * s.group), b = kUnitCost + (s.start + 0.5f * UR / s.group) / kTile + 0.5f;
+    int u = static_cast<int>((sqrtf(b * b + 4.f * a2 * static_cast<float>(x)) - b) / (2.f * a2));
+    u = max(0, min(u, units - 1));
+    while (u > 0 && cost_before<UR>(s, u) > x) --u;
+    while (u + 1 < units && cost_before<UR>(s, u + 1) <= x) ++u;
+    return u;
+}
 
 template <int DP, bool E4M3>
 struct PromptShape {
@@ -97,14 +113,23 @@ struct PromptShape {
     static constexpr int kPanels = DP / 64;
     static constexpr int kSlot = kPanels * kTile * 128;
     static constexpr int kQBytes = kQ * kPanels * 128 * 128;
-    static constexpr int kStatic = E4M3 ? 10240 : 2048;        // PromptShared
-    static constexpr int kMost = (kMaxShared - 1024 - kStatic - kQBytes) / kSlot;
+    static constexpr int kStatic = E4M3 ? 8192 : 2048;         // PromptShared
+    // Rows of the result pass through shared memory, 32 rows of a warp and kOutBytes of each at a time, to be written whole
+    // lines at a time.
+    static constexpr int kOutBytes = E4M3 && DP >= 128 ? 64 : 128;
+    static constexpr int kOut = kSoftmaxWarps * 32 * kOutBytes;
+    // e4m3: codes as they are, a tile (heads above 128 elements: half of one) a stage
+    static constexpr int kStageRows = DP == 256 ? 64 : kTile, kStage = E4M3 ? kStageRows * (DP < 128 ? 128 : DP) : 0;
+    static constexpr int kRoom = kMaxShared - 1024 - kStatic - kQBytes - kOut;
+    static constexpr int kMost = (kRoom - (DP == 256 ? 1 : 3) * kStage) / kSlot;
     static constexpr int kSlots = kMost > 6 ? 6 : kMost;
-    static constexpr int kBytes = kQBytes + kSlots * kSlot + 1024;
+    static constexpr int kFit = E4M3 ? (kRoom - kSlots * kSlot) / kStage : 0;
+    static constexpr int kStages = kFit > 6 ? 6 : kFit;
+    static constexpr int kBytes = kQBytes + kSlots * kSlot + kStages * kStage + kOut + 1024;
     static constexpr int kO = 256;                             // column of the first sums
     // 384 threads start with 168 registers each (512: 128); the softmax takes what the others leave
-    static constexpr int kSoftmaxRegs = E4M3 ? 168 : 208, kOtherRegs = E4M3 ? 56 : 88, kConvertRegs = 112;
-    static_assert(kSlots >= 2 && kBytes + kStatic <= kMaxShared, "shared memory");
+    static constexpr int kSoftmaxRegs = E4M3 ? 184 : 208, kOtherRegs = E4M3 ? 56 : 88, kConvertRegs = 88;
+    static_assert(kSlots >= 2 && (!E4M3 || kStages >= 1) && kBytes + kStatic <= kMaxShared, "shared memory");
 };
 
 constexpr int kAhead = 8;                  // tiles whose holes are kept (more than the ring of keys holds)
@@ -112,17 +137,16 @@ constexpr int kAhead = 8;                  // tiles whose holes are kept (more t
 template <bool E4M3>
 struct PromptShared {
     alignas(16) float key_factor[E4M3 ? 4 : 1][E4M3 ? kTile : 4], key_log[E4M3 ? 4 : 1][E4M3 ? kTile : 4], key_inverse[E4M3 ? 4 : 1][E4M3 ? kTile : 4];
-    float back[E4M3 ? 2 : 1][E4M3 ? 256 : 1];
     uint8_t live[kAhead][kTile];           // whether a page holds the key; looked at where `holes` is set
     int holes[kAhead];
-    uint64_t full[8], empty[8], s_full[2], p_full[2], pv_done[2], q_full[2], q_empty[2], tail, drained,
+    uint64_t full[8], empty[8], stage_full[6], stage_empty[6], q_raw[2], s_full[2], p_full[2], pv_done[2], q_full[2], q_empty[2], tail, drained,
         key_full[4], key_empty[4];
     uint32_t tmem;
     int dead, zeros;
     long long warp_sum[20];
     long long total;
     // where this CTA's part of the list starts
-    int b, kv, unit, tile;
+    int b, kv, unit, tile, pre;
     long long at, count, each, extra;
 };
 
@@ -130,6 +154,7 @@ struct PromptShared {
 template <int UR>
 struct PromptWalk {
     int b, kv, unit, t0;
+    int pre;           // what is left of the unit's own cost
     long long at, left;
     // the unit's
     PackedRows p;
@@ -140,7 +165,7 @@ struct PromptWalk {
     int end;           // positions from here on are not the sequence's
 
     __device__ __forceinline__ bool next(const PromptArgs& a) {
-        if (left <= 0) return false;
+        if (left <= pre) return false;
         uint32_t st;
         while (true) {                                           // (sequences without rows hold no tiles)
             p = packed_rows(a.rows, a.start, b, a.R, a.c.capacity, st);
@@ -150,16 +175,16 @@ struct PromptWalk {
         s = units_of(p, a.group);
         units = unit_count<UR>(s);
         T = unit_tiles<UR>(s, unit);
-        t1 = left < T - t0 ? t0 + static_cast<int>(left) : T;
+        t1 = left - pre < T - t0 ? t0 + static_cast<int>(left - pre) : T;
         r0 = static_cast<int64_t>(unit) * UR;
         rows = static_cast<int>(min(static_cast<int64_t>(UR), s.N - r0));
         end = s.start + s.count;
         return true;
     }
     __device__ __forceinline__ void step(const PromptArgs& a) {
-        at += t1 - t0;
-        left -= t1 - t0;
-        t0 = 0;
+        at += pre + (t1 - t0);
+        left -= pre + (t1 - t0);
+        t0 = 0, pre = kUnitCost;
         if (++unit == units) {
             unit = 0;
             if (++kv == a.c.heads) kv = 0, ++b;
@@ -187,6 +212,10 @@ __device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t* v) {
           "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
           "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]), "r"(addr)
         : "memory");
+}
+// 16 bytes from global to shared memory, later, or zeros.
+__device__ __forceinline__ void copy_or_zeros(void* to, const void* from, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
@@ -223,6 +252,8 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
     __shared__ __align__(16) PromptShared<E4M3> sh;
     uint8_t* ring = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
     uint8_t* const q_smem = ring + S::kSlots * S::kSlot;
+    uint8_t* const out_smem = q_smem + S::kQBytes;
+    [[maybe_unused]] uint8_t* const stages = out_smem + S::kOut;
     const CacheView& c = a.c;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = c.head_dim;
 
@@ -232,11 +263,16 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             mbar_init(&sh.full[i], E4M3 ? S::kConvertWarps : 1);
             mbar_init(&sh.empty[i], 1);
         }
+        for (int i = 0; i < 6; ++i) {
+            mbar_init(&sh.stage_full[i], 1);
+            mbar_init(&sh.stage_empty[i], E4M3 ? S::kConvertWarps : 1);
+        }
         for (int i = 0; i < 2; ++i) {
+            mbar_init(&sh.q_raw[i], 1);
             mbar_init(&sh.s_full[i], 1);
             mbar_init(&sh.p_full[i], 4);
             mbar_init(&sh.pv_done[i], 1);
-            mbar_init(&sh.q_full[i], 1);
+            mbar_init(&sh.q_full[i], E4M3 ? 4 : 1);
             mbar_init(&sh.q_empty[i], 1);
         }
         for (int i = 0; i < 4; ++i) {
@@ -252,15 +288,15 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
     pdl_enter();
     __syncthreads();
 
-    // the list: every thread counts the tiles of a strip of sequences
+    // the list: every thread counts the costs of a strip of sequences
     {
         const int strip = (a.B + kThreads - 1) / kThreads;
         const int lo = min(a.B, static_cast<int>(threadIdx.x) * strip), hi = min(a.B, lo + strip);
-        auto tiles_of = [&](int b) -> long long {
+        auto cost_of = [&](int b) -> long long {
             uint32_t st;
             const PackedRows p = packed_rows(a.rows, a.start, b, a.R, c.capacity, st);
             const Units s = units_of(p, a.group);
-            return c.heads * tiles_before<UR>(s, unit_count<UR>(s));
+            return c.heads * cost_before<UR>(s, unit_count<UR>(s));
         };
         long long mine = 0;
 #pragma unroll 1
@@ -269,7 +305,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             const PackedRows p = packed_rows(a.rows, a.start, b, a.R, c.capacity, st);
             if (st && blockIdx.x == 0 && a.status) atomicOr(a.status + b, st);
             if (p.count < p.given) sh.zeros = 1;
-            mine += tiles_of(b);
+            mine += cost_of(b);
         }
         long long upto = mine;
 #pragma unroll
@@ -285,7 +321,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             if (w == warp) upto += total;
             total += sh.warp_sum[w];
         }
-        // equal parts; the first `extra` CTAs take one tile more than the others
+        // equal parts; the first `extra` CTAs take one more than the others
         const long long most = (total + a.least - 1) / a.least;
         const int ctas = static_cast<int>(most < gridDim.x ? most : gridDim.x);
         const long long each = ctas ? total / ctas : 0, extra = ctas ? total - each * ctas : 0;
@@ -296,30 +332,23 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             int b = lo;
 #pragma unroll 1
             for (;; ++b) {
-                const long long t = tiles_of(b);
+                const long long t = cost_of(b);
                 if (g0 < before + t) break;
                 before += t;
             }
             uint32_t st;
             const Units s = units_of(packed_rows(a.rows, a.start, b, a.R, c.capacity, st), a.group);
             const int units = unit_count<UR>(s);
-            const long long per = tiles_before<UR>(s, units), in = g0 - before;
-            const int kv = static_cast<int>(in / per);
-            const long long x = in - kv * per;
-            int u0 = 0, u1 = units;                                                 // tiles_before(u0) <= x < tiles_before(u1)
-#pragma unroll 1
-            while (u1 - u0 > 1) {
-                const int mid = (u0 + u1) >> 1;
-                if (tiles_before<UR>(s, mid) <= x) u0 = mid;
-                else u1 = mid;
-            }
-            sh.b = b, sh.kv = kv, sh.unit = u0;
-            sh.tile = static_cast<int>(x - tiles_before<UR>(s, u0));
+            const long long per = cost_before<UR>(s, units), in = g0 - before;
+            const int kv = static_cast<int>(in / per), u = unit_at<UR>(s, units, in - kv * per);
+            const int x = static_cast<int>(in - kv * per - cost_before<UR>(s, u));
+            sh.b = b, sh.kv = kv, sh.unit = u;
+            sh.pre = max(0, kUnitCost - x), sh.tile = max(0, x - kUnitCost);
             sh.at = g0, sh.count = g1 - g0;
         }
         if (threadIdx.x == 0) {
             sh.each = each, sh.extra = extra;
-            if (blockIdx.x >= ctas) sh.count = 0;
+            if (blockIdx.x >= ctas) sh.count = sh.pre = 0;
         }
     }
     tmem_before_sync();
@@ -327,7 +356,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
     tmem_after_sync();
     const uint32_t tmem = sh.tmem;
     PromptWalk<UR> w;
-    w.b = sh.b, w.kv = sh.kv, w.unit = sh.unit, w.t0 = sh.tile, w.at = sh.at, w.left = sh.count;
+    w.b = sh.b, w.kv = sh.kv, w.unit = sh.unit, w.t0 = sh.tile, w.pre = sh.pre, w.at = sh.at, w.left = sh.count;
     if (sh.zeros) {
         // tokens that take no part: their rows, of all heads
 #pragma unroll 1
@@ -343,16 +372,15 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
         }
     }
 
-    if constexpr (NQ == 2) {
-        if (warp < S::kMmaWarp) more_registers<S::kSoftmaxRegs>();
-        else if (warp < S::kConvertWarp) fewer_registers<S::kOtherRegs>();
-        else fewer_registers<S::kConvertRegs>();
-    }
+    if (warp >= S::kMmaWarp && warp < S::kConvertWarp) {
+    if constexpr (NQ == 2) fewer_registers<S::kOtherRegs>();
     if (warp == S::kCopyWarp) {
-        // ---- copies: keys and values in turn, a box (positions of one page) a lane; e4m3: nothing, the converting warps load ----
-        if constexpr (!E4M3) {
-        constexpr int kDepth = S::kSlots;
-        const int boxes = kTile / a.box;
+        // ---- copies: keys and values in turn, a box (positions of one page) and its panel a lane ----
+        constexpr int kDepth = E4M3 ? S::kStages : S::kSlots, kParts = E4M3 ? kTile / S::kStageRows : 1, kPartRows = kTile / kParts;
+        constexpr int kPieces = E4M3 ? 1 : S::kPanels;                     // copies of a box
+        uint64_t* const arrived = E4M3 ? sh.stage_full : sh.full;
+        uint64_t* const left = E4M3 ? sh.stage_empty : sh.empty;
+        const int boxes = kPartRows / a.box;
         int e = 0, tile_no = 0, tails = 0;
         bool on = true;
 #pragma unroll 1
@@ -360,24 +388,25 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             const int32_t* table = c.pages + w.b * c.pages_stride;
 #pragma unroll 1
             for (int tile = w.t0; on && tile < w.t1; ++tile, ++tile_no) {
-                // boxes that hold a position of the sequence
-                const int full = min(boxes, (w.end - tile * kTile + a.box - 1) / a.box);
-                const bool tail = tile * kTile + kTile > w.end;
+                const bool tail = !E4M3 && tile * kTile + kTile > w.end;
 #pragma unroll 1
-                for (int kv = 0; on && kv < 2; ++kv, ++e) {
+                for (int part = 0; on && part < 2 * kParts; ++part, ++e) {
+                    const int kv = part / kParts, from = tile * kTile + part % kParts * kPartRows;
+                    // boxes that hold a position of the sequence
+                    const int full = max(0, min(boxes, (w.end - from + a.box - 1) / a.box));
                     const CUtensorMap* map = kv ? &v_map : &k_map;
                     const int at = e % kDepth;
-                    if (e >= kDepth) wait_for(&sh.empty[at], e / kDepth - 1, &sh.dead);
+                    if (e >= kDepth) wait_for(&left[at], e / kDepth - 1, &sh.dead);
                     on = !__any_sync(0xFFFFFFFFu, *static_cast<volatile int*>(&sh.dead));
                     if (!on) break;
-                    uint64_t* const bar = tail && kv ? &sh.tail : &sh.full[at];
-                    if (lane == 0) mbar_arrive_expect_tx(bar, full * a.box * S::kPanels * 128);
+                    uint64_t* const bar = tail && kv ? &sh.tail : &arrived[at];
+                    if (lane == 0) mbar_arrive_expect_tx(bar, full * a.box * (E4M3 ? a.pitch : S::kPanels * 128));
                     __syncwarp();
-                    uint8_t* dst = ring + at * S::kSlot;
+                    uint8_t* dst = E4M3 ? stages + at * S::kStage : ring + at * S::kSlot;
                     bool hole = false;
 #pragma unroll 1
-                    for (int box = lane; box < full; box += 32) {
-                        const int pos = tile * kTile + box * a.box;
+                    for (int i = lane; i < full * kPieces; i += 32) {
+                        const int box = i / kPieces, p = i % kPieces, pos = from + box * a.box;
                         const int pg_at = page_of(pos, c.div_mul, c.div_shift), slot = pos - pg_at * c.page_size;
                         int pg = __ldg(table + pg_at);
                         if (static_cast<unsigned>(pg) >= static_cast<unsigned>(c.n_pages)) {
@@ -385,11 +414,10 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                             hole = true;
                         }
                         const int c1 = a.head_first ? w.kv : slot, c2 = a.head_first ? slot : w.kv;
-#pragma unroll 1
-                        for (int p = 0; p < S::kPanels; ++p)
-                            tma_box(dst + p * (kTile * 128) + box * a.box * 128, map, p * 64, c1, c2, pg, bar);
+                        if constexpr (E4M3) tma_box(dst + box * a.box * a.pitch, map, 0, c1, c2, pg, bar);
+                        else tma_box(dst + p * (kTile * 128) + box * a.box * 128, map, p * 64, c1, c2, pg, bar);
                     }
-                    if (kv == 0) {
+                    if (!E4M3 && kv == 0) {
                         hole = __any_sync(0xFFFFFFFFu, hole);
                         if (hole) {
 #pragma unroll 1
@@ -413,7 +441,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                                 *reinterpret_cast<uint4*>(dst + (p >> 3) * (kTile * 128) + r * 128 + (p & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
                         fence_smem_async();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(&sh.full[at]);
+                        if (lane == 0) mbar_arrive(&arrived[at]);
                     }
                     __syncwarp();
                 }
@@ -423,12 +451,11 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
         // the last copy into each place arrives before this CTA ends, whether or not its reader has waited for it
         if (lane < kDepth) {
             const int x = e - 1 - ((e - 1 - lane) % kDepth + kDepth) % kDepth;
-            if (x >= 0) mbar_wait(&sh.full[lane], (x / kDepth) & 1, kMbarPolls);
+            if (x >= 0) mbar_wait(&arrived[lane], (x / kDepth) & 1, kMbarPolls);
         } else if (lane == 31 && tails > 0) {
             mbar_wait(&sh.tail, (tails - 1) & 1, kMbarPolls);
         }
-        }
-    } else if (warp == S::kKeyWarp) {
+    } else if (E4M3 && warp == S::kKeyWarp) {
         // ---- e4m3: the scales of each tile, four keys a lane ----
         if constexpr (E4M3) {
             int tile_no = 0;
@@ -474,64 +501,57 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 w.step(a);
             }
         }
-    } else if (warp == S::kQueryWarp) {
+    } else if (warp == S::kKeyWarp || warp == S::kQueryWarp) {
         // ---- queries of the next unit, as soon as the last scores of this one are done ----
+        // All of a tile's pieces of 16 bytes are asked for before the first is waited for; bf16: a tile of rows a warp.
+        constexpr int kLanes = DP / 8, kAt = 32 / kLanes;          // lanes a row, and rows at once
+        constexpr int kStep = E4M3 ? 1 : 2;
+        const int piece = lane % kLanes, q0 = warp == S::kQueryWarp ? 0 : 1;
+        const bool in = piece * 8 < D;
         int seg[2] = {0, 0};
 #pragma unroll 1
         while (w.next(a)) {
 #pragma unroll 1
-            for (int q = 0; q < NQ; ++q) {
+            for (int q = q0; q < NQ; q += kStep) {
                 if (q * 128 >= w.rows) break;
                 if (seg[q] > 0) wait_for(&sh.q_empty[q], seg[q] - 1, &sh.dead);
-                // a lane has a piece of 16 bytes of a row, DP / 8 lanes a row, or all of them several
-                constexpr int kLanes = DP / 8 < 32 ? DP / 8 : 32, kAt = 32 / kLanes, kBatch = 8;
-                const int piece = lane % kLanes;
                 uint8_t* const to = q_smem + q * (S::kPanels * 128 * 128) + (piece >> 3) * (128 * 128);
+                const uint32_t first = static_cast<uint32_t>(w.r0) + q * 128 + lane / kLanes, group = a.group;
+                uint32_t tok = first / group, h = first - tok * group;
+                const __nv_bfloat16* from = a.q + w.p.row * a.q_tok + static_cast<int64_t>(w.kv) * a.group * a.q_head + piece * 8;
+#pragma unroll 4
+                for (int row = lane / kLanes; row < 128; row += kAt) {
+                    const bool there = in && q * 128 + row < w.rows;
+                    copy_or_zeros(to + row * 128 + (((piece & 7) ^ (row & 7)) << 4), there ? from + tok * a.q_tok + h * a.q_head : a.q, there);
+                    h += kAt;
+                    while (h >= group) h -= group, ++tok;
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            }
 #pragma unroll 1
-                for (int row0 = 0; row0 < 128; row0 += kAt * kBatch) {
-                    uint4 x[kBatch];
-#pragma unroll
-                    for (int i = 0; i < kBatch; ++i) {
-                        const int row = row0 + i * kAt + lane / kLanes;
-                        const int64_t r = w.r0 + q * 128 + row;
-                        x[i] = make_uint4(0u, 0u, 0u, 0u);
-                        if (r < w.s.N && piece * 8 < D) {
-                            const uint32_t tok = static_cast<uint32_t>(r) / static_cast<uint32_t>(a.group), h = static_cast<uint32_t>(r) - tok * a.group;
-                            x[i] = *reinterpret_cast<const uint4*>(a.q + (w.p.row + static_cast<int64_t>(tok)) * a.q_tok +
-                                                                   (static_cast<int64_t>(w.kv) * a.group + h) * a.q_head + piece * 8);
-                            x[i].x ^= a.flip, x[i].y ^= a.flip, x[i].z ^= a.flip, x[i].w ^= a.flip;
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < kBatch; ++i) {
-                        const int row = row0 + i * kAt + lane / kLanes;
-                        if constexpr (E4M3) {
-                            // bf16 to f16: the row's largest element to 2^14..2^15 by a power of two
-                            uint32_t v[4] = {x[i].x, x[i].y, x[i].z, x[i].w}, most = 0;
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) most = max(most, max((v[k] << 16) & 0x7FFF0000u, v[k] & 0x7FFF0000u));
-#pragma unroll
-                            for (int o = kLanes / 2; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
-                            const int ex = static_cast<int>(most >> 23);
-                            const int up = ex == 0 || ex == 255 ? 0 : min(14 - (ex - 127), 120);
-                            const float lift = __uint_as_float(static_cast<uint32_t>(up + 127) << 23);
-                            if (piece == 0) sh.back[seg[q] & 1][q * 128 + row] = __uint_as_float(static_cast<uint32_t>(127 - up) << 23);
-#pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                v[k] = pack_f16(__uint_as_float(v[k] << 16) * lift, __uint_as_float(v[k] & 0xFFFF0000u) * lift);
-                            x[i] = make_uint4(v[0], v[1], v[2], v[3]);
-                        }
-                        *reinterpret_cast<uint4*>(to + row * 128 + (((piece & 7) ^ (row & 7)) << 4)) = x[i];
+            for (int q = q0; q < NQ; q += kStep) {
+                if (q * 128 >= w.rows) break;
+                if (E4M3 && q == 0 && w.rows > 128) asm volatile("cp.async.wait_group 1;" ::: "memory");
+                else asm volatile("cp.async.wait_group 0;" ::: "memory");
+                if (!E4M3 && a.flip) {
+                    // (each lane its own pieces)
+                    uint8_t* const to = q_smem + q * (S::kPanels * 128 * 128) + (piece >> 3) * (128 * 128);
+#pragma unroll 4
+                    for (int row = lane / kLanes; row < 128; row += kAt) {
+                        uint4* const at = reinterpret_cast<uint4*>(to + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
+                        uint4 x = *at;
+                        x.x ^= a.flip, x.y ^= a.flip, x.z ^= a.flip, x.w ^= a.flip;
+                        *at = x;
                     }
                 }
-                fence_smem_async();
+                if constexpr (!E4M3) fence_smem_async();
                 __syncwarp();
-                mbar_arrive_if(&sh.q_full[q], lane == 0);
+                mbar_arrive_if(E4M3 ? &sh.q_raw[q] : &sh.q_full[q], lane == 0);
                 ++seg[q];
             }
             w.step(a);
         }
-    } else if (warp == S::kMmaWarp) {
+    } else {
         // ---- matrix instructions ----
         const uint64_t q_op = smem_operand(smem_u32(q_smem), 16, 1024, swizzle_mode(128));
         const uint64_t k_op = smem_operand(smem_u32(ring), 16, 1024, swizzle_mode(128));
@@ -633,82 +653,67 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
         // nothing reads shared memory or writes tensor memory any more when they are given back
         mma_commit(&sh.drained, lead);
         mbar_wait(&sh.drained, 0, kMbarPolls);
+    }
     } else if (E4M3 && warp >= S::kConvertWarp) {
-        // ---- e4m3: the codes of a tile of keys or values to f16, 16 at a time, the next tile's on their way ----
+        // ---- e4m3: the codes of a tile of keys or values to f16, 16 at a time ----
         if constexpr (E4M3) {
-            constexpr int kConvert = S::kConvertWarps * 32;
+            if constexpr (NQ == 2) fewer_registers<S::kConvertRegs>();
+            constexpr int kConvert = S::kConvertWarps * 32, kParts = kTile / S::kStageRows;
             const int t = threadIdx.x - S::kConvertWarp * 32;
-            constexpr int kRowChunks = DP / 16, kStepRows = kConvert / kRowChunks, kTurns = kTile / kStepRows;
+            constexpr int kRowChunks = DP / 16, kStepRows = kConvert / kRowChunks, kTurns = S::kStageRows / kStepRows;
             const int chunk = t % kRowChunks, row0 = t / kRowChunks;
             const bool in = chunk * 16 < D;
             static_assert(kStepRows % 8 == 0, "rows");
+            const int first = row0 * a.pitch + chunk * 16, step = kStepRows * a.pitch;
             const int line = (chunk >> 2) * (kTile * 128) + row0 * 128;
             const int low = line + ((((chunk & 3) * 2) ^ (row0 & 7)) << 4), high = low ^ 16;
-            constexpr int kAtOnce = kTurns < 8 ? kTurns : 8, kPasses = kTurns / kAtOnce;
-            int e = 0;
-            // Pieces of the walk in order: pass 0 .. kPasses-1 of the keys, then of the values.
-            PromptWalk<UR> ahead = w;
-            bool more = ahead.next(a);
-            int tile_ahead = ahead.t0, part_ahead = 0;
-            auto fetch = [&](uint4 (&x)[kAtOnce]) {
-                if (!more) return;
-                const int kv = part_ahead / kPasses, turn = part_ahead % kPasses * kAtOnce;
-                const int32_t* table = c.pages + ahead.b * c.pages_stride;
-                const uint8_t* base = (kv ? c.v : c.k) + ahead.kv * c.head_stride + chunk * 16;
-#pragma unroll
-                for (int i = 0; i < kAtOnce; ++i) {
-                    const int pos = tile_ahead * kTile + row0 + (turn + i) * kStepRows;
-                    x[i] = make_uint4(0u, 0u, 0u, 0u);
-                    if (in && pos < ahead.end) {
-                        const int pg_at = page_of(pos, c.div_mul, c.div_shift), pg = __ldg(table + pg_at);
-                        if (static_cast<unsigned>(pg) < static_cast<unsigned>(c.n_pages))
-                            x[i] = *reinterpret_cast<const uint4*>(base + pg * c.page_stride + (pos - pg_at * c.page_size) * c.pos_stride);
-                    }
-                }
-                if (++part_ahead == 2 * kPasses) {
-                    part_ahead = 0;
-                    if (++tile_ahead == ahead.t1) {
-                        ahead.step(a);
-                        more = ahead.next(a);
-                        tile_ahead = ahead.t0;
-                    }
-                }
-            };
-            auto convert = [&](const uint4 (&x)[kAtOnce], int turn) {
-                uint8_t* const to = ring + e % S::kSlots * S::kSlot;
-                if (turn == 0 && e >= S::kSlots) wait_for(&sh.empty[e % S::kSlots], e / S::kSlots - 1, &sh.dead);
-                if (in)
-#pragma unroll
-                    for (int i = 0; i < kAtOnce; ++i) {
-                        const uint2 h0 = four_codes(x[i].x), h1 = four_codes(x[i].y), h2 = four_codes(x[i].z), h3 = four_codes(x[i].w);
-                        const int at = (turn + i) * (kStepRows * 128);
-                        *reinterpret_cast<uint4*>(to + low + at) = make_uint4(h0.x, h0.y, h1.x, h1.y);
-                        *reinterpret_cast<uint4*>(to + high + at) = make_uint4(h2.x, h2.y, h3.x, h3.y);
-                    }
-                if (turn + kAtOnce == kTurns) {
-                    fence_smem_async();
-                    __syncwarp();
-                    mbar_arrive_if(&sh.full[e % S::kSlots], lane == 0);
-                    ++e;
-                }
-            };
-            uint4 x[kAtOnce], y[kAtOnce];
-            fetch(x);
-            // (the list has an even number of pieces: keys and values)
-            int64_t pieces = w.left * 2 * kPasses;
-            int turn = 0;
+            int e = 0;                                           // parts
 #pragma unroll 1
-            for (; pieces > 0; pieces -= 2) {
-                fetch(y);
-                convert(x, turn);
-                turn = (turn + kAtOnce) % kTurns;
-                fetch(x);
-                convert(y, turn);
-                turn = (turn + kAtOnce) % kTurns;
+            while (w.next(a)) {
+#pragma unroll 1
+                for (int tile = w.t0; tile < w.t1; ++tile) {
+#pragma unroll 1
+                    for (int part = 0; part < 2 * kParts; ++part, ++e) {
+                        const int entry = e / kParts, slot = entry % S::kSlots, stage = e % S::kStages, base = part % kParts * S::kStageRows;
+                        const int rows = w.end - tile * kTile - base;           // the rest is zeros
+                        const uint8_t* from = stages + stage * S::kStage + first;
+                        uint8_t* const to = ring + slot * S::kSlot + base * 128;
+                        const bool codes = over(&sh.stage_full[stage], e / S::kStages);
+                        const bool room = entry < S::kSlots || over(&sh.empty[slot], entry / S::kSlots - 1);
+                        wait_more(codes, &sh.stage_full[stage], e / S::kStages, &sh.dead);
+                        wait_more(room, &sh.empty[slot], entry / S::kSlots - 1, &sh.dead);
+                        if (in) {
+                            constexpr int kAtOnce = kTurns < 8 ? kTurns : 8;
+#pragma unroll 1
+                            for (int turn = 0; turn < kTurns; turn += kAtOnce) {
+                                uint4 x[kAtOnce];
+#pragma unroll
+                                for (int i = 0; i < kAtOnce; ++i, from += step) x[i] = *reinterpret_cast<const uint4*>(from);
+                                if (rows < S::kStageRows)
+#pragma unroll
+                                    for (int i = 0; i < kAtOnce; ++i)
+                                        if (row0 + (turn + i) * kStepRows >= rows) x[i] = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                                for (int i = 0; i < kAtOnce; ++i) {
+                                    const uint2 h0 = four_codes(x[i].x), h1 = four_codes(x[i].y), h2 = four_codes(x[i].z), h3 = four_codes(x[i].w);
+                                    const int at = (turn + i) * (kStepRows * 128);
+                                    *reinterpret_cast<uint4*>(to + low + at) = make_uint4(h0.x, h0.y, h1.x, h1.y);
+                                    *reinterpret_cast<uint4*>(to + high + at) = make_uint4(h2.x, h2.y, h3.x, h3.y);
+                                }
+                            }
+                        }
+                        fence_smem_async();
+                        __syncwarp();
+                        mbar_arrive_if(&sh.stage_empty[stage], lane == 0);
+                        if (part % kParts == kParts - 1) mbar_arrive_if(&sh.full[slot], lane == 0);
+                    }
+                }
+                w.step(a);
             }
         }
     } else {
         // ---- softmax: a row a thread ----
+        if constexpr (NQ == 2) more_registers<S::kSoftmaxRegs>();
         const int q = warp >> 2, quad = warp & 3, j = quad * 32 + lane;
         const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16, my_o = tmem + lanes + S::kO + q * DP;
         constexpr float kLift = E4M3 ? 7.f : 0.f;       // f16 weights up to 2^15 instead of 2^8: fewer of them vanish
@@ -739,7 +744,36 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             float m = -INFINITY;                        // (of x, in powers of two; less the lift)
             uint64_t l2 = 0;
             float f = a.scale2;
-            uint64_t f2 = pack_f32x2(f, f);
+            if constexpr (E4M3) {
+                // the row's queries, bf16 to f16: its largest element to 2^14..2^15 by a power of two
+                wait_for(&sh.q_raw[q], seg, &sh.dead);
+                uint8_t* const mine_q = q_smem + q * (S::kPanels * 128 * 128) + j * 128;
+                uint32_t most = 0;
+#pragma unroll 1
+                for (int ch = 0; ch < D / 8; ++ch) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(mine_q + (ch >> 3) * (128 * 128) + (((ch & 7) ^ (j & 7)) << 4));
+                    const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) most = max(most, max((v[k] << 16) & 0x7FFF0000u, v[k] & 0x7FFF0000u));
+                }
+                const int ex = static_cast<int>(most >> 23);
+                const int up = ex == 0 || ex == 255 ? 0 : min(14 - (ex - 127), 120);
+                const float lift = __uint_as_float((static_cast<uint32_t>(up + 127) << 23) ^ (a.flip & 0x80000000u));
+                f *= __uint_as_float(static_cast<uint32_t>(127 - up) << 23);
+#pragma unroll 2
+                for (int ch = 0; ch < D / 8; ++ch) {
+                    uint4* const at = reinterpret_cast<uint4*>(mine_q + (ch >> 3) * (128 * 128) + (((ch & 7) ^ (j & 7)) << 4));
+                    uint32_t v[4] = {at->x, at->y, at->z, at->w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        v[k] = pack_f16(__uint_as_float(v[k] << 16) * lift, __uint_as_float(v[k] & 0xFFFF0000u) * lift);
+                    *at = make_uint4(v[0], v[1], v[2], v[3]);
+                }
+                fence_smem_async();
+                __syncwarp();
+                mbar_arrive_if(&sh.q_full[q], lane == 0);
+            }
+            const uint64_t f2 = pack_f32x2(f, f);
 #pragma unroll 1
             for (int tile = w.t0; tile < w.t1; ++tile, ++tile_no, ++mine) {
                 const int at = NQ == 2 ? q : mine & 1;
@@ -750,21 +784,16 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 wait_for(&sh.s_full[at], s_turn, &sh.dead);
                 __syncwarp();
                 tmem_after_sync();
-                if constexpr (E4M3) {
-                    // (written before the queries were handed to the matrix instructions; asking that barrier itself would
-                    // ask for a phase that may be two behind)
-                    if (tile == w.t0) f = a.scale2 * sh.back[seg & 1][q * 128 + j], f2 = pack_f32x2(f, f);
-                }
                 const bool masked = tile * kTile + kTile - 1 > seen_by_all;
                 const bool holes = sh.holes[tile_no % kAhead];
-                // x of 32 keys
-                auto load = [&](int ch, float (&x)[32]) {
-                    tmem_load(s_at + ch * 32, x);
+                // x of 64 keys
+                auto load = [&](int half, float (&x)[64]) {
+                    tmem_load(s_at + half * 64, x);
                     if constexpr (E4M3) {
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4) {
-                            const float4 kf = *reinterpret_cast<const float4*>(&sh.key_factor[k_at][ch * 32 + i]);
-                            const float4 lg = *reinterpret_cast<const float4*>(&sh.key_log[k_at][ch * 32 + i]);
+                        for (int i = 0; i < 64; i += 4) {
+                            const float4 kf = *reinterpret_cast<const float4*>(&sh.key_factor[k_at][half * 64 + i]);
+                            const float4 lg = *reinterpret_cast<const float4*>(&sh.key_log[k_at][half * 64 + i]);
                             const uint64_t a0 = fma_f32x2(pack_f32x2(kf.x, kf.y), f2, 0ull), a1 = fma_f32x2(pack_f32x2(kf.z, kf.w), f2, 0ull);
                             const uint64_t lo = fma_f32x2(pack_f32x2(x[i], x[i + 1]), a0, pack_f32x2(lg.x, lg.y));
                             const uint64_t hi = fma_f32x2(pack_f32x2(x[i + 2], x[i + 3]), a1, pack_f32x2(lg.z, lg.w));
@@ -772,25 +801,28 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                         }
                     }
                     if (masked) {
-                        const int most = limit - tile * kTile - ch * 32;              // keys up to here
+                        const int most = limit - tile * kTile - half * 64;            // keys up to here
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
+                        for (int i = 0; i < 64; ++i)
                             if (i > most) x[i] = -INFINITY;
                     }
                     if (holes) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (!sh.live[tile_no % kAhead][ch * 32 + i]) x[i] = -INFINITY;
+                        for (int i = 0; i < 64; ++i)
+                            if (!sh.live[tile_no % kAhead][half * 64 + i]) x[i] = -INFINITY;
                     }
                 };
-                float top = -INFINITY;
+                auto most_of = [&](const float (&x)[64]) {
+                    float t0 = x[0], t1 = x[1];
 #pragma unroll
-                for (int ch = 0; ch < 4; ++ch) {
-                    float x[32];
-                    load(ch, x);
-#pragma unroll
-                    for (int i = 0; i < 32; i += 2) top = max3(top, x[i], x[i + 1]);
-                }
+                    for (int i = 2; i < 62; i += 4) t0 = max3(t0, x[i], x[i + 1]), t1 = max3(t1, x[i + 2], x[i + 3]);
+                    return max3(fmaxf(t0, t1), x[62], x[63]);
+                };
+                float x0[64], x1[64];
+                load(0, x0);
+                float top = most_of(x0);
+                load(1, x1);
+                top = fmaxf(top, most_of(x1));
                 if constexpr (!E4M3) top = top > -INFINITY ? top * f : top;
                 // m moves: at first, or when weights would grow too large
                 const bool up = top > m + kRoomUp || (m == -INFINITY && top > -INFINITY);
@@ -818,29 +850,25 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 }
                 const float less = m == -INFINITY ? 0.f : kLift - m;
                 const uint64_t less2 = pack_f32x2(less, less);
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
+                auto weights = [&](int half, const float (&x)[64]) {
                     uint32_t p[32];
 #pragma unroll
-                    for (int ch = 0; ch < 2; ++ch) {
-                        float x[32];
-                        load(2 * half + ch, x);
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            const uint64_t e = E4M3 ? add_f32x2(pack_f32x2(x[i], x[i + 1]), less2) : fma_f32x2(pack_f32x2(x[i], x[i + 1]), f2, less2);
-                            const float p0 = ex2(lo_f32(e)), p1 = ex2(hi_f32(e));
-                            if constexpr (E4M3) {
-                                const float2 inv = *reinterpret_cast<const float2*>(&sh.key_inverse[k_at][(2 * half + ch) * 32 + i]);
-                                l2 = fma_f32x2(pack_f32x2(p0, p1), pack_f32x2(inv.x, inv.y), l2);
-                                p[ch * 16 + i / 2] = pack_f16(p0, p1);
-                            } else {
-                                l2 = add_f32x2(l2, pack_f32x2(p0, p1));
-                                p[ch * 16 + i / 2] = pack_bf16(p0, p1);
-                            }
+                    for (int i = 0; i < 64; i += 2) {
+                        const uint64_t e = E4M3 ? add_f32x2(pack_f32x2(x[i], x[i + 1]), less2) : fma_f32x2(pack_f32x2(x[i], x[i + 1]), f2, less2);
+                        const float p0 = ex2(lo_f32(e)), p1 = ex2(hi_f32(e));
+                        if constexpr (E4M3) {
+                            const float2 inv = *reinterpret_cast<const float2*>(&sh.key_inverse[k_at][half * 64 + i]);
+                            l2 = fma_f32x2(pack_f32x2(p0, p1), pack_f32x2(inv.x, inv.y), l2);
+                            p[i / 2] = pack_f16(p0, p1);
+                        } else {
+                            l2 = add_f32x2(l2, pack_f32x2(p0, p1));
+                            p[i / 2] = pack_bf16(p0, p1);
                         }
                     }
                     tmem_store32(s_at + half * 32, p);
-                }
+                };
+                weights(0, x0);
+                weights(1, x1);
                 tmem_store_wait();
                 tmem_before_sync();
                 __syncwarp();
@@ -857,17 +885,31 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 const float inverse = l > 0.f ? 1.f / l : 0.f;
                 const int64_t row = w.p.row + static_cast<int64_t>(tok);
                 if (is_row && a.lse) a.lse[row * a.q_heads + head] = l > 0.f ? (log2f(l) + m - kLift) * 0.69314718055994531f : -INFINITY;
-                __nv_bfloat16* out = a.out + row * a.o_tok + head * a.o_head;
+                // kOutBytes of each of the warp's 32 rows at a time: a row a lane into shared memory, whole pieces of rows out of it
+                constexpr int kCols = S::kOutBytes / 2, kPieces = kCols / 8, kAt = 32 / kPieces;
+                uint8_t* const room = out_smem + warp * (32 * S::kOutBytes);
+                const uint32_t wrows = static_cast<uint32_t>(max(0, min(32, w.rows - q * 128 - quad * 32)));
 #pragma unroll 1
-                for (int i = 0; i < D; i += 16) {
-                    float o[16];
-                    tmem_load(my_o + i, o);
-                    uint32_t y[8];
+                for (int i = 0; i < D; i += kCols) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) y[k] = l > 0.f ? pack_bf16(o[2 * k] * inverse, o[2 * k + 1] * inverse) : 0u;
-                    if (is_row) {
-                        *reinterpret_cast<uint4*>(out + i) = make_uint4(y[0], y[1], y[2], y[3]);
-                        *reinterpret_cast<uint4*>(out + i + 8) = make_uint4(y[4], y[5], y[6], y[7]);
+                    for (int half = 0; half < kCols / 32; ++half) {
+                        float o[32];
+                        tmem_load(my_o + i + half * 32, o);
+#pragma unroll
+                        for (int k = 0; k < 32; k += 8) {
+                            const uint4 y = make_uint4(pack_bf16(o[k] * inverse, o[k + 1] * inverse), pack_bf16(o[k + 2] * inverse, o[k + 3] * inverse),
+                                                       pack_bf16(o[k + 4] * inverse, o[k + 5] * inverse), pack_bf16(o[k + 6] * inverse, o[k + 7] * inverse));
+                            *reinterpret_cast<uint4*>(room + lane * S::kOutBytes + (((half * 4 + k / 8) ^ (lane & (kPieces - 1))) << 4)) = y;
+                        }
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int k = 0; k < kPieces; ++k) {
+                        const int rr = k * kAt + lane / kPieces, piece = lane % kPieces;
+                        const uint32_t at_tok = __shfl_sync(0xFFFFFFFFu, tok, rr), at_head = __shfl_sync(0xFFFFFFFFu, head, rr);
+                        const uint4 y = *reinterpret_cast<const uint4*>(room + rr * S::kOutBytes + ((piece ^ (rr & (kPieces - 1))) << 4));
+                        if (rr < wrows && i + piece * 8 < D)
+                            *reinterpret_cast<uint4*>(a.out + (w.p.row + static_cast<int64_t>(at_tok)) * a.o_tok + at_head * a.o_head + i + piece * 8) = y;
                     }
                     __syncwarp();
                 }
@@ -888,7 +930,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 if (w.t0 == 0) cut_here = true;
                 if (w.t0 == 0 && threadIdx.x == 0) {
                     // the CTA that has the unit's last tile
-                    const long long last = w.at + w.T - 1, edge = (sh.each + 1) * sh.extra;
+                    const long long last = w.at + w.pre + w.T - 1, edge = (sh.each + 1) * sh.extra;
                     const int c_last = static_cast<int>(last < edge ? last / (sh.each + 1) : sh.extra + (last - edge) / sh.each);
                     a.cuts[blockIdx.x] = {c_last - static_cast<int>(blockIdx.x) + 1, static_cast<int>(blockIdx.x), static_cast<int>(w.r0), w.rows,
                                           w.p.row, w.kv};

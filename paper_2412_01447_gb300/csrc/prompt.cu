@@ -133,16 +133,20 @@ PLDP_API pldp_status pldp_attend_prompt(const pldp_attend_prompt_args* p, void* 
     // keeps a masked score at -infinity.
     a.scale2 = fmaxf(fabsf(p->scale) * 1.4426950408889634f, 0x1p-126f);
     a.flip = p->scale < 0.f ? 0x80008000u : 0u;
-    a.least = 2;
+    a.least = kUnitCost + 2;
     a.box = kTile;                                           // the largest power of two that divides the page, up to a tile
     while (p->cache.page_size % a.box) a.box /= 2;
     const bool e4m3 = p->cache.dtype == PLDP_E4M3;
+    const int dp = prompt_dim(p->cache.head_dim);
+    if (e4m3 && dp == 256 && a.box > 64) a.box = 64;         // (a stage holds half a tile)
+    // a copy starts at a multiple of 128 bytes of shared memory: vectors side by side where a box of them is one
+    a.pitch = p->cache.head_dim * a.box % 128 == 0 ? p->cache.head_dim : p->cache.head_dim <= 128 ? 128 : 256;
     Maps maps = {};
     bool head_first = false;
-    if (!e4m3 && (!pool_map(&maps.k, a.c.k, a.c, false, a.box, 0, &head_first) || !pool_map(&maps.v, a.c.v, a.c, false, a.box, 0, &head_first)))
+    if (!pool_map(&maps.k, a.c.k, a.c, e4m3, a.box, a.pitch, &head_first) || !pool_map(&maps.v, a.c.v, a.c, e4m3, a.box, a.pitch, &head_first))
         return fail(PLDP_ERR_UNSUPPORTED, "%s: the cache's strides cannot be described to the copy engine", fn);
     a.head_first = head_first;
-    const int ctas = prompt_ctas(), dp = prompt_dim(p->cache.head_dim);
+    const int ctas = prompt_ctas();
     auto s = static_cast<cudaStream_t>(stream);
     cudaError_t e = e4m3 ? launch_prompt_e4m3(a, maps, ctas, s) : launch_prompt_bf16(a, maps, ctas, s);
     if (e != cudaSuccess) return launched(fn, e);
