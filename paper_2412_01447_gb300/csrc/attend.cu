@@ -29,20 +29,23 @@ size_t space_of(int64_t n, int64_t q_heads, int64_t heads, int head_dim) {
 
 }  // namespace
 
-// The pool as a tensor of (element, position, head, page), its middle dimensions by ascending
-// stride, copied in boxes of `box` positions of one head of one page: 64 elements of bf16, swizzled as the
-// matrix instructions read them, or a whole vector of codes.
-bool pool_map(CUtensorMap* map, void* base, const CacheView& c, bool e4m3, int box, int pitch, bool* head_first) {
+TensorMapEncoder tensor_map_encoder() {
     static const auto encode = [] {
         void* f = nullptr;
         cudaDriverEntryPointQueryResult found;
         if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
             found != cudaDriverEntryPointSuccess)
             f = nullptr;
-        return reinterpret_cast<CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                             const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                             CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill)>(f);
+        return reinterpret_cast<TensorMapEncoder>(f);
     }();
+    return encode;
+}
+
+// The pool as a tensor of (element, position, head, page), its middle dimensions by ascending
+// stride, copied in boxes of `box` positions of one head of one page: 64 elements of bf16, swizzled as the
+// matrix instructions read them, or a whole vector of codes.
+bool pool_map(CUtensorMap* map, void* base, const CacheView& c, bool e4m3, int box, int pitch, bool* head_first) {
+    const auto encode = tensor_map_encoder();
     if (!encode) return false;
     // the stride of a dimension of one is never used; any that the map takes will do
     const auto used = [&](int64_t stride, int size) { return static_cast<cuuint64_t>(size == 1 ? c.vec_bytes : stride); };

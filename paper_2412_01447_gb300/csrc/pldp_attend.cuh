@@ -36,6 +36,11 @@ struct AttendArgs {
 struct Maps {
     CUtensorMap k, v;
 };
+// cuTensorMapEncodeTiled, or null where the driver has none.
+using TensorMapEncoder = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                      const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                      CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+TensorMapEncoder tensor_map_encoder();
 bool pool_map(CUtensorMap* map, void* base, const CacheView& c, bool e4m3, int box, int pitch, bool* head_first);
 
 // One launch for nt columns; one translation unit a cache type.

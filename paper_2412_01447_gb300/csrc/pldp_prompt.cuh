@@ -18,6 +18,7 @@ struct PromptArgs {
     int B, R, q_heads, group;
     int box, pitch;                        // as AttendArgs
     int head_first;
+    int q_boxes;                           // queries by boxes of whole tokens
     int least;                             // of the list a CTA takes at least
     float scale2;                          // |scale| * log2(e)
     uint32_t flip;                         // what turns the signs of two queries for a negative scale
@@ -31,9 +32,13 @@ struct CutUnit {
     int row_base, kv;                      // the sequence's first row
 };
 
+struct PromptMaps {
+    Maps pool;
+    CUtensorMap q;
+};
 // One launch; one translation unit a cache type.
-cudaError_t launch_prompt_bf16(const PromptArgs& a, const Maps& m, int ctas, cudaStream_t s);
-cudaError_t launch_prompt_e4m3(const PromptArgs& a, const Maps& m, int ctas, cudaStream_t s);
+cudaError_t launch_prompt_bf16(const PromptArgs& a, const PromptMaps& m, int ctas, cudaStream_t s);
+cudaError_t launch_prompt_e4m3(const PromptArgs& a, const PromptMaps& m, int ctas, cudaStream_t s);
 
 __host__ __device__ constexpr int prompt_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 __host__ __device__ constexpr int prompt_rows(int dp) { return dp == 256 ? 128 : 256; }       // rows of a unit
@@ -85,7 +90,7 @@ __device__ __forceinline__ int64_t tiles_before(const Units& s, int u) {
 }
 // What a unit costs beside its tiles, in tiles: its queries' way in, the first scores' and the last weights' latency, its
 // results' way out.  The list counts it, so that a part of many short units is not the last to end.
-constexpr int kUnitCost = 3;
+constexpr int kUnitCost = 2;
 template <int UR>
 __device__ __forceinline__ int64_t cost_before(const Units& s, int u) { return tiles_before<UR>(s, u) + static_cast<int64_t>(u) * kUnitCost; }
 // The unit that holds place x of the list of one kv head: cost_before(u) <= x < cost_before(u + 1).
@@ -106,8 +111,8 @@ struct PromptShape {
     static constexpr int kRows = kQ * 128;
     static constexpr int kSoftmaxWarps = 4 * kQ;
     static constexpr int kConvertWarps = E4M3 ? 4 : 0;
-    // warps: softmax, matrix instructions, copies, keys' scales, queries, conversion
-    static constexpr int kMmaWarp = kSoftmaxWarps, kCopyWarp = kMmaWarp + 1, kKeyWarp = kMmaWarp + 2, kQueryWarp = kMmaWarp + 3;
+    // warps: softmax, matrix instructions, keys' scales, copies, queries, conversion
+    static constexpr int kMmaWarp = kSoftmaxWarps, kKeyWarp = kMmaWarp + 1, kCopyWarp = kMmaWarp + 2, kQueryWarp = kMmaWarp + 3;
     static constexpr int kConvertWarp = kMmaWarp + 4;
     static constexpr int kThreads = (kSoftmaxWarps + 4 + kConvertWarps) * 32;
     static constexpr int kPanels = DP / 64;
@@ -127,8 +132,8 @@ struct PromptShape {
     static constexpr int kStages = kFit > 6 ? 6 : kFit;
     static constexpr int kBytes = kQBytes + kSlots * kSlot + kStages * kStage + kOut + 1024;
     static constexpr int kO = 256;                             // column of the first sums
-    // 384 threads start with 168 registers each (512: 128); the softmax takes what the others leave
-    static constexpr int kSoftmaxRegs = E4M3 ? 184 : 208, kOtherRegs = E4M3 ? 56 : 88, kConvertRegs = 88;
+    // 384 threads start with 168 registers each (640: 96); the softmax takes what the others leave
+    static constexpr int kSoftmaxRegs = 184, kOtherRegs = E4M3 ? 56 : 136, kConvertRegs = 88;
     static_assert(kSlots >= 2 && (!E4M3 || kStages >= 1) && kBytes + kStatic <= kMaxShared, "shared memory");
 };
 
@@ -136,14 +141,17 @@ constexpr int kAhead = 8;                  // tiles whose holes are kept (more t
 
 template <bool E4M3>
 struct PromptShared {
-    alignas(16) float key_factor[E4M3 ? 4 : 1][E4M3 ? kTile : 4], key_log[E4M3 ? 4 : 1][E4M3 ? kTile : 4], key_inverse[E4M3 ? 4 : 1][E4M3 ? kTile : 4];
-    uint8_t live[kAhead][kTile];           // whether a page holds the key; looked at where `holes` is set
+    // of the keys of four tiles: the scale of the key, that of the value by 2^-unit as two f16
+    alignas(16) float key_scale[E4M3 ? 4 : 1][E4M3 ? kTile : 4];
+    uint32_t value_scale[E4M3 ? 4 : 1][E4M3 ? kTile : 4];
+    int unit_of[4];
+    uint32_t live[kAhead][4];              // whether a page holds the key, a bit each; looked at where `holes` is set
     int holes[kAhead];
-    uint64_t full[8], empty[8], stage_full[6], stage_empty[6], q_raw[2], s_full[2], p_full[2], pv_done[2], q_full[2], q_empty[2], tail, drained,
+    uint64_t full[8], empty[8], stage_full[6], stage_empty[6], q_raw[2], s_full[2], p_full[2][2], pv_half[2], pv_done[2], q_full[2], q_empty[2], tail, drained,
         key_full[4], key_empty[4];
     uint32_t tmem;
     int dead, zeros;
-    long long warp_sum[20];
+    long long warp_sum[24];
     long long total;
     // where this CTA's part of the list starts
     int b, kv, unit, tile, pre;
@@ -174,11 +182,11 @@ struct PromptWalk {
         }
         s = units_of(p, a.group);
         units = unit_count<UR>(s);
+        end = s.start + s.count;
         T = unit_tiles<UR>(s, unit);
         t1 = left - pre < T - t0 ? t0 + static_cast<int>(left - pre) : T;
         r0 = static_cast<int64_t>(unit) * UR;
         rows = static_cast<int>(min(static_cast<int64_t>(UR), s.N - r0));
-        end = s.start + s.count;
         return true;
     }
     __device__ __forceinline__ void step(const PromptArgs& a) {
@@ -192,6 +200,15 @@ struct PromptWalk {
     }
 };
 
+// tma_box by the lane that leads, all lanes with the same values.
+__device__ __forceinline__ void tma_box_if(void* dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint64_t* bar, uint32_t lead) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.u32 q, %7, 0;\n\t"
+        "@q cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}"
+        ::"r"(smem_u32(dst)), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(smem_u32(bar)), "r"(lead)
+        : "memory");
+}
 // D += A B with A in tensor memory.
 __device__ __forceinline__ void mma_f16_tmem(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t b_hi, uint32_t form, uint32_t accumulate,
                                              uint32_t lead) {
@@ -216,6 +233,49 @@ __device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t* v) {
 // 16 bytes from global to shared memory, later, or zeros.
 __device__ __forceinline__ void copy_or_zeros(void* to, const void* from, bool there) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+// 2^e, -126 <= e <= 127.
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+// The arithmetic of the weights, where it is written.
+__device__ __forceinline__ float ordered_ex2(float x) {
+    float y;
+    asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float ordered_max3(float a, float b, float c) {
+    float d;
+    asm volatile("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t ordered_fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm volatile("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t ordered_add2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm volatile("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t ordered_bf16(float lo, float hi) {
+    uint32_t d;
+    asm volatile("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+__device__ __forceinline__ uint32_t ordered_f16(float lo, float hi) {
+    uint32_t d;
+    asm volatile("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
@@ -244,7 +304,8 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // ---------------------------------------------------------------------------
 template <int DP, bool E4M3>
 __global__ void __launch_bounds__(PromptShape<DP, E4M3>::kThreads, 1)
-prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+              const __grid_constant__ CUtensorMap q_map) {
     using S = PromptShape<DP, E4M3>;
     constexpr int UR = S::kRows, NQ = S::kQ, kThreads = S::kThreads;
     static_assert(sizeof(PromptShared<E4M3>) <= S::kStatic, "shared memory");
@@ -270,14 +331,16 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.q_raw[i], 1);
             mbar_init(&sh.s_full[i], 1);
-            mbar_init(&sh.p_full[i], 4);
+            mbar_init(&sh.p_full[i][0], 4);
+            mbar_init(&sh.p_full[i][1], 4);
+            mbar_init(&sh.pv_half[i], 1);
             mbar_init(&sh.pv_done[i], 1);
             mbar_init(&sh.q_full[i], E4M3 ? 4 : 1);
             mbar_init(&sh.q_empty[i], 1);
         }
         for (int i = 0; i < 4; ++i) {
             mbar_init(&sh.key_full[i], 1);
-            mbar_init(&sh.key_empty[i], S::kSoftmaxWarps);
+            mbar_init(&sh.key_empty[i], S::kSoftmaxWarps + S::kConvertWarps);
         }
         mbar_init(&sh.tail, 1);
         mbar_init(&sh.drained, 1);
@@ -375,25 +438,33 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
     if (warp >= S::kMmaWarp && warp < S::kConvertWarp) {
     if constexpr (NQ == 2) fewer_registers<S::kOtherRegs>();
     if (warp == S::kCopyWarp) {
-        // ---- copies: keys and values in turn, a box (positions of one page) and its panel a lane ----
+        // ---- copies: keys and values in turn, a box (positions of one page) at a time ----
         constexpr int kDepth = E4M3 ? S::kStages : S::kSlots, kParts = E4M3 ? kTile / S::kStageRows : 1, kPartRows = kTile / kParts;
-        constexpr int kPieces = E4M3 ? 1 : S::kPanels;                     // copies of a box
+        const uint32_t lead = elect_lane();
         uint64_t* const arrived = E4M3 ? sh.stage_full : sh.full;
         uint64_t* const left = E4M3 ? sh.stage_empty : sh.empty;
-        const int boxes = kPartRows / a.box;
+        const int boxes = kTile / a.box, part_boxes = kPartRows / a.box;
         int e = 0, tile_no = 0, tails = 0;
         bool on = true;
 #pragma unroll 1
         while (on && w.next(a)) {
             const int32_t* table = c.pages + w.b * c.pages_stride;
+            // the page of box `box` of a tile; those of the next tile, a box a lane, are asked for before this one's
+            // copies (pages that 4 does not divide have more boxes than lanes)
+            auto look = [&](int tile, int box) {
+                const int pos = tile * kTile + box * a.box;
+                return tile < w.t1 && box < boxes && pos < w.end ? load_now(table + page_of(pos, c.div_mul, c.div_shift)) : 0;
+            };
+            int page = look(w.t0, lane);
 #pragma unroll 1
             for (int tile = w.t0; on && tile < w.t1; ++tile, ++tile_no) {
                 const bool tail = !E4M3 && tile * kTile + kTile > w.end;
+                const int page_ahead = look(tile + 1, lane);
 #pragma unroll 1
                 for (int part = 0; on && part < 2 * kParts; ++part, ++e) {
-                    const int kv = part / kParts, from = tile * kTile + part % kParts * kPartRows;
+                    const int kv = part / kParts, first = part % kParts * part_boxes;
                     // boxes that hold a position of the sequence
-                    const int full = max(0, min(boxes, (w.end - from + a.box - 1) / a.box));
+                    const int full = max(0, min(part_boxes, (w.end - tile * kTile + a.box - 1) / a.box - first));
                     const CUtensorMap* map = kv ? &v_map : &k_map;
                     const int at = e % kDepth;
                     if (e >= kDepth) wait_for(&left[at], e / kDepth - 1, &sh.dead);
@@ -404,27 +475,40 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                     __syncwarp();
                     uint8_t* dst = E4M3 ? stages + at * S::kStage : ring + at * S::kSlot;
                     bool hole = false;
+                    // issued one after the other by the lane that leads: a branch around the copy would make every
+                    // operand one lane's
 #pragma unroll 1
-                    for (int i = lane; i < full * kPieces; i += 32) {
-                        const int box = i / kPieces, p = i % kPieces, pos = from + box * a.box;
-                        const int pg_at = page_of(pos, c.div_mul, c.div_shift), slot = pos - pg_at * c.page_size;
-                        int pg = __ldg(table + pg_at);
+                    for (int b0 = 0; b0 < full; b0 += 32) {
+                        const int box = first + b0 + lane, pos = tile * kTile + box * a.box;
+                        const int slot = pos - static_cast<int>(page_of(pos, c.div_mul, c.div_shift)) * c.page_size;
+                        int pg = boxes <= 32 ? __shfl_sync(0xFFFFFFFFu, page, box & 31) : look(tile, box);
                         if (static_cast<unsigned>(pg) >= static_cast<unsigned>(c.n_pages)) {
                             pg = c.n_pages;                                // outside the tensor: zeros
-                            hole = true;
+                            hole = hole || b0 + lane < full;
                         }
-                        const int c1 = a.head_first ? w.kv : slot, c2 = a.head_first ? slot : w.kv;
-                        if constexpr (E4M3) tma_box(dst + box * a.box * a.pitch, map, 0, c1, c2, pg, bar);
-                        else tma_box(dst + p * (kTile * 128) + box * a.box * 128, map, p * 64, c1, c2, pg, bar);
+                        const int count = min(32, full - b0);
+#pragma unroll 1
+                        for (int i = 0; i < count; ++i) {
+                            const int i_slot = __shfl_sync(0xFFFFFFFFu, slot, i), i_pg = __shfl_sync(0xFFFFFFFFu, pg, i);
+                            const int c1 = a.head_first ? w.kv : i_slot, c2 = a.head_first ? i_slot : w.kv;
+                            if constexpr (E4M3) {
+                                tma_box_if(dst + (b0 + i) * a.box * a.pitch, map, 0, c1, c2, i_pg, bar, lead);
+                            } else {
+#pragma unroll
+                                for (int p = 0; p < S::kPanels; ++p)
+                                    tma_box_if(dst + p * (kTile * 128) + (b0 + i) * a.box * 128, map, p * 64, c1, c2, i_pg, bar, lead);
+                            }
+                        }
                     }
                     if (!E4M3 && kv == 0) {
                         hole = __any_sync(0xFFFFFFFFu, hole);
                         if (hole) {
 #pragma unroll 1
-                            for (int i = lane; i < kTile; i += 32) {
-                                const int pos = tile * kTile + i;
+                            for (int i = 0; i < 4; ++i) {
+                                const int pos = tile * kTile + 32 * i + lane;
                                 const int pg = pos < w.end ? __ldg(table + page_of(pos, c.div_mul, c.div_shift)) : 0;
-                                sh.live[tile_no % kAhead][i] = static_cast<unsigned>(pg) < static_cast<unsigned>(c.n_pages);
+                                const uint32_t bits = __ballot_sync(0xFFFFFFFFu, static_cast<unsigned>(pg) < static_cast<unsigned>(c.n_pages));
+                                if (lane == 0) sh.live[tile_no % kAhead][i] = bits;
                             }
                             if (lane == 0 && a.status) atomicOr(a.status + w.b, PLDP_ST_PAGE);
                         }
@@ -445,6 +529,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                     }
                     __syncwarp();
                 }
+                page = page_ahead;
             }
             w.step(a);
         }
@@ -455,22 +540,82 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
         } else if (lane == 31 && tails > 0) {
             mbar_wait(&sh.tail, (tails - 1) & 1, kMbarPolls);
         }
-    } else if (E4M3 && warp == S::kKeyWarp) {
+    } else if (warp == S::kQueryWarp || (!E4M3 && warp == S::kKeyWarp)) {
+        // ---- queries of the next unit, as soon as the last scores of this one are done; bf16: a tile of rows a warp ----
+        const uint32_t lead = elect_lane();
+        int seg0 = 0, seg1 = 0;
+        auto queries = [&](int q, int& seg) {
+            if (q * 128 >= w.rows) return;
+            if (seg > 0) wait_for(&sh.q_empty[q], seg - 1, &sh.dead);
+            if (*static_cast<volatile int*>(&sh.dead)) return;
+            uint64_t* const bar = E4M3 ? &sh.q_raw[q] : &sh.q_full[q];
+            uint8_t* const to = q_smem + q * (S::kPanels * 128 * 128);
+            const uint32_t first = static_cast<uint32_t>(w.r0) + q * 128, group = a.group;
+            if (a.q_boxes) {
+                // whole tokens: boxes of their heads (what lies behind the sequence's rows is not used)
+                if (lane == 0) mbar_arrive_expect_tx(bar, S::kPanels * 128 * 128);
+                __syncwarp();
+#pragma unroll
+                for (int p = 0; p < S::kPanels; ++p)
+                    tma_box_if(to + p * (128 * 128), &q_map, p * 64, w.kv * a.group, w.p.row + static_cast<int>(first / group), 0, bar, lead);
+            } else {
+                // all of the tile's pieces of 16 bytes are asked for before the first is waited for
+                constexpr int kLanes = DP / 8, kAt = 32 / kLanes;          // lanes a row, and rows at once
+                const int piece = lane % kLanes;
+                const bool in = piece * 8 < D;
+                uint8_t* const mine = to + (piece >> 3) * (128 * 128);
+                uint32_t tok = (first + lane / kLanes) / group, h = first + lane / kLanes - tok * group;
+                const __nv_bfloat16* from = a.q + w.p.row * a.q_tok + static_cast<int64_t>(w.kv) * a.group * a.q_head + piece * 8;
+#pragma unroll 2
+                for (int row = lane / kLanes; row < 128; row += kAt) {
+                    const bool there = in && q * 128 + row < w.rows;
+                    copy_or_zeros(mine + row * 128 + (((piece & 7) ^ (row & 7)) << 4), there ? from + tok * a.q_tok + h * a.q_head : a.q, there);
+                    h += kAt;
+                    while (h >= group) h -= group, ++tok;
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                if (!E4M3 && a.flip) {
+                    // (each lane its own pieces)
+#pragma unroll 1
+                    for (int row = lane / kLanes; row < 128; row += kAt) {
+                        uint4* const at = reinterpret_cast<uint4*>(mine + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
+                        uint4 x = *at;
+                        x.x ^= a.flip, x.y ^= a.flip, x.z ^= a.flip, x.w ^= a.flip;
+                        *at = x;
+                    }
+                }
+                if constexpr (!E4M3) fence_smem_async();
+                __syncwarp();
+                mbar_arrive_if(bar, lane == 0);
+            }
+            ++seg;
+        };
+#pragma unroll 1
+        while (w.next(a)) {
+            if (E4M3 || warp == S::kQueryWarp) queries(0, seg0);
+            if (NQ == 2 && (E4M3 || warp == S::kKeyWarp)) queries(1, seg1);
+            w.step(a);
+        }
+        // boxes that nothing has waited for arrive before this CTA ends
+        const int last = lane ? seg1 : seg0;
+        if (a.q_boxes && lane < NQ && last > 0) mbar_wait(E4M3 ? &sh.q_raw[lane] : &sh.q_full[lane], (last - 1) & 1, kMbarPolls);
+    } else if (warp == S::kKeyWarp) {
         // ---- e4m3: the scales of each tile, four keys a lane ----
         if constexpr (E4M3) {
-            int tile_no = 0;
+            int tile_no = 0, unit = 0;
 #pragma unroll 1
             while (w.next(a)) {
                 const int32_t* table = c.pages + w.b * c.pages_stride;
 #pragma unroll 1
                 for (int tile = w.t0; tile < w.t1; ++tile, ++tile_no) {
                     const int at = tile_no & 3;
-                    float f[4], g[4], inv[4];
+                    float f[4], v[4];
                     bool gone[4], hole = false;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int pos = tile * kTile + 4 * lane + i;
-                        f[i] = 0.f, g[i] = 0.f, inv[i] = 1.f;
+                        f[i] = 0.f, v[i] = 0.f;
                         gone[i] = false;
                         if (pos < w.end) {
                             const int pg_at = page_of(pos, c.div_mul, c.div_shift), pg = __ldg(table + pg_at);
@@ -478,20 +623,27 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                             hole |= gone[i];
                             if (!gone[i]) {
                                 const int64_t from = (static_cast<int64_t>(pg) * c.heads + w.kv) * c.page_size + (pos - pg_at * c.page_size);
-                                const float v = fmaxf(__ldg(c.v_scale + from), kLeastScale);
-                                // (the logarithm is 2^-22 off at most, as much as the weight's own exponential)
-                                f[i] = __ldg(c.k_scale + from), g[i] = __log2f(v), inv[i] = reciprocal(v);
+                                f[i] = __ldg(c.k_scale + from), v[i] = __ldg(c.v_scale + from);
                             }
                         }
                     }
+                    // the values' unit 2^unit: above the largest scale of a unit's first tile, and of a later one that passes it
+                    const int most = static_cast<int>(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])))) >> 23) - 126;
+                    if (tile == w.t0 || most > unit) unit = min(most + 2, 126);
+                    const float by = power_of_two(-unit);
                     if (tile_no >= 4) wait_for(&sh.key_empty[at], (tile_no >> 2) - 1, &sh.dead);
-                    *reinterpret_cast<float4*>(&sh.key_factor[at][4 * lane]) = make_float4(f[0], f[1], f[2], f[3]);
-                    *reinterpret_cast<float4*>(&sh.key_log[at][4 * lane]) = make_float4(g[0], g[1], g[2], g[3]);
-                    *reinterpret_cast<float4*>(&sh.key_inverse[at][4 * lane]) = make_float4(inv[0], inv[1], inv[2], inv[3]);
+                    *reinterpret_cast<float4*>(&sh.key_scale[at][4 * lane]) = make_float4(f[0], f[1], f[2], f[3]);
+                    *reinterpret_cast<uint4*>(&sh.value_scale[at][4 * lane]) = make_uint4(pack_f16(v[0] * by, v[0] * by), pack_f16(v[1] * by, v[1] * by),
+                                                                                          pack_f16(v[2] * by, v[2] * by), pack_f16(v[3] * by, v[3] * by));
+                    if (lane == 0) sh.unit_of[at] = unit;
                     hole = __any_sync(0xFFFFFFFFu, hole);
                     if (hole) {
+                        // (this lane's four keys are bits 4 (lane & 7) and on of a word)
+                        uint32_t bits = (gone[0] ? 0u : 1u) | (gone[1] ? 0u : 2u) | (gone[2] ? 0u : 4u) | (gone[3] ? 0u : 8u);
+                        bits <<= 4 * (lane & 7);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) sh.live[tile_no % kAhead][4 * lane + i] = !gone[i];
+                        for (int o = 1; o < 8; o <<= 1) bits |= __shfl_xor_sync(0xFFFFFFFFu, bits, o);
+                        if ((lane & 7) == 0) sh.live[tile_no % kAhead][lane >> 3] = bits;
                         if (lane == 0 && a.status) atomicOr(a.status + w.b, PLDP_ST_PAGE);
                     }
                     if (lane == 0) sh.holes[tile_no % kAhead] = hole;
@@ -501,57 +653,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 w.step(a);
             }
         }
-    } else if (warp == S::kKeyWarp || warp == S::kQueryWarp) {
-        // ---- queries of the next unit, as soon as the last scores of this one are done ----
-        // All of a tile's pieces of 16 bytes are asked for before the first is waited for; bf16: a tile of rows a warp.
-        constexpr int kLanes = DP / 8, kAt = 32 / kLanes;          // lanes a row, and rows at once
-        constexpr int kStep = E4M3 ? 1 : 2;
-        const int piece = lane % kLanes, q0 = warp == S::kQueryWarp ? 0 : 1;
-        const bool in = piece * 8 < D;
-        int seg[2] = {0, 0};
-#pragma unroll 1
-        while (w.next(a)) {
-#pragma unroll 1
-            for (int q = q0; q < NQ; q += kStep) {
-                if (q * 128 >= w.rows) break;
-                if (seg[q] > 0) wait_for(&sh.q_empty[q], seg[q] - 1, &sh.dead);
-                uint8_t* const to = q_smem + q * (S::kPanels * 128 * 128) + (piece >> 3) * (128 * 128);
-                const uint32_t first = static_cast<uint32_t>(w.r0) + q * 128 + lane / kLanes, group = a.group;
-                uint32_t tok = first / group, h = first - tok * group;
-                const __nv_bfloat16* from = a.q + w.p.row * a.q_tok + static_cast<int64_t>(w.kv) * a.group * a.q_head + piece * 8;
-#pragma unroll 4
-                for (int row = lane / kLanes; row < 128; row += kAt) {
-                    const bool there = in && q * 128 + row < w.rows;
-                    copy_or_zeros(to + row * 128 + (((piece & 7) ^ (row & 7)) << 4), there ? from + tok * a.q_tok + h * a.q_head : a.q, there);
-                    h += kAt;
-                    while (h >= group) h -= group, ++tok;
-                }
-                asm volatile("cp.async.commit_group;" ::: "memory");
-            }
-#pragma unroll 1
-            for (int q = q0; q < NQ; q += kStep) {
-                if (q * 128 >= w.rows) break;
-                if (E4M3 && q == 0 && w.rows > 128) asm volatile("cp.async.wait_group 1;" ::: "memory");
-                else asm volatile("cp.async.wait_group 0;" ::: "memory");
-                if (!E4M3 && a.flip) {
-                    // (each lane its own pieces)
-                    uint8_t* const to = q_smem + q * (S::kPanels * 128 * 128) + (piece >> 3) * (128 * 128);
-#pragma unroll 4
-                    for (int row = lane / kLanes; row < 128; row += kAt) {
-                        uint4* const at = reinterpret_cast<uint4*>(to + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
-                        uint4 x = *at;
-                        x.x ^= a.flip, x.y ^= a.flip, x.z ^= a.flip, x.w ^= a.flip;
-                        *at = x;
-                    }
-                }
-                if constexpr (!E4M3) fence_smem_async();
-                __syncwarp();
-                mbar_arrive_if(E4M3 ? &sh.q_raw[q] : &sh.q_full[q], lane == 0);
-                ++seg[q];
-            }
-            w.step(a);
-        }
-    } else {
+    } else if (warp == S::kMmaWarp) {
         // ---- matrix instructions ----
         const uint64_t q_op = smem_operand(smem_u32(q_smem), 16, 1024, swizzle_mode(128));
         const uint64_t k_op = smem_operand(smem_u32(ring), 16, 1024, swizzle_mode(128));
@@ -562,91 +664,90 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
         const uint32_t values = mma_form(128, D, !E4M3, false, true);
         const uint32_t lead = elect_lane();
         int e = 0;                                       // entry of the ring
-        int seg[2] = {0, 0}, s_no[2] = {0, 0}, p_no[2] = {0, 0};     // units, scores and weights of each tile of rows so far
-        auto scores = [&](int q, int slot, int at) {     // S of a tile of rows, to place `at`
-            const uint32_t op = k_lo + slot * (S::kSlot / 16), qo = q_lo + q * (S::kPanels * 128 * 128 / 16);
+        int seg0 = 0, seg1 = 0, s_no = 0, p_no0 = 0, p_no1 = 0;      // units and weights of each tile of rows so far, and (of one) scores
+        // Two barriers, a lane each: a wait for two costs what one does.
+        auto wait_both = [&](uint64_t* x, uint32_t x_parity, uint64_t* y, uint32_t y_parity) {
+            uint64_t* const bar = lane == 0 ? x : lane == 1 ? y : nullptr;
+            const uint32_t parity = lane == 0 ? x_parity : y_parity;
+            bool done = bar == nullptr || over(bar, parity);
+            uint32_t polls = 0;
+#pragma unroll 1
+            while (!__all_sync(0xFFFFFFFFu, done)) {
+                if (++polls >= kPolls || *static_cast<volatile int*>(&sh.dead)) {
+                    *static_cast<volatile int*>(&sh.dead) = 1;
+                    break;
+                }
+                if (!done) done = over(bar, parity);
+            }
+            __syncwarp();
+            tmem_after_sync();
+        };
+        auto full = [&](int entry) { return &sh.full[entry % S::kSlots]; };
+        auto scores = [&](int q, int slot, int at) {     // to place `at`
+            const uint32_t op = __shfl_sync(0xFFFFFFFFu, k_lo + slot * (S::kSlot / 16), 0), to = __shfl_sync(0xFFFFFFFFu, tmem + at * 128, 0);
+            const uint32_t qo = __shfl_sync(0xFFFFFFFFu, q_lo + q * (S::kPanels * 128 * 128 / 16), 0);
 #pragma unroll
             for (int s = 0; s < DP / 16; ++s)
                 if (s * 16 < D)
-                    mma_f16(tmem + at * 128, qo + (s >> 2) * (128 * 8) + (s & 3) * 2, q_hi, op + (s >> 2) * (kTile * 8) + (s & 3) * 2, k_hi,
-                            kScores, s > 0, lead);
+                    mma_f16(to, qo + (s >> 2) * (128 * 8) + (s & 3) * 2, q_hi, op + (s >> 2) * (kTile * 8) + (s & 3) * 2, k_hi, kScores, s > 0, lead);
             mma_commit(&sh.s_full[at], lead);
         };
-        auto sums = [&](int q, int slot, int at, bool more) {
-            const uint32_t op = v_lo + slot * (S::kSlot / 16);
+        auto sums = [&](int q, int half, int slot, int at, bool more) {
+            const uint32_t op = __shfl_sync(0xFFFFFFFFu, v_lo + slot * (S::kSlot / 16), 0), from = __shfl_sync(0xFFFFFFFFu, tmem + at * 128, 0);
+            const uint32_t to = __shfl_sync(0xFFFFFFFFu, tmem + S::kO + q * DP, 0);
+            if (half == 0) {
 #pragma unroll
-            for (int s = 0; s < kTile / 16; ++s)
-                mma_f16_tmem(tmem + S::kO + q * DP, tmem + at * 128 + s * 8, op + s * 128, v_hi, values, s > 0 || more, lead);
-            mma_commit(&sh.pv_done[q], lead);
+                for (int s = 0; s < 4; ++s) mma_f16_tmem(to, from + s * 8, op + s * 128, v_hi, values, s > 0 || more, lead);
+            } else {
+#pragma unroll
+                for (int s = 4; s < 8; ++s) mma_f16_tmem(to, from + s * 8, op + s * 128, v_hi, values, 1u, lead);
+            }
         };
-        auto arrived = [&](int entry) { wait_for(&sh.full[entry % S::kSlots], entry / S::kSlots, &sh.dead); };
+        // Of each tile: the product of the first half of its weights, then of the second, then (two tiles of rows) the next
+        // tile's scores, whose place the weights have left; one tile of rows has two places in turn for scores, and the
+        // next tile's come first.
 #pragma unroll 1
         while (w.next(a)) {
             const int n = w.t1 - w.t0, nq = w.rows > 128 ? 2 : 1;
-            if constexpr (NQ == 2) {
-                // tile i: entry e + 2 i keys, e + 2 i + 1 values
-                arrived(e);
+#pragma unroll 1
+            for (int q = 0; q < nq; ++q) {
+                wait_both(q == 0 ? full(e) : nullptr, e / S::kSlots, &sh.q_full[q], q ? seg1 : seg0);
+                scores(q, e % S::kSlots, NQ == 2 ? q : s_no++ & 1);
+                if (n == 1) mma_commit(&sh.q_empty[q], lead);
+            }
+            mma_commit(&sh.empty[e % S::kSlots], lead);
+#pragma unroll 1
+            for (int i = 0; i < n; ++i) {
+                const int v = e + 2 * i + 1, k = v + 1, v_slot = v % S::kSlots, k_slot = k % S::kSlots;
+                const bool next = i + 1 < n;
+                if (NQ == 1 && next) {
+                    wait_both(full(k), k / S::kSlots, nullptr, 0);
+                    scores(0, k_slot, s_no++ & 1);
+                    if (i + 2 == n) mma_commit(&sh.q_empty[0], lead);
+                    mma_commit(&sh.empty[k_slot], lead);
+                }
 #pragma unroll 1
                 for (int q = 0; q < nq; ++q) {
-                    wait_for(&sh.q_full[q], seg[q], &sh.dead);
-                    __syncwarp();
-                    tmem_after_sync();
-                    scores(q, e % S::kSlots, q);
-                    if (n == 1) mma_commit(&sh.q_empty[q], lead);
-                }
-                mma_commit(&sh.empty[e % S::kSlots], lead);
-#pragma unroll 1
-                for (int i = 0; i < n; ++i) {
-                    arrived(e + 2 * i + 1);
-                    if (i + 1 < n) arrived(e + 2 * i + 2);
-                    const int v_slot = (e + 2 * i + 1) % S::kSlots, k_slot = (e + 2 * i + 2) % S::kSlots;
-#pragma unroll 1
-                    for (int q = 0; q < nq; ++q) {
-                        wait_for(&sh.p_full[q], p_no[q]++, &sh.dead);
-                        __syncwarp();
-                        tmem_after_sync();
-                        sums(q, v_slot, q, i > 0);
-                        if (i + 1 < n) {
-                            scores(q, k_slot, q);
-                            if (i + 2 == n) mma_commit(&sh.q_empty[q], lead);
-                        }
+                    const int at = NQ == 2 ? q : p_no0 & 1;
+                    const uint32_t turn = NQ == 1 ? p_no0 >> 1 : q ? p_no1 : p_no0;
+                    wait_both(q == 0 ? full(v) : nullptr, v / S::kSlots, &sh.p_full[at][0], turn);
+                    sums(q, 0, v_slot, at, i > 0);
+                    mma_commit(&sh.pv_half[q], lead);
+                    wait_both(NQ == 2 && next && q == 0 ? full(k) : nullptr, k / S::kSlots, &sh.p_full[at][1], turn);
+                    sums(q, 1, v_slot, at, true);
+                    if (NQ == 1 || !next) mma_commit(&sh.pv_done[q], lead);
+                    if (q + 1 == nq) mma_commit(&sh.empty[v_slot], lead);
+                    if (NQ == 2 && next) {
+                        scores(q, k_slot, q);
+                        if (i + 2 == n) mma_commit(&sh.q_empty[q], lead);
+                        if (q + 1 == nq) mma_commit(&sh.empty[k_slot], lead);
                     }
-                    mma_commit(&sh.empty[v_slot], lead);
-                    if (i + 1 < n) mma_commit(&sh.empty[k_slot], lead);
                 }
-            } else {
-                // one tile of rows: the next scores before this tile's weights are waited for, two places in turn
-                wait_for(&sh.q_full[0], seg[0], &sh.dead);
-                arrived(e);
-                __syncwarp();
-                tmem_after_sync();
-                scores(0, e % S::kSlots, s_no[0] & 1);
-                ++s_no[0];
-                if (n == 1) mma_commit(&sh.q_empty[0], lead);
-                mma_commit(&sh.empty[e % S::kSlots], lead);
-#pragma unroll 1
-                for (int i = 0; i < n; ++i) {
-                    const int v_slot = (e + 2 * i + 1) % S::kSlots, k_slot = (e + 2 * i + 2) % S::kSlots;
-                    if (i + 1 < n) {
-                        arrived(e + 2 * i + 2);
-                        __syncwarp();
-                        tmem_after_sync();
-                        scores(0, k_slot, s_no[0] & 1);
-                        ++s_no[0];
-                        if (i + 2 == n) mma_commit(&sh.q_empty[0], lead);
-                        mma_commit(&sh.empty[k_slot], lead);
-                    }
-                    arrived(e + 2 * i + 1);
-                    wait_for(&sh.p_full[p_no[0] & 1], p_no[0] >> 1, &sh.dead);
-                    __syncwarp();
-                    tmem_after_sync();
-                    sums(0, v_slot, p_no[0] & 1, i > 0);
-                    ++p_no[0];
-                    mma_commit(&sh.empty[v_slot], lead);
-                }
+                ++p_no0;
+                if (nq == 2) ++p_no1;
             }
-            ++seg[0];
-            if (nq == 2) ++seg[1];
+            ++seg0;
+            if (nq == 2) ++seg1;
             e += 2 * n;
             w.step(a);
         }
@@ -662,28 +763,31 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             const int t = threadIdx.x - S::kConvertWarp * 32;
             constexpr int kRowChunks = DP / 16, kStepRows = kConvert / kRowChunks, kTurns = S::kStageRows / kStepRows;
             const int chunk = t % kRowChunks, row0 = t / kRowChunks;
-            const bool in = chunk * 16 < D;
+            const bool in = chunk * 16 < D, upper = chunk >> 2 & 1;
             static_assert(kStepRows % 8 == 0, "rows");
             const int first = row0 * a.pitch + chunk * 16, step = kStepRows * a.pitch;
             const int line = (chunk >> 2) * (kTile * 128) + row0 * 128;
             const int low = line + ((((chunk & 3) * 2) ^ (row0 & 7)) << 4), high = low ^ 16;
-            int e = 0;                                           // parts
+            int e = 0, tile_no = 0;                              // parts, tiles
 #pragma unroll 1
             while (w.next(a)) {
 #pragma unroll 1
-                for (int tile = w.t0; tile < w.t1; ++tile) {
+                for (int tile = w.t0; tile < w.t1; ++tile, ++tile_no) {
+                    const int key_at = tile_no & 3;
 #pragma unroll 1
                     for (int part = 0; part < 2 * kParts; ++part, ++e) {
                         const int entry = e / kParts, slot = entry % S::kSlots, stage = e % S::kStages, base = part % kParts * S::kStageRows;
+                        const bool values = part >= kParts;
                         const int rows = w.end - tile * kTile - base;           // the rest is zeros
                         const uint8_t* from = stages + stage * S::kStage + first;
                         uint8_t* const to = ring + slot * S::kSlot + base * 128;
                         const bool codes = over(&sh.stage_full[stage], e / S::kStages);
                         const bool room = entry < S::kSlots || over(&sh.empty[slot], entry / S::kSlots - 1);
+                        if (part == kParts) wait_for(&sh.key_full[key_at], tile_no >> 2, &sh.dead);
                         wait_more(codes, &sh.stage_full[stage], e / S::kStages, &sh.dead);
                         wait_more(room, &sh.empty[slot], entry / S::kSlots - 1, &sh.dead);
                         if (in) {
-                            constexpr int kAtOnce = kTurns < 8 ? kTurns : 8;
+                            constexpr int kAtOnce = kTurns < 4 ? kTurns : 4;
 #pragma unroll 1
                             for (int turn = 0; turn < kTurns; turn += kAtOnce) {
                                 uint4 x[kAtOnce];
@@ -693,18 +797,29 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
 #pragma unroll
                                     for (int i = 0; i < kAtOnce; ++i)
                                         if (row0 + (turn + i) * kStepRows >= rows) x[i] = make_uint4(0u, 0u, 0u, 0u);
+                                uint32_t by[kAtOnce];
+                                if (values)
+#pragma unroll
+                                    for (int i = 0; i < kAtOnce; ++i) by[i] = sh.value_scale[key_at][base + row0 + (turn + i) * kStepRows];
 #pragma unroll
                                 for (int i = 0; i < kAtOnce; ++i) {
-                                    const uint2 h0 = four_codes(x[i].x), h1 = four_codes(x[i].y), h2 = four_codes(x[i].z), h3 = four_codes(x[i].w);
+                                    uint2 h0 = four_codes(x[i].x), h1 = four_codes(x[i].y), h2 = four_codes(x[i].z), h3 = four_codes(x[i].w);
+                                    if (values) {
+                                        h0.x = mul_f16x2(h0.x, by[i]), h0.y = mul_f16x2(h0.y, by[i]), h1.x = mul_f16x2(h1.x, by[i]), h1.y = mul_f16x2(h1.y, by[i]);
+                                        h2.x = mul_f16x2(h2.x, by[i]), h2.y = mul_f16x2(h2.y, by[i]), h3.x = mul_f16x2(h3.x, by[i]), h3.y = mul_f16x2(h3.y, by[i]);
+                                    }
+                                    const uint4 a0 = make_uint4(h0.x, h0.y, h1.x, h1.y), a1 = make_uint4(h2.x, h2.y, h3.x, h3.y);
                                     const int at = (turn + i) * (kStepRows * 128);
-                                    *reinterpret_cast<uint4*>(to + low + at) = make_uint4(h0.x, h0.y, h1.x, h1.y);
-                                    *reinterpret_cast<uint4*>(to + high + at) = make_uint4(h2.x, h2.y, h3.x, h3.y);
+                                    // (eight neighbours' pieces into all banks: of the second panel the upper one first)
+                                    *reinterpret_cast<uint4*>(to + at + (upper ? high : low)) = upper ? a1 : a0;
+                                    *reinterpret_cast<uint4*>(to + at + (upper ? low : high)) = upper ? a0 : a1;
                                 }
                             }
                         }
                         fence_smem_async();
                         __syncwarp();
                         mbar_arrive_if(&sh.stage_empty[stage], lane == 0);
+                        if (part == 2 * kParts - 1) mbar_arrive_if(&sh.key_empty[key_at], lane == 0);
                         if (part % kParts == kParts - 1) mbar_arrive_if(&sh.full[slot], lane == 0);
                     }
                 }
@@ -719,7 +834,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
         constexpr float kLift = E4M3 ? 7.f : 0.f;       // f16 weights up to 2^15 instead of 2^8: fewer of them vanish
         constexpr float kRoomUp = E4M3 ? 8.f : 64.f;
         int tile_no = 0, mine = 0;                      // tiles of this CTA, and those of this warp's rows
-        [[maybe_unused]] int seg = 0;                   // and its units
+        int seg = 0;                                    // and its units
         bool cut_here = false;
 #pragma unroll 1
         while (w.next(a)) {
@@ -741,33 +856,46 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             const uint32_t head = is_row ? static_cast<uint32_t>(w.kv) * a.group + (static_cast<uint32_t>(r) - tok * a.group) : 0u;
             const int limit = is_row ? w.s.start + static_cast<int>(tok) : -1;         // last position that the row sees
             const int seen_by_all = w.s.start + static_cast<int>(static_cast<uint32_t>(w.r0 + q * 128) / static_cast<uint32_t>(a.group));
-            float m = -INFINITY;                        // (of x, in powers of two; less the lift)
-            uint64_t l2 = 0;
+            float m = -INFINITY;                        // (of x, in powers of two)
+            [[maybe_unused]] int unit = INT32_MIN;      // the values' in the sums (none yet)
+            uint64_t l2 = 0, l3 = 0;
             float f = a.scale2;
             if constexpr (E4M3) {
                 // the row's queries, bf16 to f16: its largest element to 2^14..2^15 by a power of two
                 wait_for(&sh.q_raw[q], seg, &sh.dead);
                 uint8_t* const mine_q = q_smem + q * (S::kPanels * 128 * 128) + j * 128;
                 uint32_t most = 0;
+                auto piece = [&](int ch) { return reinterpret_cast<uint4*>(mine_q + (ch >> 3) * (128 * 128) + (((ch & 7) ^ (j & 7)) << 4)); };
+                // (D / 8 pieces, an even number; eight at a time)
 #pragma unroll 1
-                for (int ch = 0; ch < D / 8; ++ch) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(mine_q + (ch >> 3) * (128 * 128) + (((ch & 7) ^ (j & 7)) << 4));
-                    const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+                for (int c0 = 0; c0 < D / 8; c0 += 8) {
+                    uint4 x[8];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) most = max(most, max((v[k] << 16) & 0x7FFF0000u, v[k] & 0x7FFF0000u));
+                    for (int i = 0; i < 8; ++i) x[i] = c0 + i < D / 8 ? *piece(c0 + i) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint32_t v[4] = {x[i].x & 0x7FFF7FFFu, x[i].y & 0x7FFF7FFFu, x[i].z & 0x7FFF7FFFu, x[i].w & 0x7FFF7FFFu};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) most = __vmaxu2(most, v[k]);
+                    }
                 }
-                const int ex = static_cast<int>(most >> 23);
+                const int ex = static_cast<int>(max(most & 0xFFFFu, most >> 16) >> 7);
                 const int up = ex == 0 || ex == 255 ? 0 : min(14 - (ex - 127), 120);
                 const float lift = __uint_as_float((static_cast<uint32_t>(up + 127) << 23) ^ (a.flip & 0x80000000u));
                 f *= __uint_as_float(static_cast<uint32_t>(127 - up) << 23);
-#pragma unroll 2
-                for (int ch = 0; ch < D / 8; ++ch) {
-                    uint4* const at = reinterpret_cast<uint4*>(mine_q + (ch >> 3) * (128 * 128) + (((ch & 7) ^ (j & 7)) << 4));
-                    uint32_t v[4] = {at->x, at->y, at->z, at->w};
+#pragma unroll 1
+                for (int c0 = 0; c0 < D / 8; c0 += 8) {
+                    uint4 x[8];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        v[k] = pack_f16(__uint_as_float(v[k] << 16) * lift, __uint_as_float(v[k] & 0xFFFF0000u) * lift);
-                    *at = make_uint4(v[0], v[1], v[2], v[3]);
+                    for (int i = 0; i < 8; ++i) x[i] = c0 + i < D / 8 ? *piece(c0 + i) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        uint32_t v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            v[k] = pack_f16(__uint_as_float(v[k] << 16) * lift, __uint_as_float(v[k] & 0xFFFF0000u) * lift);
+                        if (c0 + i < D / 8) *piece(c0 + i) = make_uint4(v[0], v[1], v[2], v[3]);
+                    }
                 }
                 fence_smem_async();
                 __syncwarp();
@@ -786,131 +914,139 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 tmem_after_sync();
                 const bool masked = tile * kTile + kTile - 1 > seen_by_all;
                 const bool holes = sh.holes[tile_no % kAhead];
-                // x of 64 keys
-                auto load = [&](int half, float (&x)[64]) {
-                    tmem_load(s_at + half * 64, x);
+                // Keys in two halves: the first's weights are in the product while the second's are taken.
+#pragma unroll 1
+                for (int half = 0; half < 2; ++half) {
+                    float y[64];
+                    tmem_load(s_at + half * 64, y);
                     if constexpr (E4M3) {
 #pragma unroll
                         for (int i = 0; i < 64; i += 4) {
-                            const float4 kf = *reinterpret_cast<const float4*>(&sh.key_factor[k_at][half * 64 + i]);
-                            const float4 lg = *reinterpret_cast<const float4*>(&sh.key_log[k_at][half * 64 + i]);
-                            const uint64_t a0 = fma_f32x2(pack_f32x2(kf.x, kf.y), f2, 0ull), a1 = fma_f32x2(pack_f32x2(kf.z, kf.w), f2, 0ull);
-                            const uint64_t lo = fma_f32x2(pack_f32x2(x[i], x[i + 1]), a0, pack_f32x2(lg.x, lg.y));
-                            const uint64_t hi = fma_f32x2(pack_f32x2(x[i + 2], x[i + 3]), a1, pack_f32x2(lg.z, lg.w));
-                            x[i] = lo_f32(lo), x[i + 1] = hi_f32(lo), x[i + 2] = lo_f32(hi), x[i + 3] = hi_f32(hi);
+                            const float4 k = *reinterpret_cast<const float4*>(&sh.key_scale[k_at][half * 64 + i]);
+                            const uint64_t lo = mul_f32x2(pack_f32x2(y[i], y[i + 1]), pack_f32x2(k.x, k.y));
+                            const uint64_t hi = mul_f32x2(pack_f32x2(y[i + 2], y[i + 3]), pack_f32x2(k.z, k.w));
+                            y[i] = lo_f32(lo), y[i + 1] = hi_f32(lo), y[i + 2] = lo_f32(hi), y[i + 3] = hi_f32(hi);
                         }
                     }
-                    if (masked) {
+                    if (masked || holes) {
                         const int most = limit - tile * kTile - half * 64;            // keys up to here
+                        uint32_t lo = most >= 31 ? 0xFFFFFFFFu : most < 0 ? 0u : (2u << most) - 1u;
+                        uint32_t hi = most >= 63 ? 0xFFFFFFFFu : most < 32 ? 0u : (2u << (most - 32)) - 1u;
+                        if (holes) lo &= sh.live[tile_no % kAhead][2 * half], hi &= sh.live[tile_no % kAhead][2 * half + 1];
 #pragma unroll
-                        for (int i = 0; i < 64; ++i)
-                            if (i > most) x[i] = -INFINITY;
-                    }
-                    if (holes) {
-#pragma unroll
-                        for (int i = 0; i < 64; ++i)
-                            if (!sh.live[tile_no % kAhead][half * 64 + i]) x[i] = -INFINITY;
-                    }
-                };
-                auto most_of = [&](const float (&x)[64]) {
-                    float t0 = x[0], t1 = x[1];
-#pragma unroll
-                    for (int i = 2; i < 62; i += 4) t0 = max3(t0, x[i], x[i + 1]), t1 = max3(t1, x[i + 2], x[i + 3]);
-                    return max3(fmaxf(t0, t1), x[62], x[63]);
-                };
-                float x0[64], x1[64];
-                load(0, x0);
-                float top = most_of(x0);
-                load(1, x1);
-                top = fmaxf(top, most_of(x1));
-                if constexpr (!E4M3) top = top > -INFINITY ? top * f : top;
-                // m moves: at first, or when weights would grow too large
-                const bool up = top > m + kRoomUp || (m == -INFINITY && top > -INFINITY);
-                if (__any_sync(0xFFFFFFFFu, up)) {
-                    float by = 1.f;
-                    if (up) {
-                        by = m == -INFINITY ? 0.f : ex2(m - top);
-                        m = top;
-                    }
-                    l2 = fma_f32x2(l2, pack_f32x2(by, by), 0ull);
-                    if (tile > w.t0) {
-                        wait_for(&sh.pv_done[q], mine - 1, &sh.dead);
-                        __syncwarp();
-                        tmem_after_sync();
-#pragma unroll 1
-                        for (int i = 0; i < DP; i += 8) {
-                            float o[8];
-                            tmem_load(my_o + i, o);
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) o[k] *= by;
-                            tmem_store8(my_o + i, o);
+                        for (int i = 0; i < 32; ++i) {
+                            if (!(lo >> i & 1u)) y[i] = -INFINITY;
+                            if (!(hi >> i & 1u)) y[32 + i] = -INFINITY;
                         }
-                        tmem_store_wait();
                     }
-                }
-                const float less = m == -INFINITY ? 0.f : kLift - m;
-                const uint64_t less2 = pack_f32x2(less, less);
-                auto weights = [&](int half, const float (&x)[64]) {
+                    // The weights with the m that there is, while the maximum is found; where m has to move, which it hardly
+                    // ever does, they are taken again.
                     uint32_t p[32];
+                    uint64_t s2, s3;
+                    bool again = false;
+#pragma unroll 1
+                    while (true) {
+                        const float less = m == -INFINITY ? 0.f : kLift - m;
+                        const uint64_t less2 = pack_f32x2(less, less);
+                        float t0 = -INFINITY, t1 = -INFINITY;
+                        s2 = l2, s3 = l3;
 #pragma unroll
-                    for (int i = 0; i < 64; i += 2) {
-                        const uint64_t e = E4M3 ? add_f32x2(pack_f32x2(x[i], x[i + 1]), less2) : fma_f32x2(pack_f32x2(x[i], x[i + 1]), f2, less2);
-                        const float p0 = ex2(lo_f32(e)), p1 = ex2(hi_f32(e));
+                        for (int i = 0; i < 64; i += 4) {
+                            const uint64_t e0 = ordered_fma2(pack_f32x2(y[i], y[i + 1]), f2, less2), e1 = ordered_fma2(pack_f32x2(y[i + 2], y[i + 3]), f2, less2);
+                            const float p0 = ordered_ex2(lo_f32(e0)), p1 = ordered_ex2(hi_f32(e0));
+                            t0 = ordered_max3(t0, y[i], y[i + 1]), t1 = ordered_max3(t1, y[i + 2], y[i + 3]);
+                            const float p2 = ordered_ex2(lo_f32(e1)), p3 = ordered_ex2(hi_f32(e1));
+                            s2 = ordered_add2(s2, pack_f32x2(p0, p1));
+                            s3 = ordered_add2(s3, pack_f32x2(p2, p3));
+                            p[i / 2] = E4M3 ? ordered_f16(p0, p1) : ordered_bf16(p0, p1);
+                            p[i / 2 + 1] = E4M3 ? ordered_f16(p2, p3) : ordered_bf16(p2, p3);
+                        }
+                        if (again) break;
+                        float top = fmaxf(t0, t1);
+                        top = top > -INFINITY ? top * f : top;
+                        const bool up = top > m + kRoomUp || (m == -INFINITY && top > -INFINITY);
+                        if (!__any_sync(0xFFFFFFFFu, up) && (!E4M3 || sh.unit_of[k_at] == unit)) break;
+                        again = true;
+                        float by = 1.f;
+                        if (up) {
+                            by = m == -INFINITY ? 0.f : ex2(m - top);
+                            m = top;
+                        }
+                        l2 = mul_f32x2(l2, pack_f32x2(by, by)), l3 = mul_f32x2(l3, pack_f32x2(by, by));
                         if constexpr (E4M3) {
-                            const float2 inv = *reinterpret_cast<const float2*>(&sh.key_inverse[k_at][half * 64 + i]);
-                            l2 = fma_f32x2(pack_f32x2(p0, p1), pack_f32x2(inv.x, inv.y), l2);
-                            p[i / 2] = pack_f16(p0, p1);
-                        } else {
-                            l2 = add_f32x2(l2, pack_f32x2(p0, p1));
-                            p[i / 2] = pack_bf16(p0, p1);
+                            const int now = sh.unit_of[k_at];
+                            if (now != unit && tile > w.t0) by *= power_of_two(max(unit - now, -126));
+                            unit = now;
+                        }
+                        if (tile > w.t0 || half) {
+                            // (Of two tiles of rows the scores came behind the last tile's product, of one behind that of
+                            // the one before: a barrier asked for a phase that is two behind would answer at once.)
+                            if (NQ == 1 && tile > w.t0) wait_for(&sh.pv_done[q], mine - 1, &sh.dead);
+                            if (half) wait_for(&sh.pv_half[q], mine, &sh.dead);
+                            __syncwarp();
+                            tmem_after_sync();
+#pragma unroll 1
+                            for (int i = 0; i < DP; i += 8) {
+                                float o[8];
+                                tmem_load(my_o + i, o);
+#pragma unroll
+                                for (int k = 0; k < 8; ++k) o[k] *= by;
+                                tmem_store8(my_o + i, o);
+                            }
+                            tmem_store_wait();
                         }
                     }
+                    l2 = s2, l3 = s3;
                     tmem_store32(s_at + half * 32, p);
-                };
-                weights(0, x0);
-                weights(1, x1);
-                tmem_store_wait();
-                tmem_before_sync();
-                __syncwarp();
-                mbar_arrive_if(&sh.p_full[at], lane == 0);
+                    tmem_store_wait();
+                    tmem_before_sync();
+                    __syncwarp();
+                    mbar_arrive_if(&sh.p_full[at][half], lane == 0);
+                }
                 if constexpr (E4M3) mbar_arrive_if(&sh.key_empty[k_at], lane == 0);
             }
             // ---- the unit's end ----
-            wait_for(&sh.pv_done[q], mine - 1, &sh.dead);
+            if (NQ == 1 && w.t1 - w.t0 > 1) wait_for(&sh.pv_done[q], mine - 2, &sh.dead);
+            wait_for(&sh.pv_done[q], NQ == 2 ? seg : mine - 1, &sh.dead);
             __syncwarp();
             tmem_after_sync();
-            const float l = lo_f32(l2) + hi_f32(l2);
+            const float l = (lo_f32(l2) + hi_f32(l2)) + (lo_f32(l3) + hi_f32(l3));
             const bool whole = w.t0 == 0 && w.t1 == w.T;
             if (whole) {
-                const float inverse = l > 0.f ? 1.f / l : 0.f;
+                const float inverse = l > 0.f ? (E4M3 ? power_of_two(unit) : 1.f) / l : 0.f;
                 const int64_t row = w.p.row + static_cast<int64_t>(tok);
                 if (is_row && a.lse) a.lse[row * a.q_heads + head] = l > 0.f ? (log2f(l) + m - kLift) * 0.69314718055994531f : -INFINITY;
                 // kOutBytes of each of the warp's 32 rows at a time: a row a lane into shared memory, whole pieces of rows out of it
                 constexpr int kCols = S::kOutBytes / 2, kPieces = kCols / 8, kAt = 32 / kPieces;
                 uint8_t* const room = out_smem + warp * (32 * S::kOutBytes);
-                const uint32_t wrows = static_cast<uint32_t>(max(0, min(32, w.rows - q * 128 - quad * 32)));
+                const int wrows = w.rows - q * 128 - quad * 32, piece = lane % kPieces;
+                const int64_t at_out = row * a.o_tok + static_cast<int64_t>(head) * a.o_head;
+                __nv_bfloat16* to[kPieces];                  // where this lane's pieces go, null: no such row
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) {
+                    const int rr = k * kAt + lane / kPieces;
+                    to[k] = a.out + __shfl_sync(0xFFFFFFFFu, at_out, rr) + piece * 8;
+                    if (rr >= wrows) to[k] = nullptr;
+                }
 #pragma unroll 1
                 for (int i = 0; i < D; i += kCols) {
+                    float o[kCols];
+                    tmem_load(my_o + i, o);
 #pragma unroll
-                    for (int half = 0; half < kCols / 32; ++half) {
-                        float o[32];
-                        tmem_load(my_o + i + half * 32, o);
-#pragma unroll
-                        for (int k = 0; k < 32; k += 8) {
-                            const uint4 y = make_uint4(pack_bf16(o[k] * inverse, o[k + 1] * inverse), pack_bf16(o[k + 2] * inverse, o[k + 3] * inverse),
-                                                       pack_bf16(o[k + 4] * inverse, o[k + 5] * inverse), pack_bf16(o[k + 6] * inverse, o[k + 7] * inverse));
-                            *reinterpret_cast<uint4*>(room + lane * S::kOutBytes + (((half * 4 + k / 8) ^ (lane & (kPieces - 1))) << 4)) = y;
-                        }
-                    }
+                    for (int k = 0; k < kCols; k += 8)
+                        *reinterpret_cast<uint4*>(room + lane * S::kOutBytes + ((k / 8 ^ (lane & (kPieces - 1))) << 4)) =
+                            make_uint4(pack_bf16(o[k] * inverse, o[k + 1] * inverse), pack_bf16(o[k + 2] * inverse, o[k + 3] * inverse),
+                                       pack_bf16(o[k + 4] * inverse, o[k + 5] * inverse), pack_bf16(o[k + 6] * inverse, o[k + 7] * inverse));
                     __syncwarp();
+                    uint4 y[kPieces];
 #pragma unroll
                     for (int k = 0; k < kPieces; ++k) {
-                        const int rr = k * kAt + lane / kPieces, piece = lane % kPieces;
-                        const uint32_t at_tok = __shfl_sync(0xFFFFFFFFu, tok, rr), at_head = __shfl_sync(0xFFFFFFFFu, head, rr);
-                        const uint4 y = *reinterpret_cast<const uint4*>(room + rr * S::kOutBytes + ((piece ^ (rr & (kPieces - 1))) << 4));
-                        if (rr < wrows && i + piece * 8 < D)
-                            *reinterpret_cast<uint4*>(a.out + (w.p.row + static_cast<int64_t>(at_tok)) * a.o_tok + at_head * a.o_head + i + piece * 8) = y;
+                        const int rr = k * kAt + lane / kPieces;
+                        y[k] = *reinterpret_cast<const uint4*>(room + rr * S::kOutBytes + ((piece ^ (rr & (kPieces - 1))) << 4));
                     }
+#pragma unroll
+                    for (int k = 0; k < kPieces; ++k)
+                        if (to[k] && i + piece * 8 < D) *reinterpret_cast<uint4*>(to[k] + i) = y[k];
                     __syncwarp();
                 }
             } else {
@@ -920,6 +1056,9 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 for (int i = 0; i < D; i += 16) {
                     float o[16];
                     tmem_load(my_o + i, o);
+                    if constexpr (E4M3)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) o[k] *= power_of_two(unit);
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
                         *reinterpret_cast<float4*>(part + ((i / 4 + k) * 128 + j) * 4) = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
@@ -952,7 +1091,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
 }
 
 template <int DP, bool E4M3>
-cudaError_t launch_prompt(const PromptArgs& a, const Maps& m, int ctas, cudaStream_t s) {
+cudaError_t launch_prompt(const PromptArgs& a, const PromptMaps& m, int ctas, cudaStream_t s) {
     using Shape = PromptShape<DP, E4M3>;
     const cudaError_t e = cudaFuncSetAttribute(prompt_kernel<DP, E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::kBytes);
     if (e != cudaSuccess) return e;
@@ -963,10 +1102,10 @@ cudaError_t launch_prompt(const PromptArgs& a, const Maps& m, int ctas, cudaStre
     }();
     constexpr int kSplit = (Shape::kSoftmaxWarps * Shape::kSoftmaxRegs + 4 * Shape::kOtherRegs + Shape::kConvertWarps * Shape::kConvertRegs) * 32;
     if (Shape::kQ == 2 && regs * Shape::kThreads < kSplit) return cudaErrorLaunchOutOfResources;
-    return launch_pdl(prompt_kernel<DP, E4M3>, dim3(ctas), dim3(Shape::kThreads), Shape::kBytes, s, 0, a, m.k, m.v);
+    return launch_pdl(prompt_kernel<DP, E4M3>, dim3(ctas), dim3(Shape::kThreads), Shape::kBytes, s, 0, a, m.pool.k, m.pool.v, m.q);
 }
 template <bool E4M3>
-cudaError_t launch_prompt_dims(const PromptArgs& a, const Maps& m, int ctas, cudaStream_t s) {
+cudaError_t launch_prompt_dims(const PromptArgs& a, const PromptMaps& m, int ctas, cudaStream_t s) {
     const int dp = prompt_dim(a.c.head_dim);
     return dp == 64 ? launch_prompt<64, E4M3>(a, m, ctas, s) : dp == 128 ? launch_prompt<128, E4M3>(a, m, ctas, s) : launch_prompt<256, E4M3>(a, m, ctas, s);
 }

@@ -9,6 +9,20 @@ namespace {
 constexpr size_t kCutBytes = 8192;
 static_assert(kPromptCtas * sizeof(CutUnit) <= kCutBytes, "cuts");
 
+// The queries as a tensor of (element, head, row), in boxes of 64 elements of the heads of one kv head and as many rows as
+// make 128 with them.
+bool query_map(CUtensorMap* map, const PromptArgs& a, int head_dim) {
+    const auto encode = tensor_map_encoder();
+    if (!encode) return false;
+    const auto used = [&](int64_t stride, int size) { return static_cast<cuuint64_t>(size == 1 ? head_dim : stride) * 2; };
+    const cuuint64_t dims[4] = {static_cast<cuuint64_t>(head_dim), static_cast<cuuint64_t>(a.q_heads), static_cast<cuuint64_t>(a.R), 1};
+    const cuuint64_t strides[3] = {used(a.q_head, a.q_heads), used(a.q_tok, a.R), static_cast<cuuint64_t>(head_dim) * 2};
+    const cuuint32_t size[4] = {64u, static_cast<cuuint32_t>(a.group), static_cast<cuuint32_t>(128 / a.group), 1u}, step[4] = {1u, 1u, 1u, 1u};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<__nv_bfloat16*>(a.q), dims, strides, size, step,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 int prompt_ctas() {
     const int n = sm_count();
     return n < kPromptCtas ? n : kPromptCtas;
@@ -141,11 +155,13 @@ PLDP_API pldp_status pldp_attend_prompt(const pldp_attend_prompt_args* p, void* 
     if (e4m3 && dp == 256 && a.box > 64) a.box = 64;         // (a stage holds half a tile)
     // a copy starts at a multiple of 128 bytes of shared memory: vectors side by side where a box of them is one
     a.pitch = p->cache.head_dim * a.box % 128 == 0 ? p->cache.head_dim : p->cache.head_dim <= 128 ? 128 : 256;
-    Maps maps = {};
+    PromptMaps maps = {};
     bool head_first = false;
-    if (!pool_map(&maps.k, a.c.k, a.c, e4m3, a.box, a.pitch, &head_first) || !pool_map(&maps.v, a.c.v, a.c, e4m3, a.box, a.pitch, &head_first))
+    if (!pool_map(&maps.pool.k, a.c.k, a.c, e4m3, a.box, a.pitch, &head_first) || !pool_map(&maps.pool.v, a.c.v, a.c, e4m3, a.box, a.pitch, &head_first))
         return fail(PLDP_ERR_UNSUPPORTED, "%s: the cache's strides cannot be described to the copy engine", fn);
     a.head_first = head_first;
+    // (signs are turned on the way by the other form)
+    a.q_boxes = 128 % a.group == 0 && (e4m3 || !a.flip) && p->R > 0 && query_map(&maps.q, a, p->cache.head_dim);
     const int ctas = prompt_ctas();
     auto s = static_cast<cudaStream_t>(stream);
     cudaError_t e = e4m3 ? launch_prompt_e4m3(a, maps, ctas, s) : launch_prompt_bf16(a, maps, ctas, s);

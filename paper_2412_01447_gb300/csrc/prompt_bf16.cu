@@ -3,7 +3,7 @@
 
 namespace pldp {
 
-cudaError_t launch_prompt_bf16(const PromptArgs& a, const Maps& m, int ctas, cudaStream_t s) {
+cudaError_t launch_prompt_bf16(const PromptArgs& a, const PromptMaps& m, int ctas, cudaStream_t s) {
     return launch_prompt_dims<false>(a, m, ctas, s);
 }
 
