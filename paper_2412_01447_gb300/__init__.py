@@ -256,6 +256,10 @@ _CALLS = ("pldp_find_candidates", "pldp_rank_hidden", "pldp_rank_attention", "pl
 # ... and of its `CacheLibrary`.
 _CACHE_CALLS = ("pldp_cache_append", "pldp_cache_read", "pldp_attend_cache", "pldp_rank_cache", "pldp_token_logprobs")
 
+# ... and of its `PromptLibrary`.
+_PROMPT_CALLS = ("pldp_cache_append_prompt", "pldp_attend_prompt", "pldp_pages_reserve", "pldp_pages_fork", "pldp_pages_free",
+                 "pldp_pages_compact", "pldp_cache_copy_pages")
+
 
 def _load_calls(lib):
     """The native form of the calls below, bound to the loaded library.  Each takes a
@@ -271,6 +275,7 @@ def _load_calls(lib):
         spec.loader.exec_module(m)
         m.bind(tuple(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in _CALLS))
         m.bind_cache(tuple(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in _CACHE_CALLS))
+        m.bind_prompt(tuple(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in _PROMPT_CALLS))
     except Exception as e:                               # the Python below makes every call by itself
         warnings.warn(f"{os.path.basename(path)} does not load, the binding's calls go through ctypes: {e}",
                       RuntimeWarning, stacklevel=2)
@@ -1099,6 +1104,9 @@ def pldp_cache_append_prompt(cache, q, k, v, rows, q_out, start=None, q_norm=Non
     """pldp_cache_append of prompts packed behind one another: rows rows[b] .. rows[b+1]-1 (int32
     [B + 1]) of q [rows, q_heads, head_dim] and of k and v [rows, heads, head_dim] are sequence b's
     tokens at positions start[b] (int32 [B], None: 0) and on.  Other arguments as pldp_cache_append."""
+    if _calls is not None and type(cache) is pldp_cache and _done("pldp_cache_append_prompt", _calls.cache_append_prompt(
+            cache.address, cache.B, q, k, v, rows, q_out, start, q_norm, k_norm, eps, cos, sin, interleaved, status, stream)):
+        return
     kinds = (torch.float32, torch.bfloat16)
     a = pldp_cache_append_prompt_args()
     a.q, a.q_strides = _packed(q, "q", (None,) * 3, kinds)
@@ -1134,6 +1142,9 @@ def pldp_attend_prompt(cache, q, rows, out, workspace, start=None, lse=None, sca
     holds of it before.  lse float32 [rows, q_heads] (optional); scale default 1/sqrt(head_dim).
     workspace: uint8 CUDA tensor of pldp_attend_prompt_workspace_size(q_heads, heads, head_dim)
     bytes, 256-byte aligned; calls of any lengths that follow one another may share it."""
+    if _calls is not None and type(cache) is pldp_cache and _done("pldp_attend_prompt", _calls.attend_prompt(
+            cache.address, cache.B, q, rows, out, workspace, start, lse, scale, status, stream)):
+        return
     a = pldp_attend_prompt_args()
     a.q, a.q_strides = _packed(q, "q", (None,) * 3, (torch.bfloat16,))
     R, Hq, D = q.shape
@@ -1199,6 +1210,9 @@ def pldp_pages_reserve(table, start, copies, workspace, n, count=None, status=No
     for pages that others hold too.  copies int32 [B, 2]: the page that pldp_cache_copy_pages then has
     to copy in every layer, and where to.  workspace: uint8 CUDA tensor of
     pldp_pages_workspace_size(table) bytes."""
+    if _calls is not None and type(table) is pldp_page_table and _done("pldp_pages_reserve", _calls.pages_reserve(
+            table.address, start, copies, workspace, n, count, status, stream)):
+        return
     t = _table(table)
     _check("pldp_pages_reserve", _load().pldp_pages_reserve(
         t, _dense(start, "start", torch.int32, n=table.B), _dense(count, "count", torch.int32, allow_none=True, n=table.B), int(n),
@@ -1209,6 +1223,9 @@ def pldp_pages_reserve(table, start, copies, workspace, n, count=None, status=No
 def pldp_pages_fork(table, parent, len, status=None, stream=None):
     """Row b of the table becomes those of row parent[b]'s entries that hold its first len[b]
     positions, shared with it (int32 [B]; parent -1: the row stays as it is)."""
+    if _calls is not None and type(table) is pldp_page_table and _done("pldp_pages_fork", _calls.pages_fork(
+            table.address, parent, len, status, stream)):
+        return
     t = _table(table)
     _check("pldp_pages_fork", _load().pldp_pages_fork(
         t, _dense(parent, "parent", torch.int32, n=table.B), _dense(len, "len", torch.int32, n=table.B),
@@ -1218,6 +1235,9 @@ def pldp_pages_fork(table, parent, len, status=None, stream=None):
 def pldp_pages_free(table, keep_len, stream=None):
     """Gives back the pages past each sequence's first keep_len[b] positions (int32 [B]; 0: all of
     them, negative: none)."""
+    if _calls is not None and type(table) is pldp_page_table and _done("pldp_pages_free", _calls.pages_free(
+            table.address, keep_len, stream)):
+        return
     t = _table(table)
     _check("pldp_pages_free", _load().pldp_pages_free(t, _dense(keep_len, "keep_len", torch.int32, n=table.B), _stream(stream)))
 
@@ -1226,6 +1246,9 @@ def pldp_pages_compact(table, copies, n_copies, workspace, used=None, stream=Non
     """Moves the held pages to the front of the pool in the table and refs; copies int32 [at least
     n_pages // 2, 2] and n_copies int32 [1] are what pldp_cache_copy_pages then has to copy in every
     layer, used (int32 [1], optional) the number of held pages."""
+    if _calls is not None and type(table) is pldp_page_table and _done("pldp_pages_compact", _calls.pages_compact(
+            table.address, copies, n_copies, workspace, used, stream)):
+        return
     t = _table(table)
     p, cap = _pairs(copies)
     _check("pldp_pages_compact", _load().pldp_pages_compact(
@@ -1236,6 +1259,9 @@ def pldp_pages_compact(table, copies, n_copies, workspace, used=None, stream=Non
 def pldp_cache_copy_pages(cache, copies, n_copies=None, stream=None):
     """Copies pages of one layer's cache, copies[i, 0] to copies[i, 1] (int32 [n, 2]; pairs with an
     entry that is no page are skipped), the first n_copies[0] pairs (int32 [1], None: all)."""
+    if _calls is not None and type(cache) is pldp_cache and _done("pldp_cache_copy_pages", _calls.cache_copy_pages(
+            cache.address, copies, n_copies, stream)):
+        return
     if not isinstance(cache, pldp_cache):
         raise ValueError("cache must be a pldp_cache")
     p, n = _pairs(copies)

@@ -51,6 +51,17 @@ struct CacheLibrary {
     decltype(&pldp_token_logprobs) logprobs;
 } cache_lib;
 
+// And for those of prompts and pages (bind_prompt()).
+struct PromptLibrary {
+    decltype(&pldp_cache_append_prompt) append;
+    decltype(&pldp_attend_prompt) attend;
+    decltype(&pldp_pages_reserve) reserve;
+    decltype(&pldp_pages_fork) fork;
+    decltype(&pldp_pages_free) free;
+    decltype(&pldp_pages_compact) compact;
+    decltype(&pldp_cache_copy_pages) copy;
+} prompt_lib;
+
 #ifdef PLDP_TEST_ANY_DEVICE
 constexpr bool kAnyDevice = true;    // test build: host tensors pass, so that the checks run without a GPU
 #else
@@ -197,6 +208,60 @@ struct Args {
             return nullptr;
         }
         return t->data_ptr();
+    }
+    // A [rows, heads, head_dim] tensor with unit inner stride, and its other strides.
+    const at::Tensor* packed(PyObject* o, int64_t (&strides)[2]) {
+        const at::Tensor* t = tensor(o);
+        if (!t) return nullptr;
+        if (t->dim() != 3 || t->stride(2) != 1) {
+            ok = false;
+            return nullptr;
+        }
+        for (int i = 0; i < 2; ++i) strides[i] = t->stride(i);
+        for (int i = 0; i < 3; ++i)
+            if (t->size(i) > INT32_MAX) ok = false;
+        return t;
+    }
+    // Of the shape and type that the call needs.
+    void* packed(PyObject* o, int64_t (&strides)[2], int64_t R, int64_t heads, int64_t d, c10::ScalarType type) {
+        const at::Tensor* t = packed(o, strides);
+        if (!t) return nullptr;
+        if (t->size(0) != R || t->size(1) != heads || t->size(2) != d || t->scalar_type() != type) {
+            ok = false;
+            return nullptr;
+        }
+        return t->data_ptr();
+    }
+    // `rows` of B + 1 prompts: where they are, and B.
+    const int32_t* sequences(PyObject* o, int64_t* B) {
+        const int32_t* p = ints(o, 1);
+        const at::Tensor* t = tensor(o);
+        *B = 0;
+        if (!p || !t || t->dim() != 1 || t->numel() > INT32_MAX) {
+            ok = false;
+            return nullptr;
+        }
+        *B = t->numel() - 1;
+        return p;
+    }
+    // Pairs [n, 2] (n < 0: any number), and how many.
+    int32_t* pairs(PyObject* o, int64_t n, int* count) {
+        int32_t* p = ints(o, 0);
+        const at::Tensor* t = tensor(o);
+        *count = 0;
+        if (!t || t->dim() != 2 || t->size(1) != 2 || t->size(0) > INT32_MAX || (n >= 0 && t->size(0) != n)) {
+            ok = false;
+            return nullptr;
+        }
+        *count = static_cast<int>(t->size(0));
+        return p;
+    }
+    // The description that a pldp_page_table object holds, by its address.
+    pldp_page_table table(PyObject* address) {
+        pldp_page_table t = {};
+        const int64_t at = integer(address, 1, INT64_MAX);
+        if (ok) std::memcpy(&t, reinterpret_cast<const void*>(at), sizeof t);
+        return t;
     }
     // The description that a pldp_cache object holds, by its address, with a page table of at least B rows.
     pldp_cache cache(PyObject* address, PyObject* rows, int64_t B) {
@@ -831,6 +896,142 @@ PLDP_CALL(token_logprobs) {
     PLDP_END
 }
 
+// cache's address, its page table's rows, q, k, v, rows, q_out, start, q_norm, k_norm, eps, cos, sin, interleaved, status,
+// stream
+PLDP_CALL(cache_append_prompt) {
+    PLDP_BEGIN(16)
+    pldp_cache_append_prompt_args p = {};
+    const at::Tensor* q = a.packed(v[2], p.q_strides);
+    if (!q || !prompt_lib.append) Py_RETURN_NONE;
+    const int64_t R = q->size(0), Hq = q->size(1), D = q->size(2);
+    const c10::ScalarType type = q->scalar_type();
+    int64_t B;
+    p.rows = a.sequences(v[5], &B);
+    p.cache = a.cache(v[0], v[1], B);
+    if (p.cache.head_dim != D) a.ok = false;
+    p.dtype = a.code(q);
+    p.q = q->data_ptr();
+    p.k = a.packed(v[3], p.k_strides, R, p.cache.heads, D, type);
+    p.v = a.packed(v[4], p.v_strides, R, p.cache.heads, D, type);
+    p.q_out = a.packed(v[6], p.q_out_strides, R, Hq, D, at::kBFloat16);
+    p.B = static_cast<int>(B), p.R = static_cast<int>(R), p.q_heads = static_cast<int>(Hq);
+    p.start = a.ints(v[7], B, true);
+    p.q_norm = a.dense(v[8], D, true, type);
+    p.k_norm = a.dense(v[9], D, true, type);
+    p.eps = a.real(v[10]);
+    if (v[11] != Py_None || v[12] != Py_None) {
+        const at::Tensor *c = a.tensor(v[11]), *s = a.tensor(v[12]);
+        if (!c || !s || c->dim() != 2 || s->dim() != 2 || c->size(0) != s->size(0) || c->size(1) != s->size(1) ||
+            c->size(1) > INT32_MAX / 2 || c->numel() == 0)
+            Py_RETURN_NONE;
+        p.cos = a.floats(v[11], -1);
+        p.sin = a.floats(v[12], -1);
+        p.rot_rows = c->size(0);
+        p.rot = 2 * static_cast<int>(c->size(1));
+    }
+    p.interleaved = a.flag(v[13]);
+    p.status = a.words(v[14], B);
+    void* s = a.stream(v[15]);
+    return finish(a, [&] { return prompt_lib.append(&p, s); });
+    PLDP_END
+}
+
+// cache's address, its page table's rows, q, rows, out, workspace, start, lse, scale, status, stream
+PLDP_CALL(attend_prompt) {
+    PLDP_BEGIN(11)
+    pldp_attend_prompt_args p = {};
+    const at::Tensor* q = a.packed(v[2], p.q_strides);
+    if (!q || !prompt_lib.attend) Py_RETURN_NONE;
+    const int64_t R = q->size(0), Hq = q->size(1), D = q->size(2);
+    int64_t B;
+    p.rows = a.sequences(v[3], &B);
+    p.cache = a.cache(v[0], v[1], B);
+    if (p.cache.head_dim != D || q->scalar_type() != at::kBFloat16) a.ok = false;
+    p.q = q->data_ptr();
+    p.out = a.packed(v[4], p.out_strides, R, Hq, D, at::kBFloat16);
+    p.B = static_cast<int>(B), p.R = static_cast<int>(R), p.q_heads = static_cast<int>(Hq);
+    p.workspace = a.bytes(v[5], &p.workspace_bytes);
+    p.start = a.ints(v[6], B, true);
+    p.lse = a.floats(v[7], R * Hq, true);
+    p.scale = a.scale(v[8], D);
+    p.status = a.words(v[9], B);
+    void* s = a.stream(v[10]);
+    return finish(a, [&] { return prompt_lib.attend(&p, s); });
+    PLDP_END
+}
+
+// table's address, start, copies, workspace, n, count, status, stream
+PLDP_CALL(pages_reserve) {
+    PLDP_BEGIN(8)
+    const pldp_page_table t = a.table(v[0]);
+    if (!a.ok || !prompt_lib.reserve) Py_RETURN_NONE;
+    const int32_t* start = a.ints(v[1], t.B);
+    int count;
+    int32_t* copies = a.pairs(v[2], t.B, &count);
+    size_t bytes = 0;
+    void* ws = a.bytes(v[3], &bytes);
+    const int most = static_cast<int>(a.integer(v[4]));
+    const int32_t* counts = a.ints(v[5], t.B, true);
+    uint32_t* st = a.words(v[6], t.B);
+    void* s = a.stream(v[7]);
+    return finish(a, [&] { return prompt_lib.reserve(&t, start, counts, most, copies, st, ws, bytes, s); });
+    PLDP_END
+}
+
+// table's address, parent, len, status, stream
+PLDP_CALL(pages_fork) {
+    PLDP_BEGIN(5)
+    const pldp_page_table t = a.table(v[0]);
+    if (!a.ok || !prompt_lib.fork) Py_RETURN_NONE;
+    const int32_t *parent = a.ints(v[1], t.B), *len = a.ints(v[2], t.B);
+    uint32_t* st = a.words(v[3], t.B);
+    void* s = a.stream(v[4]);
+    return finish(a, [&] { return prompt_lib.fork(&t, parent, len, st, s); });
+    PLDP_END
+}
+
+// table's address, keep_len, stream
+PLDP_CALL(pages_free) {
+    PLDP_BEGIN(3)
+    const pldp_page_table t = a.table(v[0]);
+    if (!a.ok || !prompt_lib.free) Py_RETURN_NONE;
+    const int32_t* keep = a.ints(v[1], t.B);
+    void* s = a.stream(v[2]);
+    return finish(a, [&] { return prompt_lib.free(&t, keep, s); });
+    PLDP_END
+}
+
+// table's address, copies, n_copies, workspace, used, stream
+PLDP_CALL(pages_compact) {
+    PLDP_BEGIN(6)
+    const pldp_page_table t = a.table(v[0]);
+    if (!a.ok || !prompt_lib.compact) Py_RETURN_NONE;
+    int cap;
+    int32_t* copies = a.pairs(v[1], -1, &cap);
+    int32_t* n_copies = a.ints(v[2], 1);
+    size_t bytes = 0;
+    void* ws = a.bytes(v[3], &bytes);
+    int32_t* used = a.ints(v[4], 1, true);
+    void* s = a.stream(v[5]);
+    return finish(a, [&] { return prompt_lib.compact(&t, copies, cap, n_copies, used, ws, bytes, s); });
+    PLDP_END
+}
+
+// cache's address, copies, n_copies, stream
+PLDP_CALL(cache_copy_pages) {
+    PLDP_BEGIN(4)
+    const int64_t at = a.integer(v[0], 1, INT64_MAX);
+    if (!a.ok || !prompt_lib.copy) Py_RETURN_NONE;
+    pldp_cache c;
+    std::memcpy(&c, reinterpret_cast<const void*>(at), sizeof c);
+    int count;
+    const int32_t* copies = a.pairs(v[1], -1, &count);
+    const int32_t* n_copies = a.ints(v[2], 1, true);
+    void* s = a.stream(v[3]);
+    return finish(a, [&] { return prompt_lib.copy(&c, copies, count, n_copies, s); });
+    PLDP_END
+}
+
 // Entry points' addresses into a table of them.
 template <typename T>
 PyObject* bind_table(T& table, PyObject* addresses) {
@@ -851,9 +1052,10 @@ PyObject* bind_table(T& table, PyObject* addresses) {
     Py_RETURN_NONE;
 }
 
-// bind(addresses), bind_cache(addresses): the library's entry points, in the order of `Library` and `CacheLibrary`.
+// bind(addresses) and so on: the library's entry points, in the order of `Library`, `CacheLibrary` and `PromptLibrary`.
 PyObject* bind(PyObject*, PyObject* addresses) noexcept { return bind_table(lib, addresses); }
 PyObject* bind_cache(PyObject*, PyObject* addresses) noexcept { return bind_table(cache_lib, addresses); }
+PyObject* bind_prompt(PyObject*, PyObject* addresses) noexcept { return bind_table(prompt_lib, addresses); }
 
 #define PLDP_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
@@ -861,7 +1063,10 @@ PyMethodDef methods[] = {
     PLDP_METHOD(draft_step), PLDP_METHOD(index_build), PLDP_METHOD(verify_greedy), PLDP_METHOD(verify_greedy_draft),
     PLDP_METHOD(verify_sample), PLDP_METHOD(verify_sample_draft), PLDP_METHOD(identify_heads), PLDP_METHOD(top_heads),
     PLDP_METHOD(cache_append), PLDP_METHOD(cache_read), PLDP_METHOD(attend_cache), PLDP_METHOD(rank_cache),
-    PLDP_METHOD(token_logprobs), {"bind", bind, METH_O, nullptr}, {"bind_cache", bind_cache, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+    PLDP_METHOD(token_logprobs), PLDP_METHOD(cache_append_prompt), PLDP_METHOD(attend_prompt), PLDP_METHOD(pages_reserve),
+    PLDP_METHOD(pages_fork), PLDP_METHOD(pages_free), PLDP_METHOD(pages_compact), PLDP_METHOD(cache_copy_pages),
+    {"bind", bind, METH_O, nullptr}, {"bind_cache", bind_cache, METH_O, nullptr}, {"bind_prompt", bind_prompt, METH_O, nullptr},
+    {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pldp_calls", "Native argument checks of the PLD+ binding.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

@@ -437,8 +437,13 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
 
     if (warp >= S::kMmaWarp && warp < S::kConvertWarp) {
     if constexpr (NQ == 2) fewer_registers<S::kOtherRegs>();
-    if (warp == S::kCopyWarp) {
+    // bf16: a warp the keys and one the values (issuing bounds small pages: 16 positions, heads of 128, 8192 tokens 519 us with
+    // one warp); where the queries need a warp for each tile of rows, one warp both
+    const bool two_copy = !E4M3 && (NQ == 1 || a.q_boxes);
+    if (warp == S::kCopyWarp || (two_copy && warp == S::kKeyWarp)) {
         // ---- copies: keys and values in turn, a box (positions of one page) at a time ----
+        static_assert(E4M3 || S::kSlots % 2 == 0, "a slot is the keys' or the values'");
+        const int first_kv = warp == S::kCopyWarp ? 0 : 1, last_kv = two_copy ? first_kv : 1;
         constexpr int kDepth = E4M3 ? S::kStages : S::kSlots, kParts = E4M3 ? kTile / S::kStageRows : 1, kPartRows = kTile / kParts;
         const uint32_t lead = elect_lane();
         uint64_t* const arrived = E4M3 ? sh.stage_full : sh.full;
@@ -467,6 +472,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                     const int full = max(0, min(part_boxes, (w.end - tile * kTile + a.box - 1) / a.box - first));
                     const CUtensorMap* map = kv ? &v_map : &k_map;
                     const int at = e % kDepth;
+                    if (kv < first_kv || kv > last_kv) continue;
                     if (e >= kDepth) wait_for(&left[at], e / kDepth - 1, &sh.dead);
                     on = !__any_sync(0xFFFFFFFFu, *static_cast<volatile int*>(&sh.dead));
                     if (!on) break;
@@ -536,12 +542,12 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
         // the last copy into each place arrives before this CTA ends, whether or not its reader has waited for it
         if (lane < kDepth) {
             const int x = e - 1 - ((e - 1 - lane) % kDepth + kDepth) % kDepth;
-            if (x >= 0) mbar_wait(&arrived[lane], (x / kDepth) & 1, kMbarPolls);
+            if (x >= 0 && (!two_copy || (x & 1) == first_kv)) mbar_wait(&arrived[lane], (x / kDepth) & 1, kMbarPolls);
         } else if (lane == 31 && tails > 0) {
             mbar_wait(&sh.tail, (tails - 1) & 1, kMbarPolls);
         }
     } else if (warp == S::kQueryWarp || (!E4M3 && warp == S::kKeyWarp)) {
-        // ---- queries of the next unit, as soon as the last scores of this one are done; bf16: a tile of rows a warp ----
+        // ---- queries of the next unit, as soon as the last scores of this one are done; those without boxes of bf16: a tile of rows a warp ----
         const uint32_t lead = elect_lane();
         int seg0 = 0, seg1 = 0;
         auto queries = [&](int q, int& seg) {
@@ -593,8 +599,8 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
         };
 #pragma unroll 1
         while (w.next(a)) {
-            if (E4M3 || warp == S::kQueryWarp) queries(0, seg0);
-            if (NQ == 2 && (E4M3 || warp == S::kKeyWarp)) queries(1, seg1);
+            if (warp == S::kQueryWarp) queries(0, seg0);
+            if (NQ == 2 && (E4M3 || a.q_boxes || warp == S::kKeyWarp)) queries(1, seg1);
             w.step(a);
         }
         // boxes that nothing has waited for arrive before this CTA ends
