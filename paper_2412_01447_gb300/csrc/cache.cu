@@ -52,10 +52,7 @@ pldp_status cache_view(const char* fn, const pldp_cache& c, int B, CacheView* ou
     w.max_pages = c.max_pages;
     w.capacity = static_cast<int>(capacity);
     w.vec_bytes = c.head_dim * es;
-    uint32_t l = 0;
-    while ((uint64_t(1) << l) < static_cast<uint64_t>(c.page_size)) ++l;
-    w.div_shift = l;
-    w.div_mul = static_cast<uint32_t>((((uint64_t(1) << l) - c.page_size) << 32) / c.page_size + 1);
+    divide_by(c.page_size, &w.div_mul, &w.div_shift);
     return PLDP_OK;
 }
 

@@ -35,6 +35,14 @@ __host__ __device__ __forceinline__ uint32_t page_of(uint32_t p, uint32_t mul, u
 #endif
 }
 
+// page_of's constants for a divisor from 1 on.
+inline void divide_by(int d, uint32_t* mul, uint32_t* shift) {
+    uint32_t l = 0;
+    while ((uint64_t(1) << l) < static_cast<uint64_t>(d)) ++l;
+    *shift = l;
+    *mul = static_cast<uint32_t>((((uint64_t(1) << l) - d) << 32) / d + 1);
+}
+
 // Where position p of a sequence lies: byte offset of head 0's vector, or -1 where the page
 // table holds no page; `scale_at` the index of head 0's scale.
 __device__ __forceinline__ int64_t locate(const CacheView& c, const int32_t* table, int p, int64_t& scale_at) {

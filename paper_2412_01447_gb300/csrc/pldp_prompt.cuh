@@ -16,6 +16,7 @@ struct PromptArgs {
     float* parts;                          // [2 a CTA][Part]
     struct CutUnit* cuts;                  // [CTAs]
     int B, R, q_heads, group;
+    uint32_t group_mul, group_shift;       // division by group, as CacheView's by the page
     int box, pitch;                        // as AttendArgs
     int head_first;
     int q_boxes;                           // queries by boxes of whole tokens
@@ -48,16 +49,26 @@ constexpr int kPromptCtas = 192;           // at most
 
 namespace {
 
+// (32 bits where they do: a division of 64 takes some 100 cycles, and these are done before anything else can start)
+__host__ __device__ inline uint64_t quotient(uint64_t x, uint64_t y) {
+    return (x | y) >> 32 ? x / y : (uint32_t)x / (uint32_t)y;
+}
 // sum over i < n of floor((a i + b) / m), by the steps of Euclid's algorithm.
 __host__ __device__ inline uint64_t floor_sum(uint64_t n, uint64_t m, uint64_t a, uint64_t b) {
     uint64_t sum = 0;
     if (n == 0) return 0;
     while (true) {
-        if (a >= m) sum += n * (n - 1) / 2 * (a / m), a %= m;
-        if (b >= m) sum += n * (b / m), b %= m;
+        if (a >= m) {
+            const uint64_t q = quotient(a, m);
+            sum += n * (n - 1) / 2 * q, a -= q * m;
+        }
+        if (b >= m) {
+            const uint64_t q = quotient(b, m);
+            sum += n * q, b -= q * m;
+        }
         const uint64_t y = a * n + b;
         if (y < m) return sum;
-        n = y / m, b = y % m;
+        n = quotient(y, m), b = y - n * m;
         const uint64_t t = m;
         m = a, a = t;
     }
@@ -133,11 +144,22 @@ struct PromptShape {
     static constexpr int kBytes = kQBytes + kSlots * kSlot + kStages * kStage + kOut + 1024;
     static constexpr int kO = 256;                             // column of the first sums
     // 384 threads start with 168 registers each (640: 96); the softmax takes what the others leave
-    static constexpr int kSoftmaxRegs = 184, kOtherRegs = E4M3 ? 56 : 136, kConvertRegs = 88;
+    static constexpr int kSoftmaxRegs = E4M3 ? 184 : 192, kOtherRegs = E4M3 ? 72 : 120, kConvertRegs = 72;
     static_assert(kSlots >= 2 && (!E4M3 || kStages >= 1) && kBytes + kStatic <= kMaxShared, "shared memory");
 };
 
 constexpr int kAhead = 8;                  // tiles whose holes are kept (more than the ring of keys holds)
+
+// A unit, or what a CTA has of it, as one warp works it out for the others (rows: token * group + head).
+struct alignas(16) PromptUnit {
+    int b, kv;
+    int row, start, end;         // the sequence's first row, that one's position, and the first position that is not its
+    int r0, rows;                // the unit's first row of the sequence and kv head, and how many (below 256 or 128 in the last)
+    int t0, t1, T;               // this CTA's tiles of keys, of all; T 0: there is no more
+    int last_cta;                // where the unit begins and others have the rest: the CTA of its last tile
+    int unused;
+};
+constexpr int kUnits = 8;                  // worked out and not yet done by all
 
 template <bool E4M3>
 struct PromptShared {
@@ -147,7 +169,8 @@ struct PromptShared {
     int unit_of[4];
     uint32_t live[kAhead][4];              // whether a page holds the key, a bit each; looked at where `holes` is set
     int holes[kAhead];
-    uint64_t full[8], empty[8], stage_full[6], stage_empty[6], q_raw[2], s_full[2], p_full[2][2], pv_half[2], pv_done[2], q_full[2], q_empty[2], tail, drained,
+    PromptUnit units[kUnits];
+    uint64_t unit_full[kUnits], unit_empty[kUnits], full[8], empty[8], stage_full[6], stage_empty[6], q_raw[2], s_full[2], p_full[2][2], pv_half[2], pv_done[2], q_full[2], q_empty[2], tail, drained,
         key_full[4], key_empty[4];
     uint32_t tmem;
     int dead, zeros;
@@ -342,6 +365,10 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             mbar_init(&sh.key_full[i], 1);
             mbar_init(&sh.key_empty[i], S::kSoftmaxWarps + S::kConvertWarps);
         }
+        for (int i = 0; i < kUnits; ++i) {
+            mbar_init(&sh.unit_full[i], 1);
+            mbar_init(&sh.unit_empty[i], kThreads / 32 - 1);
+        }
         mbar_init(&sh.tail, 1);
         mbar_init(&sh.drained, 1);
         fence_mbar_init();
@@ -418,8 +445,21 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
     __syncthreads();
     tmem_after_sync();
     const uint32_t tmem = sh.tmem;
-    PromptWalk<UR> w;
-    w.b = sh.b, w.kv = sh.kv, w.unit = sh.unit, w.t0 = sh.tile, w.pre = sh.pre, w.at = sh.at, w.left = sh.count;
+    // The query warp works the units out for all: the sequence's rows, divisions and the cut, which every role would fetch
+    // code for and wait for loads for at every unit.
+    PromptUnit w;
+    int unit_no = 0;
+    auto next_unit = [&] {
+        wait_for(&sh.unit_full[unit_no % kUnits], unit_no / kUnits, &sh.dead);
+        if (*static_cast<volatile int*>(&sh.dead)) return false;
+        w = sh.units[unit_no % kUnits];
+        return w.T > 0;
+    };
+    auto unit_done = [&] {
+        __syncwarp();
+        mbar_arrive_if(&sh.unit_empty[unit_no % kUnits], lane == 0);
+        ++unit_no;
+    };
     if (sh.zeros) {
         // tokens that take no part: their rows, of all heads
 #pragma unroll 1
@@ -452,7 +492,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
         int e = 0, tile_no = 0, tails = 0;
         bool on = true;
 #pragma unroll 1
-        while (on && w.next(a)) {
+        while (on && next_unit()) {
             const int32_t* table = c.pages + w.b * c.pages_stride;
             // the page of box `box` of a tile; those of the next tile, a box a lane, are asked for before this one's
             // copies (pages that 4 does not divide have more boxes than lanes)
@@ -537,7 +577,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 }
                 page = page_ahead;
             }
-            w.step(a);
+            unit_done();
         }
         // the last copy into each place arrives before this CTA ends, whether or not its reader has waited for it
         if (lane < kDepth) {
@@ -563,7 +603,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 __syncwarp();
 #pragma unroll
                 for (int p = 0; p < S::kPanels; ++p)
-                    tma_box_if(to + p * (128 * 128), &q_map, p * 64, w.kv * a.group, w.p.row + static_cast<int>(first / group), 0, bar, lead);
+                    tma_box_if(to + p * (128 * 128), &q_map, p * 64, w.kv * a.group, w.row + static_cast<int>(page_of(first, a.group_mul, a.group_shift)), 0, bar, lead);
             } else {
                 // all of the tile's pieces of 16 bytes are asked for before the first is waited for
                 constexpr int kLanes = DP / 8, kAt = 32 / kLanes;          // lanes a row, and rows at once
@@ -571,7 +611,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 const bool in = piece * 8 < D;
                 uint8_t* const mine = to + (piece >> 3) * (128 * 128);
                 uint32_t tok = (first + lane / kLanes) / group, h = first + lane / kLanes - tok * group;
-                const __nv_bfloat16* from = a.q + w.p.row * a.q_tok + static_cast<int64_t>(w.kv) * a.group * a.q_head + piece * 8;
+                const __nv_bfloat16* from = a.q + w.row * a.q_tok + static_cast<int64_t>(w.kv) * a.group * a.q_head + piece * 8;
 #pragma unroll 2
                 for (int row = lane / kLanes; row < 128; row += kAt) {
                     const bool there = in && q * 128 + row < w.rows;
@@ -597,11 +637,43 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             }
             ++seg;
         };
+        if (warp == S::kQueryWarp) {
+            PromptWalk<UR> walk;
+            walk.b = sh.b, walk.kv = sh.kv, walk.unit = sh.unit, walk.t0 = sh.tile, walk.pre = sh.pre, walk.at = sh.at, walk.left = sh.count;
+            bool more = true;
+            int ahead = 0;
 #pragma unroll 1
-        while (w.next(a)) {
-            if (warp == S::kQueryWarp) queries(0, seg0);
-            if (NQ == 2 && (E4M3 || a.q_boxes || warp == S::kKeyWarp)) queries(1, seg1);
-            w.step(a);
+            while (true) {
+                // units are three ahead of their queries, which wait for the last ones' scores
+#pragma unroll 1
+                for (; more && ahead <= unit_no + 3; ++ahead) {
+                    if (ahead >= kUnits) wait_for(&sh.unit_empty[ahead % kUnits], ahead / kUnits - 1, &sh.dead);
+                    more = walk.next(a);
+                    PromptUnit u = {};
+                    if (more) {
+                        u = {walk.b, walk.kv, walk.p.row, walk.s.start, walk.end, static_cast<int>(walk.r0), walk.rows, walk.t0, walk.t1, walk.T, 0, 0};
+                        if (walk.t0 == 0 && walk.t1 < walk.T) {
+                            const long long last = walk.at + walk.pre + walk.T - 1, edge = (sh.each + 1) * sh.extra;
+                            u.last_cta = static_cast<int>(last < edge ? last / (sh.each + 1) : sh.extra + (last - edge) / sh.each);
+                        }
+                        walk.step(a);
+                    }
+                    if (lane == 0) sh.units[ahead % kUnits] = u;
+                    __syncwarp();
+                    mbar_arrive_if(&sh.unit_full[ahead % kUnits], lane == 0);
+                }
+                w = sh.units[unit_no % kUnits];
+                ++unit_no;
+                if (w.T == 0 || *static_cast<volatile int*>(&sh.dead)) break;
+                queries(0, seg0);
+                if (NQ == 2 && (E4M3 || a.q_boxes)) queries(1, seg1);
+            }
+        } else {
+#pragma unroll 1
+            while (next_unit()) {
+                queries(1, seg1);
+                unit_done();
+            }
         }
         // boxes that nothing has waited for arrive before this CTA ends
         const int last = lane ? seg1 : seg0;
@@ -611,7 +683,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
         if constexpr (E4M3) {
             int tile_no = 0, unit = 0;
 #pragma unroll 1
-            while (w.next(a)) {
+            while (next_unit()) {
                 const int32_t* table = c.pages + w.b * c.pages_stride;
 #pragma unroll 1
                 for (int tile = w.t0; tile < w.t1; ++tile, ++tile_no) {
@@ -621,7 +693,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int pos = tile * kTile + 4 * lane + i;
-                        f[i] = 0.f, v[i] = 0.f;
+                        f[i] = 1.f, v[i] = 0.f;                     // (a masked score stays -infinity by 1, not by 0)
                         gone[i] = false;
                         if (pos < w.end) {
                             const int pg_at = page_of(pos, c.div_mul, c.div_shift), pg = __ldg(table + pg_at);
@@ -656,7 +728,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                     __syncwarp();
                     mbar_arrive_if(&sh.key_full[at], lane == 0);
                 }
-                w.step(a);
+                unit_done();
             }
         }
     } else if (warp == S::kMmaWarp) {
@@ -713,7 +785,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
         // tile's scores, whose place the weights have left; one tile of rows has two places in turn for scores, and the
         // next tile's come first.
 #pragma unroll 1
-        while (w.next(a)) {
+        while (next_unit()) {
             const int n = w.t1 - w.t0, nq = w.rows > 128 ? 2 : 1;
 #pragma unroll 1
             for (int q = 0; q < nq; ++q) {
@@ -755,7 +827,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             ++seg0;
             if (nq == 2) ++seg1;
             e += 2 * n;
-            w.step(a);
+            unit_done();
         }
         // nothing reads shared memory or writes tensor memory any more when they are given back
         mma_commit(&sh.drained, lead);
@@ -776,7 +848,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             const int low = line + ((((chunk & 3) * 2) ^ (row0 & 7)) << 4), high = low ^ 16;
             int e = 0, tile_no = 0;                              // parts, tiles
 #pragma unroll 1
-            while (w.next(a)) {
+            while (next_unit()) {
 #pragma unroll 1
                 for (int tile = w.t0; tile < w.t1; ++tile, ++tile_no) {
                     const int key_at = tile_no & 3;
@@ -829,7 +901,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                         if (part % kParts == kParts - 1) mbar_arrive_if(&sh.full[slot], lane == 0);
                     }
                 }
-                w.step(a);
+                unit_done();
             }
         }
     } else {
@@ -843,7 +915,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
         int seg = 0;                                    // and its units
         bool cut_here = false;
 #pragma unroll 1
-        while (w.next(a)) {
+        while (next_unit()) {
             if (q * 128 >= w.rows) {                    // no rows for these warps
                 if constexpr (E4M3)
 #pragma unroll 1
@@ -853,15 +925,15 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                         mbar_arrive_if(&sh.key_empty[tile_no & 3], lane == 0);
                     }
                 else tile_no += w.t1 - w.t0;
-                w.step(a);
+                unit_done();
                 continue;
             }
-            const int64_t r = w.r0 + q * 128 + j;
-            const bool is_row = r < w.s.N;
-            const uint32_t tok = is_row ? static_cast<uint32_t>(r) / static_cast<uint32_t>(a.group) : 0u;
-            const uint32_t head = is_row ? static_cast<uint32_t>(w.kv) * a.group + (static_cast<uint32_t>(r) - tok * a.group) : 0u;
-            const int limit = is_row ? w.s.start + static_cast<int>(tok) : -1;         // last position that the row sees
-            const int seen_by_all = w.s.start + static_cast<int>(static_cast<uint32_t>(w.r0 + q * 128) / static_cast<uint32_t>(a.group));
+            const uint32_t r = static_cast<uint32_t>(w.r0) + q * 128 + j;
+            const bool is_row = q * 128 + j < w.rows;
+            const uint32_t tok = is_row ? page_of(r, a.group_mul, a.group_shift) : 0u;
+            const uint32_t head = is_row ? static_cast<uint32_t>(w.kv) * a.group + (r - tok * a.group) : 0u;
+            const int limit = is_row ? w.start + static_cast<int>(tok) : -1;         // last position that the row sees
+            const int seen_by_all = w.start + static_cast<int>(page_of(static_cast<uint32_t>(w.r0) + q * 128, a.group_mul, a.group_shift));
             float m = -INFINITY;                        // (of x, in powers of two)
             [[maybe_unused]] int unit = INT32_MIN;      // the values' in the sums (none yet)
             uint64_t l2 = 0, l3 = 0;
@@ -872,14 +944,14 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 uint8_t* const mine_q = q_smem + q * (S::kPanels * 128 * 128) + j * 128;
                 uint32_t most = 0;
                 auto piece = [&](int ch) { return reinterpret_cast<uint4*>(mine_q + (ch >> 3) * (128 * 128) + (((ch & 7) ^ (j & 7)) << 4)); };
-                // (D / 8 pieces, an even number; eight at a time)
+                // (D / 8 pieces, an even number)
 #pragma unroll 1
-                for (int c0 = 0; c0 < D / 8; c0 += 8) {
-                    uint4 x[8];
+                for (int c0 = 0; c0 < D / 8; c0 += 4) {
+                    uint4 x[4];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = c0 + i < D / 8 ? *piece(c0 + i) : make_uint4(0u, 0u, 0u, 0u);
+                    for (int i = 0; i < 4; ++i) x[i] = c0 + i < D / 8 ? *piece(c0 + i) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
+                    for (int i = 0; i < 4; ++i) {
                         const uint32_t v[4] = {x[i].x & 0x7FFF7FFFu, x[i].y & 0x7FFF7FFFu, x[i].z & 0x7FFF7FFFu, x[i].w & 0x7FFF7FFFu};
 #pragma unroll
                         for (int k = 0; k < 4; ++k) most = __vmaxu2(most, v[k]);
@@ -890,12 +962,12 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 const float lift = __uint_as_float((static_cast<uint32_t>(up + 127) << 23) ^ (a.flip & 0x80000000u));
                 f *= __uint_as_float(static_cast<uint32_t>(127 - up) << 23);
 #pragma unroll 1
-                for (int c0 = 0; c0 < D / 8; c0 += 8) {
-                    uint4 x[8];
+                for (int c0 = 0; c0 < D / 8; c0 += 4) {
+                    uint4 x[4];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = c0 + i < D / 8 ? *piece(c0 + i) : make_uint4(0u, 0u, 0u, 0u);
+                    for (int i = 0; i < 4; ++i) x[i] = c0 + i < D / 8 ? *piece(c0 + i) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
+                    for (int i = 0; i < 4; ++i) {
                         uint32_t v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
@@ -920,31 +992,30 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 tmem_after_sync();
                 const bool masked = tile * kTile + kTile - 1 > seen_by_all;
                 const bool holes = sh.holes[tile_no % kAhead];
+                if (masked || holes) {
+                    // scores of keys that the row does not see become -infinity where they are (code that is seldom run is
+                    // kept short: it is fetched anew every time)
+#pragma unroll 1
+                    for (int i = 0; i < kTile; i += 16) {
+                        const int most = limit - tile * kTile - i;                    // keys up to here
+                        uint32_t bits = most >= 15 ? 0xFFFFu : most < 0 ? 0u : (2u << most) - 1u;
+                        if (holes) bits &= sh.live[tile_no % kAhead][i >> 5] >> (i & 16);
+                        if (!__any_sync(0xFFFFFFFFu, (bits & 0xFFFFu) != 0xFFFFu)) continue;
+                        float y[16];
+                        tmem_load(s_at + i, y);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k)
+                            if (!(bits >> k & 1u)) y[k] = -INFINITY;
+                        tmem_store8(s_at + i, y);
+                        tmem_store8(s_at + i + 8, y + 8);
+                    }
+                    tmem_store_wait();
+                }
                 // Keys in two halves: the first's weights are in the product while the second's are taken.
 #pragma unroll 1
                 for (int half = 0; half < 2; ++half) {
                     float y[64];
                     tmem_load(s_at + half * 64, y);
-                    if constexpr (E4M3) {
-#pragma unroll
-                        for (int i = 0; i < 64; i += 4) {
-                            const float4 k = *reinterpret_cast<const float4*>(&sh.key_scale[k_at][half * 64 + i]);
-                            const uint64_t lo = mul_f32x2(pack_f32x2(y[i], y[i + 1]), pack_f32x2(k.x, k.y));
-                            const uint64_t hi = mul_f32x2(pack_f32x2(y[i + 2], y[i + 3]), pack_f32x2(k.z, k.w));
-                            y[i] = lo_f32(lo), y[i + 1] = hi_f32(lo), y[i + 2] = lo_f32(hi), y[i + 3] = hi_f32(hi);
-                        }
-                    }
-                    if (masked || holes) {
-                        const int most = limit - tile * kTile - half * 64;            // keys up to here
-                        uint32_t lo = most >= 31 ? 0xFFFFFFFFu : most < 0 ? 0u : (2u << most) - 1u;
-                        uint32_t hi = most >= 63 ? 0xFFFFFFFFu : most < 32 ? 0u : (2u << (most - 32)) - 1u;
-                        if (holes) lo &= sh.live[tile_no % kAhead][2 * half], hi &= sh.live[tile_no % kAhead][2 * half + 1];
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            if (!(lo >> i & 1u)) y[i] = -INFINITY;
-                            if (!(hi >> i & 1u)) y[32 + i] = -INFINITY;
-                        }
-                    }
                     // The weights with the m that there is, while the maximum is found; where m has to move, which it hardly
                     // ever does, they are taken again.
                     uint32_t p[32];
@@ -958,9 +1029,14 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                         s2 = l2, s3 = l3;
 #pragma unroll
                         for (int i = 0; i < 64; i += 4) {
-                            const uint64_t e0 = ordered_fma2(pack_f32x2(y[i], y[i + 1]), f2, less2), e1 = ordered_fma2(pack_f32x2(y[i + 2], y[i + 3]), f2, less2);
+                            uint64_t x0 = pack_f32x2(y[i], y[i + 1]), x1 = pack_f32x2(y[i + 2], y[i + 3]);
+                            if constexpr (E4M3) {
+                                const float4 k = *reinterpret_cast<const float4*>(&sh.key_scale[k_at][half * 64 + i]);
+                                x0 = mul_f32x2(x0, pack_f32x2(k.x, k.y)), x1 = mul_f32x2(x1, pack_f32x2(k.z, k.w));
+                            }
+                            const uint64_t e0 = ordered_fma2(x0, f2, less2), e1 = ordered_fma2(x1, f2, less2);
                             const float p0 = ordered_ex2(lo_f32(e0)), p1 = ordered_ex2(hi_f32(e0));
-                            t0 = ordered_max3(t0, y[i], y[i + 1]), t1 = ordered_max3(t1, y[i + 2], y[i + 3]);
+                            t0 = ordered_max3(t0, lo_f32(x0), hi_f32(x0)), t1 = ordered_max3(t1, lo_f32(x1), hi_f32(x1));
                             const float p2 = ordered_ex2(lo_f32(e1)), p3 = ordered_ex2(hi_f32(e1));
                             s2 = ordered_add2(s2, pack_f32x2(p0, p1));
                             s3 = ordered_add2(s3, pack_f32x2(p2, p3));
@@ -1020,39 +1096,36 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             const bool whole = w.t0 == 0 && w.t1 == w.T;
             if (whole) {
                 const float inverse = l > 0.f ? (E4M3 ? power_of_two(unit) : 1.f) / l : 0.f;
-                const int64_t row = w.p.row + static_cast<int64_t>(tok);
+                const int64_t row = w.row + static_cast<int64_t>(tok);
                 if (is_row && a.lse) a.lse[row * a.q_heads + head] = l > 0.f ? (log2f(l) + m - kLift) * 0.69314718055994531f : -INFINITY;
                 // kOutBytes of each of the warp's 32 rows at a time: a row a lane into shared memory, whole pieces of rows out of it
                 constexpr int kCols = S::kOutBytes / 2, kPieces = kCols / 8, kAt = 32 / kPieces;
                 uint8_t* const room = out_smem + warp * (32 * S::kOutBytes);
                 const int wrows = w.rows - q * 128 - quad * 32, piece = lane % kPieces;
                 const int64_t at_out = row * a.o_tok + static_cast<int64_t>(head) * a.o_head;
-                __nv_bfloat16* to[kPieces];                  // where this lane's pieces go, null: no such row
-#pragma unroll
-                for (int k = 0; k < kPieces; ++k) {
-                    const int rr = k * kAt + lane / kPieces;
-                    to[k] = a.out + __shfl_sync(0xFFFFFFFFu, at_out, rr) + piece * 8;
-                    if (rr >= wrows) to[k] = nullptr;
-                }
 #pragma unroll 1
                 for (int i = 0; i < D; i += kCols) {
-                    float o[kCols];
-                    tmem_load(my_o + i, o);
+                    // (e4m3, where more roles share the instruction cache: short code; bf16: 111 us for 24 short prompts, heads of
+                    // 128, with 64 columns at once, 114 with 16; e4m3, heads of 64: 151 and 145)
+                    constexpr int kLoad = E4M3 ? 16 : kCols;
+#pragma unroll 1
+                    for (int k = 0; k < kCols; k += kLoad) {
+                        float o[kLoad];
+                        tmem_load(my_o + i + k, o);
 #pragma unroll
-                    for (int k = 0; k < kCols; k += 8)
-                        *reinterpret_cast<uint4*>(room + lane * S::kOutBytes + ((k / 8 ^ (lane & (kPieces - 1))) << 4)) =
-                            make_uint4(pack_bf16(o[k] * inverse, o[k + 1] * inverse), pack_bf16(o[k + 2] * inverse, o[k + 3] * inverse),
-                                       pack_bf16(o[k + 4] * inverse, o[k + 5] * inverse), pack_bf16(o[k + 6] * inverse, o[k + 7] * inverse));
+                        for (int h = 0; h < kLoad; h += 8)
+                            *reinterpret_cast<uint4*>(room + lane * S::kOutBytes + (((k + h) / 8 ^ (lane & (kPieces - 1))) << 4)) =
+                                make_uint4(pack_bf16(o[h] * inverse, o[h + 1] * inverse), pack_bf16(o[h + 2] * inverse, o[h + 3] * inverse),
+                                           pack_bf16(o[h + 4] * inverse, o[h + 5] * inverse), pack_bf16(o[h + 6] * inverse, o[h + 7] * inverse));
+                    }
                     __syncwarp();
-                    uint4 y[kPieces];
-#pragma unroll
+#pragma unroll (E4M3 ? 2 : 4)
                     for (int k = 0; k < kPieces; ++k) {
                         const int rr = k * kAt + lane / kPieces;
-                        y[k] = *reinterpret_cast<const uint4*>(room + rr * S::kOutBytes + ((piece ^ (rr & (kPieces - 1))) << 4));
+                        const int64_t to = __shfl_sync(0xFFFFFFFFu, at_out, rr) + i + piece * 8;
+                        const uint4 y = *reinterpret_cast<const uint4*>(room + rr * S::kOutBytes + ((piece ^ (rr & (kPieces - 1))) << 4));
+                        if (rr < wrows && i + piece * 8 < D) *reinterpret_cast<uint4*>(a.out + to) = y;
                     }
-#pragma unroll
-                    for (int k = 0; k < kPieces; ++k)
-                        if (to[k] && i + piece * 8 < D) *reinterpret_cast<uint4*>(to[k] + i) = y[k];
                     __syncwarp();
                 }
             } else {
@@ -1073,20 +1146,17 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 part[128 * DP + j] = l > 0.f ? m - kLift : -INFINITY;
                 part[128 * DP + 128 + j] = l;
                 if (w.t0 == 0) cut_here = true;
-                if (w.t0 == 0 && threadIdx.x == 0) {
-                    // the CTA that has the unit's last tile
-                    const long long last = w.at + w.pre + w.T - 1, edge = (sh.each + 1) * sh.extra;
-                    const int c_last = static_cast<int>(last < edge ? last / (sh.each + 1) : sh.extra + (last - edge) / sh.each);
-                    a.cuts[blockIdx.x] = {c_last - static_cast<int>(blockIdx.x) + 1, static_cast<int>(blockIdx.x), static_cast<int>(w.r0), w.rows,
-                                          w.p.row, w.kv};
-                }
+                if (w.t0 == 0 && threadIdx.x == 0)
+                    a.cuts[blockIdx.x] = {w.last_cta - static_cast<int>(blockIdx.x) + 1, static_cast<int>(blockIdx.x), w.r0, w.rows, w.row, w.kv};
             }
-            if (sh.dead && j == 0 && a.status) atomicOr(a.status + w.b, PLDP_ST_TIMEOUT);
             tmem_before_sync();
             ++seg;
-            w.step(a);
+            unit_done();
         }
         if (threadIdx.x == 0 && !cut_here) a.cuts[blockIdx.x].parts = 0;
+        if (sh.dead && a.status)
+#pragma unroll 1
+            for (int b = threadIdx.x; b < a.B; b += S::kSoftmaxWarps * 32) atomicOr(a.status + b, PLDP_ST_TIMEOUT);
     }
     tmem_before_sync();
     __syncthreads();

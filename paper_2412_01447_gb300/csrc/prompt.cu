@@ -143,6 +143,7 @@ PLDP_API pldp_status pldp_attend_prompt(const pldp_attend_prompt_args* p, void* 
     a.cuts = static_cast<CutUnit*>(p->workspace);
     a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(p->workspace) + kCutBytes);
     a.B = p->B, a.R = p->R, a.q_heads = p->q_heads;
+    divide_by(a.group, &a.group_mul, &a.group_shift);
     // A negative scale turns the queries' signs, so that larger scores are larger weights; one of zero is the least that
     // keeps a masked score at -infinity.
     a.scale2 = fmaxf(fabsf(p->scale) * 1.4426950408889634f, 0x1p-126f);
