@@ -20,7 +20,6 @@ struct PromptArgs {
     int box, pitch;                        // as AttendArgs
     int head_first;
     int q_boxes;                           // queries by boxes of whole tokens
-    int least;                             // of the list a CTA takes at least
     float scale2;                          // |scale| * log2(e)
     uint32_t flip;                         // what turns the signs of two queries for a negative scale
 };
@@ -49,12 +48,16 @@ constexpr int kPromptCtas = 192;           // at most
 
 namespace {
 
+#ifdef __CUDACC__
+#define PLDP_ONE_COPY __noinline__
+#endif
 // (32 bits where they do: a division of 64 takes some 100 cycles, and these are done before anything else can start)
 __host__ __device__ inline uint64_t quotient(uint64_t x, uint64_t y) {
     return (x | y) >> 32 ? x / y : (uint32_t)x / (uint32_t)y;
 }
-// sum over i < n of floor((a i + b) / m), by the steps of Euclid's algorithm.
-__host__ __device__ inline uint64_t floor_sum(uint64_t n, uint64_t m, uint64_t a, uint64_t b) {
+// sum over i < n of floor((a i + b) / m), by the steps of Euclid's algorithm.  (One copy of its code: at a kernel's start
+// every new line of code is a miss in the instruction cache, which takes longer than what it holds.)
+__host__ __device__ inline PLDP_ONE_COPY uint64_t floor_sum(uint64_t n, uint64_t m, uint64_t a, uint64_t b) {
     uint64_t sum = 0;
     if (n == 0) return 0;
     while (true) {
@@ -103,18 +106,24 @@ __device__ __forceinline__ int64_t tiles_before(const Units& s, int u) {
 // results' way out.  The list counts it, so that a part of many short units is not the last to end.
 constexpr int kUnitCost = 2;
 template <int UR>
-__device__ __forceinline__ int64_t cost_before(const Units& s, int u) { return tiles_before<UR>(s, u) + static_cast<int64_t>(u) * kUnitCost; }
+__device__ __noinline__ int64_t cost_before(const Units& s, int u) { return tiles_before<UR>(s, u) + static_cast<int64_t>(u) * kUnitCost; }
 // The unit that holds place x of the list of one kv head: cost_before(u) <= x < cost_before(u + 1).
 template <int UR>
-__device__ __forceinline__ int unit_at(const Units& s, int units, int64_t x) {
+__device__ __forceinline__ int unit_at(const Units& s, int units, int64_t x, int64_t* before) {
     // tiles grow linearly from unit to unit: the root of their sum, and from there to the unit itself
     const float a2 = UR / (2.f * kTile * s.group), b = kUnitCost + (s.start + 0.5f * UR / s.group) / kTile + 0.5f;
     int u = static_cast<int>((sqrtf(b * b + 4.f * a2 * static_cast<float>(x)) - b) / (2.f * a2));
     u = max(0, min(u, units - 1));
-    while (u > 0 && cost_before<UR>(s, u) > x) --u;
-    while (u + 1 < units && cost_before<UR>(s, u + 1) <= x) ++u;
+    int64_t at = cost_before<UR>(s, u);
+    while (at > x) at -= kUnitCost + unit_tiles<UR>(s, --u);
+    for (int next; at + (next = kUnitCost + unit_tiles<UR>(s, u)) <= x; ++u) at += next;
+    *before = at;
     return u;
 }
+// Units of so few tiles are one CTA's, that of the place in the list where they begin.
+constexpr int kWhole = 4;
+// And a part is no smaller than this: of a unit that several have, a few tiles each pay for the join.
+constexpr int kLeast = 3;
 
 template <int DP, bool E4M3>
 struct PromptShape {
@@ -137,7 +146,7 @@ struct PromptShape {
     // e4m3: codes as they are, a tile (heads above 128 elements: half of one) a stage
     static constexpr int kStageRows = DP == 256 ? 64 : kTile, kStage = E4M3 ? kStageRows * (DP < 128 ? 128 : DP) : 0;
     static constexpr int kRoom = kMaxShared - 1024 - kStatic - kQBytes - kOut;
-    static constexpr int kMost = (kRoom - (DP == 256 ? 1 : 3) * kStage) / kSlot;
+    static constexpr int kMost = (kRoom - (DP == 256 ? 1 : 2) * kStage) / kSlot;
     static constexpr int kSlots = kMost > 6 ? 6 : kMost;
     static constexpr int kFit = E4M3 ? (kRoom - kSlots * kSlot) / kStage : 0;
     static constexpr int kStages = kFit > 6 ? 6 : kFit;
@@ -177,7 +186,7 @@ struct PromptShared {
     long long warp_sum[24];
     long long total;
     // where this CTA's part of the list starts
-    int b, kv, unit, tile, pre;
+    int b, kv, unit, in;                   // (in: how far into the unit, its own cost first)
     long long at, count, each, extra;
 };
 
@@ -196,7 +205,7 @@ struct PromptWalk {
     int end;           // positions from here on are not the sequence's
 
     __device__ __forceinline__ bool next(const PromptArgs& a) {
-        if (left <= pre) return false;
+        if (left <= 0) return false;
         uint32_t st;
         while (true) {                                           // (sequences without rows hold no tiles)
             p = packed_rows(a.rows, a.start, b, a.R, a.c.capacity, st);
@@ -207,10 +216,30 @@ struct PromptWalk {
         units = unit_count<UR>(s);
         end = s.start + s.count;
         T = unit_tiles<UR>(s, unit);
-        t1 = left - pre < T - t0 ? t0 + static_cast<int>(left - pre) : T;
+        if (T <= kWhole) {
+            t1 = T;
+        } else {
+            if (left <= pre) return false;
+            t1 = left - pre < T - t0 ? t0 + static_cast<int>(left - pre) : T;
+        }
         r0 = static_cast<int64_t>(unit) * UR;
         rows = static_cast<int>(min(static_cast<int64_t>(UR), s.N - r0));
         return true;
+    }
+    // Where a part begins inside a unit that is another CTA's whole, it begins behind it.
+    __device__ __forceinline__ bool first(const PromptArgs& a, int in) {
+        if (in > 0) {
+            uint32_t st;
+            p = packed_rows(a.rows, a.start, b, a.R, a.c.capacity, st);
+            s = units_of(p, a.group);
+            units = unit_count<UR>(s);
+            T = unit_tiles<UR>(s, unit);
+            if (T <= kWhole) {
+                t0 = 0, t1 = T, pre = kUnitCost - in;                   // (what of the unit lies in this part goes with it)
+                step(a);
+            }
+        }
+        return next(a);
     }
     __device__ __forceinline__ void step(const PromptArgs& a) {
         at += pre + (t1 - t0);
@@ -382,12 +411,6 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
     {
         const int strip = (a.B + kThreads - 1) / kThreads;
         const int lo = min(a.B, static_cast<int>(threadIdx.x) * strip), hi = min(a.B, lo + strip);
-        auto cost_of = [&](int b) -> long long {
-            uint32_t st;
-            const PackedRows p = packed_rows(a.rows, a.start, b, a.R, c.capacity, st);
-            const Units s = units_of(p, a.group);
-            return c.heads * cost_before<UR>(s, unit_count<UR>(s));
-        };
         long long mine = 0;
 #pragma unroll 1
         for (int b = lo; b < hi; ++b) {
@@ -395,7 +418,9 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             const PackedRows p = packed_rows(a.rows, a.start, b, a.R, c.capacity, st);
             if (st && blockIdx.x == 0 && a.status) atomicOr(a.status + b, st);
             if (p.count < p.given) sh.zeros = 1;
-            mine += cost_of(b);
+            if (p.count == 0) continue;
+            const Units s = units_of(p, a.group);
+            mine += c.heads * cost_before<UR>(s, unit_count<UR>(s));
         }
         long long upto = mine;
 #pragma unroll
@@ -412,33 +437,36 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             total += sh.warp_sum[w];
         }
         // equal parts; the first `extra` CTAs take one more than the others
-        const long long most = (total + a.least - 1) / a.least;
+        const long long most = quotient(total + kLeast - 1, kLeast);
         const int ctas = static_cast<int>(most < gridDim.x ? most : gridDim.x);
-        const long long each = ctas ? total / ctas : 0, extra = ctas ? total - each * ctas : 0;
+        const long long each = ctas ? quotient(total, ctas) : 0, extra = ctas ? total - each * ctas : 0;
         const long long g0 = each * blockIdx.x + min(static_cast<long long>(blockIdx.x), extra);
         const long long g1 = g0 + each + (blockIdx.x < extra ? 1 : 0);
         long long before = upto - mine;
         if (blockIdx.x < ctas && before <= g0 && g0 < before + mine) {              // one thread's
-            int b = lo;
 #pragma unroll 1
-            for (;; ++b) {
-                const long long t = cost_of(b);
-                if (g0 < before + t) break;
-                before += t;
+            for (int b = lo;; ++b) {
+                uint32_t st;
+                const Units s = units_of(packed_rows(a.rows, a.start, b, a.R, c.capacity, st), a.group);
+                if (s.N == 0) continue;
+                const int units = unit_count<UR>(s);
+                const long long per = strip == 1 ? quotient(mine, c.heads) : cost_before<UR>(s, units);
+                if (g0 >= before + per * c.heads) {
+                    before += per * c.heads;
+                    continue;
+                }
+                const int kv = static_cast<int>(quotient(g0 - before, per));
+                int64_t at;
+                sh.unit = unit_at<UR>(s, units, g0 - before - kv * per, &at);
+                sh.b = b, sh.kv = kv;
+                sh.in = static_cast<int>(g0 - before - kv * per - at);
+                sh.at = g0, sh.count = g1 - g0;
+                break;
             }
-            uint32_t st;
-            const Units s = units_of(packed_rows(a.rows, a.start, b, a.R, c.capacity, st), a.group);
-            const int units = unit_count<UR>(s);
-            const long long per = cost_before<UR>(s, units), in = g0 - before;
-            const int kv = static_cast<int>(in / per), u = unit_at<UR>(s, units, in - kv * per);
-            const int x = static_cast<int>(in - kv * per - cost_before<UR>(s, u));
-            sh.b = b, sh.kv = kv, sh.unit = u;
-            sh.pre = max(0, kUnitCost - x), sh.tile = max(0, x - kUnitCost);
-            sh.at = g0, sh.count = g1 - g0;
         }
         if (threadIdx.x == 0) {
             sh.each = each, sh.extra = extra;
-            if (blockIdx.x >= ctas) sh.count = sh.pre = 0;
+            if (blockIdx.x >= ctas) sh.count = 0;
         }
     }
     tmem_before_sync();
@@ -590,8 +618,9 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
         // ---- queries of the next unit, as soon as the last scores of this one are done; those without boxes of bf16: a tile of rows a warp ----
         const uint32_t lead = elect_lane();
         int seg0 = 0, seg1 = 0;
-        auto queries = [&](int q, int& seg) {
+        auto queries = [&](int q) {
             if (q * 128 >= w.rows) return;
+            int& seg = q ? seg1 : seg0;
             if (seg > 0) wait_for(&sh.q_empty[q], seg - 1, &sh.dead);
             if (*static_cast<volatile int*>(&sh.dead)) return;
             uint64_t* const bar = E4M3 ? &sh.q_raw[q] : &sh.q_full[q];
@@ -637,18 +666,24 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             }
             ++seg;
         };
+        auto tile_rows = [&](int from, int to) {
+#pragma unroll 1
+            for (int q = from; q < to; ++q) queries(q);
+        };
         if (warp == S::kQueryWarp) {
             PromptWalk<UR> walk;
-            walk.b = sh.b, walk.kv = sh.kv, walk.unit = sh.unit, walk.t0 = sh.tile, walk.pre = sh.pre, walk.at = sh.at, walk.left = sh.count;
-            bool more = true;
+            walk.b = sh.b, walk.kv = sh.kv, walk.unit = sh.unit, walk.at = sh.at, walk.left = sh.count;
+            walk.pre = max(0, kUnitCost - sh.in), walk.t0 = max(0, sh.in - kUnitCost);
+            bool more = walk.left > 0;
+            bool ended = false;
             int ahead = 0;
 #pragma unroll 1
             while (true) {
                 // units are three ahead of their queries, which wait for the last ones' scores
 #pragma unroll 1
-                for (; more && ahead <= unit_no + 3; ++ahead) {
+                for (; !ended && ahead <= unit_no + 3; ++ahead) {
                     if (ahead >= kUnits) wait_for(&sh.unit_empty[ahead % kUnits], ahead / kUnits - 1, &sh.dead);
-                    more = walk.next(a);
+                    if (more) more = ahead == 0 ? walk.first(a, sh.in) : walk.next(a);
                     PromptUnit u = {};
                     if (more) {
                         u = {walk.b, walk.kv, walk.p.row, walk.s.start, walk.end, static_cast<int>(walk.r0), walk.rows, walk.t0, walk.t1, walk.T, 0, 0};
@@ -657,6 +692,8 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                             u.last_cta = static_cast<int>(last < edge ? last / (sh.each + 1) : sh.extra + (last - edge) / sh.each);
                         }
                         walk.step(a);
+                    } else {
+                        ended = true;
                     }
                     if (lane == 0) sh.units[ahead % kUnits] = u;
                     __syncwarp();
@@ -665,13 +702,12 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 w = sh.units[unit_no % kUnits];
                 ++unit_no;
                 if (w.T == 0 || *static_cast<volatile int*>(&sh.dead)) break;
-                queries(0, seg0);
-                if (NQ == 2 && (E4M3 || a.q_boxes)) queries(1, seg1);
+                tile_rows(0, NQ == 2 && (E4M3 || a.q_boxes) ? 2 : 1);
             }
         } else {
 #pragma unroll 1
             while (next_unit()) {
-                queries(1, seg1);
+                tile_rows(1, 2);
                 unit_done();
             }
         }

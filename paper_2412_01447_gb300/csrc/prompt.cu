@@ -148,7 +148,6 @@ PLDP_API pldp_status pldp_attend_prompt(const pldp_attend_prompt_args* p, void* 
     // keeps a masked score at -infinity.
     a.scale2 = fmaxf(fabsf(p->scale) * 1.4426950408889634f, 0x1p-126f);
     a.flip = p->scale < 0.f ? 0x80008000u : 0u;
-    a.least = kUnitCost + 2;
     a.box = kTile;                                           // the largest power of two that divides the page, up to a tile
     while (p->cache.page_size % a.box) a.box /= 2;
     const bool e4m3 = p->cache.dtype == PLDP_E4M3;

@@ -146,7 +146,7 @@ def test_sums_of_tiles(tmp_path):
     """The closed form of the list's sums (host code of the kernel's header) against adding up."""
     src = open(os.path.join(os.path.dirname(HEADER), "..", "paper_2412_01447_gb300", "csrc", "pldp_prompt.cuh")).read()
     body = src[src.index("__host__ __device__ inline uint64_t quotient"):src.index("// The rows of a sequence and kv head")]
-    (tmp_path / "sum.c").write_text("#include <stdint.h>\n#include <stdbool.h>\n#include <stdio.h>\n#define __host__\n#define __device__\n" + body +
+    (tmp_path / "sum.c").write_text("#include <stdint.h>\n#include <stdbool.h>\n#include <stdio.h>\n#define __host__\n#define __device__\n#define PLDP_ONE_COPY\n" + body +
                                     'int main(void) { unsigned long long n, m, a, b; while (scanf("%llu %llu %llu %llu", &n, &m, &a, &b) == 4) '
                                     'printf("%llu\\n", (unsigned long long)floor_sum(n, m, a, b)); return 0; }')
     subprocess.check_call(["gcc", "-std=c99", "-Dinline=static", str(tmp_path / "sum.c"), "-o", str(tmp_path / "sum")])
