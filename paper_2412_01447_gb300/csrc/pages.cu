@@ -73,9 +73,8 @@ struct Counts {
 };
 
 // Every warp's count -> the count before this warp in the whole cluster (`before`) and of all (`all`); where they may
-// pass `most`, they stay there.  All threads of the cluster come here, once for each `c`.
-__device__ __forceinline__ void cluster_count(cg::cluster_group& cluster, Counts& c, int mine, int& before, int& all,
-                                              int most = INT32_MAX) {
+// pass `most`, they stay there.  A cluster barrier lies between the two halves, once for each `c`.
+__device__ __forceinline__ void give_count(Counts& c, int mine, int most) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (lane == 0) c.warp[warp] = mine;
     __syncthreads();
@@ -90,7 +89,8 @@ __device__ __forceinline__ void cluster_count(cg::cluster_group& cluster, Counts
         c.warp[lane] = lane ? prior : 0;
         if (lane == 31) c.total = upto;
     }
-    cluster.sync();
+}
+__device__ __forceinline__ void take_count(cg::cluster_group& cluster, Counts& c, int most, int& before, int& all) {
     unsigned ahead = 0, sum = 0;
 #pragma unroll
     for (int k = 0; k < kCluster; ++k) {
@@ -98,7 +98,7 @@ __device__ __forceinline__ void cluster_count(cg::cluster_group& cluster, Counts
         if (k < static_cast<int>(cluster.block_rank())) ahead = min(ahead + x, static_cast<unsigned>(most));
         sum = min(sum + x, static_cast<unsigned>(most));
     }
-    before = min(ahead + c.warp[warp], static_cast<unsigned>(most)), all = sum;
+    before = min(ahead + c.warp[threadIdx.x >> 5], static_cast<unsigned>(most)), all = sum;
 }
 
 // A warp's run of pages, four neighbours a lane.
@@ -177,8 +177,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(kCluster, 1, 1) 
 
     // which entries need a page, a word of 32 a warp
     const int64_t items = static_cast<int64_t>(t.B) * a.W;
-    for (int64_t i = rank * kWarps + warp; i < items; i += kCluster * kWarps) {
-        const int b = static_cast<int>(i / a.W), w = static_cast<int>(i - static_cast<int64_t>(b) * a.W);
+    auto look = [&](int b, int w) {
         const Range r = range_of(a, b);
         const int k = w * 32 + lane;
         bool need = false;
@@ -187,14 +186,13 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(kCluster, 1, 1) 
             need = !is_page(t, page) || t.refs[page] > 1;
         }
         const uint32_t word = __ballot_sync(0xFFFFFFFFu, need);
-        if (lane == 0) a.words[i] = word;
-    }
-    int mine = 0;
-    for (int p = run.lo + 4 * lane; p - 4 * lane < run.hi; p += 128) mine += __popc(four_pages<false>(t.refs, vectors, p, run.hi));
-    int before, all;
-    cluster_count(cluster, free_pages, warp_total(mine), before, all);
-
+        if (lane == 0) a.words[static_cast<int64_t>(b) * a.W + w] = word;
+        return __popc(word);
+    };
     // how many pages each sequence needs: CTAs have runs of sequences, their warps neighbouring ones
+    // (no more than there are pages count: sums stay in range, and more are not given out)
+    const int most = t.n_pages + 1;
+    auto plus = [&](int x, int y) { return static_cast<int>(min(static_cast<unsigned>(x) + static_cast<unsigned>(y), static_cast<unsigned>(most))); };
     const int each = (t.B + kCluster * kWarps - 1) / (kCluster * kWarps);
     const int b0 = min(t.B, (rank * kWarps + warp) * each), b1 = min(t.B, b0 + each);
     auto needs = [&](int b) {
@@ -202,13 +200,28 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(kCluster, 1, 1) 
         for (int w = lane; w < a.W; w += 32) n += __popc(__ldcg(a.words + static_cast<int64_t>(b) * a.W + w));
         return warp_total(n);
     };
-    // (no more than there are pages count: sums stay in range, and more are not given out)
-    const int most = t.n_pages < INT32_MAX ? t.n_pages + 1 : INT32_MAX;
-    auto plus = [&](int x, int y) { return static_cast<int>(min(static_cast<unsigned>(x) + static_cast<unsigned>(y), static_cast<unsigned>(most))); };
     int warp_needs = 0;
-    for (int b = b0; b < b1; ++b) warp_needs = plus(warp_needs, needs(b));
-    int need_before, need_all;
-    cluster_count(cluster, wanted, warp_needs, need_before, need_all, most);
+    if (a.W == 1) {                                          // (a step: its counts go with those of the free pages)
+        for (int b = b0; b < b1; ++b) warp_needs = plus(warp_needs, look(b, 0));
+    } else {
+        for (int64_t i = rank * kWarps + warp; i < items; i += kCluster * kWarps) {
+            const int b = static_cast<int>(i / a.W);
+            look(b, static_cast<int>(i - static_cast<int64_t>(b) * a.W));
+        }
+    }
+    int mine = 0;
+    for (int p = run.lo + 4 * lane; p - 4 * lane < run.hi; p += 128) mine += __popc(four_pages<false>(t.refs, vectors, p, run.hi));
+    give_count(free_pages, warp_total(mine), INT32_MAX);
+    if (a.W == 1) give_count(wanted, warp_needs, most);
+    cluster.sync();
+    int before, all, need_before, need_all;
+    take_count(cluster, free_pages, INT32_MAX, before, all);
+    if (a.W > 1) {
+        for (int b = b0; b < b1; ++b) warp_needs = plus(warp_needs, needs(b));
+        give_count(wanted, warp_needs, most);
+        cluster.sync();
+    }
+    take_count(cluster, wanted, most, need_before, need_all);
     for (int b = b0; b < b1; ++b) {
         const int n = needs(b);
         const bool served = n == 0 || static_cast<int64_t>(need_before) + n <= all;
@@ -280,8 +293,10 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(kCluster, 1, 1) 
     if (threadIdx.x == 0) moves = 0;
     int mine = 0;
     for (int p = run.lo + 4 * lane; p - 4 * lane < run.hi; p += 128) mine += __popc(four_pages<true>(t.refs, vectors, p, run.hi));
+    give_count(held, warp_total(mine), INT32_MAX);
+    cluster.sync();
     int before, U;
-    cluster_count(cluster, held, warp_total(mine), before, U);
+    take_count(cluster, held, INT32_MAX, before, U);
 
     // free pages below U by ascending number, held ones from U on by descending number
     int moving = 0;
