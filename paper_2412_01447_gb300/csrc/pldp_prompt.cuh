@@ -181,6 +181,9 @@ struct PromptShared {
     PromptUnit units[kUnits];
     uint64_t unit_full[kUnits], unit_empty[kUnits], full[8], empty[8], stage_full[6], stage_empty[6], q_raw[2], s_full[2], p_full[2][2], pv_half[2], pv_done[2], q_full[2], q_empty[2], tail, drained,
         key_full[4], key_empty[4];
+#ifdef PLDP_TEST_STUCK_SCORES
+    uint64_t never;                        // test build: a barrier that nothing arrives on
+#endif
     uint32_t tmem;
     int dead, zeros;
     long long warp_sum[24];
@@ -347,9 +350,20 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // f16): weights may be large, their rounding is relative.
 //
 // Weights are rounded to bf16 (2^-8 of each) over a bf16 cache, whose values need bf16's range: two terms, as a step's attention takes
-// them, would make the second product, half of the work here, twice as long.  Over an e4m3 cache codes, exact in f16, are
-// converted by warps of their own and weights are f16 (2^-11); k's scales multiply the scores, v's go into the exponent
-// and are divided out of the sums.
+// them, would make the second product, half of the work here, twice as long.  Over an e4m3 cache codes are converted by warps
+// of their own and weights are f16 (2^-11): keys as f16, which holds every code, their scales multiplying the scores; values
+// times scale / 2^unit, each rounded to f16 (2^-11), where 2^unit is above the largest scale that the unit has met, and O is
+// multiplied when that rises.
+//
+// What bounds it: the matrix unit, 64 cycles for each 16 elements of a product of 128 rows and 128 columns, and beside it
+// the special functions' rate, 4 cycles a warp's 32 exponentials, and the hand-over of each tile between the roles.  Measured, bf16, heads of
+// 128, 32 over 8: a prompt of 8192 tokens 370 us (1490 TFLOP/s, 0.79 of the rate measured for one large matrix
+// product), four of 16384 4.3 ms (1430, where the clock falls under the power limit).  Steps on the way there, the former's us:
+// 2530 as one CTA's products and softmax in turn; 685 by two tiles of rows, queries asynchronous; 428 with weights in halves, of
+// which the first is multiplied while the second is taken; 370 with the units worked out by one warp and seldom-run code kept
+// short, as every new line of it is a miss in the instruction cache.  Tried and not kept: a warp for each tile of rows'
+// products (494 for 425), their issue as a loop (522 for 364), a tile's maximum before its weights (two passes over the scores).
+// e4m3: 563 us; there the conversion shares the issue slots with the softmax, whose halves take 1000 cycles each.
 //
 // The tiles of all units form one list, cut into equal parts, one a CTA (one a SM), whatever the lengths are; what
 // a part holds of a unit that others share goes to the workspace, and the join, a kernel behind this one, adds them in order.
@@ -400,6 +414,9 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
         }
         mbar_init(&sh.tail, 1);
         mbar_init(&sh.drained, 1);
+#ifdef PLDP_TEST_STUCK_SCORES
+        mbar_init(&sh.never, 1);
+#endif
         fence_mbar_init();
         sh.dead = 0;
         sh.zeros = 0;
@@ -683,6 +700,9 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
 #pragma unroll 1
                 for (; !ended && ahead <= unit_no + 3; ++ahead) {
                     if (ahead >= kUnits) wait_for(&sh.unit_empty[ahead % kUnits], ahead / kUnits - 1, &sh.dead);
+                    // (after a wait that ran out a place may still be read: half of one unit and half of another would put
+                    // results anywhere)
+                    if (__any_sync(0xFFFFFFFFu, *static_cast<volatile int*>(&sh.dead))) break;
                     if (more) more = ahead == 0 ? walk.first(a, sh.in) : walk.next(a);
                     PromptUnit u = {};
                     if (more) {
@@ -1023,6 +1043,9 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 const uint32_t s_turn = NQ == 2 ? mine : mine >> 1;
                 [[maybe_unused]] const int k_at = tile_no & 3;
                 if constexpr (E4M3) wait_for(&sh.key_full[k_at], tile_no >> 2, &sh.dead);
+#ifdef PLDP_TEST_STUCK_SCORES
+                wait_for(&sh.never, 0, &sh.dead);
+#endif
                 wait_for(&sh.s_full[at], s_turn, &sh.dead);
                 __syncwarp();
                 tmem_after_sync();
