@@ -5,6 +5,9 @@
 The model is a few attention layers with random weights (no MLP, no training), enough to produce queries,
 keys, values and logits; what is shown is the step around it:
 
+  prompts     pldp_pages_reserve, then per layer pldp_cache_append_prompt and pldp_attend_prompt, all
+              sequences' tokens packed
+  a step      pldp_pages_reserve   pages for the tokens that it appends
   per layer   pldp_cache_append    norms and rotates the step's queries and keys, writes keys and values
               pldp_attend_cache    attends over the cache with all of the step's tokens at once
   then        pldp_verify_greedy   accepts the draft's prefix and appends it with the bonus token
@@ -60,10 +63,11 @@ class Decoder:
             10000.0 ** (-torch.arange(0, s.head_dim, 2, device=device, dtype=torch.float64) / s.head_dim))
         self.cos, self.sin = angle.cos().float(), angle.sin().float()
 
-        # one pool of pages a layer; every sequence has its pages anywhere in it, the same in all layers
+        # one pool of pages a layer; every sequence has its pages anywhere in it, the same in all layers, as it needs them
         per = -(-context // s.page)
         n_pages = B * per
-        self.pages = torch.randperm(n_pages, generator=g, device=device).to(torch.int32).view(B, per)
+        self.pages = torch.full((B, per), -1, dtype=torch.int32, device=device)
+        self.table = pk.pldp_page_table(self.pages, torch.zeros(n_pages, dtype=torch.int32, device=device), s.page)
         kind = torch.bfloat16 if s.cache == "bf16" else torch.float8_e4m3fn
         pool = lambda: torch.zeros((n_pages, s.page, s.heads, s.head_dim), device=device, dtype=torch.bfloat16).to(kind)  # noqa: E731
         scale = lambda: torch.ones((n_pages, s.heads, s.page), device=device) if s.cache == "e4m3" else None  # noqa: E731
@@ -71,6 +75,9 @@ class Decoder:
 
         n, i32 = s.K + 1, dict(dtype=torch.int32, device=device)
         self.workspace = torch.zeros(pk.pldp_attend_workspace_size(B, n, s.q_heads, s.heads, s.head_dim), dtype=torch.uint8, device=device)
+        self.prompt_ws = torch.empty(pk.pldp_attend_prompt_workspace_size(s.q_heads, s.heads, s.head_dim), dtype=torch.uint8, device=device)
+        self.pages_ws = torch.empty(pk.pldp_pages_workspace_size(self.table), dtype=torch.uint8, device=device)
+        self.copies = torch.empty((B, 2), **i32)
         self.verify_ws = torch.zeros(pk.pldp_verify_workspace_size(B, s.K, s.vocab), dtype=torch.uint8, device=device)
         self.score_ws = torch.empty(pk.pldp_token_logprobs_workspace_size(B * n, s.vocab), dtype=torch.uint8, device=device)
         self.draft, self.draft_len = torch.zeros((B, s.K), **i32), torch.zeros(B, **i32)
@@ -79,6 +86,26 @@ class Decoder:
         self.scores, self.best = torch.zeros((B, 1024), device=device), torch.zeros(B, **i32)
         self.status = torch.zeros(B, **i32)
 
+    def reserve(self, start, n, count=None):
+        # (no page here is held by two sequences, so that none has to be copied)
+        pk.pldp_pages_reserve(self.table, start, self.copies, self.pages_ws, n, count=count, status=self.status)
+
+    def prompts(self, tokens, rows, n):
+        """Takes the prompts into the caches: sequence b's tokens are tokens[rows[b]:rows[b + 1]], n of one at most."""
+        s, R = self.s, tokens.shape[0]
+        x, start = self.embed[tokens.long()], torch.zeros_like(rows[:-1])
+        self.reserve(start, n, rows[1:] - rows[:-1])
+        for layer in range(s.layers):
+            h = torch.nn.functional.layer_norm(x, (self.d,))
+            qkv = (h @ self.qkv[layer]).to(torch.bfloat16).view(R, s.q_heads + 2 * s.heads, s.head_dim)
+            q, k, v = qkv.split((s.q_heads, s.heads, s.heads), 1)
+            out = torch.empty((R, s.q_heads, s.head_dim), device=self.dev, dtype=torch.bfloat16)
+            pk.pldp_cache_append_prompt(self.caches[layer], q, k, v, rows, q, start=start, q_norm=self.norms[layer][0],
+                                        k_norm=self.norms[layer][1], cos=self.cos, sin=self.sin, status=self.status)
+            if layer + 1 < s.layers:                              # (nothing reads what the last layer would give)
+                pk.pldp_attend_prompt(self.caches[layer], q, rows, out, self.prompt_ws, start=start, status=self.status)
+                x = x + out.float().view(R, self.d) @ self.proj[layer]
+
     def forward(self, tokens, seq_len, draft_len):
         """Logits [B, n, vocab] of x_t and its draft (tokens [B, n], x_t first); what ranking needs of
         each layer stays in self.rows."""
@@ -86,9 +113,7 @@ class Decoder:
         x = self.embed[tokens.long()]
         self.rows = []
         ws = self.workspace
-        need = pk.pldp_attend_workspace_size(B, n, s.q_heads, s.heads, s.head_dim)
-        if ws.numel() < need:                                     # a prompt is one long draft
-            ws = torch.zeros(need, dtype=torch.uint8, device=self.dev)
+        self.reserve(seq_len - 1, n, draft_len + 1)
         for layer in range(s.layers):
             h = torch.nn.functional.layer_norm(x, (self.d,))
             qkv = (h @ self.qkv[layer]).to(torch.bfloat16).view(B, n, s.q_heads + 2 * s.heads, s.head_dim)
@@ -121,8 +146,9 @@ class Decoder:
         ids[:, : prompt.shape[1]] = prompt
         seq_len = torch.full((B,), prompt.shape[1], dtype=torch.int32, device=self.dev)
         start = seq_len.clone()
-        # the prompt but its last token, as a draft behind its first
-        self.forward(prompt[:, :-1], torch.ones_like(seq_len), torch.full_like(seq_len, prompt.shape[1] - 2))
+        # the prompts but their last tokens
+        n = prompt.shape[1] - 1
+        self.prompts(prompt[:, :-1].reshape(-1), torch.arange(B + 1, dtype=torch.int32, device=self.dev) * n, n)
         self.draft_len.zero_()
         self.draft.zero_()
         rows = torch.arange(s.K + 1, device=self.dev)
