@@ -358,12 +358,15 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // What bounds it: the matrix unit, 64 cycles for each 16 elements of a product of 128 rows and 128 columns, and beside it
 // the special functions' rate, 4 cycles a warp's 32 exponentials, and the hand-over of each tile between the roles.  Measured, bf16, heads of
 // 128, 32 over 8: a prompt of 8192 tokens 370 us (1490 TFLOP/s, 0.79 of the rate measured for one large matrix
-// product), four of 16384 4.3 ms (1430, where the clock falls under the power limit).  Steps on the way there, the former's us:
+// product), four of 16384 4.3 to 4.5 ms (1360 to 1430, where the clock falls under the power limit).  Steps on the way there, the former's us:
 // 2530 as one CTA's products and softmax in turn; 685 by two tiles of rows, queries asynchronous; 428 with weights in halves, of
 // which the first is multiplied while the second is taken; 370 with the units worked out by one warp and seldom-run code kept
 // short, as every new line of it is a miss in the instruction cache.  Tried and not kept: a warp for each tile of rows'
 // products (494 for 425), their issue as a loop (522 for 364), a tile's maximum before its weights (two passes over the scores).
-// e4m3: 563 us; there the conversion shares the issue slots with the softmax, whose halves take 1000 cycles each.
+// e4m3: 542 us; there the conversion (without its work 8 % less) and the scales of the keys (6 %, which each warp reads for
+// each of its rows' tiles) take issue slots and shared memory's bandwidth, all of which the first product's operands need,
+// from the softmax, whose halves take 1000 cycles each.  Keys as codes in an 8-bit product, the queries split into two of
+// them, would save no more than the keys' half of the conversion, 3 %.
 //
 // The tiles of all units form one list, cut into equal parts, one a CTA (one a SM), whatever the lengths are; what
 // a part holds of a unit that others share goes to the workspace, and the join, a kernel behind this one, adds them in order.
@@ -917,7 +920,8 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                         uint8_t* const to = ring + slot * S::kSlot + base * 128;
                         const bool codes = over(&sh.stage_full[stage], e / S::kStages);
                         const bool room = entry < S::kSlots || over(&sh.empty[slot], entry / S::kSlots - 1);
-                        if (part == kParts) wait_for(&sh.key_full[key_at], tile_no >> 2, &sh.dead);
+                        // (waited for before the keys go on, so that the softmax, to which their scores come, need not ask)
+                        if (part == 0) wait_for(&sh.key_full[key_at], tile_no >> 2, &sh.dead);
                         wait_more(codes, &sh.stage_full[stage], e / S::kStages, &sh.dead);
                         wait_more(room, &sh.empty[slot], entry / S::kSlots - 1, &sh.dead);
                         if (in) {
@@ -1042,7 +1046,6 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 const uint32_t s_at = tmem + lanes + at * 128;
                 const uint32_t s_turn = NQ == 2 ? mine : mine >> 1;
                 [[maybe_unused]] const int k_at = tile_no & 3;
-                if constexpr (E4M3) wait_for(&sh.key_full[k_at], tile_no >> 2, &sh.dead);
 #ifdef PLDP_TEST_STUCK_SCORES
                 wait_for(&sh.never, 0, &sh.dead);
 #endif
@@ -1070,6 +1073,8 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                     }
                     tmem_store_wait();
                 }
+                // (asked for here: at the end of each half it would be waited for, 566 us for 542)
+                [[maybe_unused]] const int now = E4M3 ? sh.unit_of[k_at] : 0;
                 // Keys in two halves: the first's weights are in the product while the second's are taken.
 #pragma unroll 1
                 for (int half = 0; half < 2; ++half) {
@@ -1106,7 +1111,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                         float top = fmaxf(t0, t1);
                         top = top > -INFINITY ? top * f : top;
                         const bool up = top > m + kRoomUp || (m == -INFINITY && top > -INFINITY);
-                        if (!__any_sync(0xFFFFFFFFu, up) && (!E4M3 || sh.unit_of[k_at] == unit)) break;
+                        if (!__any_sync(0xFFFFFFFFu, up) && (!E4M3 || now == unit)) break;
                         again = true;
                         float by = 1.f;
                         if (up) {
@@ -1115,7 +1120,6 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                         }
                         l2 = mul_f32x2(l2, pack_f32x2(by, by)), l3 = mul_f32x2(l3, pack_f32x2(by, by));
                         if constexpr (E4M3) {
-                            const int now = sh.unit_of[k_at];
                             if (now != unit && tile > w.t0) by *= power_of_two(max(unit - now, -126));
                             unit = now;
                         }
