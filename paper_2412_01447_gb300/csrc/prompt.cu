@@ -162,10 +162,16 @@ PLDP_API pldp_status pldp_attend_prompt(const pldp_attend_prompt_args* p, void* 
     a.head_first = head_first;
     // (signs are turned on the way by the other form)
     a.q_boxes = 128 % a.group == 0 && (e4m3 || !a.flip) && p->R > 0 && query_map(&maps.q, a, p->cache.head_dim);
-    const int ctas = prompt_ctas();
+    // No more CTAs than the most tiles make parts for (rows that several sequences claim, which is none of their uses, make
+    // parts longer), and no join where no unit is long enough to be cut: 47 tokens, 32 heads over 8, 19.6 us before and
+    // 17.5 with both, from a cold L2.
+    const int64_t positions = p->start || p->R > a.c.capacity ? a.c.capacity : p->R, tiles = (positions + kTile - 1) / kTile;
+    const int64_t units = p->cache.heads * (static_cast<int64_t>(p->R) * a.group / prompt_rows(dp) + p->B);
+    const int64_t parts = (units * (tiles + kUnitCost) + kLeast - 1) / kLeast;
+    const int most = prompt_ctas(), ctas = parts < most ? static_cast<int>(parts > 0 ? parts : 1) : most;
     auto s = static_cast<cudaStream_t>(stream);
     cudaError_t e = e4m3 ? launch_prompt_e4m3(a, maps, ctas, s) : launch_prompt_bf16(a, maps, ctas, s);
-    if (e != cudaSuccess) return launched(fn, e);
+    if (e != cudaSuccess || tiles <= kWhole) return launched(fn, e);
     const dim3 grid(ctas, prompt_rows(dp) / 32);
     e = dp == 64    ? launch_pdl(prompt_join_kernel<64>, grid, dim3(kJoinThreads), 0, s, 0, a)
         : dp == 128 ? launch_pdl(prompt_join_kernel<128>, grid, dim3(kJoinThreads), 0, s, 0, a)
