@@ -872,7 +872,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                     mma_commit(&sh.pv_half[q], lead);
                     wait_both(NQ == 2 && next && q == 0 ? full(k) : nullptr, k / S::kSlots, &sh.p_full[at][1], turn);
                     sums(q, 1, v_slot, at, true);
-                    if (NQ == 1 || !next) mma_commit(&sh.pv_done[q], lead);
+                    if (NQ == 1 || !next) mma_commit(&sh.pv_done[NQ == 1 ? p_no0 & 1 : q], lead);
                     if (q + 1 == nq) mma_commit(&sh.empty[v_slot], lead);
                     if (NQ == 2 && next) {
                         scores(q, k_slot, q);
@@ -1124,9 +1124,10 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                             unit = now;
                         }
                         if (tile > w.t0 || half) {
-                            // (Of two tiles of rows the scores came behind the last tile's product, of one behind that of
-                            // the one before: a barrier asked for a phase that is two behind would answer at once.)
-                            if (NQ == 1 && tile > w.t0) wait_for(&sh.pv_done[q], mine - 1, &sh.dead);
+                            // (Of two tiles of rows the scores came behind the last tile's product.  Of one they came behind
+                            // that of the one before, and the last one's may be over or not: a barrier for every other tile,
+                            // as one asked for a phase that is two ahead or behind answers wrongly.)
+                            if (NQ == 1 && tile > w.t0) wait_for(&sh.pv_done[(mine - 1) & 1], (mine - 1) >> 1, &sh.dead);
                             if (half) wait_for(&sh.pv_half[q], mine, &sh.dead);
                             __syncwarp();
                             tmem_after_sync();
@@ -1151,8 +1152,8 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 if constexpr (E4M3) mbar_arrive_if(&sh.key_empty[k_at], lane == 0);
             }
             // ---- the unit's end ----
-            if (NQ == 1 && w.t1 - w.t0 > 1) wait_for(&sh.pv_done[q], mine - 2, &sh.dead);
-            wait_for(&sh.pv_done[q], NQ == 2 ? seg : mine - 1, &sh.dead);
+            if constexpr (NQ == 1) wait_for(&sh.pv_done[(mine - 1) & 1], (mine - 1) >> 1, &sh.dead);
+            else wait_for(&sh.pv_done[q], seg, &sh.dead);
             __syncwarp();
             tmem_after_sync();
             const float l = (lo_f32(l2) + hi_f32(l2)) + (lo_f32(l3) + hi_f32(l3));

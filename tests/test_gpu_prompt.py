@@ -144,6 +144,21 @@ def test_many_short_sequences(lib, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("D,Hq,H", [(64, 32, 16), (128, 32, 16), (256, 16, 16)])
+def test_units_in_turn(lib, D, Hq, H, dtype):
+    """Several units a CTA, of few tiles each, over and over: what a role finds of another one, which may be a tile ahead or not,
+    is different every time, and the result is not."""
+    counts, starts = [300] * 24, [7] * 24
+    c, rows = Cache(lib, 24, 307, H, D, 16, dtype, seed=8), _rows(counts)
+    q = _queries(rows[-1], Hq, D)
+    first, lse, status = _run(lib, c, q, rows, starts)
+    _check(first, lse, prompt64(c, q, rows, starts, D ** -0.5), dtype)
+    for _ in range(30):
+        out, again, status = _run(lib, c, q, rows, starts)
+        assert status == [0] * 24 and torch.equal(out, first) and torch.equal(again, lse)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
 def test_peaked_and_growing_scores(lib, dtype):
     """Scores that grow along the context (each tile's maximum above the last, in the end by more than any lazy
     maximum may leave), a few that hold all the weight, large negative ones, and a scale of zero."""
