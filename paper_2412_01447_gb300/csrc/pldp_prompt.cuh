@@ -19,6 +19,10 @@ struct PromptArgs {
     uint32_t group_mul, group_shift;       // division by group, as CacheView's by the page
     int box, pitch;                        // as AttendArgs
     int head_first;
+    // bf16, heads above 128 elements: a box holds all of a vector's panels of 64 elements (1: their places in the map go on
+    // with the next head's, 2: a head's positions with the next head's), or (0) one of them
+    int whole;
+    int group_step, panel_step;            // bytes of shared memory from 8 positions to the next ones, and from panel to panel
     int q_boxes;                           // queries by boxes of whole tokens
     float scale2;                          // |scale| * log2(e)
     uint32_t flip;                         // what turns the signs of two queries for a negative scale
@@ -262,6 +266,15 @@ __device__ __forceinline__ void tma_box_if(void* dst, const CUtensorMap* map, in
         "setp.ne.u32 q, %7, 0;\n\t"
         "@q cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}"
         ::"r"(smem_u32(dst)), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(smem_u32(bar)), "r"(lead)
+        : "memory");
+}
+__device__ __forceinline__ void tma_box5_if(void* dst, const CUtensorMap* map, int c2, int c3, int c4, uint64_t* bar, uint32_t lead) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t.reg .b32 z;\n\t"
+        "mov.u32 z, 0;\n\t"
+        "setp.ne.u32 q, %6, 0;\n\t"
+        "@q cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {z, z, %2, %3, %4}], [%5];\n\t}"
+        ::"r"(smem_u32(dst)), "l"(map), "r"(c2), "r"(c3), "r"(c4), "r"(smem_u32(bar)), "r"(lead)
         : "memory");
 }
 // D += A B with A in tensor memory.
@@ -581,16 +594,28 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                             hole = hole || b0 + lane < full;
                         }
                         const int count = min(32, full - b0);
-#pragma unroll 1
-                        for (int i = 0; i < count; ++i) {
-                            const int i_slot = __shfl_sync(0xFFFFFFFFu, slot, i), i_pg = __shfl_sync(0xFFFFFFFFu, pg, i);
-                            const int c1 = a.head_first ? w.kv : i_slot, c2 = a.head_first ? i_slot : w.kv;
-                            if constexpr (E4M3) {
-                                tma_box_if(dst + (b0 + i) * a.box * a.pitch, map, 0, c1, c2, i_pg, bar, lead);
-                            } else {
+                        // (several at once: a box's way from its lanes to the copy is a chain of some 100 cycles.  8192 tokens, heads of
+                        // 128, pages of 8: 454 us one at a time, 382 with four, 374 with eight; e4m3: 698, 638 with two, 566 with four, but
+                        // code crowds the instruction cache there: 24 short prompts in pages of 32 take 142, 144 and 151)
+                        if (S::kPanels == 4 && !E4M3 && a.whole) {
+#pragma unroll 8
+                            for (int i = 0; i < count; ++i) {
+                                const int i_slot = __shfl_sync(0xFFFFFFFFu, slot, i), i_pg = __shfl_sync(0xFFFFFFFFu, pg, i);
+                                tma_box5_if(dst + (b0 + i) * a.box * (S::kPanels * 128), map, a.whole == 1 ? w.kv * S::kPanels : 0,
+                                            (a.whole == 1 ? 0 : w.kv * (c.page_size >> 3)) + (i_slot >> 3), i_pg, bar, lead);
+                            }
+                        } else {
+#pragma unroll (E4M3 ? DP == 256 ? 4 : 2 : S::kPanels == 4 ? 1 : 8)
+                            for (int i = 0; i < count; ++i) {
+                                const int i_slot = __shfl_sync(0xFFFFFFFFu, slot, i), i_pg = __shfl_sync(0xFFFFFFFFu, pg, i);
+                                const int c1 = a.head_first ? w.kv : i_slot, c2 = a.head_first ? i_slot : w.kv;
+                                if constexpr (E4M3) {
+                                    tma_box_if(dst + (b0 + i) * a.box * a.pitch, map, 0, c1, c2, i_pg, bar, lead);
+                                } else {
 #pragma unroll
-                                for (int p = 0; p < S::kPanels; ++p)
-                                    tma_box_if(dst + p * (kTile * 128) + (b0 + i) * a.box * 128, map, p * 64, c1, c2, i_pg, bar, lead);
+                                    for (int p = 0; p < S::kPanels; ++p)
+                                        tma_box_if(dst + p * (kTile * 128) + (b0 + i) * a.box * 128, map, p * 64, c1, c2, i_pg, bar, lead);
+                                }
                             }
                         }
                     }
@@ -610,13 +635,14 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                     }
                     if (tail && kv) {
                         // what the pages hold past the end is not used: zeros, in the values' tile
+                        const int group_step = S::kPanels == 4 ? a.group_step : 1024, panel_step = S::kPanels == 4 ? a.panel_step : kTile * 128;
                         wait_for(&sh.tail, tails, &sh.dead);
                         ++tails;
 #pragma unroll 1
                         for (int r = w.end - tile * kTile; r < kTile; ++r)
 #pragma unroll 1
                             for (int p = lane; p < 8 * S::kPanels; p += 32)
-                                *reinterpret_cast<uint4*>(dst + (p >> 3) * (kTile * 128) + r * 128 + (p & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                                *reinterpret_cast<uint4*>(dst + (p >> 3) * panel_step + (r >> 3) * group_step + (r & 7) * 128 + (p & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
                         fence_smem_async();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&arrived[at]);
@@ -793,8 +819,9 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
     } else if (warp == S::kMmaWarp) {
         // ---- matrix instructions ----
         const uint64_t q_op = smem_operand(smem_u32(q_smem), 16, 1024, swizzle_mode(128));
-        const uint64_t k_op = smem_operand(smem_u32(ring), 16, 1024, swizzle_mode(128));
-        const uint64_t v_op = smem_operand(smem_u32(ring), kTile * 128, 1024, swizzle_mode(128));
+        const int group_step = !E4M3 && S::kPanels == 4 ? a.group_step : 1024, panel_step = !E4M3 && S::kPanels == 4 ? a.panel_step : kTile * 128;
+        const uint64_t k_op = smem_operand(smem_u32(ring), 16, group_step, swizzle_mode(128));
+        const uint64_t v_op = smem_operand(smem_u32(ring), panel_step, group_step, swizzle_mode(128));
         const uint32_t q_lo = static_cast<uint32_t>(q_op), q_hi = q_op >> 32, k_lo = static_cast<uint32_t>(k_op), k_hi = k_op >> 32;
         const uint32_t v_lo = static_cast<uint32_t>(v_op), v_hi = v_op >> 32;
         constexpr uint32_t kScores = mma_form(128, 128, !E4M3, false, false);
@@ -826,7 +853,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
 #pragma unroll
             for (int s = 0; s < DP / 16; ++s)
                 if (s * 16 < D)
-                    mma_f16(to, qo + (s >> 2) * (128 * 8) + (s & 3) * 2, q_hi, op + (s >> 2) * (kTile * 8) + (s & 3) * 2, k_hi, kScores, s > 0, lead);
+                    mma_f16(to, qo + (s >> 2) * (128 * 8) + (s & 3) * 2, q_hi, op + (s >> 2) * (panel_step / 16) + (s & 3) * 2, k_hi, kScores, s > 0, lead);
             mma_commit(&sh.s_full[at], lead);
         };
         auto sums = [&](int q, int half, int slot, int at, bool more) {
@@ -834,10 +861,10 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             const uint32_t to = __shfl_sync(0xFFFFFFFFu, tmem + S::kO + q * DP, 0);
             if (half == 0) {
 #pragma unroll
-                for (int s = 0; s < 4; ++s) mma_f16_tmem(to, from + s * 8, op + s * 128, v_hi, values, s > 0 || more, lead);
+                for (int s = 0; s < 4; ++s) mma_f16_tmem(to, from + s * 8, op + s * (group_step / 8), v_hi, values, s > 0 || more, lead);
             } else {
 #pragma unroll
-                for (int s = 4; s < 8; ++s) mma_f16_tmem(to, from + s * 8, op + s * 128, v_hi, values, 1u, lead);
+                for (int s = 4; s < 8; ++s) mma_f16_tmem(to, from + s * 8, op + s * (group_step / 8), v_hi, values, 1u, lead);
             }
         };
         // Of each tile: the product of the first half of its weights, then of the second, then (two tiles of rows) the next

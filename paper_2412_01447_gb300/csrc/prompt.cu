@@ -23,6 +23,25 @@ bool query_map(CUtensorMap* map, const PromptArgs& a, int head_dim) {
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Keys or values of heads of 256 with all four panels of 64 elements of `box` positions in one box: (element, position of 8, panel,
+// 8 positions, page).  Two places are all that shared memory has for such tiles, so the time that a box's issue takes
+// is not hidden: pages of 24 positions (boxes of 8), three prompts of 2000 behind 4096: 231 us with a box a panel, 183 so.  (Heads
+// of 128, which have six places: nothing.)
+bool whole_map(CUtensorMap* map, void* base, const CacheView& c, int box, int* whole) {
+    const auto encode = tensor_map_encoder();
+    constexpr int panels = 4;
+    if (!encode || c.head_dim != panels * 64 || box % 8) return false;
+    *whole = c.heads == 1 || c.head_stride == c.vec_bytes ? 1 : c.head_stride == c.page_size * c.pos_stride ? 2 : 0;
+    if (!*whole) return false;
+    const cuuint64_t p = c.page_size / 8, h = c.heads, n = panels;
+    const cuuint64_t dims[5] = {64, 8, *whole == 1 ? n * h : n, *whole == 1 ? p : p * h, static_cast<cuuint64_t>(c.n_pages)};
+    const cuuint64_t pos = static_cast<cuuint64_t>(c.pos_stride), page = c.n_pages == 1 ? pos * 8 : static_cast<cuuint64_t>(c.page_stride);
+    const cuuint64_t strides[4] = {pos, 128, pos * 8, page};
+    const cuuint32_t size[5] = {64u, 8u, static_cast<cuuint32_t>(panels), static_cast<cuuint32_t>(box / 8), 1u}, step[5] = {1u, 1u, 1u, 1u, 1u};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, base, dims, strides, size, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 int prompt_ctas() {
     const int n = sm_count();
     return n < kPromptCtas ? n : kPromptCtas;
@@ -157,7 +176,10 @@ PLDP_API pldp_status pldp_attend_prompt(const pldp_attend_prompt_args* p, void* 
     a.pitch = p->cache.head_dim * a.box % 128 == 0 ? p->cache.head_dim : p->cache.head_dim <= 128 ? 128 : 256;
     PromptMaps maps = {};
     bool head_first = false;
-    if (!pool_map(&maps.pool.k, a.c.k, a.c, e4m3, a.box, a.pitch, &head_first) || !pool_map(&maps.pool.v, a.c.v, a.c, e4m3, a.box, a.pitch, &head_first))
+    a.group_step = 1024, a.panel_step = kTile * 128;
+    if (!e4m3 && whole_map(&maps.pool.k, a.c.k, a.c, a.box, &a.whole) && whole_map(&maps.pool.v, a.c.v, a.c, a.box, &a.whole))
+        a.group_step = dp / 64 * 1024, a.panel_step = 1024;
+    else if (a.whole = 0, !pool_map(&maps.pool.k, a.c.k, a.c, e4m3, a.box, a.pitch, &head_first) || !pool_map(&maps.pool.v, a.c.v, a.c, e4m3, a.box, a.pitch, &head_first))
         return fail(PLDP_ERR_UNSUPPORTED, "%s: the cache's strides cannot be described to the copy engine", fn);
     a.head_first = head_first;
     // (signs are turned on the way by the other form)

@@ -204,6 +204,48 @@ def test_strides_and_streams(lib, dtype):
     assert (room[Hq] == -7).all() and (room[:, 0] == -7).all() and (room[:, rows[-1] + 1:] == -7).all()
 
 
+# how a pool [pages, positions, heads, D] lies in memory: keys and values of a position side by side, of a head, and heads' positions
+# with room behind them
+def _side_by_side(k, v):
+    both = torch.cat((k, v), 2)
+    return both[:, :, : k.shape[2]], both[:, :, k.shape[2]:]
+
+
+def _in_heads(k, v):
+    both = torch.stack((k, v), 3)
+    return both[:, :, :, 0], both[:, :, :, 1]
+
+
+def _with_room(k, v):
+    n, page, H, D = k.shape
+    out = []
+    for x in (k, v):
+        room = torch.full((n, H, page + 8, D), float("nan"), device=DEV, dtype=torch.float32).to(x.dtype)
+        room[:, :, :page] = x.permute(0, 2, 1, 3)
+        out.append(room[:, :, :page].permute(0, 2, 1, 3))
+    return out
+
+
+@pytest.mark.parametrize("lie", [_side_by_side, _in_heads, _with_room])
+@pytest.mark.parametrize("D,H,page", [(256, 2, 24), (256, 1, 8), (256, 2, 4), (256, 3, 64), (128, 2, 8), (256, 1, 512)])
+def test_pools(lib, D, H, page, lie):
+    """Keys and values in pools of other strides, and a page that is none."""
+    counts, starts, Hq = [150, 33, 290], [10, 0, 200], 2 * H
+    lens, rows = [a + b for a, b in zip(counts, starts)], _rows(counts)
+    c = Cache(lib, 3, 512, H, D, page, lens=lens, seed=5)
+    c.pools = dict(zip("kv", lie(c.pools["k"], c.pools["v"])))
+    c.handle = lib.pldp_cache(c.pools["k"], c.pools["v"], c.pages)
+    q = _queries(rows[-1], Hq, D)
+    out, lse, status = _run(lib, c, q, rows, starts)
+    assert status == [0] * 3
+    _check(out, lse, prompt64(c, q, rows, starts, D ** -0.5))
+    c.pages[2, 100 // page] = -1
+    live = torch.arange(lens[2], device=DEV) // page != 100 // page
+    out, lse, status = _run(lib, c, q, rows, starts)
+    assert status == [0, 0, lib.PLDP_ST_PAGE]
+    _check(out, lse, prompt64(c, q, rows, starts, D ** -0.5, live=[None, None, live]))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
 def test_status(lib, dtype):
     """Starts and rows out of range, the capacity, pages that are none, rows of no sequence."""
