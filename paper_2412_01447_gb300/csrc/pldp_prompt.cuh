@@ -595,8 +595,9 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                         }
                         const int count = min(32, full - b0);
                         // (several at once: a box's way from its lanes to the copy is a chain of some 100 cycles.  8192 tokens, heads of
-                        // 128, pages of 8: 454 us one at a time, 382 with four, 374 with eight; e4m3: 698, 638 with two, 566 with four, but
-                        // code crowds the instruction cache there: 24 short prompts in pages of 32 take 142, 144 and 151)
+                        // 128, pages of 8: 454 us one at a time, 411 with two, 382 with four, 376 with eight, of which 24 short prompts in
+                        // pages of 32 take 118 us for 114; e4m3: 698, 638, 566, and 142, 144 and 151 there, as code crowds the
+                        // instruction cache)
                         if (S::kPanels == 4 && !E4M3 && a.whole) {
 #pragma unroll 8
                             for (int i = 0; i < count; ++i) {
@@ -605,7 +606,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                                             (a.whole == 1 ? 0 : w.kv * (c.page_size >> 3)) + (i_slot >> 3), i_pg, bar, lead);
                             }
                         } else {
-#pragma unroll (E4M3 ? DP == 256 ? 4 : 2 : S::kPanels == 4 ? 1 : 8)
+#pragma unroll (E4M3 ? DP == 256 ? 4 : 2 : S::kPanels == 4 ? 1 : 4)
                             for (int i = 0; i < count; ++i) {
                                 const int i_slot = __shfl_sync(0xFFFFFFFFu, slot, i), i_pg = __shfl_sync(0xFFFFFFFFu, pg, i);
                                 const int c1 = a.head_first ? w.kv : i_slot, c2 = a.head_first ? i_slot : w.kv;
