@@ -304,6 +304,27 @@ def test_long_offsets(lib):
     _check(out, lse, prompt64(small, q, [0, 200], [0], D ** -0.5))
 
 
+def test_two_at_once(lib):
+    """Calls on two streams, each with a workspace of its own, while the other's run."""
+    calls = []
+    for seed, (counts, starts, Hq, H, D, dtype) in enumerate([([900, 40, 1300], [0, 700, 5], 8, 2, 128, "bf16"), ([700] * 9, [3] * 9, 4, 4, 64, "e4m3")]):
+        rows = _rows(counts)
+        c = Cache(lib, len(counts), max(a + b for a, b in zip(counts, starts)), H, D, 16, dtype, lens=[a + b for a, b in zip(counts, starts)], seed=seed)
+        q, r, st = _queries(rows[-1], Hq, D, seed), i32(rows), i32(starts)
+        ws = torch.empty(lib.pldp_attend_prompt_workspace_size(Hq, H, D), dtype=torch.uint8, device=DEV)
+        outs = [torch.zeros_like(q) for _ in range(12)]
+        _check(*_run(lib, c, q, rows, starts)[:2], prompt64(c, q, rows, starts, D ** -0.5), dtype)
+        calls.append((c, q, r, st, ws, outs, _run(lib, c, q, rows, starts)[0], torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for i in range(12):
+        for c, q, r, st, ws, outs, _, stream in calls:
+            with torch.cuda.stream(stream):
+                lib.pldp_attend_prompt(c.handle, q, r, outs[i], ws, start=st)
+    torch.cuda.synchronize()
+    for *_, outs, want, _ in calls:
+        assert all(torch.equal(x, want) for x in outs)
+
+
 def test_graph_replay_and_one_workspace(lib):
     """Captured once, replayed on other rows and starts; calls of other shapes on the same workspace between."""
     H, D, R = 2, 64, 700
