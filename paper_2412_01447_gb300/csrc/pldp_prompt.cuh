@@ -345,12 +345,6 @@ __device__ __forceinline__ uint32_t ordered_f16(float lo, float hi) {
     asm volatile("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
 }
-__device__ __forceinline__ float max3(float a, float b, float c) {
-    float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
-
 // ---------------------------------------------------------------------------
 // One pass over the keys that a unit sees, 128 at a time.  A unit is 256 (heads above 128 elements: 128) rows of one
 // sequence and key/value head: the rows of all of its query heads, token by token, so short prompts with grouped heads
