@@ -572,8 +572,14 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                     on = !__any_sync(0xFFFFFFFFu, *static_cast<volatile int*>(&sh.dead));
                     if (!on) break;
                     uint64_t* const bar = tail && kv ? &sh.tail : &arrived[at];
-                    if (lane == 0) mbar_arrive_expect_tx(bar, full * a.box * (E4M3 ? a.pitch : S::kPanels * 128));
-                    __syncwarp();
+                    // (bf16 keys: behind their flags of missing pages, which the softmax reads once the scores are there; until
+                    // this arrival the phase stays open, whatever has been copied)
+                    const bool flags = !E4M3 && kv == 0;
+                    auto arrive = [&] {
+                        if (lane == 0) mbar_arrive_expect_tx(bar, full * a.box * (E4M3 ? a.pitch : S::kPanels * 128));
+                        __syncwarp();
+                    };
+                    if (!flags) arrive();
                     uint8_t* dst = E4M3 ? stages + at * S::kStage : ring + at * S::kSlot;
                     bool hole = false;
                     // issued one after the other by the lane that leads: a branch around the copy would make every
@@ -614,7 +620,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                             }
                         }
                     }
-                    if (!E4M3 && kv == 0) {
+                    if (flags) {
                         hole = __any_sync(0xFFFFFFFFu, hole);
                         if (hole) {
 #pragma unroll 1
@@ -627,6 +633,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                             if (lane == 0 && a.status) atomicOr(a.status + w.b, PLDP_ST_PAGE);
                         }
                         if (lane == 0) sh.holes[tile_no % kAhead] = hole;
+                        arrive();
                     }
                     if (tail && kv) {
                         // what the pages hold past the end is not used: zeros, in the values' tile
