@@ -504,9 +504,12 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
     // code for and wait for loads for at every unit.
     PromptUnit w;
     int unit_no = 0;
+    // Whether a wait has run out, as all lanes of a warp see it together: another warp may set it between their looks, and lanes
+    // that left a loop alone would be waited for by the rest at the next vote.
+    auto given_up = [&] { return __any_sync(0xFFFFFFFFu, *static_cast<volatile int*>(&sh.dead)); };
     auto next_unit = [&] {
         wait_for(&sh.unit_full[unit_no % kUnits], unit_no / kUnits, &sh.dead);
-        if (*static_cast<volatile int*>(&sh.dead)) return false;
+        if (given_up()) return false;
         w = sh.units[unit_no % kUnits];
         return w.T > 0;
     };
@@ -569,7 +572,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                     const int at = e % kDepth;
                     if (kv < first_kv || kv > last_kv) continue;
                     if (e >= kDepth) wait_for(&left[at], e / kDepth - 1, &sh.dead);
-                    on = !__any_sync(0xFFFFFFFFu, *static_cast<volatile int*>(&sh.dead));
+                    on = !given_up();
                     if (!on) break;
                     uint64_t* const bar = tail && kv ? &sh.tail : &arrived[at];
                     // (bf16 keys: behind their flags of missing pages, which the softmax reads once the scores are there; until
@@ -670,7 +673,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             if (q * 128 >= w.rows) return;
             int& seg = q ? seg1 : seg0;
             if (seg > 0) wait_for(&sh.q_empty[q], seg - 1, &sh.dead);
-            if (*static_cast<volatile int*>(&sh.dead)) return;
+            if (given_up()) return;
             uint64_t* const bar = E4M3 ? &sh.q_raw[q] : &sh.q_full[q];
             uint8_t* const to = q_smem + q * (S::kPanels * 128 * 128);
             const uint32_t first = static_cast<uint32_t>(w.r0) + q * 128, group = a.group;
@@ -733,7 +736,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                     if (ahead >= kUnits) wait_for(&sh.unit_empty[ahead % kUnits], ahead / kUnits - 1, &sh.dead);
                     // (after a wait that ran out a place may still be read: half of one unit and half of another would put
                     // results anywhere)
-                    if (__any_sync(0xFFFFFFFFu, *static_cast<volatile int*>(&sh.dead))) break;
+                    if (given_up()) break;
                     if (more) more = ahead == 0 ? walk.first(a, sh.in) : walk.next(a);
                     PromptUnit u = {};
                     if (more) {
@@ -752,7 +755,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 }
                 w = sh.units[unit_no % kUnits];
                 ++unit_no;
-                if (w.T == 0 || *static_cast<volatile int*>(&sh.dead)) break;
+                if (w.T == 0 || given_up()) break;
                 tile_rows(0, NQ == 2 && (E4M3 || a.q_boxes) ? 2 : 1);
             }
         } else {
@@ -839,7 +842,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             uint32_t polls = 0;
 #pragma unroll 1
             while (!__all_sync(0xFFFFFFFFu, done)) {
-                if (++polls >= kPolls || *static_cast<volatile int*>(&sh.dead)) {
+                if (++polls >= kPolls || given_up()) {
                     *static_cast<volatile int*>(&sh.dead) = 1;
                     break;
                 }
