@@ -129,7 +129,7 @@ struct Raw {                            // eight elements as they are in memory
 // cosines and sines of this lane's elements) is worked out once a token.
 // 4 x 4095 tokens of 48 heads of 128, bf16 to e4m3, with the read of the last positions behind it: 99 us (428 MB,
 // 4.3 TB/s); 1 x 11 tokens, fp32 to bf16: 5.3 us, two launches' latency.
-// PACKED: prompts of different lengths behind one another; a token looks its sequence up (its CTA's last one, or by
+// PACKED: prompts of different lengths behind one another; a token looks its sequence up (its group's last one, or by
 // bisection), and the first CTA tells what is wrong with the sequences.
 template <typename T, int GS, bool E4M3, bool PACKED>
 __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_kernel(const AppendArgs a) {
@@ -157,13 +157,12 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
     // The stage's two places, in turn from one rotated vector to the next, over the end of a token as well: the one barrier
     // between a place's write and its reads then also lies between those reads and the write after next.
     int turn = 0;
-    [[maybe_unused]] int in = 0;                       // the last packed token's sequence
+    [[maybe_unused]] int in = 0, ascends = -1;         // the last packed token's sequence; whether their rows ascend
 #pragma unroll 1
     for (uint32_t token = blockIdx.x * a.at_once + sub; token < a.tokens; token += gridDim.x * a.at_once) {
         int b, i;
         if constexpr (PACKED) {
             // (strides of one sequence: i counts from the first row of all)
-            in = sequence_of(a.rows, a.B, static_cast<int>(token), in);
             b = 0, i = token;
         } else {
             b = token / static_cast<uint32_t>(a.n), i = token - b * a.n;
@@ -178,9 +177,12 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendBlocks) cache_append_ke
         if (first < total && live) next.load(source(first));
         int pos, seq;
         if constexpr (PACKED) {
+            const int found = sequence_of<GS>(a.rows, a.B, static_cast<int>(a.tokens), i, in, at, mates, ascends);
+            if (found < 0) continue;
+            in = found;
             uint32_t st;
             const PackedRows pr = packed_rows(a.rows, a.start, in, static_cast<int>(a.tokens), a.capacity, st);
-            if (i < pr.row || i - pr.row >= pr.count) continue;
+            if (i - pr.row >= pr.count) continue;
             pos = pr.first + (i - pr.row), seq = in;
         } else {
             uint32_t st;

@@ -113,16 +113,36 @@ __device__ __forceinline__ PackedRows packed_rows(const int32_t* rows, const int
     return {r0, p, count, r1 - r0};
 }
 
-// The last sequence whose rows start at or before `row` (the first where none does); `hint` is looked at first.
-__device__ __forceinline__ int sequence_of(const int32_t* rows, int B, int row, int hint) {
-    if (__ldg(rows + hint) <= row && row < __ldg(rows + hint + 1)) return hint;
+// The sequence that a row belongs to, one whose pair lies within [0, R] and holds it, or -1; `hint` is looked at first.  Where
+// the list ascends, bisection finds the one pair that can be it.  Where it does not, bisection may end elsewhere, and all pairs are
+// looked at by the GS lanes (`lane` of `mates`) that ask together; `ascends` (-1: not known yet) is theirs to keep, so that the rows
+// behind the last sequence pay for that look once.
+template <int GS>
+__device__ __forceinline__ int sequence_of(const int32_t* rows, int B, int R, int row, int hint, int lane, unsigned mates, int& ascends) {
+    auto holds = [&](int b) {
+        const int r0 = __ldg(rows + b), r1 = __ldg(rows + b + 1);
+        return r0 >= 0 && r0 <= row && row < r1 && r1 <= R;
+    };
+    if (holds(hint)) return hint;
     int lo = 0, hi = B;
     while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
+        const int mid = lo + ((hi - lo) >> 1);
         if (__ldg(rows + mid) <= row) lo = mid;
         else hi = mid;
     }
-    return lo;
+    if (holds(lo)) return lo;
+    if (ascends < 0) {
+        bool up = true;
+#pragma unroll 1
+        for (int64_t b = lane; b < B; b += GS) up = up && __ldg(rows + b) <= __ldg(rows + b + 1);
+        ascends = __all_sync(mates, up);
+    }
+    if (ascends) return -1;
+    unsigned found = 0xFFFFFFFFu;
+#pragma unroll 1
+    for (int64_t b = lane; b < B && found == 0xFFFFFFFFu; b += GS)
+        if (holds(static_cast<int>(b))) found = static_cast<unsigned>(b);
+    return static_cast<int>(__reduce_min_sync(mates, found));
 }
 
 }  // namespace pldp
