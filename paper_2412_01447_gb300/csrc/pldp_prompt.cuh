@@ -1052,7 +1052,8 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 const int ex = static_cast<int>(max(most & 0xFFFFu, most >> 16) >> 7);
                 const int up = ex == 0 || ex == 255 ? 0 : min(14 - (ex - 127), 120);
                 const float lift = __uint_as_float((static_cast<uint32_t>(up + 127) << 23) ^ (a.flip & 0x80000000u));
-                f *= __uint_as_float(static_cast<uint32_t>(127 - up) << 23);
+                // (never 0, so that a masked score stays -infinity: what is left of so small a scale moves no weight)
+                f = fmaxf(f * __uint_as_float(static_cast<uint32_t>(127 - up) << 23), 0x1p-126f);
 #pragma unroll 1
                 for (int c0 = 0; c0 < D / 8; c0 += 4) {
                     uint4 x[4];

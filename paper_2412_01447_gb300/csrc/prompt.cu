@@ -164,7 +164,7 @@ PLDP_API pldp_status pldp_attend_prompt(const pldp_attend_prompt_args* p, void* 
     a.B = p->B, a.R = p->R, a.q_heads = p->q_heads;
     divide_by(a.group, &a.group_mul, &a.group_shift);
     // A negative scale turns the queries' signs, so that larger scores are larger weights; one of zero is the least that
-    // keeps a masked score at -infinity.
+    // keeps a masked score at -infinity (as it is once an e4m3 cache's kernel has taken its queries' power of two out).
     a.scale2 = fmaxf(fabsf(p->scale) * 1.4426950408889634f, 0x1p-126f);
     a.flip = p->scale < 0.f ? 0x80008000u : 0u;
     a.box = kTile;                                           // the largest power of two that divides the page, up to a tile
