@@ -161,6 +161,11 @@ struct PromptShape {
     static_assert(kSlots >= 2 && (!E4M3 || kStages >= 1) && kBytes + kStatic <= kMaxShared, "shared memory");
 };
 
+constexpr int kApart = INT32_MAX;
+constexpr int kAbove = 7;                  // a scale may be this many powers of two above the unit: 448 * 2^7 is f16
+// A positive float is below 2^(exponent_of it); 0: -126.
+__device__ __forceinline__ int exponent_of(float x) { return static_cast<int>(__float_as_uint(x) >> 23) - 126; }
+
 constexpr int kAhead = 8;                  // tiles whose holes are kept (more than the ring of keys holds)
 
 // A unit, or what a CTA has of it, as one warp works it out for the others (rows: token * group + head).
@@ -176,10 +181,10 @@ constexpr int kUnits = 8;                  // worked out and not yet done by all
 
 template <bool E4M3>
 struct PromptShared {
-    // of the keys of four tiles: the scale of the key, that of the value by 2^-unit as two f16
-    alignas(16) float key_scale[E4M3 ? 4 : 1][E4M3 ? kTile : 4];
+    // of the keys of four tiles: the scale of the key, that of the value, and by 2^-unit as two f16
+    alignas(16) float key_scale[E4M3 ? 4 : 1][E4M3 ? kTile : 4], value[E4M3 ? 4 : 1][E4M3 ? kTile : 4];
     uint32_t value_scale[E4M3 ? 4 : 1][E4M3 ? kTile : 4];
-    int unit_of[4];
+    int unit_of[4];                        // kApart: the weights take the values' scales, each row in a unit of its own
     uint32_t live[kAhead][4];              // whether a page holds the key, a bit each; looked at where `holes` is set
     int holes[kAhead];
     PromptUnit units[kUnits];
@@ -345,6 +350,74 @@ __device__ __forceinline__ uint32_t ordered_f16(float lo, float hi) {
     asm volatile("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
 }
+// A tile of keys (e4m3) of which some rows see only a part, and whose other values are so much larger that a unit for all of them
+// would cost these rows theirs.  The values' codes go into the product as they are (by 1/4), and each weight takes its value's
+// scale: weights w_j = 2^(x_j - m + 7) become w_j 4 v_j / 2^unit, where unit is the row's own, above the largest scale that it
+// sees.  Done here in the scores, so that the loops over tiles need not know of it: x_j (by f, the queries' factor) becomes
+// x_j + log2(4 v_j / 2^unit), and the sum of the weights takes the difference in advance, the w_j and not what the loop will add.  The
+// scores are divided by the keys' scales, as the loop multiplies by them, and f is 1 from here on.  (A function, as the loops of all
+// roles share one instruction cache: 24 short prompts, which never come here, 139 us without it, 145 so, 157 with its code in the
+// loop over tiles.)
+struct ApartRow {
+    float m, l;
+    int unit;
+};
+template <int DP>
+__device__ __noinline__ ApartRow apart_tile(uint32_t s_at, uint32_t o_at, const float* key_scale, const float* value, float f, bool sums, ApartRow r) {
+    constexpr float kLift = 7.f, kRoomUp = 8.f;
+    float top = -INFINITY, largest = 0.f;
+#pragma unroll 1
+    for (int i = 0; i < kTile; i += 8) {
+        float y[8];
+        tmem_load(s_at + i, y);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float x = y[k] * key_scale[i + k] * f;
+            top = fmaxf(top, x);
+            if (x > -INFINITY) largest = fmaxf(largest, value[i + k]);
+        }
+    }
+    float by = 1.f;
+    if (top > r.m + kRoomUp || (r.m == -INFINITY && top > -INFINITY)) {
+        by = r.m == -INFINITY ? 0.f : ex2(r.m - top);
+        r.m = top;
+    }
+    r.l *= by;
+    if (top > -INFINITY) {                                     // (a row that sees nothing of the tile stays as it is)
+        const int now = max(r.unit, min(exponent_of(largest) + 2, 126));
+        if (now != r.unit && r.unit != INT32_MIN) by *= power_of_two(max(r.unit - now, -126));
+        r.unit = now;
+    }
+    __syncwarp();
+    tmem_after_sync();
+    if (sums && __any_sync(0xFFFFFFFFu, by != 1.f)) {
+#pragma unroll 1
+        for (int i = 0; i < DP; i += 8) {
+            float o[8];
+            tmem_load(o_at + i, o);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[k] *= by;
+            tmem_store8(o_at + i, o);
+        }
+    }
+    const float less = r.m == -INFINITY ? 0.f : kLift - r.m, lift = top > -INFINITY ? power_of_two(2 - r.unit) : 0.f;
+#pragma unroll 1
+    for (int i = 0; i < kTile; i += 8) {
+        float y[8];
+        tmem_load(s_at + i, y);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float scale = key_scale[i + k], x = y[k] * scale * f;
+            // (keys that the row does not see: -infinity)
+            y[k] = x > -INFINITY ? (x + log2f(value[i + k] * lift)) / scale : -INFINITY;
+            r.l += ex2(x + less) - ex2(__fmaf_rn(__fmul_rn(y[k], scale), 1.f, less));
+        }
+        tmem_store8(s_at + i, y);
+    }
+    tmem_store_wait();
+    return r;
+}
+
 // ---------------------------------------------------------------------------
 // One pass over the keys that a unit sees, 128 at a time.  A unit is 256 (heads above 128 elements: 128) rows of one
 // sequence and key/value head: the rows of all of its query heads, token by token, so short prompts with grouped heads
@@ -359,8 +432,8 @@ __device__ __forceinline__ uint32_t ordered_f16(float lo, float hi) {
 // Weights are rounded to bf16 (2^-8 of each) over a bf16 cache, whose values need bf16's range: two terms, as a step's attention takes
 // them, would make the second product, half of the work here, twice as long.  Over an e4m3 cache codes are converted by warps
 // of their own and weights are f16 (2^-11): keys as f16, which holds every code, their scales multiplying the scores; values
-// times scale / 2^unit, each rounded to f16 (2^-11), where 2^unit is above the largest scale that the unit has met, and O is
-// multiplied when that rises.
+// times scale / 2^unit, each rounded to f16 (2^-11), where 2^unit is above the largest scale that the unit has met of keys that its
+// rows see, and O is multiplied when that rises (apart_tile: where keys that only some of them see are much larger).
 //
 // What bounds it: the matrix unit, 64 cycles for each 16 elements of a product of 128 rows and 128 columns, and beside it
 // the special functions' rate, 4 cycles a warp's 32 exponentials, and the hand-over of each tile between the roles.  Measured, bf16, heads of
@@ -775,6 +848,8 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
 #pragma unroll 1
             while (next_unit()) {
                 const int32_t* table = c.pages + w.b * c.pages_stride;
+                const int first = w.start + static_cast<int>(page_of(static_cast<uint32_t>(w.r0), a.group_mul, a.group_shift));
+                bool apart = false;
 #pragma unroll 1
                 for (int tile = w.t0; tile < w.t1; ++tile, ++tile_no) {
                     const int at = tile_no & 3;
@@ -795,15 +870,33 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                             }
                         }
                     }
-                    // the values' unit 2^unit: above the largest scale of a unit's first tile, and of a later one that passes it
-                    const int most = static_cast<int>(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])))) >> 23) - 126;
-                    if (tile == w.t0 || most > unit) unit = min(most + 2, 126);
+                    // The values' unit 2^unit: above the largest scale of a unit's first tile, and of a later one that passes it.
+                    // Of a tile that some rows see in part only the keys count that all of those rows see, and only where it is
+                    // the first, so that no row's result depends on later tokens' values; where that leaves a scale too far above
+                    // the unit, from there on the weights take the scales.
+                    const int all = __reduce_max_sync(0xFFFFFFFFu, exponent_of(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]))));
+                    const int partly = first - tile * kTile;                  // keys up to here: all rows see them that see any
+                    if (tile == w.t0 || (all > unit && partly >= kTile - 1)) {
+                        const int mine = max(partly, 0) - 4 * lane;
+                        unit = min(2 + __reduce_max_sync(0xFFFFFFFFu, exponent_of(fmaxf(fmaxf(mine >= 0 ? v[0] : 0.f, mine >= 1 ? v[1] : 0.f),
+                                                                                        fmaxf(mine >= 2 ? v[2] : 0.f, mine >= 3 ? v[3] : 0.f)))), 126);
+                    }
+                    apart = apart || (all > unit + kAbove && partly < kTile - 1);
                     const float by = power_of_two(-unit);
                     if (tile_no >= 4) wait_for(&sh.key_empty[at], (tile_no >> 2) - 1, &sh.dead);
-                    *reinterpret_cast<float4*>(&sh.key_scale[at][4 * lane]) = make_float4(f[0], f[1], f[2], f[3]);
-                    *reinterpret_cast<uint4*>(&sh.value_scale[at][4 * lane]) = make_uint4(pack_f16(v[0] * by, v[0] * by), pack_f16(v[1] * by, v[1] * by),
-                                                                                          pack_f16(v[2] * by, v[2] * by), pack_f16(v[3] * by, v[3] * by));
-                    if (lane == 0) sh.unit_of[at] = unit;
+                    // (keys' scales never 0: scores are divided by them where the weights take the values')
+                    *reinterpret_cast<float4*>(&sh.key_scale[at][4 * lane]) = make_float4(fmaxf(f[0], 0x1p-120f), fmaxf(f[1], 0x1p-120f),
+                                                                                          fmaxf(f[2], 0x1p-120f), fmaxf(f[3], 0x1p-120f));
+                    *reinterpret_cast<float4*>(&sh.value[at][4 * lane]) = make_float4(v[0], v[1], v[2], v[3]);
+                    // (codes / 4 are exact)
+                    uint32_t h[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float x = apart ? 0.25f : v[i] * by;
+                        h[i] = pack_f16(x, x);
+                    }
+                    *reinterpret_cast<uint4*>(&sh.value_scale[at][4 * lane]) = make_uint4(h[0], h[1], h[2], h[3]);
+                    if (lane == 0) sh.unit_of[at] = apart ? kApart : unit;
                     hole = __any_sync(0xFFFFFFFFu, hole);
                     if (hole) {
                         // (this lane's four keys are bits 4 (lane & 7) and on of a word)
@@ -1025,7 +1118,8 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             const uint32_t tok = is_row ? page_of(r, a.group_mul, a.group_shift) : 0u;
             const uint32_t head = is_row ? static_cast<uint32_t>(w.kv) * a.group + (r - tok * a.group) : 0u;
             const int limit = is_row ? w.start + static_cast<int>(tok) : -1;         // last position that the row sees
-            const int seen_by_all = w.start + static_cast<int>(page_of(static_cast<uint32_t>(w.r0) + q * 128, a.group_mul, a.group_shift));
+            // (e4m3: by all rows of the unit, as the values' units go)
+            const int seen_by_all = w.start + static_cast<int>(page_of(static_cast<uint32_t>(w.r0) + (E4M3 ? 0 : q * 128), a.group_mul, a.group_shift));
             float m = -INFINITY;                        // (of x, in powers of two)
             [[maybe_unused]] int unit = INT32_MIN;      // the values' in the sums (none yet)
             uint64_t l2 = 0, l3 = 0;
@@ -1072,7 +1166,8 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 __syncwarp();
                 mbar_arrive_if(&sh.q_full[q], lane == 0);
             }
-            const uint64_t f2 = pack_f32x2(f, f);
+            [[maybe_unused]] const float scale_f = f;
+            uint64_t f2 = pack_f32x2(f, f);
 #pragma unroll 1
             for (int tile = w.t0; tile < w.t1; ++tile, ++tile_no, ++mine) {
                 const int at = NQ == 2 ? q : mine & 1;
@@ -1087,6 +1182,8 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                 tmem_after_sync();
                 const bool masked = tile * kTile + kTile - 1 > seen_by_all;
                 const bool holes = sh.holes[tile_no % kAhead];
+                // (asked for here: at the end of each half it would be waited for, 566 us for 542)
+                [[maybe_unused]] int now = E4M3 ? sh.unit_of[k_at] : 0;
                 if (masked || holes) {
                     // scores of keys that the row does not see become -infinity where they are (code that is seldom run is
                     // kept short: it is fetched anew every time)
@@ -1105,9 +1202,15 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                         tmem_store8(s_at + i + 8, y + 8);
                     }
                     tmem_store_wait();
+                    if constexpr (E4M3)
+                        if (now == kApart) {
+                            if (NQ == 1 && tile > w.t0) wait_for(&sh.pv_done[(mine - 1) & 1], (mine - 1) >> 1, &sh.dead);
+                            const ApartRow x = apart_tile<DP>(s_at, my_o, sh.key_scale[k_at], sh.value[k_at], scale_f, tile > w.t0,
+                                                              {m, (lo_f32(l2) + hi_f32(l2)) + (lo_f32(l3) + hi_f32(l3)), unit});
+                            m = x.m, l2 = pack_f32x2(x.l, 0.f), l3 = 0, unit = now = x.unit;
+                            f = 1.f, f2 = pack_f32x2(1.f, 1.f);
+                        }
                 }
-                // (asked for here: at the end of each half it would be waited for, 566 us for 542)
-                [[maybe_unused]] const int now = E4M3 ? sh.unit_of[k_at] : 0;
                 // Keys in two halves: the first's weights are in the product while the second's are taken.
 #pragma unroll 1
                 for (int half = 0; half < 2; ++half) {
