@@ -46,7 +46,7 @@ cudaError_t launch_prompt_e4m3(const PromptArgs& a, const PromptMaps& m, int cta
 
 __host__ __device__ constexpr int prompt_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 __host__ __device__ constexpr int prompt_rows(int dp) { return dp == 256 ? 128 : 256; }       // rows of a unit
-// What a part of a unit leaves: per 128 rows the sums [DP / 4][128][4], then the maxima [128] and the weights' sums [128].
+// What a part of a unit leaves: per 128 rows the averages [DP / 4][128][4], then the maxima [128] and the weights' sums [128].
 __host__ __device__ constexpr int prompt_part(int dp) { return prompt_rows(dp) * (dp + 2); }
 constexpr int kPromptCtas = 192;           // at most
 
@@ -1294,8 +1294,8 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             tmem_after_sync();
             const float l = (lo_f32(l2) + hi_f32(l2)) + (lo_f32(l3) + hi_f32(l3));
             const bool whole = w.t0 == 0 && w.t1 == w.T;
+            const float inverse = l > 0.f ? (E4M3 ? power_of_two(unit) : 1.f) / l : 0.f;
             if (whole) {
-                const float inverse = l > 0.f ? (E4M3 ? power_of_two(unit) : 1.f) / l : 0.f;
                 const int64_t row = w.row + static_cast<int64_t>(tok);
                 if (is_row && a.lse) a.lse[row * a.q_heads + head] = l > 0.f ? (log2f(l) + m - kLift) * 0.69314718055994531f : -INFINITY;
                 // kOutBytes of each of the warp's 32 rows at a time: a row a lane into shared memory, whole pieces of rows out of it
@@ -1329,15 +1329,15 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                     __syncwarp();
                 }
             } else {
-                // (which of this CTA's two places: the unit began in another's part, or in this one's)
+                // (which of this CTA's two places: the unit began in another's part, or in this one's.  Averages, as sums of values
+                // near fp32's largest pass it)
                 float* part = a.parts + static_cast<int64_t>(2 * blockIdx.x + (w.t0 == 0 ? 1 : 0)) * prompt_part(DP) + q * 128 * (DP + 2);
 #pragma unroll 1
                 for (int i = 0; i < D; i += 16) {
                     float o[16];
                     tmem_load(my_o + i, o);
-                    if constexpr (E4M3)
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) o[k] *= power_of_two(unit);
+                    for (int k = 0; k < 16; ++k) o[k] *= inverse;
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
                         *reinterpret_cast<float4*>(part + ((i / 4 + k) * 128 + j) * 4) = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);

@@ -88,29 +88,26 @@ __global__ void __launch_bounds__(kJoinThreads) prompt_join_kernel(const PromptA
 #pragma unroll 1
         for (int k0 = 0; k0 < cut.parts; k0 += 4) {
             float4 x[4][2];
-            float by[4];
+            float by[4], l[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                by[i] = 0.f;
+                by[i] = -INFINITY, l[i] = 0.f;
                 if (k0 + i < cut.parts) {
                     const float* p = place(k0 + i);
-                    by[i] = __ldcg(p + 128 * DP + j);
+                    by[i] = __ldcg(p + 128 * DP + j), l[i] = __ldcg(p + 128 * DP + 128 + j);
                     x[i][0] = __ldcg(reinterpret_cast<const float4*>(p + (d / 4 * 128 + j) * 4));
                     x[i][1] = __ldcg(reinterpret_cast<const float4*>(p + ((d / 4 + 1) * 128 + j) * 4));
-                } else {
-                    by[i] = -INFINITY;
                 }
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float f = sum > 0.f ? ex2(by[i] - M) : 0.f;
+                const float f = sum > 0.f ? ex2(by[i] - M) * l[i] * inverse : 0.f;            // the part's share, 1 at most
                 if (f == 0.f) continue;
                 o[0] = fmaf(f, x[i][0].x, o[0]), o[1] = fmaf(f, x[i][0].y, o[1]), o[2] = fmaf(f, x[i][0].z, o[2]), o[3] = fmaf(f, x[i][0].w, o[3]);
                 o[4] = fmaf(f, x[i][1].x, o[4]), o[5] = fmaf(f, x[i][1].y, o[5]), o[6] = fmaf(f, x[i][1].z, o[6]), o[7] = fmaf(f, x[i][1].w, o[7]);
             }
         }
-        *reinterpret_cast<uint4*>(out + d) = make_uint4(pack_bf16(o[0] * inverse, o[1] * inverse), pack_bf16(o[2] * inverse, o[3] * inverse),
-                                                        pack_bf16(o[4] * inverse, o[5] * inverse), pack_bf16(o[6] * inverse, o[7] * inverse));
+        *reinterpret_cast<uint4*>(out + d) = make_uint4(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]), pack_bf16(o[4], o[5]), pack_bf16(o[6], o[7]));
     }
 }
 
