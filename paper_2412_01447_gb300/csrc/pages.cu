@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const CopyArgs
     const CacheView& c = a.c;
     int n = a.n;
     if (a.n_copies) n = max(0, min(n, __ldg(a.n_copies)));
-    const int64_t items = n * 2 * a.pieces, chunks = a.runs * (a.run / 16), per_run = a.run / 16;
+    const int64_t items = static_cast<int64_t>(n) * 2 * a.pieces, chunks = a.runs * (a.run / 16), per_run = a.run / 16;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
         const int64_t part = item / a.pieces, piece = item - part * a.pieces;
         const int pair = static_cast<int>(part >> 1), kv = part & 1;
