@@ -59,26 +59,12 @@ namespace {
 __host__ __device__ inline uint64_t quotient(uint64_t x, uint64_t y) {
     return (x | y) >> 32 ? x / y : (uint32_t)x / (uint32_t)y;
 }
-// sum over i < n of floor((a i + b) / m), by the steps of Euclid's algorithm.  (One copy of its code: at a kernel's start
-// every new line of code is a miss in the instruction cache, which takes longer than what it holds.)
-__host__ __device__ inline PLDP_ONE_COPY uint64_t floor_sum(uint64_t n, uint64_t m, uint64_t a, uint64_t b) {
-    uint64_t sum = 0;
-    if (n == 0) return 0;
-    while (true) {
-        if (a >= m) {
-            const uint64_t q = quotient(a, m);
-            sum += n * (n - 1) / 2 * q, a -= q * m;
-        }
-        if (b >= m) {
-            const uint64_t q = quotient(b, m);
-            sum += n * q, b -= q * m;
-        }
-        const uint64_t y = a * n + b;
-        if (y < m) return sum;
-        n = quotient(y, m), b = y - n * m;
-        const uint64_t t = m;
-        m = a, a = t;
-    }
+// sum over i < n of floor((c + i) / d): the first x numbers from 0 on have quotients of 0 to x / d - 1, d of each, and then the
+// last one.  (What both sums have above 2^64 is the same.  One copy of its code: at a kernel's start every new line of code is a miss
+// in the instruction cache, which takes longer than what it holds.)
+__host__ __device__ inline PLDP_ONE_COPY uint64_t quotients_sum(uint64_t n, uint64_t c, uint64_t d) {
+    const uint64_t q1 = quotient(c + n, d), q0 = quotient(c, d);
+    return d * (q1 * (q1 - 1) / 2) + q1 * (c + n - q1 * d) - d * (q0 * (q0 - 1) / 2) - q0 * (c - q0 * d);
 }
 
 // The rows of a sequence and kv head, token * group + head, cut into units of `UR`; unit u sees the keys up to its last
@@ -91,18 +77,21 @@ __device__ __forceinline__ Units units_of(const PackedRows& p, int group) {
     return {static_cast<int64_t>(p.count) * group, group, p.first, p.count};
 }
 template <int UR>
-__device__ __forceinline__ int unit_count(const Units& s) { return static_cast<int>((s.N + UR - 1) / UR); }
+__host__ __device__ __forceinline__ int unit_count(const Units& s) { return static_cast<int>((s.N + UR - 1) / UR); }
 template <int UR>
-__device__ __forceinline__ int unit_tiles(const Units& s, int u) {
+__host__ __device__ __forceinline__ int unit_tiles(const Units& s, int u) {
     const int64_t end = min(s.N, (static_cast<int64_t>(u) + 1) * UR);
     return (s.start + static_cast<int>(static_cast<uint32_t>(end - 1) / static_cast<uint32_t>(s.group)) + kTile) / kTile;
 }
 template <int UR>
-__device__ __forceinline__ int64_t tiles_before(const Units& s, int u) {
+__host__ __device__ __forceinline__ int64_t tiles_before(const Units& s, int u) {
     if (u == 0) return 0;
     const int whole = static_cast<int64_t>(u) * UR > s.N ? u - 1 : u;          // the last unit may have fewer rows
-    const uint64_t m = static_cast<uint64_t>(kTile) * s.group;
-    int64_t n = floor_sum(whole, m, UR, static_cast<uint64_t>(s.start) * s.group + UR - 1 + m);
+    // A whole unit i has floor((i UR / 128 + c) / group) tiles.  With UR of 256, floor(2 x) = floor(x) + floor(x + 1/2).
+    static_assert(UR == kTile || UR == 2 * kTile, "rows of a unit");
+    const uint64_t g = s.group, c = (static_cast<uint64_t>(s.start) * g + UR - 1) / kTile + g;
+    int64_t n = 0;
+    if (whole > 0) n = UR == kTile ? quotients_sum(whole, c, g) : quotients_sum(whole, c / 2, g) + quotients_sum(whole, (c + g) / 2, g);
     if (whole < u) n += unit_tiles<UR>(s, whole);
     return n;
 }
@@ -110,10 +99,10 @@ __device__ __forceinline__ int64_t tiles_before(const Units& s, int u) {
 // results' way out.  The list counts it, so that a part of many short units is not the last to end.
 constexpr int kUnitCost = 2;
 template <int UR>
-__device__ __noinline__ int64_t cost_before(const Units& s, int u) { return tiles_before<UR>(s, u) + static_cast<int64_t>(u) * kUnitCost; }
+__host__ __device__ PLDP_ONE_COPY int64_t cost_before(const Units& s, int u) { return tiles_before<UR>(s, u) + static_cast<int64_t>(u) * kUnitCost; }
 // The unit that holds place x of the list of one kv head: cost_before(u) <= x < cost_before(u + 1).
 template <int UR>
-__device__ __forceinline__ int unit_at(const Units& s, int units, int64_t x, int64_t* before) {
+__host__ __device__ __forceinline__ int unit_at(const Units& s, int units, int64_t x, int64_t* before) {
     // tiles grow linearly from unit to unit: the root of their sum, and from there to the unit itself
     const float a2 = UR / (2.f * kTile * s.group), b = kUnitCost + (s.start + 0.5f * UR / s.group) / kTile + 0.5f;
     int u = static_cast<int>((sqrtf(b * b + 4.f * a2 * static_cast<float>(x)) - b) / (2.f * a2));
