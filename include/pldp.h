@@ -917,10 +917,11 @@ PLDP_API pldp_status pldp_cache_append_prompt(const pldp_cache_append_prompt_arg
  *  status     uint32 [B] or NULL.  TIMEOUT: a wait inside the kernel ran out; the call's
  *             results are none.
  * Rows of a sequence with nothing to attend to (skipped, past the capacity, no page holds any
- * of their positions) are written as zeros, their lse as -INFINITY; of a sequence whose rows
- * are not within [0, R] nothing is written.  Keys and values past a sequence's last row are never
- * used, whatever they hold; those before it must be finite, a bf16 cache's values below 2^32
- * in size and an e4m3 one's scales below 2^124.  Sums and the running maximum are held in fp32.  On the way into the product with the
+ * of their positions) are written as zeros, their lse as -INFINITY; of the others those whose
+ * query holds NaN as NaN.  Of a sequence whose rows are not within [0, R] nothing is written.
+ * Keys and values past a sequence's last row are never used, whatever they hold; those before
+ * it must be finite, a bf16 cache's values below 2^32 in size and an e4m3 one's scales below
+ * 2^124.  Sums and the running maximum are held in fp32.  On the way into the product with the
  * values each weight exp(s_j - lse) is rounded, over a bf16 cache to bf16 (by up to 2^-8 of it), over
  * an e4m3 one to f16, as are the values' scales and the values (each by up to 2^-11; small ones by
  * up to 2^-32 of the row's largest weight, and 2^-21 of the largest value that the row sees).

@@ -1283,10 +1283,11 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
             tmem_after_sync();
             const float l = (lo_f32(l2) + hi_f32(l2)) + (lo_f32(l3) + hi_f32(l3));
             const bool whole = w.t0 == 0 && w.t1 == w.T;
-            const float inverse = l > 0.f ? (E4M3 ? power_of_two(unit) : 1.f) / l : 0.f;
+            // (l 0: a row that sees nothing; NaN: a query that holds it)
+            const float inverse = l == 0.f ? 0.f : (E4M3 ? power_of_two(unit) : 1.f) / l;
             if (whole) {
                 const int64_t row = w.row + static_cast<int64_t>(tok);
-                if (is_row && a.lse) a.lse[row * a.q_heads + head] = l > 0.f ? (log2f(l) + m - kLift) * 0.69314718055994531f : -INFINITY;
+                if (is_row && a.lse) a.lse[row * a.q_heads + head] = l == 0.f ? -INFINITY : (log2f(l) + m - kLift) * 0.69314718055994531f;
                 // kOutBytes of each of the warp's 32 rows at a time: a row a lane into shared memory, whole pieces of rows out of it
                 constexpr int kCols = S::kOutBytes / 2, kPieces = kCols / 8, kAt = 32 / kPieces;
                 uint8_t* const room = out_smem + warp * (32 * S::kOutBytes);
@@ -1332,7 +1333,7 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                         *reinterpret_cast<float4*>(part + ((i / 4 + k) * 128 + j) * 4) = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
                     __syncwarp();
                 }
-                part[128 * DP + j] = l > 0.f ? m - kLift : -INFINITY;
+                part[128 * DP + j] = l == 0.f ? -INFINITY : m == -INFINITY ? 0.f : m - kLift;            // (of NaN a number, so that it counts)
                 part[128 * DP + 128 + j] = l;
                 if (w.t0 == 0) cut_here = true;
                 if (w.t0 == 0 && threadIdx.x == 0)

@@ -79,8 +79,8 @@ __global__ void __launch_bounds__(kJoinThreads) prompt_join_kernel(const PromptA
     }
     const int r = cut.row0 + row, tok = r / a.group;
     const int64_t at = cut.row_base + static_cast<int64_t>(tok), head = static_cast<int64_t>(cut.kv) * a.group + (r - tok * a.group);
-    if (warp == 0 && a.lse) a.lse[at * a.q_heads + head] = sum > 0.f ? (log2f(sum) + M) * 0.69314718055994531f : -INFINITY;
-    const float inverse = sum > 0.f ? 1.f / sum : 0.f;
+    if (warp == 0 && a.lse) a.lse[at * a.q_heads + head] = sum == 0.f ? -INFINITY : (log2f(sum) + M) * 0.69314718055994531f;
+    const float inverse = sum == 0.f ? 0.f : 1.f / sum;
     __nv_bfloat16* out = a.out + at * a.o_tok + head * a.o_head;
 #pragma unroll 1
     for (int d = warp * 8; d < D; d += kJoinThreads / 32 * 8) {
@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(kJoinThreads) prompt_join_kernel(const PromptA
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float f = sum > 0.f ? ex2(by[i] - M) * l[i] * inverse : 0.f;            // the part's share, 1 at most
+                const float f = sum == 0.f ? 0.f : ex2(by[i] - M) * l[i] * inverse;            // the part's share, 1 at most
                 if (f == 0.f) continue;
                 o[0] = fmaf(f, x[i][0].x, o[0]), o[1] = fmaf(f, x[i][0].y, o[1]), o[2] = fmaf(f, x[i][0].z, o[2]), o[3] = fmaf(f, x[i][0].w, o[3]);
                 o[4] = fmaf(f, x[i][1].x, o[4]), o[5] = fmaf(f, x[i][1].y, o[5]), o[6] = fmaf(f, x[i][1].z, o[6]), o[7] = fmaf(f, x[i][1].w, o[7]);
