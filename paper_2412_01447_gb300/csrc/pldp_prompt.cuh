@@ -66,6 +66,13 @@ __host__ __device__ inline PLDP_ONE_COPY uint64_t quotients_sum(uint64_t n, uint
     const uint64_t q1 = quotient(c + n, d), q0 = quotient(c, d);
     return d * (q1 * (q1 - 1) / 2) + q1 * (c + n - q1 * d) - d * (q0 * (q0 - 1) / 2) - q0 * (c - q0 * d);
 }
+// sum over i < n of floor((a i + b) / m), for an `a` of 128 or 256 and an m that 128 divides: by 128 these are the quotients above, or
+// of 2 i + c, for which floor(2 x) = floor(x) + floor(x + 1/2).
+__host__ __device__ inline uint64_t floor_sum(uint64_t n, uint64_t m, uint64_t a, uint64_t b) {
+    const uint64_t d = m / 128, c = b / 128;
+    if (a == 128) return quotients_sum(n, c, d);
+    return quotients_sum(n, c / 2, d) + quotients_sum(n, (c + d) / 2, d);
+}
 
 // The rows of a sequence and kv head, token * group + head, cut into units of `UR`; unit u sees the keys up to its last
 // row's token, T(u) tiles.  tiles_before: those of the units before u, u up to the number of units.
@@ -87,11 +94,10 @@ template <int UR>
 __host__ __device__ __forceinline__ int64_t tiles_before(const Units& s, int u) {
     if (u == 0) return 0;
     const int whole = static_cast<int64_t>(u) * UR > s.N ? u - 1 : u;          // the last unit may have fewer rows
-    // A whole unit i has floor((i UR / 128 + c) / group) tiles.  With UR of 256, floor(2 x) = floor(x) + floor(x + 1/2).
-    static_assert(UR == kTile || UR == 2 * kTile, "rows of a unit");
-    const uint64_t g = s.group, c = (static_cast<uint64_t>(s.start) * g + UR - 1) / kTile + g;
+    static_assert(kTile == 128 && (UR == kTile || UR == 2 * kTile), "rows of a unit");
+    const uint64_t m = static_cast<uint64_t>(kTile) * s.group;
     int64_t n = 0;
-    if (whole > 0) n = UR == kTile ? quotients_sum(whole, c, g) : quotients_sum(whole, c / 2, g) + quotients_sum(whole, (c + g) / 2, g);
+    if (whole > 0) n = floor_sum(whole, m, UR, static_cast<uint64_t>(s.start) * s.group + UR - 1 + m);
     if (whole < u) n += unit_tiles<UR>(s, whole);
     return n;
 }
