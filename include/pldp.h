@@ -861,8 +861,8 @@ PLDP_API size_t pldp_token_logprobs_workspace_size(int64_t rows, int V);
  *  R          rows of the tensors, >= 0 and below 2^31 - 256; rows behind rows[B] (or before
  *             rows[0]) belong to no sequence: nothing of them is used, nothing is written there.
  *  rows       int32 [B+1], ascending, 0 <= rows[b] <= rows[b+1] <= R; a sequence may have no
- *             rows.  Where a pair descends or leaves [0, R]: SEQ_LEN, that sequence is skipped
- *             (rows that two sequences then claim are one of theirs).
+ *             rows.  Where a pair descends or leaves [0, R]: SEQ_LEN, that sequence is skipped, and
+ *             no other one (rows that two sequences then claim hold what either gives them).
  *  start      int32 [B], or NULL for 0; outside [0, capacity]: SEQ_LEN, skipped.  Tokens at
  *             or past the capacity: CAPACITY, they take no part.
  */
@@ -924,7 +924,8 @@ PLDP_API pldp_status pldp_cache_append_prompt(const pldp_cache_append_prompt_arg
  * 2^124.  Sums and the running maximum are held in fp32.  On the way into the product with the
  * values each weight exp(s_j - lse) is rounded, over a bf16 cache to bf16 (by up to 2^-8 of it), over
  * an e4m3 one to f16, as are the values' scales and the values (each by up to 2^-11; small ones by
- * up to 2^-32 of the row's largest weight, and 2^-21 of the largest value that the row sees).
+ * up to 2^-32 of the row's largest weight, and 2^-21 of the largest value that the row sees);
+ * pldp_attend_cache, which takes such rows as one long draft, holds weights over a bf16 cache to 2^-17.
  * Results are the same for the same inputs, however the work is scheduled.
  */
 typedef struct {

@@ -121,7 +121,8 @@ __host__ __device__ __forceinline__ int unit_at(const Units& s, int units, int64
 }
 // Units of so few tiles are one CTA's, that of the place in the list where they begin.
 constexpr int kWhole = 4;
-// And a part is no smaller than this: of a unit that several have, a few tiles each pay for the join.
+// And there are no more parts than make some this many tiles each (never fewer than two): of a unit that several have, a few tiles
+// each pay for the join.
 constexpr int kLeast = 3;
 
 template <int DP, bool E4M3>
@@ -432,13 +433,14 @@ __device__ __noinline__ ApartRow apart_tile(uint32_t s_at, uint32_t o_at, const 
 //
 // What bounds it: the matrix unit, 64 cycles for each 16 elements of a product of 128 rows and 128 columns, and beside it
 // the special functions' rate, 4 cycles a warp's 32 exponentials, and the hand-over of each tile between the roles.  Measured, bf16, heads of
-// 128, 32 over 8: a prompt of 8192 tokens 370 us (1490 TFLOP/s, 0.79 of the rate measured for one large matrix
-// product), four of 16384 4.3 to 4.5 ms (1360 to 1430, where the clock falls under the power limit).  Steps on the way there, the former's us:
+// 128, 32 over 8: a prompt of 8192 tokens 374 to 394 us (1400 to 1470 TFLOP/s, 0.74 to 0.78 of the rate measured for one large matrix
+// product), four of 16384 3.2 to 3.5 ms (1420 to 1520, where the clock falls under the power limit); 40 over 8, whose groups of five do
+// not divide 128 rows, 4.6 to 4.9 ms (1260 to 1350).  Steps on the way there, the former's us:
 // 2530 as one CTA's products and softmax in turn; 685 by two tiles of rows, queries asynchronous; 428 with weights in halves, of
 // which the first is multiplied while the second is taken; 370 with the units worked out by one warp and seldom-run code kept
 // short, as every new line of it is a miss in the instruction cache.  Tried and not kept: a warp for each tile of rows'
 // products (494 for 425), their issue as a loop (522 for 364), a tile's maximum before its weights (two passes over the scores).
-// e4m3: 542 us; there the conversion (without its work 8 % less) and the scales of the keys (6 %, which each warp reads for
+// e4m3: 550 us; there the conversion (without its work 8 % less) and the scales of the keys (6 %, which each warp reads for
 // each of its rows' tiles) take issue slots and shared memory's bandwidth, all of which the first product's operands need,
 // from the softmax, whose halves take 1000 cycles each.  Keys as codes in an 8-bit product, the queries split into two of
 // them, would save no more than the keys' half of the conversion, 3 %.
@@ -666,9 +668,9 @@ prompt_kernel(const PromptArgs a, const __grid_constant__ CUtensorMap k_map, con
                         }
                         const int count = min(32, full - b0);
                         // (several at once: a box's way from its lanes to the copy is a chain of some 100 cycles.  8192 tokens, heads of
-                        // 128, pages of 8: 454 us one at a time, 411 with two, 382 with four, 376 with eight, of which 24 short prompts in
-                        // pages of 32 take 118 us for 114; e4m3: 698, 638, 566, and 142, 144 and 151 there, as code crowds the
-                        // instruction cache)
+                        // 128, pages of 8: 454 us one at a time, 411 with two, 382 with four (392 with the keys' arrival behind the boxes), 376 with
+                        // eight, of which 24 short prompts in pages of 32 take 118 us for 114; e4m3: 698, 638, 566, and 142, 144 and 151
+                        // there, as code crowds the instruction cache)
                         if (S::kPanels == 4 && !E4M3 && a.whole) {
 #pragma unroll 8
                             for (int i = 0; i < count; ++i) {

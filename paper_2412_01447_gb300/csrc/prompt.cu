@@ -25,7 +25,7 @@ bool query_map(CUtensorMap* map, const PromptArgs& a, int head_dim) {
 
 // Keys or values of heads of 256 with all four panels of 64 elements of `box` positions in one box: (element, position of 8, panel,
 // 8 positions, page).  Two places are all that shared memory has for such tiles, so the time that a box's issue takes
-// is not hidden: pages of 24 positions (boxes of 8), three prompts of 2000 behind 4096: 231 us with a box a panel, 183 so.  (Heads
+// is not hidden: pages of 24 positions (boxes of 8), three prompts of 2000 behind 4096: 231 us with a box a panel, 183 to 188 so.  (Heads
 // of 128, which have six places: nothing.)
 bool whole_map(CUtensorMap* map, void* base, const CacheView& c, int box, int* whole) {
     const auto encode = tensor_map_encoder();
